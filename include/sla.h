@@ -434,6 +434,59 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
                                       const void* q, const void* k, const void* v, const void* dout,
                                       void* dq, void* dk, void* dv, float* dtau, sla_stream_t stream);
 
+/*
+ * The gated delta rule: linear attention in its causal, recurrent form (Eq. (1)'s state
+ * S_t = S_{t-1} + k_t^T v_t; Tab. 7 compares gated linear attentions) with a state that decays and
+ * that writes only what it does not hold yet.  For window w and value head h, over the window's
+ * rows t in order, with the dk x dv state S at state_in[w][h] (zero if state_in is NULL):
+ *     S   <- exp(g_t) S,          u_t = beta_t (v_t - S^T k_t),
+ *     S   <- S + k_t u_t^T,       o_t = scale S^T q_t,
+ * and state_out[w][h] (if not NULL) receives the last S.
+ *   offsets  int32 [num_windows + 1], device: window w is the positions offsets[w] ..
+ *            offsets[w + 1] - 1; 0 <= offsets[0], non-decreasing, offsets[num_windows] <= n.
+ *            Empty windows are allowed (state_out = state_in).  Offsets that are not like that
+ *            are clamped so that nothing is read or written out of range; results are undefined.
+ *   order    int32 [n], device, or NULL: position p is row order[p] (e.g. a plan's perm with its
+ *            offsets); NULL: row p.  The rows at positions before offsets[0] and from
+ *            offsets[num_windows] on are in no window: their outputs are left as they were.
+ *   q, k     [n, heads_qk, dim_k], v, o [n, heads, dim_v], in `dtype`, contiguous, 16-byte
+ *            aligned; heads a multiple of heads_qk, value head h reads query/key head
+ *            h / (heads / heads_qk).  dim_k a multiple of 16 up to 128, dim_v a multiple of 16 up to
+ *            256, heads up to 65,535, else SLA_E_UNSUPPORTED.
+ *   g        fp32 [n, heads], the log decay (<= 0 to forget; exp(g) that underflows, -infinity too,
+ *            forgets everything);  beta fp32 [n, heads].
+ *   states   fp32 [num_windows, heads, dim_k, dim_v].  state_out may be state_in.
+ *   workspace  device, 256-byte aligned, at least sla_delta_workspace_bytes(...) bytes (0 for
+ *            sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
+ * The rule is stable where beta_t |k_t|^2 <= 2 (keys are usually normalised to 1); where it is not,
+ * states grow exponentially and results may not be finite.  Sums, states and decays are fp32, decay
+ * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
+ * held exactly down to 2^-17 of its row's largest value).  A value that is not finite reaches only its
+ * own window (v's, only its own head and column).  Deterministic.
+ */
+size_t sla_delta_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t heads_qk,
+                                 int32_t heads, int32_t dim_k, int32_t dim_v);
+
+sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order,
+                               sla_dtype_t dtype, int32_t heads_qk, int32_t heads, int32_t dim_k,
+                               int32_t dim_v, float scale, const void* q, const void* k, const void* v,
+                               const float* g, const float* beta, const float* state_in, void* o,
+                               float* state_out, void* workspace, size_t workspace_bytes,
+                               sla_stream_t stream);
+
+/*
+ * The gated delta rule one row at a time: `state` is a pool of num_slots states
+ * [num_slots, heads, dim_k, dim_v] (fp32, 16-byte aligned), row b of the batch belongs to the
+ * sequence in slot slots[b] (int32 [n], device), whose state it updates in place, and o[b] receives
+ * its output.  Rows with the same slot are successive rows of one sequence, in row order.  A slot
+ * outside [0, num_slots) marks a padding row: it touches neither o nor a state.  Other arguments as
+ * sla_forward_delta; all arithmetic is fp32.
+ */
+sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
+                            int32_t heads_qk, int32_t heads, int32_t dim_k, int32_t dim_v, float scale,
+                            float* state, const void* q, const void* k, const void* v, const float* g,
+                            const float* beta, void* o, sla_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

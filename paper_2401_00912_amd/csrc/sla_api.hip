@@ -54,6 +54,15 @@ hipError_t launch_backward_xca_noalloc(const void* plan, int32_t n, int32_t W, i
                                        const float* tau, const void* q, const void* k, const void* v,
                                        const void* dout, void* dq, void* dk, void* dv, float* dtau,
                                        hipStream_t stream);
+size_t delta_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv);
+hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,
+                                int32_t Hk, int32_t H, int32_t dk, int32_t dv, float scale, const void* q,
+                                const void* k, const void* v, const float* g, const float* beta,
+                                const float* state_in, void* o, float* state_out, void* workspace,
+                                hipStream_t stream);
+hipError_t launch_step_delta(const int32_t* slots, int32_t n, int32_t num_slots, int dtype, int32_t Hk, int32_t H,
+                             int32_t dk, int32_t dv, float scale, float* state, const void* q, const void* k,
+                             const void* v, const float* g, const float* beta, void* o, hipStream_t stream);
 }  // namespace sla
 
 namespace {
@@ -465,4 +474,67 @@ SLA_EXPORT sla_status_t sla_cwi_backward(const int32_t* map, int32_t gx, int32_t
   return hip_status(sla::launch_cwi_backward(map, gx, gy, gz, coords, (int32_t)n, order, (int)dtype,
                                              channels, taps_x, taps_y, x, w_x, w_y, w_3, dy, dx, dw_x,
                                              dw_y, dw_3, workspace, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// Sizes of a gated delta rule call; also bounds the grids (slots and rows in x, heads in y).
+sla_status_t check_delta_sizes(int64_t n, int32_t W, int dtype, int32_t heads_qk, int32_t heads, int32_t dim_k,
+                               int32_t dim_v) {
+  if (!sizes_ok(n, W) || heads_qk < 1 || heads < 1 || heads % heads_qk) return SLA_E_ARG;
+  if (dtype < 0 || dtype > 2) return SLA_E_ARG;
+  if (dim_k < 16 || dim_k > 128 || dim_k % 16 || dim_v < 16 || dim_v > 256 || dim_v % 16) return SLA_E_UNSUPPORTED;
+  if (heads > 65535) return SLA_E_UNSUPPORTED;
+  // HIP bounds a grid at 2^32 - 1 threads in x
+  if (n / 64 + (int64_t)W > UINT32_MAX / 256 || n > UINT32_MAX / 256) return SLA_E_UNSUPPORTED;
+  return SLA_OK;
+}
+
+bool finite(float x) { return x >= -3.0e38f && x <= 3.0e38f; }
+
+}  // namespace
+
+SLA_EXPORT size_t sla_delta_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t heads_qk,
+                                            int32_t heads, int32_t dim_k, int32_t dim_v) {
+  if (check_delta_sizes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v) != SLA_OK) return 0;
+  return sla::delta_workspace_bytes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v);
+}
+
+SLA_EXPORT sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                          const int32_t* order, sla_dtype_t dtype, int32_t heads_qk, int32_t heads,
+                                          int32_t dim_k, int32_t dim_v, float scale, const void* q, const void* k,
+                                          const void* v, const float* g, const float* beta, const float* state_in,
+                                          void* o, float* state_out, void* workspace, size_t workspace_bytes,
+                                          sla_stream_t stream) {
+  const sla_status_t st = check_delta_sizes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v);
+  if (st != SLA_OK) return st;
+  if (!finite(scale)) return SLA_E_ARG;
+  if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !aligned(state_in, 4) || !aligned(state_out, 4))
+    return SLA_E_ARG;
+  if (n == 0 && !state_out) return SLA_OK;
+  if (n > 0 && (!q || !k || !v || !g || !beta || !o)) return SLA_E_ARG;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(g, 4) || !aligned(beta, 4))
+    return SLA_E_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  if (workspace_bytes < sla::delta_workspace_bytes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v))
+    return SLA_E_WORKSPACE;
+  return hip_status(sla::launch_forward_delta(offsets, (int32_t)n, num_windows, order, (int)dtype, heads_qk, heads,
+                                              dim_k, dim_v, scale, q, k, v, g, beta, state_in, o, state_out,
+                                              workspace, static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
+                                       int32_t heads_qk, int32_t heads, int32_t dim_k, int32_t dim_v, float scale,
+                                       float* state, const void* q, const void* k, const void* v, const float* g,
+                                       const float* beta, void* o, sla_stream_t stream) {
+  const sla_status_t st = check_delta_sizes(n, num_slots, (int)dtype, heads_qk, heads, dim_k, dim_v);
+  if (st != SLA_OK) return st;
+  if (!finite(scale)) return SLA_E_ARG;
+  if (n == 0) return SLA_OK;
+  if (!slots || !state || !q || !k || !v || !g || !beta || !o) return SLA_E_ARG;
+  if (!aligned(slots, 4) || !aligned(state, 16) || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) ||
+      !aligned(o, 16) || !aligned(g, 4) || !aligned(beta, 4))
+    return SLA_E_ARG;
+  return hip_status(sla::launch_step_delta(slots, (int32_t)n, num_slots, (int)dtype, heads_qk, heads, dim_k, dim_v,
+                                           scale, state, q, k, v, g, beta, o, static_cast<hipStream_t>(stream)));
 }

@@ -1,0 +1,230 @@
+// Shared parts of the gated delta rule (sla_delta.hip, sla_delta_bwd.hip,
+// sla_delta_step.hip): the chunk form, the workspace, operands in two 16-bit terms.
+//
+// Chunk form.  A window is cut into chunks of 64 rows.  With gam_i the log decays summed from
+// the chunk's first row to row i, D_ij = exp(gam_i - gam_j) for j <= i, S0 the state before the
+// chunk and u_j = beta_j r_j:
+//     r = T (v - exp(gam) k S0),   T = (I + [D_ij (k_i . k_j) beta_j]_{j < i})^-1,
+//     o = scale (exp(gam) q S0 + P u),   P_ij = D_ij (q_i . k_j) for j <= i,
+//     S1 = exp(gam_last) S0 + sum_j exp(gam_last - gam_j) k_j u_j^T.
+// T and P depend on no state: one kernel makes them for all chunks at once, a second one goes
+// through every window's chunks in order with the state in registers.
+//
+// Two-term operands.  The matrix cores' 16-bit products are 16 times as fast as their fp32 ones,
+// and one 16-bit rounding of a state loses what fp32 states are kept for.  So an fp32 operand is
+// scaled by a power of two and split into two fp16 terms, x = hi + lo (22 bits), and a product is
+// the sum of hi hi, hi lo and lo hi in fp32.  A 16-bit input needs no second term: its row is
+// scaled by a power of two that puts the row's largest value into [1, 2), and then fp16 holds
+// fp16 and bf16 values exactly down to 2^-17 of the row's largest (below that, to 2^-25 of it).
+// With k = 2^kap k' and q = 2^rho q' the rule reads the same for k', v' = 2^-kap v,
+// beta' = 2^(2 kap) beta, r' = 2^-kap r, u' = 2^kap u and o' = 2^-rho o: the scales cost one
+// factor a row, and wherever beta |k|^2 <= 2 (where the rule is stable) T's entries stay below
+// 2 sqrt(4 dk).
+#pragma once
+
+#include "sla_common.h"
+
+namespace sla {
+namespace delta {
+
+constexpr int kChunk = 64;
+constexpr int kFrag = 512;            // halfs of one 16 x 32 operand: 64 lanes x 8
+constexpr int kTri = 6;               // 16 x 32 operands of a lower triangular 64 x 64 matrix
+constexpr int kTriHalfs = 2 * kTri * kFrag;
+// T and P are kept 64 times as large (T's entries stay below 45, P's below 512): an entry's error is
+// then below 2^-31 of the diagonal's 1
+constexpr float kTriUp = 64.f;
+constexpr int kScal = 448;            // floats: 6 rows of 64 and one value
+// rows of the per-chunk scalars
+enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kLast = 384 };
+
+struct Args {
+  const int32_t* offsets;
+  const int32_t* order;
+  int32_t n, W, Hk, H, dk, dv;
+  float scale;
+  uint32_t slots;                     // n / 64 + W
+};
+
+// Workspace of the chunk form: per chunk slot and query/key head the images of k' and q', per
+// slot and value head T, P and the scalars.
+struct Space {
+  size_t image, images, tri, scal, total;   // halfs of one image; byte offsets
+};
+
+__host__ __device__ inline int pad_dk(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
+
+__host__ __device__ inline size_t slots_of(int64_t n, int32_t W) { return (size_t)(n / kChunk + W); }
+
+__host__ __device__ inline Space space_of(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk,
+                                          int tris) {
+  Space s;
+  const size_t ns = slots_of(n, W);
+  s.image = (size_t)(dtype == 0 ? 2 : 1) * kChunk * pad_dk(dk);
+  s.images = 0;
+  s.tri = align_up(s.images + ns * Hk * 2 * s.image * 2, 256);
+  s.scal = align_up(s.tri + ns * H * tris * kTriHalfs * 2, 256);
+  s.total = align_up(s.scal + ns * H * kScal * 4, 256);
+  return s;
+}
+
+// ------------------------------------------------------------------ windows and slots
+struct Win {
+  int32_t begin, rows;
+};
+__device__ __forceinline__ Win window(const Args& a, int w) {
+  int b = a.offsets[w], e = a.offsets[w + 1];
+  b = b < 0 ? 0 : b > a.n ? a.n : b;
+  e = e < b ? b : e > a.n ? a.n : e;
+  return {b, e - b};
+}
+// First chunk slot of a window: chunks of different windows never share a slot, since a window of
+// m rows from row b has at most floor((b + m) / 64) - floor(b / 64) + 1 chunks, and no scan over
+// the windows is needed to place them.
+__device__ __forceinline__ uint32_t first_slot(int begin, int w) { return (uint32_t)begin / kChunk + (uint32_t)w; }
+
+// Original row of position p (order: the caller's, clamped so that nothing is read out of range).
+__device__ __forceinline__ int row_at(const Args& a, int p) {
+  if (a.order == nullptr) return p;
+  const int r = a.order[p];
+  return r < 0 ? 0 : r >= a.n ? a.n - 1 : r;
+}
+
+// ------------------------------------------------------------------ operands
+struct Pair {
+  half8_t hi, lo;
+};
+
+__device__ __forceinline__ floatx4 mma(half8_t a, half8_t b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// products with both operands in two terms; the lo lo term is below 2^-22 of the product
+__device__ __forceinline__ floatx4 mma2(const Pair& a, const Pair& b, floatx4 c) {
+  c = mma(a.lo, b.hi, c);
+  c = mma(a.hi, b.lo, c);
+  return mma(a.hi, b.hi, c);
+}
+__device__ __forceinline__ floatx4 mma1(half8_t a, const Pair& b, floatx4 c) {
+  c = mma(a, b.lo, c);
+  return mma(a, b.hi, c);
+}
+__device__ __forceinline__ floatx4 mma1(const Pair& a, half8_t b, floatx4 c) {
+  c = mma(a.lo, b, c);
+  return mma(a.hi, b, c);
+}
+
+// x scaled by s as two fp16 terms
+__device__ __forceinline__ Pair split(const floatx4& x0, const floatx4& x1, float s) {
+  Pair p;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float y0 = x0[r] * s, y1 = x1[r] * s;
+    p.hi[r] = (_Float16)y0;
+    p.hi[4 + r] = (_Float16)y1;
+    p.lo[r] = (_Float16)(y0 - (float)p.hi[r]);
+    p.lo[4 + r] = (_Float16)(y1 - (float)p.hi[4 + r]);
+  }
+  return p;
+}
+
+// Largest value of the wave of a lane's non-negative m; a lane with an infinity or a NaN does not
+// count (its column is lost, the others keep their scale).
+__device__ __forceinline__ uint32_t wave_max_bits(float m) {
+  uint32_t b = __float_as_uint(m);
+  b = b >= 0x7f800000u ? 0u : b;
+  auto step = [&](int v) {
+    const uint32_t o = (uint32_t)v;
+    b = o > b ? o : b;
+  };
+  step(__builtin_amdgcn_mov_dpp((int)b, 0x128, 0xf, 0xf, false));   // row_ror:8
+  step(__builtin_amdgcn_mov_dpp((int)b, 0x124, 0xf, 0xf, false));
+  step(__builtin_amdgcn_mov_dpp((int)b, 0x122, 0xf, 0xf, false));
+  step(__builtin_amdgcn_mov_dpp((int)b, 0x121, 0xf, 0xf, false));
+  const uint32_t r0 = __builtin_amdgcn_readlane(b, 0), r1 = __builtin_amdgcn_readlane(b, 16);
+  const uint32_t r2 = __builtin_amdgcn_readlane(b, 32), r3 = __builtin_amdgcn_readlane(b, 48);
+  const uint32_t x = r0 > r1 ? r0 : r1, y = r2 > r3 ? r2 : r3;
+  return x > y ? x : y;
+}
+
+// The power of two that puts a largest value with these bits into [2^13, 2^14), and its inverse.
+// At 2^14 the products of 64 terms stay far inside fp32, and a value has its 22 bits down to 2^-17
+// of the largest.
+struct Scale {
+  float up, down;
+};
+__device__ __forceinline__ Scale scale_of(uint32_t max_bits) {
+  const int e = (int)(max_bits >> 23);
+  const int s = 267 - e < 240 ? 267 - e : 240;
+  return {__uint_as_float((uint32_t)s << 23), __uint_as_float((uint32_t)(254 - s) << 23)};
+}
+
+template <int N>
+__device__ __forceinline__ Scale scale_for(const floatx4 (&x)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[t][r]));
+  return scale_of(wave_max_bits(m));
+}
+
+// ------------------------------------------------------------------ images
+// Half index of (row, column) in the image of a 64 x DK matrix: operands of 16 rows x 32 columns
+// in the matrix cores' order (lane (i, g) holds row i, columns 8g .. 8g + 7), the rows of lane
+// group g turned by 4g, so that the transpose reads of 4 rows x 4 column groups fall into
+// different banks.
+template <int DK>
+__device__ __forceinline__ int image_at(int row, int kb, int g) {
+  return (((row >> 4) * (DK / 32) + kb) * 64 + g * 16 + (((row & 15) + 4 * g) & 15)) * 8;
+}
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+// rows of tile `tau`, columns 32 kb .. + 31: contraction over columns
+template <int DK>
+__device__ __forceinline__ half8_t image_rows(const _Float16* img, int tau, int kb, int i, int g) {
+  return *reinterpret_cast<const half8_t*>(img + image_at<DK>(16 * tau + i, kb, g));
+}
+// Columns as rows: operand row m stands for column 32 t + 8 (m / 4) + 4 p + m % 4 (the order in
+// which the state's tiles hold their rows), contraction over rows 32 s .. 32 s + 31, element e of
+// lane group g standing for row 32 s + 16 (e / 4) + 4 g + e % 4 (the order in which two 16-row
+// result tiles make one operand).  Lane j of 16 addresses row j / 4 and column group j % 4 of a
+// 4 x 16 block and receives column j of its four rows.
+template <int DK>
+__device__ __forceinline__ half8_t image_cols(const _Float16* img, int t, int p, int s, int i, int g) {
+  half8_t x;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const _Float16* at = img + image_at<DK>(32 * s + 16 * h + 4 * g + (i >> 2), t, i & 3) + 4 * p;
+    const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(at)));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[4 * h + r] = __builtin_bit_cast(_Float16, (short)y[r]);
+  }
+  return x;
+}
+// number of the triangle's operand for row tile tau and column block s
+__device__ __forceinline__ constexpr int tri_at(int tau, int s) { return tau < 2 ? tau : 2 * tau - 2 + s; }
+
+// ------------------------------------------------------------------ storage types
+template <typename T>
+__device__ __forceinline__ float load1(const T* p) {
+  if constexpr (std::is_same<T, float>::value) return *p;
+  else return u16_to_f32<T>(*reinterpret_cast<const unsigned short*>(p));
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const floatx4& x) {
+  if constexpr (std::is_same<T, float>::value) {
+    *reinterpret_cast<floatx4*>(p) = x;
+  } else {
+    u16x4 y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = f32_to_u16<T>(x[r]);
+    *reinterpret_cast<u16x4*>(p) = y;
+  }
+}
+template <typename T>
+constexpr int kTerms = std::is_same<T, float>::value ? 2 : 1;
+
+}  // namespace delta
+}  // namespace sla

@@ -1,0 +1,60 @@
+// The gated delta rule in chunk form, forward (sla_delta.h has the mathematics).  Two launches:
+// k_delta_prep makes T and P of every chunk, k_delta_walk goes through every window's chunks.
+#include "sla_delta_chunk.h"
+
+namespace sla {
+namespace {
+
+using namespace delta;
+
+template <typename T, int DK>
+hipError_t forward_impl(const Args& a, int dtype, const void* q, const void* k, const void* v, const float* g,
+                        const float* beta, const float* state_in, void* o, float* state_out, void* workspace,
+                        hipStream_t stream) {
+  const Space sp = space_of(a.n, a.W, dtype, a.Hk, a.H, a.dk, 2);
+  char* ws = static_cast<char*>(workspace);
+  _Float16* images = reinterpret_cast<_Float16*>(ws + sp.images);
+  _Float16* tri = reinterpret_cast<_Float16*>(ws + sp.tri);
+  float* scal = reinterpret_cast<float*>(ws + sp.scal);
+  if (a.n > 0)
+    k_delta_prep<T, DK, false><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
+        a, static_cast<const T*>(q), static_cast<const T*>(k), g, beta, images, tri, scal);
+  const int groups = a.dv / 16, waves = groups < 4 ? groups : 4;
+  k_delta_walk<T, DK, false><<<dim3(a.W, a.H, (groups + waves - 1) / waves), 64 * waves, 0, stream>>>(
+      a, static_cast<const T*>(v), state_in, images, tri, 2, scal, static_cast<T*>(o), nullptr,
+      WalkOut{state_out, nullptr, nullptr, nullptr});
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward_dk(const Args& a, int dtype, const void* q, const void* k, const void* v, const float* g,
+                      const float* beta, const float* state_in, void* o, float* state_out, void* workspace,
+                      hipStream_t stream) {
+  switch (pad_dk(a.dk)) {
+    case 32: return forward_impl<T, 32>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
+    case 64: return forward_impl<T, 64>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
+    default: return forward_impl<T, 128>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
+  }
+}
+
+}  // namespace
+
+size_t delta_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv) {
+  (void)dv;
+  return space_of(n, W, dtype, Hk, H, dk, 2).total;
+}
+
+hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,
+                                int32_t Hk, int32_t H, int32_t dk, int32_t dv, float scale, const void* q,
+                                const void* k, const void* v, const float* g, const float* beta,
+                                const float* state_in, void* o, float* state_out, void* workspace,
+                                hipStream_t stream) {
+  const Args a{offsets, order, n, W, Hk, H, dk, dv, scale, (uint32_t)slots_of(n, W)};
+  if (dtype == 0)
+    return forward_dk<float>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
+  if (dtype == 1)
+    return forward_dk<_Float16>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
+  return forward_dk<bf16_t>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
+}
+
+}  // namespace sla

@@ -1,0 +1,509 @@
+// The chunk form's two forward kernels: T and P of every chunk, and the walk through a window's
+// chunks.  Included by the forward and by the backward, which makes the states again.
+#pragma once
+
+#include "sla_delta.h"
+
+namespace sla {
+namespace delta {
+
+constexpr int kLd = 68;   // floats a row of a 64 x 64 matrix in LDS: 16-byte rows, banks turned by 4
+
+// ------------------------------------------------------------------ T and P
+// Per chunk and query/key head, 256 threads: k' and q' into LDS in operand order (and into the
+// workspace: the walk stages them from there as they are), k'k'^T and q'k'^T lower tiles one tile
+// row per wave, then for each value head of the group the decays, the inverse and the two
+// triangles.  The inverse of the unit lower triangular 64 x 64 matrix goes by 16 x 16 blocks: the
+// four diagonal ones by substitution (one wave each, a column a lane), the others, diagonal after
+// diagonal, as X_ij = -X_ii sum_k N_ik X_kj on the fp32 matrix cores.
+//
+// REV: also the transposed triangles for the reverse walk, with the inverse of
+// I + [beta_i D_ij k_i . k_j], whose rows and not columns carry beta.
+struct PrepShared {
+  float n[kChunk * kLd];
+  float x[kChunk * kLd];
+};
+
+__device__ __forceinline__ floatx4 mma_f32(const floatx4& a, const floatx4& b, floatx4 c) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
+  return c;
+}
+
+// x = (I + n)^-1 for strictly lower n; upper blocks of x that the operands read become zero.
+__device__ __forceinline__ void invert(PrepShared& s, int wave, int i, int g) {
+  {
+    float col[16];
+#pragma unroll
+    for (int a = 0; a < 16; ++a) {
+      const float* row = s.n + (16 * wave + a) * kLd + 16 * wave;
+      float sum = a == i ? 1.f : 0.f;
+#pragma unroll
+      for (int b = 0; b < a; ++b) sum -= row[b] * col[b];
+      col[a] = sum;
+    }
+#pragma unroll
+    for (int a = 0; a < 16; ++a)
+      if ((a >> 2) == g) s.x[(16 * wave + a) * kLd + 16 * wave + i] = col[a];
+    if ((wave & 1) == 0)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s.x[(16 * wave + 4 * g + r) * kLd + 16 * (wave + 1) + i] = 0.f;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int d = 1; d < 4; ++d) {
+    if (wave < 4 - d) {
+      const int bi = wave + d, bj = wave;
+      floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+      for (int k = bj; k < bi; ++k) {
+        const floatx4 a = *reinterpret_cast<const floatx4*>(s.n + (16 * bi + i) * kLd + 16 * k + 4 * g);
+        floatx4 b;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) b[r] = s.x[(16 * k + 4 * g + r) * kLd + 16 * bj + i];
+        sum = mma_f32(a, b, sum);
+      }
+      floatx4 a = *reinterpret_cast<const floatx4*>(s.x + (16 * bi + i) * kLd + 16 * bi + 4 * g);
+      floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+      sum = mma_f32(a, sum, zero);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s.x[(16 * bi + 4 * g + r) * kLd + 16 * bj + i] = -sum[r];
+    }
+    __syncthreads();
+  }
+}
+
+// The triangle's operands of tile row `tau` out of a matrix in LDS: rows as operand rows, columns
+// in the order of two stacked result tiles.
+__device__ __forceinline__ void put_tri(const float* m, _Float16* out, int tau, int lane, int i, int g) {
+  for (int s = 0; s <= tau / 2; ++s) {
+    const floatx4 x0 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 4 * g);
+    const floatx4 x1 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 16 + 4 * g);
+    const Pair p = split(x0, x1, kTriUp);
+    _Float16* at = out + 2 * tri_at(tau, s) * kFrag + lane * 8;
+    *reinterpret_cast<half8_t*>(at) = p.hi;
+    *reinterpret_cast<half8_t*>(at + kFrag) = p.lo;
+  }
+}
+// The transposed matrix's operands of tile row `tau`: upper triangular, kept under the mirrored
+// numbers (row tile 3 - tau, column block 1 - s).
+__device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, int tau, int lane, int i, int g) {
+  for (int s = tau / 2; s < 2; ++s) {
+    floatx4 x0, x1;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      x0[r] = m[(32 * s + 4 * g + r) * kLd + 16 * tau + i];
+      x1[r] = m[(32 * s + 16 + 4 * g + r) * kLd + 16 * tau + i];
+    }
+    const Pair p = split(x0, x1, kTriUp);
+    _Float16* at = out + 2 * tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
+    *reinterpret_cast<half8_t*>(at) = p.hi;
+    *reinterpret_cast<half8_t*>(at + kFrag) = p.lo;
+  }
+}
+
+template <typename T, int DK, bool REV>
+__global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict__ q, const T* __restrict__ k,
+                                                    const float* __restrict__ gin, const float* __restrict__ beta,
+                                                    _Float16* __restrict__ images, _Float16* __restrict__ tri,
+                                                    float* __restrict__ scal) {
+  constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK;
+  constexpr size_t kImages = (size_t)2 * NT * IMG * 2;
+  __shared__ __attribute__((aligned(16))) char s_mem[kImages > sizeof(PrepShared) ? kImages : sizeof(PrepShared)];
+  __shared__ double s_gam[kChunk];
+  __shared__ int s_cut[kChunk];
+  __shared__ float s_beta[kChunk], s_vs[kChunk], s_os[kChunk];
+  _Float16* s_img = reinterpret_cast<_Float16*>(s_mem);
+  PrepShared& sm = *reinterpret_cast<PrepShared*>(s_mem);
+
+  const uint32_t slot = blockIdx.x;
+  const int hk = blockIdx.y;
+  // the window of this slot: first slots grow with the window
+  int lo = 0, hi = a.W;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_slot(window(a, mid).begin, mid) <= slot) lo = mid;
+    else hi = mid;
+  }
+  const Win win = window(a, lo);
+  const uint32_t f = first_slot(win.begin, lo);
+  if (slot < f || (int64_t)(slot - f) * kChunk >= win.rows) return;
+  const int base = win.begin + (int)(slot - f) * kChunk;
+  const int rows = min(kChunk, win.rows - (int)(slot - f) * kChunk);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+  {
+    const int row = tid >> 2, gg = tid & 3;
+    const bool real = row < rows;
+    const int r = real ? row_at(a, base + row) : 0;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {   // 0: q, 1: k
+      const T* src = (which ? k : q) + ((size_t)r * a.Hk + hk) * a.dk;
+      float x[KB][8];
+      float m = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const int c = 32 * kb + 8 * gg;
+        Raw<T, 8> raw = Frag<T, 8>::zero();
+        if (real && c < a.dk) raw = *reinterpret_cast<const Raw<T, 8>*>(src + c);
+        Frag<T, 8>::to_f32(raw, x[kb]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[kb][e]));
+      }
+      m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0xB1, 0xf, 0xf, false)));
+      m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x4E, 0xf, 0xf, false)));
+      int e2 = (int)(__float_as_uint(m) >> 23) - 127;
+      e2 = m == 0.f || e2 > 127 ? 0 : e2 < -60 ? -60 : e2 > 60 ? 60 : e2;
+      const float down = __uint_as_float((uint32_t)(127 - e2) << 23), up = __uint_as_float((uint32_t)(127 + e2) << 23);
+      _Float16* img = s_img + which * NT * IMG;
+      _Float16* gimg = images + (((size_t)slot * a.Hk + hk) * 2 + which) * NT * IMG;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        half8_t h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = x[kb][e] * down;
+          h[e] = (_Float16)y;
+          if constexpr (NT == 2) l[e] = (_Float16)(y - (float)h[e]);
+        }
+        const int at = image_at<DK>(row, kb, gg);
+        *reinterpret_cast<half8_t*>(img + at) = h;
+        *reinterpret_cast<half8_t*>(gimg + at) = h;
+        if constexpr (NT == 2) {
+          *reinterpret_cast<half8_t*>(img + IMG + at) = l;
+          *reinterpret_cast<half8_t*>(gimg + IMG + at) = l;
+        }
+      }
+      if (gg == 0) {
+        if (which) s_vs[row] = down;
+        else s_os[row] = up;
+      }
+    }
+  }
+  __syncthreads();
+
+  // lower tiles of k'k'^T and q'k'^T, tile row `wave`
+  floatx4 kk[4], qk[4];
+  const _Float16 *qi = s_img, *ki = s_img + NT * IMG;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    kk[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    qk[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (j > wave) continue;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const half8_t kr = image_rows<DK>(ki, wave, kb, i, g), qr = image_rows<DK>(qi, wave, kb, i, g);
+      const half8_t kc = image_rows<DK>(ki, j, kb, i, g);
+      if constexpr (NT == 2) {
+        const half8_t krl = image_rows<DK>(ki + IMG, wave, kb, i, g), qrl = image_rows<DK>(qi + IMG, wave, kb, i, g);
+        const half8_t kcl = image_rows<DK>(ki + IMG, j, kb, i, g);
+        kk[j] = mma(kr, kcl, mma(krl, kc, kk[j]));
+        qk[j] = mma(qr, kcl, mma(qrl, kc, qk[j]));
+      }
+      kk[j] = mma(kr, kc, kk[j]);
+      qk[j] = mma(qr, kc, qk[j]);
+    }
+  }
+  __syncthreads();   // the images' place is the matrices' from here
+
+  const int group = a.H / a.Hk;
+  for (int hv = 0; hv < group; ++hv) {
+    const int h = hk * group + hv;
+    const size_t sh = (size_t)slot * a.H + h;
+    if (wave == 0) {
+      // log decays summed in 64 bits: their differences are small where they are large.  A decay of
+      // zero (g below -104, -infinity) starts a new stretch, over which nothing is carried.
+      const bool real = lane < rows;
+      const size_t at = real ? (size_t)row_at(a, base + lane) * a.H + h : 0;
+      const float g1 = real ? gin[at] : 0.f, b1 = real ? beta[at] : 0.f;
+      const bool cut1 = g1 < -104.f;
+      double gam = cut1 ? 0.0 : (double)g1;
+      int cut = cut1 ? 1 : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const double og = __shfl_up(gam, d);
+        const int oc = __shfl_up(cut, d);
+        if (lane >= d) gam += og, cut += oc;
+      }
+      const float vs = s_vs[lane];
+      const float bp = b1 / vs / vs;   // powers of two
+      s_gam[lane] = gam;
+      s_cut[lane] = cut;
+      s_beta[lane] = bp;
+      const double last = __shfl(gam, 63);
+      const int lcut = __shfl(cut, 63);
+      float* sc = scal + sh * kScal;
+      sc[kSince + lane] = real && cut == 0 ? expf((float)gam) : 0.f;
+      sc[kBeta + lane] = bp;
+      sc[kUntil + lane] = real && cut == lcut ? expf((float)(last - gam)) : 0.f;
+      sc[kVScale + lane] = vs;
+      sc[kOScale + lane] = s_os[lane] * a.scale;
+      if (lane == 0) sc[kLast] = lcut == 0 ? expf((float)last) : 0.f;
+    }
+    __syncthreads();
+    floatx4 p[4], b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = 16 * j + i;
+      const double gc = s_gam[col];
+      const int cc = s_cut[col];
+      const float bc = s_beta[col];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * wave + 4 * g + r;
+        const bool low = j <= wave && row >= col && s_cut[row] == cc;
+        const float d = low ? expf((float)(s_gam[row] - gc)) : 0.f;
+        p[j][r] = low ? d * qk[j][r] : 0.f;
+        b[j][r] = low && row > col ? d * kk[j][r] : 0.f;
+        sm.n[row * kLd + col] = b[j][r] * bc;
+      }
+    }
+    __syncthreads();
+    invert(sm, wave, i, g);
+    _Float16* out = tri + sh * (size_t)((REV ? 4 : 2) * kTriHalfs);
+    put_tri(sm.x, out, wave, lane, i, g);
+    if constexpr (REV) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * wave + 4 * g + r;
+          sm.n[row * kLd + 16 * j + i] = b[j][r] * s_beta[row];
+        }
+      __syncthreads();
+      invert(sm, wave, i, g);
+      put_tri_t(sm.x, out + 2 * kTriHalfs, wave, lane, i, g);
+    }
+    // every wave is past its reads of n (the inverse's last barrier)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = p[j][r];
+    __syncthreads();
+    put_tri(sm.n, out + kTriHalfs, wave, lane, i, g);
+    if constexpr (REV) put_tri_t(sm.n, out + 3 * kTriHalfs, wave, lane, i, g);
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ the walk
+// A wave holds 16 of the state's dv columns in registers, as result tiles: tile 2t + p, component r
+// of lane (i, g) is state row 32 t + 8 g + 4 p + r, column i.  Two tiles are then an operand of the
+// products with k' and q' without moving a value, and so are the chunk's r and u (16 rows a tile);
+// the columns are independent of each other, so no wave waits for another but for the staging.
+struct WalkOut {
+  float* state_out;    // final states or null
+  float* states;       // the states before every chunk, in register order, or null
+  float* resid;        // r' of every chunk row [slot][H][64][dv], or null
+  float* odo;          // sums over 16 columns of o dout [slot][H][dv / 16][64], or null
+};
+
+template <typename T, int DK, bool KEEP>
+__global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict__ v, const float* __restrict__ state_in,
+                                                    const _Float16* __restrict__ images,
+                                                    const _Float16* __restrict__ tri, int tris,
+                                                    const float* __restrict__ scal, T* __restrict__ o,
+                                                    const T* __restrict__ dout, WalkOut out) {
+  constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
+  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG];
+  __shared__ __attribute__((aligned(16))) _Float16 s_tri[2 * kTriHalfs];
+  __shared__ __attribute__((aligned(16))) float s_scal[kScal];
+
+  const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int threads = blockDim.x;
+  const int cg = blockIdx.z * (threads >> 6) + (tid >> 6);
+  const bool live = 16 * cg < a.dv;
+  const int col = 16 * cg + i;
+  const Win win = window(a, w);
+  const uint32_t slot0 = first_slot(win.begin, w);
+
+  floatx4 S[ST];
+#pragma unroll
+  for (int t = 0; t < ST; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
+      S[t][r] = state_in != nullptr && live && d < a.dk ? state_in[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] : 0.f;
+    }
+  bool carried = state_in != nullptr;   // no products with a state that is zero
+
+  for (int c0 = 0; c0 < win.rows; c0 += kChunk) {
+    const uint32_t slot = slot0 + c0 / kChunk;
+    const int rows = min(kChunk, win.rows - c0);
+    const size_t sh = (size_t)slot * a.H + h;
+    __syncthreads();
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
+      uint4* dst = reinterpret_cast<uint4*>(s_img);
+      for (int x = tid; x < 2 * NT * IMG / 8; x += threads) dst[x] = src[x];
+      const uint4* st = reinterpret_cast<const uint4*>(tri + sh * (size_t)tris * kTriHalfs);
+      uint4* dt = reinterpret_cast<uint4*>(s_tri);
+      for (int x = tid; x < 2 * kTriHalfs / 8; x += threads) dt[x] = st[x];
+      const uint4* ss = reinterpret_cast<const uint4*>(scal + sh * kScal);
+      uint4* ds = reinterpret_cast<uint4*>(s_scal);
+      for (int x = tid; x < kScal / 4; x += threads) ds[x] = ss[x];
+    }
+    floatx4 Y[4];
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * tau + 4 * g + r;
+        Y[tau][r] = 0.f;
+        if (live && row < rows) {
+          const size_t at = (size_t)row_at(a, win.begin + c0 + row) * a.H + h;
+          Y[tau][r] = load1(v + at * a.dv + col);
+        }
+      }
+    __syncthreads();
+    if (!live) continue;
+    const _Float16 *qi = s_img, *ki = s_img + NT * IMG, *st = s_tri, *sp = s_tri + kTriHalfs;
+    auto row4 = [&](int what, int tau) {
+      return *reinterpret_cast<const floatx4*>(s_scal + what + 16 * tau + 4 * g);
+    };
+
+    if constexpr (KEEP) {
+      float* at = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(at + t * 256) = S[t];
+    }
+    // y = 2^-kap v - exp(gam) k' S
+    Pair Sp[KB];
+    Scale sc = {1.f, 1.f};
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau) {
+      const floatx4 vs = row4(kVScale, tau);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) Y[tau][r] *= vs[r];
+    }
+    if (carried) {
+      sc = scale_for(S);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const half8_t kr = image_rows<DK>(ki, tau, kb, i, g);
+          if constexpr (NT == 2) x = mma(image_rows<DK>(ki + IMG, tau, kb, i, g), Sp[kb].hi, x);
+          x = mma1(kr, Sp[kb], x);
+        }
+        const floatx4 since = row4(kSince, tau);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Y[tau][r] -= since[r] * (x[r] * sc.down);
+      }
+    }
+    // r = T y, u = beta' r
+    floatx4 U[4];
+    {
+      const Scale sy = scale_for(Y);
+      const float ydown = sy.down * (1.f / kTriUp);
+      Pair Yp[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) Yp[s] = split(Y[2 * s], Y[2 * s + 1], sy.up);
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s <= tau / 2; ++s) {
+          const _Float16* at = st + 2 * tri_at(tau, s) * kFrag + lane * 8;
+          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
+          x = mma2(t, Yp[s], x);
+        }
+        const floatx4 be = row4(kBeta, tau);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float y = x[r] * ydown;
+          if constexpr (KEEP) out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = y;
+          U[tau][r] = be[r] * y;
+        }
+      }
+    }
+    // o, transposed: a lane holds 4 columns of one row
+    {
+      const Scale su = scale_for(U);
+      const float udown = su.down * (1.f / kTriUp);
+      Pair Up[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) Up[s] = split(U[2 * s], U[2 * s + 1], su.up);
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
+        if (carried) {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) {
+            const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
+            if constexpr (NT == 2) x = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), x);
+            x = mma1(Sp[kb], qr, x);
+          }
+        }
+#pragma unroll
+        for (int s = 0; s <= tau / 2; ++s) {
+          const _Float16* at = sp + 2 * tri_at(tau, s) * kFrag + lane * 8;
+          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
+          y = mma2(Up[s], t, y);
+        }
+        const int row = 16 * tau + i;
+        const float since = s_scal[kSince + row] * sc.down, os = s_scal[kOScale + row];
+        floatx4 z;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[r] = os * (since * x[r] + udown * y[r]);
+        if constexpr (!KEEP) {
+          if (row < rows) {
+            const size_t at = (size_t)row_at(a, win.begin + c0 + row) * a.H + h;
+            store4(o + at * a.dv + 16 * cg + 4 * g, z);
+          }
+        } else {
+          float dot = 0.f;
+          if (row < rows) {
+            const size_t at = (size_t)row_at(a, win.begin + c0 + row) * a.H + h;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot += z[r] * load1(dout + at * a.dv + 16 * cg + 4 * g + r);
+          }
+          dot += __shfl_xor(dot, 16);
+          dot += __shfl_xor(dot, 32);
+          if (g == 0) out.odo[(sh * (a.dv / 16) + cg) * kChunk + row] = dot;
+        }
+      }
+    }
+    // S = exp(gam_last) S + k'^T (until u)
+    {
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        const floatx4 un = row4(kUntil, tau);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) U[tau][r] *= un[r];
+      }
+      const Scale su = scale_for(U);
+      Pair Up[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) Up[s] = split(U[2 * s], U[2 * s + 1], su.up);
+      const float last = s_scal[kLast];
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          if constexpr (NT == 2) x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s, i, g), Up[s].hi, x);
+          x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s, i, g), Up[s], x);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][r] = last * S[t][r] + su.down * x[r];
+      }
+      carried = true;
+    }
+  }
+  if (out.state_out != nullptr && live)
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
+        if (d < a.dk) out.state_out[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] = S[t][r];
+      }
+}
+
+}  // namespace delta
+}  // namespace sla

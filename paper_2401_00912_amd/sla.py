@@ -20,6 +20,8 @@ Functions mirror the C ABI in include/sla.h:
     cwi_backward(map, grid, coords, x, w_x, w_y, w_3, dy, order=None) -> (dx, dw_x, dw_y, dw_3)
     scatter_workspace_bytes(n, heads, head_dim)
     forward_scatter(plan, q, k, v, out=None, workspace=None) -> o   (naive comparator)
+    forward_delta(q, k, v, g, beta, offsets, scale=None, order=None, state=None) -> (o, final_state)
+    step_delta(state, slots, q, k, v, g, beta, scale=None) -> o
 """
 from __future__ import annotations
 
@@ -59,6 +61,9 @@ EXPORTED = (
     "sla_xca_backward_workspace_bytes",
     "sla_backward_xca",
     "sla_backward_xca_noalloc",
+    "sla_delta_workspace_bytes",
+    "sla_forward_delta",
+    "sla_step_delta",
 )
 
 
@@ -146,6 +151,12 @@ def lib() -> ctypes.CDLL:
     L.sla_backward_xca.restype = ctypes.c_int
     L.sla_backward_xca.argtypes = [vp, sz, i64, i32, ctypes.c_int, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                    vp, sz, vp]
+    L.sla_delta_workspace_bytes.restype = sz
+    L.sla_delta_workspace_bytes.argtypes = [i64, i32, en, i32, i32, i32, i32]
+    L.sla_forward_delta.restype = ctypes.c_int
+    L.sla_forward_delta.argtypes = [vp, i64, i32, vp, en, i32, i32, i32, i32, f32] + [vp] * 9 + [sz, vp]
+    L.sla_step_delta.restype = ctypes.c_int
+    L.sla_step_delta.argtypes = [vp, i64, i32, en, i32, i32, i32, i32, f32] + [vp] * 8
     _lib = L
     return L
 
@@ -620,6 +631,101 @@ def forward_scatter(plan: Plan, q, k, v, out=None, workspace=None):
                                    _ptr(workspace), int(workspace.numel() * workspace.element_size()),
                                    _stream(q.device))
     _check(st, "sla_forward_scatter")
+    return out
+
+
+def _check_like(name, t, shape, dtype, device):
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device
+                          or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} {dtype} tensor on the inputs' device")
+
+
+def _delta_check(q, k, v, g, beta):
+    """Shapes, dtypes, devices and layouts of the rows of a gated delta rule call:
+    (n, heads_qk, heads, dim_k, dim_v)."""
+    torch = _torch()
+    if q.dim() != 3 or v.dim() != 3 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous [n, heads_qk, dim_k] tensor and v [n, heads, dim_v]")
+    (n, hk, dk), (h, dv) = q.shape, v.shape[1:]
+    _check_like("k", k, (n, hk, dk), q.dtype, q.device)
+    _check_like("v", v, (n, h, dv), q.dtype, q.device)
+    _check_like("g", g, (n, h), torch.float32, q.device)
+    _check_like("beta", beta, (n, h), torch.float32, q.device)
+    if hk < 1 or h < 1 or h % hk:
+        raise ValueError("heads must be a multiple of heads_qk")
+    return n, hk, h, dk, dv
+
+
+def _check_windows(offsets, order, n, device):
+    torch = _torch()
+    if offsets.dim() != 1 or offsets.numel() < 2 or offsets.dtype != torch.int32 or not offsets.is_contiguous() \
+            or offsets.device != device:
+        raise ValueError("offsets must be a contiguous int32 [num_windows + 1] tensor on the inputs' device")
+    _check_like("order", order, (n,), torch.int32, device)
+    return offsets.numel() - 1
+
+
+def delta_workspace_bytes(n: int, num_windows: int, dtype, heads_qk: int, heads: int, dim_k: int, dim_v: int) -> int:
+    """Workspace of forward_delta (0: unsupported sizes); dtype a torch dtype."""
+    return int(lib().sla_delta_workspace_bytes(int(n), int(num_windows), _dtype_code(dtype), int(heads_qk),
+                                               int(heads), int(dim_k), int(dim_v)))
+
+
+def _delta_workspace(need, workspace, device, what):
+    if need == 0:
+        raise SlaError(SLA_E_UNSUPPORTED, what)
+    if workspace is None:
+        workspace = _torch().empty(need, dtype=_torch().uint8, device=device)
+    _check_workspace(workspace, device)
+    return workspace, int(workspace.numel() * workspace.element_size())
+
+
+def forward_delta(q, k, v, g, beta, offsets, scale=None, order=None, state=None, out=None, final_state=None,
+                  workspace=None):
+    """The gated delta rule over the rows of every window (sla_forward_delta): q, k
+    [n, heads_qk, dim_k], v [n, heads, dim_v], g (log decay) and beta float32 [n, heads],
+    offsets int32 [num_windows + 1], order an int32 [n] row of every position or None (a
+    plan's offsets and perm), scale dim_k ** -0.5 by default, state float32
+    [num_windows, heads, dim_k, dim_v] or None (zero).  Returns (o, final_state); rows in
+    no window are left as they were in out."""
+    torch = _torch()
+    n, hk, h, dk, dv = _delta_check(q, k, v, g, beta)
+    w = _check_windows(offsets, order, n, q.device)
+    out = torch.empty_like(v) if out is None else out
+    _check_like("out", out, v.shape, q.dtype, q.device)
+    if final_state is None:
+        final_state = torch.empty((w, h, dk, dv), dtype=torch.float32, device=q.device)
+    for name, t in (("state", state), ("final_state", final_state)):
+        _check_like(name, t, (w, h, dk, dv), torch.float32, q.device)
+    workspace, nbytes = _delta_workspace(delta_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace, q.device,
+                                         "sla_delta_workspace_bytes")
+    with torch.cuda.device(q.device):
+        st = lib().sla_forward_delta(_ptr(offsets), n, w, _ptr(order), _dtype_code(q.dtype), hk, h, dk, dv,
+                                     float(dk ** -0.5 if scale is None else scale), _ptr(q), _ptr(k), _ptr(v),
+                                     _ptr(g), _ptr(beta), _ptr(state), _ptr(out), _ptr(final_state),
+                                     _ptr(workspace), nbytes, _stream(q.device))
+    _check(st, "sla_forward_delta")
+    return out, final_state
+
+
+def step_delta(state, slots, q, k, v, g, beta, scale=None, out=None):
+    """One row for each of many sequences (sla_step_delta): state float32
+    [num_slots, heads, dim_k, dim_v], updated in place, slots int32 [n] (rows of the same
+    slot follow each other in row order; a slot outside the pool marks a padding row), the
+    rows as in forward_delta.  Returns o, where padding rows are left as they were."""
+    torch = _torch()
+    n, hk, h, dk, dv = _delta_check(q, k, v, g, beta)
+    if state.dim() != 4 or state.shape[0] < 1:
+        raise ValueError("state must be a [num_slots, heads, dim_k, dim_v] tensor")
+    _check_like("state", state, (state.shape[0], h, dk, dv), torch.float32, q.device)
+    _check_like("slots", slots, (n,), torch.int32, q.device)
+    out = torch.empty_like(v) if out is None else out
+    _check_like("out", out, v.shape, q.dtype, q.device)
+    with torch.cuda.device(q.device):
+        st = lib().sla_step_delta(_ptr(slots), n, state.shape[0], _dtype_code(q.dtype), hk, h, dk, dv,
+                                  float(dk ** -0.5 if scale is None else scale), _ptr(state), _ptr(q), _ptr(k),
+                                  _ptr(v), _ptr(g), _ptr(beta), _ptr(out), _stream(q.device))
+    _check(st, "sla_step_delta")
     return out
 
 
