@@ -475,6 +475,28 @@ sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_wi
                                sla_stream_t stream);
 
 /*
+ * Backward of sla_forward_delta (the chain rule of the recurrence; the paper does not write it):
+ * given dout = dL/do and dstate_out = dL/d(state_out) (NULL: zero), writes dq, dk (summed over the
+ * value heads that share them, in head order), dv in `dtype`, dg, dbeta (fp32 [n, heads]) and, if not
+ * NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  Rows in no window are left as they were.
+ * The gradient of a log decay whose exp underflows is zero.  States are made again from the inputs.
+ * Other arguments, limits and errors as sla_forward_delta; the outputs must not be inputs.
+ * `workspace` (256-byte aligned) has at least sla_delta_backward_workspace_bytes(...) bytes:
+ * the states and their gradients at every 64th row are most of it.  16-bit rows: the products that end
+ * in dq and dk alone have operands of 11 bits, all others 22.  Deterministic.
+ */
+size_t sla_delta_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                          int32_t heads_qk, int32_t heads, int32_t dim_k, int32_t dim_v);
+
+sla_status_t sla_backward_delta(const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order,
+                                sla_dtype_t dtype, int32_t heads_qk, int32_t heads, int32_t dim_k,
+                                int32_t dim_v, float scale, const void* q, const void* k, const void* v,
+                                const float* g, const float* beta, const float* state_in, const void* dout,
+                                const float* dstate_out, void* dq, void* dk, void* dv, float* dg,
+                                float* dbeta, float* dstate_in, void* workspace, size_t workspace_bytes,
+                                sla_stream_t stream);
+
+/*
  * The gated delta rule one row at a time: `state` is a pool of num_slots states
  * [num_slots, heads, dim_k, dim_v] (fp32, 16-byte aligned), row b of the batch belongs to the
  * sequence in slot slots[b] (int32 [n], device), whose state it updates in place, and o[b] receives

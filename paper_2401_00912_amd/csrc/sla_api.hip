@@ -60,6 +60,13 @@ hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, co
                                 const void* k, const void* v, const float* g, const float* beta,
                                 const float* state_in, void* o, float* state_out, void* workspace,
                                 hipStream_t stream);
+size_t delta_backward_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv);
+hipError_t launch_backward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,
+                                 int32_t Hk, int32_t H, int32_t dk, int32_t dv, float scale, const void* q,
+                                 const void* k, const void* v, const float* g, const float* beta,
+                                 const float* state_in, const void* dout, const float* dstate_out, void* dq,
+                                 void* dk_out, void* dv_out, float* dg, float* dbeta, float* dstate_in,
+                                 void* workspace, hipStream_t stream);
 hipError_t launch_step_delta(const int32_t* slots, int32_t n, int32_t num_slots, int dtype, int32_t Hk, int32_t H,
                              int32_t dk, int32_t dv, float scale, float* state, const void* q, const void* k,
                              const void* v, const float* g, const float* beta, void* o, hipStream_t stream);
@@ -521,6 +528,41 @@ SLA_EXPORT sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int
   return hip_status(sla::launch_forward_delta(offsets, (int32_t)n, num_windows, order, (int)dtype, heads_qk, heads,
                                               dim_k, dim_v, scale, q, k, v, g, beta, state_in, o, state_out,
                                               workspace, static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT size_t sla_delta_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                                     int32_t heads_qk, int32_t heads, int32_t dim_k, int32_t dim_v) {
+  if (check_delta_sizes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v) != SLA_OK) return 0;
+  return sla::delta_backward_workspace_bytes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v);
+}
+
+SLA_EXPORT sla_status_t sla_backward_delta(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                           const int32_t* order, sla_dtype_t dtype, int32_t heads_qk, int32_t heads,
+                                           int32_t dim_k, int32_t dim_v, float scale, const void* q, const void* k,
+                                           const void* v, const float* g, const float* beta, const float* state_in,
+                                           const void* dout, const float* dstate_out, void* dq, void* dk, void* dv,
+                                           float* dg, float* dbeta, float* dstate_in, void* workspace,
+                                           size_t workspace_bytes, sla_stream_t stream) {
+  const sla_status_t st = check_delta_sizes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v);
+  if (st != SLA_OK) return st;
+  if (!finite(scale)) return SLA_E_ARG;
+  if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !aligned(state_in, 4) || !aligned(dstate_out, 4) ||
+      !aligned(dstate_in, 4))
+    return SLA_E_ARG;
+  if (n == 0 && !dstate_in) return SLA_OK;
+  if (n > 0 && (!q || !k || !v || !g || !beta || !dout || !dq || !dk || !dv || !dg || !dbeta)) return SLA_E_ARG;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(dout, 16) || !aligned(dq, 16) ||
+      !aligned(dk, 16) || !aligned(dv, 16) || !aligned(g, 4) || !aligned(beta, 4) || !aligned(dg, 4) ||
+      !aligned(dbeta, 4))
+    return SLA_E_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  if (workspace_bytes <
+      sla::delta_backward_workspace_bytes(n, num_windows, (int)dtype, heads_qk, heads, dim_k, dim_v))
+    return SLA_E_WORKSPACE;
+  return hip_status(sla::launch_backward_delta(offsets, (int32_t)n, num_windows, order, (int)dtype, heads_qk, heads,
+                                               dim_k, dim_v, scale, q, k, v, g, beta, state_in, dout, dstate_out, dq,
+                                               dk, dv, dg, dbeta, dstate_in, workspace,
+                                               static_cast<hipStream_t>(stream)));
 }
 
 SLA_EXPORT sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,

@@ -22,7 +22,7 @@ hipError_t forward_impl(const Args& a, int dtype, const void* q, const void* k, 
   const int groups = a.dv / 16, waves = groups < 4 ? groups : 4;
   k_delta_walk<T, DK, false><<<dim3(a.W, a.H, (groups + waves - 1) / waves), 64 * waves, 0, stream>>>(
       a, static_cast<const T*>(v), state_in, images, tri, 2, scal, static_cast<T*>(o), nullptr,
-      WalkOut{state_out, nullptr, nullptr, nullptr});
+      WalkOut{state_out, nullptr, nullptr, nullptr, nullptr});
   return hipGetLastError();
 }
 

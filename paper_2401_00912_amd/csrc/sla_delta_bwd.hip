@@ -1,0 +1,696 @@
+// Backward of the gated delta rule in chunk form.  The paper trains its linear attentions but
+// writes no backward; this is the chain rule of the recurrence in sla.h.
+//
+// With D_ij, T, P, r, u of the forward (sla_delta.h), dS1 the gradient of the state after a chunk
+// and lam_j the whole gradient of u_j:
+//     du  = P^T (scale do) + exp(gam_last - gam) k dS1,
+//     lam = (I + [beta_i D_ij k_i . k_j]_{j < i})^-T du,   mu = beta lam  (= dv),
+//     dS0 = exp(gam_last) dS1 + scale (exp(gam) q)^T do - (exp(gam) k)^T mu,
+//     dbeta_j = lam_j . r_j,
+//     dq_i = scale (exp(gam_i) S0 do_i + sum_{j <= i} D_ij (do_i . u_j) k_j),
+//     dk_j = exp(gam_last - gam_j) dS1 u_j - exp(gam_j) S0 mu_j - sum_{i < j} D_ji (mu_j . u_i) k_i
+//            - sum_{i > j} D_ij (mu_i . u_j) k_i + scale sum_{i >= j} D_ij (do_i . u_j) q_i.
+// The decay's gradient needs no products of its own: dg_t is the inner product of the decayed state
+// and its gradient, and from one row to the next these differ by vectors that are at hand,
+//     dg_t = dg_{t+1} + o_t . do_t - v_t . dv_t,   and at a chunk's first row dg = <dS0, S0>,
+// which starts the sum anew in every chunk, so that it never runs over more than 64 rows.
+//
+// Four launches: T, P and their transposes (k_delta_prep); the forward walk, which keeps the states
+// before every chunk, r and o . do (k_delta_walk); the walk back, which keeps lam and the gradients
+// of the states after every chunk (k_delta_back); and, all chunks at once, everything that is no
+// recurrence (k_delta_grad).  States are made again and not kept from the forward: they are dk / 16
+// times as large as the rows.
+#include "sla_delta_chunk.h"
+
+namespace sla {
+namespace {
+
+using namespace delta;
+
+// Workspace behind the chunk form's: byte offsets.
+struct BackSpace {
+  Space base;
+  size_t states, dstates, resid, lam, odo, smax, dmax, start, total;
+};
+BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv) {
+  BackSpace s;
+  s.base = space_of(n, W, dtype, Hk, H, dk, 4);
+  const size_t sh = slots_of(n, W) * H, groups = dv / 16;
+  size_t at = s.base.total;
+  const auto take = [&](size_t floats) {
+    const size_t here = at;
+    at = align_up(at + floats * 4, 256);
+    return here;
+  };
+  s.states = take(sh * pad_dk(dk) * dv);
+  s.dstates = take(sh * pad_dk(dk) * dv);
+  s.resid = take(sh * kChunk * dv);
+  s.lam = take(sh * kChunk * dv);
+  s.odo = take(sh * groups * kChunk);
+  s.smax = take(sh * groups);
+  s.dmax = take(sh * groups);
+  s.start = take(sh * groups);
+  s.total = at;
+  return s;
+}
+
+// ------------------------------------------------------------------ the walk back
+// As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
+template <typename T, int DK>
+__global__ __launch_bounds__(256) void k_delta_back(Args a, const T* __restrict__ dout, const float* __restrict__ dstate,
+                                                    const _Float16* __restrict__ images,
+                                                    const _Float16* __restrict__ tri, const float* __restrict__ scal,
+                                                    const float* __restrict__ states, float* __restrict__ lam,
+                                                    float* __restrict__ dstates, float* __restrict__ dmax,
+                                                    float* __restrict__ start, float* __restrict__ dstate_in) {
+  constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
+  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG];
+  __shared__ __attribute__((aligned(16))) _Float16 s_tri[2 * kTriHalfs];
+  __shared__ __attribute__((aligned(16))) float s_scal[kScal];
+
+  const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int threads = blockDim.x;
+  const int cg = blockIdx.z * (threads >> 6) + (tid >> 6);
+  const bool live = 16 * cg < a.dv;
+  const int col = 16 * cg + i;
+  const Win win = window(a, w);
+  const uint32_t slot0 = first_slot(win.begin, w);
+
+  floatx4 S[ST];
+#pragma unroll
+  for (int t = 0; t < ST; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
+      S[t][r] = dstate != nullptr && live && d < a.dk ? dstate[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] : 0.f;
+    }
+  bool carried = dstate != nullptr;
+
+  for (int c = (win.rows + kChunk - 1) / kChunk - 1; c >= 0; --c) {
+    const uint32_t slot = slot0 + c;
+    const int rows = min(kChunk, win.rows - c * kChunk);
+    const size_t sh = (size_t)slot * a.H + h;
+    __syncthreads();
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
+      uint4* dst = reinterpret_cast<uint4*>(s_img);
+      for (int x = tid; x < 2 * NT * IMG / 8; x += threads) dst[x] = src[x];
+      const uint4* st = reinterpret_cast<const uint4*>(tri + (sh * 4 + 2) * kTriHalfs);
+      uint4* dt = reinterpret_cast<uint4*>(s_tri);
+      for (int x = tid; x < 2 * kTriHalfs / 8; x += threads) dt[x] = st[x];
+      const uint4* ss = reinterpret_cast<const uint4*>(scal + sh * kScal);
+      uint4* ds = reinterpret_cast<uint4*>(s_scal);
+      for (int x = tid; x < kScal / 4; x += threads) ds[x] = ss[x];
+    }
+    floatx4 Y[4];
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * tau + 4 * g + r;
+        Y[tau][r] = 0.f;
+        if (live && row < rows) {
+          const size_t at = (size_t)row_at(a, win.begin + c * kChunk + row) * a.H + h;
+          Y[tau][r] = load1(dout + at * a.dv + col);
+        }
+      }
+    __syncthreads();
+    if (!live) continue;
+    const _Float16 *qi = s_img, *ki = s_img + NT * IMG, *st = s_tri, *sp = s_tri + kTriHalfs;
+    auto row4 = [&](int what, int tau) {
+      return *reinterpret_cast<const floatx4*>(s_scal + what + 16 * tau + 4 * g);
+    };
+    const size_t sgrp = sh * (a.dv / 16) + cg;
+
+    uint32_t top = 0;
+    {
+      float m = 0.f;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        *reinterpret_cast<floatx4*>(dstates + sgrp * ST * 256 + t * 256 + lane * 4) = S[t];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[t][r]));
+      }
+      top = wave_max_bits(m);
+      if (lane == 0) dmax[sgrp] = __uint_as_float(top);
+    }
+    // du = P^T do' + until k' dS
+    floatx4 X[4];
+    {
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        const floatx4 os = row4(kOScale, tau);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Y[tau][r] *= os[r];
+      }
+      const Scale sy = scale_for(Y);
+      const float ydown = sy.down * (1.f / kTriUp);
+      Pair Yp[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) Yp[s] = split(Y[2 * s], Y[2 * s + 1], sy.up);
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = tau / 2; s < 2; ++s) {
+          const _Float16* at = sp + 2 * tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
+          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
+          x = mma2(t, Yp[s], x);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) X[tau][r] = x[r] * ydown;
+      }
+    }
+    if (carried) {
+      const Scale sc = scale_of(top);
+      Pair Sp[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const half8_t kr = image_rows<DK>(ki, tau, kb, i, g);
+          if constexpr (NT == 2) x = mma(image_rows<DK>(ki + IMG, tau, kb, i, g), Sp[kb].hi, x);
+          x = mma1(kr, Sp[kb], x);
+        }
+        const floatx4 un = row4(kUntil, tau);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) X[tau][r] += un[r] * (x[r] * sc.down);
+      }
+    }
+    // lam, then -since mu in X and since do' in Y
+    {
+      const Scale sx = scale_for(X);
+      const float xdown = sx.down * (1.f / kTriUp);
+      Pair Xp[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) Xp[s] = split(X[2 * s], X[2 * s + 1], sx.up);
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = tau / 2; s < 2; ++s) {
+          const _Float16* at = st + 2 * tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
+          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
+          x = mma2(t, Xp[s], x);
+        }
+        const floatx4 be = row4(kBeta, tau), since = row4(kSince, tau);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float y = x[r] * xdown;
+          lam[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = y;
+          X[tau][r] = -since[r] * (be[r] * y);
+          Y[tau][r] *= since[r];
+        }
+      }
+    }
+    // dS = exp(gam_last) dS + q'^T (since do') - k'^T (since mu)
+    {
+      float m = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, fmaxf(fabsf(X[t][r]), fabsf(Y[t][r])));
+      const Scale sc = scale_of(wave_max_bits(m));
+      Pair Xp[2], Yp[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        Xp[s] = split(X[2 * s], X[2 * s + 1], sc.up);
+        Yp[s] = split(Y[2 * s], Y[2 * s + 1], sc.up);
+      }
+      const float last = s_scal[kLast];
+      float dot = 0.f;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        const floatx4 s0 = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          if constexpr (NT == 2) {
+            x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s, i, g), Xp[s].hi, x);
+            x = mma(image_cols<DK>(qi + IMG, t >> 1, t & 1, s, i, g), Yp[s].hi, x);
+          }
+          x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s, i, g), Xp[s], x);
+          x = mma1(image_cols<DK>(qi, t >> 1, t & 1, s, i, g), Yp[s], x);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          S[t][r] = last * S[t][r] + sc.down * x[r];
+          dot += s0[r] * S[t][r];
+        }
+      }
+#pragma unroll
+      for (int m2 = 1; m2 < 64; m2 *= 2) dot += __shfl_xor(dot, m2);
+      if (lane == 0) start[sgrp] = dot;
+      carried = true;
+    }
+  }
+  if (dstate_in != nullptr && live)
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
+        if (d < a.dk) dstate_in[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] = S[t][r];
+      }
+}
+
+// ------------------------------------------------------------------ the rest, all chunks at once
+// A workgroup per chunk and query/key head, its value heads one after the other, their dq and dk
+// summed in registers (in head order: deterministic).  Wave w owns rows 16w .. 16w + 15, one a lane
+// (i) and four lane groups over the columns, and makes the transposed dq and dk tiles: a lane ends
+// with 8 neighbouring columns of its row.  The value columns go by in blocks of 32.
+//
+// Computed operands (states, mu, u, the products over columns) have two fp16 terms, and one, 2^-11
+// of a value, where dq and dk are bf16, whose own rounding is 8 times as coarse; dg and dbeta, which
+// are fp32, take nothing from these products.  With one term for fp16 rows too their dq and dk were
+// off by 3.7e-4 of their norm, where rounding alone is 2.1e-4.
+constexpr int kBlockCols = 32;
+
+template <int NT>
+struct Op {
+  half8_t t[NT];
+};
+template <int NA, int NB>
+__device__ __forceinline__ floatx4 mma_op(const Op<NA>& a, const Op<NB>& b, floatx4 c) {
+  if constexpr (NA == 2) c = mma(a.t[1], b.t[0], c);
+  if constexpr (NB == 2) c = mma(a.t[0], b.t[1], c);
+  return mma(a.t[0], b.t[0], c);
+}
+template <int NT>
+__device__ __forceinline__ Op<NT> op_of(const float (&x)[8], float s) {
+  Op<NT> p;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float y = x[e] * s;
+    p.t[0][e] = (_Float16)y;
+    if constexpr (NT == 2) p.t[1][e] = (_Float16)(y - (float)p.t[0][e]);
+  }
+  return p;
+}
+__device__ __forceinline__ float max8(const float (&x)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]));
+  return m;
+}
+
+template <typename T, int DK>
+__global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
+                                                    const float* __restrict__ gin,
+                                                    const _Float16* __restrict__ images,
+                                                    const float* __restrict__ scal, const float* __restrict__ states,
+                                                    const float* __restrict__ dstates, const float* __restrict__ smax,
+                                                    const float* __restrict__ dmax, const float* __restrict__ resid,
+                                                    const float* __restrict__ lam, const float* __restrict__ odo,
+                                                    const float* __restrict__ start, int has_state, int has_dstate,
+                                                    T* __restrict__ dq, T* __restrict__ dk, T* __restrict__ dv,
+                                                    float* __restrict__ dg, float* __restrict__ dbeta) {
+  constexpr int NT = kTerms<T>, IMG = kChunk * DK, ST = DK / 16;
+  constexpr int NC = std::is_same<T, bf16_t>::value ? 1 : 2;   // terms of computed operands
+  constexpr int kStateHalfs = ST * 256;   // one group of 16 columns, in register order
+  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG];
+  __shared__ __attribute__((aligned(16))) _Float16 s_state[2][NC][2 * kStateHalfs];   // S0, dS1
+  __shared__ __attribute__((aligned(16))) _Float16 s_do[4][NT][kFrag], s_mu[4][NC][kFrag], s_u[4][NC][kFrag];
+  __shared__ float s_scale[3][4];
+  __shared__ __attribute__((aligned(16))) float s_scal[kScal];
+  __shared__ double s_gam[kChunk];
+  __shared__ int s_cut[kChunk];
+  __shared__ float s_dot[kChunk];
+
+  const uint32_t slot = blockIdx.x;
+  const int hk = blockIdx.y;
+  int lo = 0, hi = a.W;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_slot(window(a, mid).begin, mid) <= slot) lo = mid;
+    else hi = mid;
+  }
+  const Win win = window(a, lo);
+  const uint32_t f = first_slot(win.begin, lo);
+  if (slot < f || (int64_t)(slot - f) * kChunk >= win.rows) return;
+  const int base = win.begin + (int)(slot - f) * kChunk;
+  const int rows = min(kChunk, win.rows - (int)(slot - f) * kChunk);
+  const bool more = (int64_t)(slot - f + 1) * kChunk < win.rows;   // the window has a chunk after this one
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+  const int own = 16 * wave + i;
+  const bool real = own < rows;
+  const int orig = real ? row_at(a, base + own) : 0;
+  {
+    const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
+    uint4* dst = reinterpret_cast<uint4*>(s_img);
+    for (int x = tid; x < 2 * NT * IMG / 8; x += 256) dst[x] = src[x];
+  }
+  const _Float16 *qi = s_img, *ki = s_img + NT * IMG;
+  floatx4 DQ[ST], DKc[ST];
+#pragma unroll
+  for (int t = 0; t < ST; ++t) {
+    DQ[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    DKc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int group = a.H / a.Hk, groups = a.dv / 16;
+  for (int hv = 0; hv < group; ++hv) {
+    const int h = hk * group + hv;
+    const size_t sh = (size_t)slot * a.H + h;
+    __syncthreads();
+    for (int x = tid; x < kScal / 4; x += 256)
+      reinterpret_cast<uint4*>(s_scal)[x] = reinterpret_cast<const uint4*>(scal + sh * kScal)[x];
+    if (wave == 0) {   // the decay sums, as k_delta_prep makes them
+      const bool r1 = lane < rows;
+      const float g1 = r1 ? gin[(size_t)row_at(a, base + lane) * a.H + h] : 0.f;
+      const bool cut1 = g1 < -104.f;
+      double gam = cut1 ? 0.0 : (double)g1;
+      int cut = cut1 ? 1 : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const double og = __shfl_up(gam, d);
+        const int oc = __shfl_up(cut, d);
+        if (lane >= d) gam += og, cut += oc;
+      }
+      s_gam[lane] = gam;
+      s_cut[lane] = cut;
+    }
+    // one power of two for all of a state: the largest of its column groups
+    uint32_t sbits = 0, dbits = 0;
+    for (int c = 0; c < groups; ++c) {
+      sbits = max(sbits, __float_as_uint(smax[sh * groups + c]));
+      dbits = max(dbits, __float_as_uint(dmax[sh * groups + c]));
+    }
+    const Scale ss = scale_of(sbits), sd = scale_of(dbits);
+    __syncthreads();
+    const float since = s_scal[kSince + own], until = s_scal[kUntil + own], be = s_scal[kBeta + own];
+    const float vs = s_scal[kVScale + own];
+
+    // products over the value columns: M[.][j], transposed tiles with this wave's rows in the lanes;
+    // 0: do of own rows with u of tile j, 1: mu of own rows with u of tile j (j <= wave),
+    // 2: u of own rows with do of tile j, 3: with mu of tile j (j >= wave)
+    floatx4 M[4][4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) M[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    float lr = 0.f, vdv = 0.f;
+    for (int c0 = 0; c0 < a.dv; c0 += kBlockCols) {
+      // own rows of the block: 8 columns a lane
+      const int col = c0 + 8 * g;
+      const bool here = real && col < a.dv;
+      float xo[8], xm[8], xu[8];
+      {
+        Raw<T, 8> ro = Frag<T, 8>::zero(), rv = Frag<T, 8>::zero();
+        f32x8 rl = {}, rr = {};
+        const size_t at = ((size_t)orig * a.H + h) * a.dv + col;
+        if (here) {
+          ro = *reinterpret_cast<const Raw<T, 8>*>(dout + at);
+          rv = *reinterpret_cast<const Raw<T, 8>*>(v + at);
+          rl = *reinterpret_cast<const f32x8*>(lam + (sh * kChunk + own) * a.dv + col);
+          rr = *reinterpret_cast<const f32x8*>(resid + (sh * kChunk + own) * a.dv + col);
+        }
+        float xv[8], xd[8];
+        Frag<T, 8>::to_f32(ro, xo);
+        Frag<T, 8>::to_f32(rv, xv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          lr += rl[e] * rr[e];
+          xm[e] = be * rl[e];
+          xu[e] = be * rr[e];
+          xd[e] = vs * xm[e];
+          vdv += xv[e] * xd[e];
+        }
+        if (here) *reinterpret_cast<Raw<T, 8>*>(dv + at) = Frag<T, 8>::from_f32(xd);
+      }
+      __syncthreads();   // the last block's reads are done
+      const Scale so = scale_of(wave_max_bits(max8(xo))), sm = scale_of(wave_max_bits(max8(xm)));
+      const Scale su = scale_of(wave_max_bits(max8(xu)));
+      const Op<NT> oo = op_of<NT>(xo, so.up);
+      const Op<NC> om = op_of<NC>(xm, sm.up), ou = op_of<NC>(xu, su.up);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) *reinterpret_cast<half8_t*>(&s_do[wave][t][lane * 8]) = oo.t[t];
+#pragma unroll
+      for (int t = 0; t < NC; ++t) {
+        *reinterpret_cast<half8_t*>(&s_mu[wave][t][lane * 8]) = om.t[t];
+        *reinterpret_cast<half8_t*>(&s_u[wave][t][lane * 8]) = ou.t[t];
+      }
+      if (lane == 0) {
+        s_scale[0][wave] = so.down;
+        s_scale[1][wave] = sm.down;
+        s_scale[2][wave] = su.down;
+      }
+      // S0 and dS1 of the block's two column groups, as the walks left them, in 16-bit terms
+      for (int x = tid; x < 2 * 2 * ST * 64; x += 256) {
+        const int which = x / (2 * ST * 64), y = x % (2 * ST * 64), cgl = y / (ST * 64);
+        floatx4 z = {0.f, 0.f, 0.f, 0.f};
+        if (c0 + 16 * cgl < a.dv)
+          z = *reinterpret_cast<const floatx4*>((which ? dstates : states) +
+                                                (sh * groups + c0 / 16) * (size_t)(ST * 256) + (size_t)y * 4);
+        const float up = which ? sd.up : ss.up;
+        half4_t p, l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float u = z[r] * up;
+          p[r] = (_Float16)u;
+          l[r] = (_Float16)(u - (float)p[r]);
+        }
+        *reinterpret_cast<half4_t*>(&s_state[which][0][y * 4]) = p;
+        if constexpr (NC == 2) *reinterpret_cast<half4_t*>(&s_state[which][NC - 1][y * 4]) = l;
+      }
+      __syncthreads();
+      // rows of the block's states as operand rows: tile t's 16 state rows, contraction over 32 columns
+      const auto state_rows = [&](int which, int t) {
+        Op<NC> x;
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const int c = 8 * g + 4 * hh;   // the columns' place in the block
+            const _Float16* at = &s_state[which][n][(((c >> 4) * ST + t) * 64 + (i & 3) * 16 + (c & 15) + (i >> 2)) * 4];
+            const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(at)));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x.t[n][4 * hh + r] = __builtin_bit_cast(_Float16, (short)y[r]);
+          }
+        return x;
+      };
+      const float fq = a.scale * since * (ss.down * so.down), fk0 = -since * (ss.down * sm.down);
+      const float fk1 = until * (sd.down * su.down);
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+        const Op<NC> s0 = state_rows(0, t), d1 = state_rows(1, t);
+        const floatx4 x = mma_op(s0, oo, zero), y = mma_op(s0, om, zero), z = mma_op(d1, ou, zero);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          DQ[t][r] += fq * x[r];
+          DKc[t][r] += vs * (fk0 * y[r] + fk1 * z[r]);
+        }
+      }
+      const auto rows_of = [&](auto& rows, auto& x, int j) {
+#pragma unroll
+        for (int n = 0; n < (int)(sizeof(x.t) / sizeof(x.t[0])); ++n)
+          x.t[n] = *reinterpret_cast<const half8_t*>(&rows[j][n][lane * 8]);
+      };
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+        if (j <= wave) {
+          Op<NC> u;
+          rows_of(s_u, u, j);
+          const floatx4 x = mma_op(u, oo, zero), y = mma_op(u, om, zero);
+          const float d = s_scale[2][j];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            M[0][j][r] += d * so.down * x[r];
+            M[1][j][r] += d * sm.down * y[r];
+          }
+        }
+        if (j >= wave) {
+          Op<NT> o;
+          Op<NC> m;
+          rows_of(s_do, o, j);
+          rows_of(s_mu, m, j);
+          const floatx4 x = mma_op(o, ou, zero), y = mma_op(m, ou, zero);
+          const float d0 = s_scale[0][j], d1 = s_scale[1][j];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            M[2][j][r] += d0 * su.down * x[r];
+            M[3][j][r] += d1 * su.down * y[r];
+          }
+        }
+      }
+    }
+    // the decays between own row and the others, then the products over the chunk's rows
+    floatx4 A[4], B[4], C[4];   // for dq from k; dk from k; dk from q
+    const double go = s_gam[own];
+    const int co = s_cut[own];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int o = 16 * j + 4 * g + r;   // the other row
+        const bool joined = s_cut[o] == co;
+        const bool before = o <= own, after = o >= own;
+        const float db = joined && before ? expf((float)(go - s_gam[o])) : 0.f;
+        const float da = joined && after ? expf((float)(s_gam[o] - go)) : 0.f;
+        A[j][r] = before ? a.scale * db * M[0][j][r] : 0.f;
+        B[j][r] = o < own ? -db * M[1][j][r] : o > own ? -da * M[3][j][r] : 0.f;
+        C[j][r] = after ? da * M[2][j][r] * s_scal[kOScale + o] : 0.f;
+      }
+    const Scale sa = scale_for(A), sb = scale_for(B), sc = scale_for(C);
+    Op<NC> Ap[2], Bp[2], Cp[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float xa[8], xb[8], xc[8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        xa[r] = A[2 * s][r], xa[4 + r] = A[2 * s + 1][r];
+        xb[r] = B[2 * s][r], xb[4 + r] = B[2 * s + 1][r];
+        xc[r] = C[2 * s][r], xc[4 + r] = C[2 * s + 1][r];
+      }
+      Ap[s] = op_of<NC>(xa, sa.up);
+      Bp[s] = op_of<NC>(xb, sb.up);
+      Cp[s] = op_of<NC>(xc, sc.up);
+    }
+    const float vsb = vs * sb.down, vsc = vs * sc.down;
+#pragma unroll
+    for (int t = 0; t < ST; ++t) {
+      floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f}, z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        Op<NT> kc, qc;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          kc.t[n] = image_cols<DK>(ki + n * IMG, t >> 1, t & 1, s, i, g);
+          qc.t[n] = image_cols<DK>(qi + n * IMG, t >> 1, t & 1, s, i, g);
+        }
+        x = mma_op(kc, Ap[s], x);
+        y = mma_op(kc, Bp[s], y);
+        z = mma_op(qc, Cp[s], z);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        DQ[t][r] += sa.down * x[r];
+        DKc[t][r] += vsb * y[r] + vsc * z[r];
+      }
+    }
+    // dbeta = lam . r and the terms of dg: sums over the lane groups
+    lr += __shfl_xor(lr, 16);
+    lr += __shfl_xor(lr, 32);
+    vdv += __shfl_xor(vdv, 16);
+    vdv += __shfl_xor(vdv, 32);
+    if (g == 0) {
+      if (real) dbeta[(size_t)orig * a.H + h] = lr / vs / vs;
+      float od = 0.f;
+      for (int c = 0; c < groups; ++c) od += real ? odo[(sh * groups + c) * kChunk + own] : 0.f;
+      s_dot[own] = real ? od - vdv : 0.f;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      float x = s_dot[lane];
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {   // sums to the end
+        const float y = __shfl_down(x, d);
+        if (lane + d < 64) x += y;
+      }
+      float at_end = 0.f;
+      if (more || has_dstate) {
+        const size_t from = more ? sh + a.H : sh;
+        for (int c = 0; c < groups; ++c) at_end += start[from * groups + c];
+        if (!more) at_end -= __shfl(x, 0);
+      }
+      const bool r1 = lane < rows;
+      if (r1) {
+        const size_t at = (size_t)row_at(a, base + lane) * a.H + h;
+        // nothing to decay: a decay that forgets everything, the first row without a state
+        const bool none = gin[at] < -104.f || (slot == f && lane == 0 && !has_state);
+        dg[at] = none ? 0.f : x + at_end;
+      }
+    }
+  }
+  // 8 neighbouring columns of the own row from two tiles
+  if (real)
+#pragma unroll
+    for (int t = 0; t < ST / 2; ++t) {
+      const int c = 32 * t + 8 * g;
+      if (c >= a.dk) continue;
+      float x[8], y[8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[r] = DQ[2 * t][r], x[4 + r] = DQ[2 * t + 1][r];
+        y[r] = DKc[2 * t][r], y[4 + r] = DKc[2 * t + 1][r];
+      }
+      const size_t at = ((size_t)orig * a.Hk + hk) * a.dk + c;
+      *reinterpret_cast<Raw<T, 8>*>(dq + at) = Frag<T, 8>::from_f32(x);
+      *reinterpret_cast<Raw<T, 8>*>(dk + at) = Frag<T, 8>::from_f32(y);
+    }
+}
+
+struct BackArgs {
+  const void *q, *k, *v, *dout;
+  const float *g, *beta, *state_in, *dstate_out;
+  void *dq, *dk, *dv;
+  float *dg, *dbeta, *dstate_in;
+};
+
+template <typename T, int DK>
+hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* workspace, hipStream_t stream) {
+  const BackSpace sp = back_space(a.n, a.W, dtype, a.Hk, a.H, a.dk, a.dv);
+  char* ws = static_cast<char*>(workspace);
+  _Float16* images = reinterpret_cast<_Float16*>(ws + sp.base.images);
+  _Float16* tri = reinterpret_cast<_Float16*>(ws + sp.base.tri);
+  const auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  float* scal = at(sp.base.scal);
+  const T *v = static_cast<const T*>(b.v), *dout = static_cast<const T*>(b.dout);
+  const int groups = a.dv / 16, waves = groups < 4 ? groups : 4;
+  const dim3 walk(a.W, a.H, (groups + waves - 1) / waves);
+  if (a.n > 0) {
+    k_delta_prep<T, DK, true><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
+        a, static_cast<const T*>(b.q), static_cast<const T*>(b.k), b.g, b.beta, images, tri, scal);
+    k_delta_walk<T, DK, true><<<walk, 64 * waves, 0, stream>>>(
+        a, v, b.state_in, images, tri, 4, scal, nullptr, dout,
+        WalkOut{nullptr, at(sp.states), at(sp.smax), at(sp.resid), at(sp.odo)});
+  }
+  k_delta_back<T, DK><<<walk, 64 * waves, 0, stream>>>(a, dout, b.dstate_out, images, tri, scal, at(sp.states),
+                                                       at(sp.lam), at(sp.dstates), at(sp.dmax), at(sp.start),
+                                                       b.dstate_in);
+  if (a.n > 0)
+    k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
+        a, v, dout, b.g, images, scal, at(sp.states), at(sp.dstates), at(sp.smax), at(sp.dmax), at(sp.resid),
+        at(sp.lam), at(sp.odo), at(sp.start), b.state_in != nullptr, b.dstate_out != nullptr, static_cast<T*>(b.dq), static_cast<T*>(b.dk),
+        static_cast<T*>(b.dv), b.dg, b.dbeta);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward_dk(const Args& a, int dtype, const BackArgs& b, void* workspace, hipStream_t stream) {
+  switch (pad_dk(a.dk)) {
+    case 32: return backward_impl<T, 32>(a, dtype, b, workspace, stream);
+    case 64: return backward_impl<T, 64>(a, dtype, b, workspace, stream);
+    default: return backward_impl<T, 128>(a, dtype, b, workspace, stream);
+  }
+}
+
+}  // namespace
+
+size_t delta_backward_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk,
+                                      int32_t dv) {
+  return back_space(n, W, dtype, Hk, H, dk, dv).total;
+}
+
+hipError_t launch_backward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,
+                                 int32_t Hk, int32_t H, int32_t dk, int32_t dv, float scale, const void* q,
+                                 const void* k, const void* v, const float* g, const float* beta,
+                                 const float* state_in, const void* dout, const float* dstate_out, void* dq,
+                                 void* dk_out, void* dv_out, float* dg, float* dbeta, float* dstate_in,
+                                 void* workspace, hipStream_t stream) {
+  const Args a{offsets, order, n, W, Hk, H, dk, dv, scale, (uint32_t)slots_of(n, W)};
+  const BackArgs b{q, k, v, dout, g, beta, state_in, dstate_out, dq, dk_out, dv_out, dg, dbeta, dstate_in};
+  if (dtype == 0) return backward_dk<float>(a, dtype, b, workspace, stream);
+  if (dtype == 1) return backward_dk<_Float16>(a, dtype, b, workspace, stream);
+  return backward_dk<bf16_t>(a, dtype, b, workspace, stream);
+}
+
+}  // namespace sla

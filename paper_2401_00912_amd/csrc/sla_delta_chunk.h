@@ -293,7 +293,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
 // the columns are independent of each other, so no wave waits for another but for the staging.
 struct WalkOut {
   float* state_out;    // final states or null
-  float* states;       // the states before every chunk, in register order, or null
+  float* states;       // the states before every chunk [slot][H][dv / 16], in register order, or null
+  float* smax;         // their largest magnitudes [slot][H][dv / 16], or null
   float* resid;        // r' of every chunk row [slot][H][64][dv], or null
   float* odo;          // sums over 16 columns of o dout [slot][H][dv / 16][64], or null
 };
@@ -367,6 +368,7 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
       float* at = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
 #pragma unroll
       for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(at + t * 256) = S[t];
+      if (!carried && lane == 0) out.smax[sh * (a.dv / 16) + cg] = 0.f;
     }
     // y = 2^-kap v - exp(gam) k' S
     Pair Sp[KB];
@@ -378,7 +380,15 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
       for (int r = 0; r < 4; ++r) Y[tau][r] *= vs[r];
     }
     if (carried) {
-      sc = scale_for(S);
+      float m = 0.f;
+#pragma unroll
+      for (int t = 0; t < ST; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[t][r]));
+      const uint32_t top = wave_max_bits(m);
+      sc = scale_of(top);
+      if constexpr (KEEP)
+        if (lane == 0) out.smax[sh * (a.dv / 16) + cg] = __uint_as_float(top);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
 #pragma unroll

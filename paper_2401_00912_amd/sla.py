@@ -21,6 +21,8 @@ Functions mirror the C ABI in include/sla.h:
     scatter_workspace_bytes(n, heads, head_dim)
     forward_scatter(plan, q, k, v, out=None, workspace=None) -> o   (naive comparator)
     forward_delta(q, k, v, g, beta, offsets, scale=None, order=None, state=None) -> (o, final_state)
+    backward_delta(q, k, v, g, beta, offsets, dout, dstate=None, scale=None, order=None, state=None)
+        -> (dq, dk, dv, dg, dbeta, dstate_in)
     step_delta(state, slots, q, k, v, g, beta, scale=None) -> o
 """
 from __future__ import annotations
@@ -63,6 +65,8 @@ EXPORTED = (
     "sla_backward_xca_noalloc",
     "sla_delta_workspace_bytes",
     "sla_forward_delta",
+    "sla_delta_backward_workspace_bytes",
+    "sla_backward_delta",
     "sla_step_delta",
 )
 
@@ -155,6 +159,10 @@ def lib() -> ctypes.CDLL:
     L.sla_delta_workspace_bytes.argtypes = [i64, i32, en, i32, i32, i32, i32]
     L.sla_forward_delta.restype = ctypes.c_int
     L.sla_forward_delta.argtypes = [vp, i64, i32, vp, en, i32, i32, i32, i32, f32] + [vp] * 9 + [sz, vp]
+    L.sla_delta_backward_workspace_bytes.restype = sz
+    L.sla_delta_backward_workspace_bytes.argtypes = [i64, i32, en, i32, i32, i32, i32]
+    L.sla_backward_delta.restype = ctypes.c_int
+    L.sla_backward_delta.argtypes = [vp, i64, i32, vp, en, i32, i32, i32, i32, f32] + [vp] * 15 + [sz, vp]
     L.sla_step_delta.restype = ctypes.c_int
     L.sla_step_delta.argtypes = [vp, i64, i32, en, i32, i32, i32, i32, f32] + [vp] * 8
     _lib = L
@@ -706,6 +714,44 @@ def forward_delta(q, k, v, g, beta, offsets, scale=None, order=None, state=None,
                                      _ptr(workspace), nbytes, _stream(q.device))
     _check(st, "sla_forward_delta")
     return out, final_state
+
+
+def delta_backward_workspace_bytes(n: int, num_windows: int, dtype, heads_qk: int, heads: int, dim_k: int,
+                                   dim_v: int) -> int:
+    """Workspace of backward_delta (0: unsupported sizes); dtype a torch dtype."""
+    return int(lib().sla_delta_backward_workspace_bytes(int(n), int(num_windows), _dtype_code(dtype), int(heads_qk),
+                                                        int(heads), int(dim_k), int(dim_v)))
+
+
+def backward_delta(q, k, v, g, beta, offsets, dout, dstate=None, scale=None, order=None, state=None, out=None,
+                   workspace=None):
+    """Gradients of forward_delta (sla_backward_delta): dout like v, dstate (the gradient of
+    final_state) or None; returns (dq, dk, dv, dg, dbeta, dstate_in), dstate_in None when no
+    state is given.  out: tensors to write the first five into (rows in no window are left as
+    they were)."""
+    torch = _torch()
+    n, hk, h, dk, dv = _delta_check(q, k, v, g, beta)
+    w = _check_windows(offsets, order, n, q.device)
+    _check_like("dout", dout, v.shape, q.dtype, q.device)
+    for name, t in (("state", state), ("dstate", dstate)):
+        _check_like(name, t, (w, h, dk, dv), torch.float32, q.device)
+    like = (q, k, v, g, beta)
+    out = [torch.empty_like(t) for t in like] if out is None else list(out)
+    if len(out) != 5:
+        raise ValueError("out must be the five tensors dq, dk, dv, dg, dbeta")
+    for name, t, ref in zip(("dq", "dk", "dv", "dg", "dbeta"), out, like):
+        _check_like(name, t, ref.shape, ref.dtype, q.device)
+    dstate_in = None if state is None else torch.empty_like(state)
+    workspace, nbytes = _delta_workspace(delta_backward_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace,
+                                         q.device, "sla_delta_backward_workspace_bytes")
+    with torch.cuda.device(q.device):
+        st = lib().sla_backward_delta(_ptr(offsets), n, w, _ptr(order), _dtype_code(q.dtype), hk, h, dk, dv,
+                                      float(dk ** -0.5 if scale is None else scale), _ptr(q), _ptr(k), _ptr(v),
+                                      _ptr(g), _ptr(beta), _ptr(state), _ptr(dout), _ptr(dstate),
+                                      *(_ptr(t) for t in out), _ptr(dstate_in), _ptr(workspace), nbytes,
+                                      _stream(q.device))
+    _check(st, "sla_backward_delta")
+    return (*out, dstate_in)
 
 
 def step_delta(state, slots, q, k, v, g, beta, scale=None, out=None):

@@ -224,6 +224,117 @@ def test_forward_joins(sla):
     close(s2, st.double().cpu().numpy(), "f32", "state")
 
 
+# ------------------------------------------------------------------ gradients
+GRADS = ("dq", "dk", "dv", "dg", "dbeta", "dstate_in")
+# dq and dk of bf16 rows: three sums (the state, rows before, rows behind) of products with up to two
+# operands in one fp16 term, each off by half a step, 2^-11: 6 * 2^-11 of the largest result if all were
+# off that much to the same side; they are random, so a quarter of it.
+OWN_BAR = {"f32": FP32_BAR, "f16": FP32_BAR, "bf16": 1.5 * 2.0 ** -11}
+
+
+def check_backward(S, c):
+    import torch
+
+    outs = [torch.full_like(c.dev(x), 7.0) for x in ("q", "k", "v", "g", "beta")]
+    got = S.backward_delta(*(c.dev(x) for x in ("q", "k", "v", "g", "beta", "offsets", "dout")), dstate=c.dev("dstate"),
+                           order=c.dev("order"), state=c.dev("state"), out=outs)
+    ref = delta_ref.delta_backward_ref(*(c.wide(x) for x in ("q", "k", "v", "g", "beta")), c.offsets, c.wide("dout"),
+                                       c.scale, c.wide("state"), c.wide("dstate"), c.wide("order"))
+    for name, x, r in zip(GRADS, got, ref):
+        if x is None:
+            assert name == "dstate_in" and c.state is None
+            continue
+        close(x, r, c.dtype if name in ("dq", "dk", "dv") else "f32", name,
+              OWN_BAR[c.dtype] if name in ("dq", "dk") else FP32_BAR)
+        assert (x.double().cpu().numpy()[np.isnan(r)] == 7.0).all(), f"{name}: rows in no window are left as they were"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("hk,h,dk,dv", [(1, 1, 32, 16), (2, 4, 64, 64), (1, 2, 128, 128), (3, 3, 16, 48),
+                                        (1, 4, 96, 144), (2, 2, 48, 256), (1, 1, 112, 32)])
+def test_backward_widths(sla, hk, h, dk, dv, dtype):
+    check_backward(sla, Case([70, 1, 0, 64, 129, 17], hk, h, dk, dv, dtype, seed=dk + dv, state=dk % 32 == 0, grads=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lengths", [[1], [2], [15], [16], [17], [32], [33], [63], [64], [65], [128], [129], [500], [0],
+                                     [0, 0, 5, 0], [1] * 70, [64, 64, 64], [63, 65, 0, 1, 130]])
+def test_backward_lengths(sla, lengths, dtype):
+    check_backward(sla, Case(lengths, 1, 2, 32, 32, dtype, seed=len(lengths) + sum(lengths), state=len(lengths) % 2 == 0,
+                             behind=3, grads=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_order(sla, dtype):
+    check_backward(sla, Case([40, 0, 90, 7, 64], 2, 4, 64, 32, dtype, seed=5, state=True, behind=6, order=True,
+                             grads=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_backward_decays(sla, dtype):
+    import torch
+
+    c = Case([200, 64], 1, 2, 32, 32, dtype, seed=9, state=True, grads=True)
+    c.g[:, 0] = 0.0
+    c.g[10:20, 0] = -30.0
+    c.g[70, 0] = -torch.inf
+    c.g[100, 1] = -torch.inf
+    c.g[101, 1] = -torch.inf
+    c.g[130, 1] = -200.0
+    c.g[200, 1] = -torch.inf
+    check_backward(sla, c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_backward_scales(sla, dtype):
+    """Queries and output gradients far from 1, a zero key, a zero beta, beta |k|^2 = 2."""
+    c = Case([150], 1, 2, 64, 32, dtype, seed=10, grads=True)
+    c.k[7] = 0
+    c.beta[9] = 0
+    c.beta[11] = 2.0 / c.k[11].float().square().sum()
+    c.k = (c.k.float() * 8.0).to(c.k.dtype)
+    c.beta /= 64.0
+    c.q = (c.q.float() * 64.0).to(c.q.dtype)
+    c.dout = (c.dout.float() / 16.0).to(c.dout.dtype)
+    check_backward(sla, c)
+
+
+def test_backward_by_differences(sla):
+    """The gradients against differences of the forward kernel itself, in directions over every input."""
+    import torch
+
+    c = Case([70, 33], 1, 2, 32, 32, "f32", seed=21, state=True, grads=True)
+    x = {n: c.dev(n).double() for n in ("q", "k", "v", "g", "beta", "state")}
+    off, dout, dst = c.dev("offsets"), c.dev("dout"), c.dev("dstate")
+
+    def loss(y):
+        y = {n: t.float() for n, t in y.items()}
+        o, st = sla.forward_delta(*(y[n] for n in ("q", "k", "v", "g", "beta")), off, state=y["state"])
+        return float((o.double() * dout.double()).sum() + (st.double() * dst.double()).sum())
+
+    grads = sla.backward_delta(*(x[n].float() for n in ("q", "k", "v", "g", "beta")), off, dout, dstate=dst,
+                               state=x["state"].float())
+    gen = torch.Generator().manual_seed(4)
+    for name, grad in zip(("q", "k", "v", "g", "beta", "state"), grads):
+        d = torch.randn(x[name].shape, generator=gen, dtype=torch.float64).cuda()
+        h = 1e-3
+        up, down = ({**x, name: x[name] + s * h * d} for s in (1, -1))
+        got, want = float((grad.double() * d).sum()), (loss(up) - loss(down)) / (2 * h)
+        # the loss is off by 1e-6 of its terms' norm and the difference by its third derivative h^2
+        norm = float((dout.double().norm() ** 2 + dst.double().norm() ** 2) ** 0.5)
+        assert abs(got - want) <= 1e-6 * norm / h * 2 + 1e-3 * abs(want), name
+
+
+def test_backward_same_twice(sla):
+    import torch
+
+    c = Case([300, 5, 64], 2, 4, 64, 64, "bf16", seed=12, state=True, grads=True)
+    args = [c.dev(x) for x in ("q", "k", "v", "g", "beta", "offsets", "dout")]
+    a = sla.backward_delta(*args, dstate=c.dev("dstate"), state=c.dev("state"))
+    b = sla.backward_delta(*args, dstate=c.dev("dstate"), state=c.dev("state"))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 # ------------------------------------------------------------------ row by row
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("hk,h,dk,dv", [(1, 1, 32, 16), (2, 4, 64, 64), (1, 2, 128, 128), (3, 3, 16, 48), (1, 2, 80, 256)])
