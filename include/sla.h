@@ -509,6 +509,53 @@ sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t num_slots, 
                             float* state, const void* q, const void* k, const void* v, const float* g,
                             const float* beta, void* o, sla_stream_t stream);
 
+/*
+ * Group normalisation with an activation, channels last, for the rows between the layers (every
+ * block of Sec. 3.1 normalises; a group's statistics do not depend on the rest of the batch) and
+ * for attention outputs (one group per head).  With windows (e.g. the scenes of a batch), over the
+ * rows of window s and the channels of group j,
+ *     mean, var   the mean and the variance (over all values) of x,   rstd = 1 / sqrt(var + eps),
+ *     y = act(weight (x - mean) rstd + bias);
+ * without windows (offsets NULL, num_windows = n) every row is a window of its own.
+ *   offsets   int32 [num_windows + 1], device, or NULL: window s is rows offsets[s] .. offsets[s + 1] - 1;
+ *             clamped as in sla_forward_delta.  Rows in no window are left as they were; a window
+ *             without rows has mean 0 and rstd 1 / sqrt(eps).
+ *   x, y      [n, channels] in `dtype`, contiguous, 16-byte aligned; channels up to 4,096, a multiple of
+ *             groups with a multiple of 4 channels in each, else SLA_E_UNSUPPORTED.
+ *   weight, bias  fp32 [channels], 16-byte aligned, or NULL (1, 0);  eps finite and >= 0.
+ *   mean, rstd    fp32 [num_windows, groups], outputs (the backward reads them).
+ *   workspace     device, 256-byte aligned, sla_group_norm_workspace_bytes() bytes (num_windows = 0
+ *             there: no windows; 0 for sizes that are not supported), else SLA_E_WORKSPACE.
+ * Statistics are fp32, variances summed around means.  Deterministic.  The activation of a value is
+ * fp32, y is rounded once.
+ */
+typedef enum { SLA_ACT_NONE = 0, SLA_ACT_RELU = 1, SLA_ACT_SILU = 2 } sla_activation_t;
+
+size_t sla_group_norm_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t channels,
+                                      int32_t groups);
+
+sla_status_t sla_forward_group_norm(const int32_t* offsets, int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                    int32_t channels, int32_t groups, float eps, sla_activation_t activation,
+                                    const void* x, const float* weight, const float* bias, void* y,
+                                    float* mean, float* rstd, void* workspace, size_t workspace_bytes,
+                                    sla_stream_t stream);
+
+/*
+ * Backward of sla_forward_group_norm (the chain rule), from x, the forward's mean and rstd and
+ * dy = dL/dy: dx in `dtype` (rows in no window are left as they were), dweight and dbias (fp32
+ * [channels], each may be NULL), summed over all rows in windows in a fixed order.  relu's slope at 0
+ * is 0.  Limits and errors as the forward.
+ */
+size_t sla_group_norm_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                               int32_t channels, int32_t groups);
+
+sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                     int32_t channels, int32_t groups, sla_activation_t activation,
+                                     const void* x, const float* weight, const float* bias, const void* dy,
+                                     const float* mean, const float* rstd, void* dx, float* dweight,
+                                     float* dbias, void* workspace, size_t workspace_bytes,
+                                     sla_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -54,6 +54,14 @@ hipError_t launch_backward_xca_noalloc(const void* plan, int32_t n, int32_t W, i
                                        const float* tau, const void* q, const void* k, const void* v,
                                        const void* dout, void* dq, void* dk, void* dv, float* dtau,
                                        hipStream_t stream);
+size_t norm_workspace_bytes(bool windows, int64_t n, int32_t S, int dtype, int32_t C, int32_t G, bool backward);
+hipError_t launch_forward_group_norm(const int32_t* offsets, int32_t n, int32_t S, int dtype, int32_t C, int32_t G,
+                                     float eps, int activation, const void* x, const float* weight, const float* bias,
+                                     void* y, float* mean, float* rstd, void* workspace, hipStream_t stream);
+hipError_t launch_backward_group_norm(const int32_t* offsets, int32_t n, int32_t S, int dtype, int32_t C, int32_t G,
+                                      int activation, const void* x, const float* weight, const float* bias,
+                                      const void* dy, const float* mean, const float* rstd, void* dx, float* dweight,
+                                      float* dbias, void* workspace, hipStream_t stream);
 size_t delta_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv);
 hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,
                                 int32_t Hk, int32_t H, int32_t dk, int32_t dv, float scale, const void* q,
@@ -579,4 +587,83 @@ SLA_EXPORT sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t 
     return SLA_E_ARG;
   return hip_status(sla::launch_step_delta(slots, (int32_t)n, num_slots, (int)dtype, heads_qk, heads, dim_k, dim_v,
                                            scale, state, q, k, v, g, beta, o, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// Sizes of a group normalisation call; num_windows = 0: every row is a window.
+sla_status_t check_norm_sizes(int64_t n, int32_t num_windows, int dtype, int32_t channels, int32_t groups) {
+  if (n < 0 || n >= INT32_MAX || num_windows < 0 || channels < 1 || groups < 1 || channels % groups) return SLA_E_ARG;
+  if (dtype < 0 || dtype > 2) return SLA_E_ARG;
+  if (channels > 4096 || channels / groups % 4) return SLA_E_UNSUPPORTED;
+  // HIP bounds a grid at 2^32 - 1 threads in x (the joining launch has 1,024 a window)
+  if (num_windows > (int32_t)(UINT32_MAX / 1024) - 4096) return SLA_E_UNSUPPORTED;
+  return SLA_OK;
+}
+
+sla_status_t check_norm_call(const int32_t* offsets, int64_t n, int32_t num_windows, int dtype, int32_t channels,
+                             int32_t groups, int activation, const float* weight, const float* bias,
+                             const void* workspace, size_t workspace_bytes, bool backward) {
+  if (offsets == nullptr ? num_windows != n : num_windows < 1) return SLA_E_ARG;
+  const int32_t w = offsets == nullptr ? 0 : num_windows;
+  const sla_status_t st = check_norm_sizes(n, w, dtype, channels, groups);
+  if (st != SLA_OK) return st;
+  if (activation < SLA_ACT_NONE || activation > SLA_ACT_SILU) return SLA_E_ARG;
+  if (!aligned(offsets, 4) || !aligned(weight, 16) || !aligned(bias, 16)) return SLA_E_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  const size_t need = sla::norm_workspace_bytes(offsets != nullptr, n, offsets ? num_windows : (int32_t)n, dtype,
+                                                channels, groups, backward);
+  return workspace_bytes < need ? SLA_E_WORKSPACE : SLA_OK;
+}
+
+}  // namespace
+
+SLA_EXPORT size_t sla_group_norm_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t channels,
+                                                 int32_t groups) {
+  if (check_norm_sizes(n, num_windows, (int)dtype, channels, groups) != SLA_OK) return 0;
+  return sla::norm_workspace_bytes(num_windows > 0, n, num_windows > 0 ? num_windows : (int32_t)n, (int)dtype, channels,
+                                   groups, false);
+}
+
+SLA_EXPORT size_t sla_group_norm_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                                          int32_t channels, int32_t groups) {
+  if (check_norm_sizes(n, num_windows, (int)dtype, channels, groups) != SLA_OK) return 0;
+  return sla::norm_workspace_bytes(num_windows > 0, n, num_windows > 0 ? num_windows : (int32_t)n, (int)dtype, channels,
+                                   groups, true);
+}
+
+SLA_EXPORT sla_status_t sla_forward_group_norm(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                               sla_dtype_t dtype, int32_t channels, int32_t groups, float eps,
+                                               sla_activation_t activation, const void* x, const float* weight,
+                                               const float* bias, void* y, float* mean, float* rstd, void* workspace,
+                                               size_t workspace_bytes, sla_stream_t stream) {
+  const sla_status_t st = check_norm_call(offsets, n, num_windows, (int)dtype, channels, groups, (int)activation,
+                                          weight, bias, workspace, workspace_bytes, false);
+  if (st != SLA_OK) return st;
+  if (!(eps >= 0.f && finite(eps))) return SLA_E_ARG;
+  if (n == 0 && offsets == nullptr) return SLA_OK;
+  if (!mean || !rstd || !aligned(mean, 4) || !aligned(rstd, 4) || (n > 0 && (!x || !y)) || !aligned(x, 16) ||
+      !aligned(y, 16))
+    return SLA_E_ARG;
+  return hip_status(sla::launch_forward_group_norm(offsets, (int32_t)n, num_windows, (int)dtype, channels, groups, eps,
+                                                   (int)activation, x, weight, bias, y, mean, rstd, workspace,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                                sla_dtype_t dtype, int32_t channels, int32_t groups,
+                                                sla_activation_t activation, const void* x, const float* weight,
+                                                const float* bias, const void* dy, const float* mean,
+                                                const float* rstd, void* dx, float* dweight, float* dbias,
+                                                void* workspace, size_t workspace_bytes, sla_stream_t stream) {
+  const sla_status_t st = check_norm_call(offsets, n, num_windows, (int)dtype, channels, groups, (int)activation,
+                                          weight, bias, workspace, workspace_bytes, true);
+  if (st != SLA_OK) return st;
+  if (n > 0 && (!x || !dy || !mean || !rstd || !dx)) return SLA_E_ARG;
+  if (!aligned(x, 16) || !aligned(dy, 16) || !aligned(dx, 16) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+      !aligned(dweight, 4) || !aligned(dbias, 4))
+    return SLA_E_ARG;
+  return hip_status(sla::launch_backward_group_norm(offsets, (int32_t)n, num_windows, (int)dtype, channels, groups,
+                                                    (int)activation, x, weight, bias, dy, mean, rstd, dx, dweight,
+                                                    dbias, workspace, static_cast<hipStream_t>(stream)));
 }

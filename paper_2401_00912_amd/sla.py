@@ -24,6 +24,10 @@ Functions mirror the C ABI in include/sla.h:
     backward_delta(q, k, v, g, beta, offsets, dout, dstate=None, scale=None, order=None, state=None)
         -> (dq, dk, dv, dg, dbeta, dstate_in)
     step_delta(state, slots, q, k, v, g, beta, scale=None) -> o
+    forward_group_norm(x, groups, weight=None, bias=None, offsets=None, eps=1e-5, activation="none")
+        -> (y, mean, rstd)
+    backward_group_norm(x, groups, dy, mean, rstd, weight=None, bias=None, offsets=None, activation="none")
+        -> (dx, dweight, dbias)
 """
 from __future__ import annotations
 
@@ -36,6 +40,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsla.so")
 SLA_OK, SLA_E_ARG, SLA_E_UNSUPPORTED, SLA_E_WORKSPACE, SLA_E_HIP = range(5)
 
 FEATURE_MAPS = {"elu1": 0, "relu": 1}   # sla_feature_map_t
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}   # sla_activation_t
 
 EXPORTED = (
     "sla_abi_version",
@@ -68,6 +73,10 @@ EXPORTED = (
     "sla_delta_backward_workspace_bytes",
     "sla_backward_delta",
     "sla_step_delta",
+    "sla_group_norm_workspace_bytes",
+    "sla_forward_group_norm",
+    "sla_group_norm_backward_workspace_bytes",
+    "sla_backward_group_norm",
 )
 
 
@@ -165,6 +174,13 @@ def lib() -> ctypes.CDLL:
     L.sla_backward_delta.argtypes = [vp, i64, i32, vp, en, i32, i32, i32, i32, f32] + [vp] * 15 + [sz, vp]
     L.sla_step_delta.restype = ctypes.c_int
     L.sla_step_delta.argtypes = [vp, i64, i32, en, i32, i32, i32, i32, f32] + [vp] * 8
+    for name in ("sla_group_norm_workspace_bytes", "sla_group_norm_backward_workspace_bytes"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [i64, i32, en, i32, i32]
+    L.sla_forward_group_norm.restype = ctypes.c_int
+    L.sla_forward_group_norm.argtypes = [vp, i64, i32, en, i32, i32, f32, en] + [vp] * 7 + [sz, vp]
+    L.sla_backward_group_norm.restype = ctypes.c_int
+    L.sla_backward_group_norm.argtypes = [vp, i64, i32, en, i32, i32, en] + [vp] * 10 + [sz, vp]
     _lib = L
     return L
 
@@ -679,7 +695,7 @@ def delta_workspace_bytes(n: int, num_windows: int, dtype, heads_qk: int, heads:
                                                int(heads), int(dim_k), int(dim_v)))
 
 
-def _delta_workspace(need, workspace, device, what):
+def _own_workspace(need, workspace, device, what):
     if need == 0:
         raise SlaError(SLA_E_UNSUPPORTED, what)
     if workspace is None:
@@ -705,7 +721,7 @@ def forward_delta(q, k, v, g, beta, offsets, scale=None, order=None, state=None,
         final_state = torch.empty((w, h, dk, dv), dtype=torch.float32, device=q.device)
     for name, t in (("state", state), ("final_state", final_state)):
         _check_like(name, t, (w, h, dk, dv), torch.float32, q.device)
-    workspace, nbytes = _delta_workspace(delta_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace, q.device,
+    workspace, nbytes = _own_workspace(delta_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace, q.device,
                                          "sla_delta_workspace_bytes")
     with torch.cuda.device(q.device):
         st = lib().sla_forward_delta(_ptr(offsets), n, w, _ptr(order), _dtype_code(q.dtype), hk, h, dk, dv,
@@ -742,7 +758,7 @@ def backward_delta(q, k, v, g, beta, offsets, dout, dstate=None, scale=None, ord
     for name, t, ref in zip(("dq", "dk", "dv", "dg", "dbeta"), out, like):
         _check_like(name, t, ref.shape, ref.dtype, q.device)
     dstate_in = None if state is None else torch.empty_like(state)
-    workspace, nbytes = _delta_workspace(delta_backward_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace,
+    workspace, nbytes = _own_workspace(delta_backward_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace,
                                          q.device, "sla_delta_backward_workspace_bytes")
     with torch.cuda.device(q.device):
         st = lib().sla_backward_delta(_ptr(offsets), n, w, _ptr(order), _dtype_code(q.dtype), hk, h, dk, dv,
@@ -773,6 +789,76 @@ def step_delta(state, slots, q, k, v, g, beta, scale=None, out=None):
                                   _ptr(v), _ptr(g), _ptr(beta), _ptr(out), _stream(q.device))
     _check(st, "sla_step_delta")
     return out
+
+
+def _norm_check(x, groups, weight, bias, offsets, activation):
+    """Shapes, dtypes, devices and layouts of a group normalisation call: (n, channels, windows)."""
+    torch = _torch()
+    if x.dim() != 2 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous [n, channels] tensor")
+    n, C = x.shape
+    if groups < 1 or C < 1 or C % groups:
+        raise ValueError("channels must be a multiple of groups")
+    for name, t in (("weight", weight), ("bias", bias)):
+        _check_like(name, t, (C,), torch.float32, x.device)
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, not {activation!r}")
+    return n, C, n if offsets is None else _check_windows(offsets, None, n, x.device)
+
+
+def group_norm_workspace_bytes(n: int, num_windows: int, dtype, channels: int, groups: int,
+                               backward: bool = False) -> int:
+    """Workspace of forward_group_norm or backward_group_norm (0: unsupported sizes);
+    num_windows 0 for calls without offsets."""
+    f = lib().sla_group_norm_backward_workspace_bytes if backward else lib().sla_group_norm_workspace_bytes
+    return int(f(int(n), int(num_windows), _dtype_code(dtype), int(channels), int(groups)))
+
+
+def forward_group_norm(x, groups: int, weight=None, bias=None, offsets=None, eps=1e-5, activation="none", y=None,
+                       mean=None, rstd=None, workspace=None):
+    """Group normalisation and an activation (sla_forward_group_norm): x [n, channels], weight
+    and bias float32 [channels] or None, offsets int32 [windows + 1] or None (every row by
+    itself), activation "none", "relu" or "silu".  Returns (y, mean, rstd), the statistics
+    float32 [windows, groups]; rows in no window are left as they were in y."""
+    torch = _torch()
+    n, C, w = _norm_check(x, groups, weight, bias, offsets, activation)
+    y = torch.empty_like(x) if y is None else y
+    _check_like("y", y, x.shape, x.dtype, x.device)
+    mean = torch.empty((w, groups), dtype=torch.float32, device=x.device) if mean is None else mean
+    rstd = torch.empty((w, groups), dtype=torch.float32, device=x.device) if rstd is None else rstd
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _check_like(name, t, (w, groups), torch.float32, x.device)
+    need = group_norm_workspace_bytes(n, 0 if offsets is None else w, x.dtype, C, groups)
+    workspace, nbytes = _own_workspace(need, workspace, x.device, "sla_group_norm_workspace_bytes")
+    with torch.cuda.device(x.device):
+        st = lib().sla_forward_group_norm(_ptr(offsets), n, w, _dtype_code(x.dtype), C, groups, float(eps),
+                                          ACTIVATIONS[activation], _ptr(x), _ptr(weight), _ptr(bias), _ptr(y),
+                                          _ptr(mean), _ptr(rstd), _ptr(workspace), nbytes, _stream(x.device))
+    _check(st, "sla_forward_group_norm")
+    return y, mean, rstd
+
+
+def backward_group_norm(x, groups: int, dy, mean, rstd, weight=None, bias=None, offsets=None, activation="none",
+                        dx=None, workspace=None):
+    """Gradients of forward_group_norm (sla_backward_group_norm), from its input and statistics:
+    (dx, dweight, dbias), the last two float32 [channels]."""
+    torch = _torch()
+    n, C, w = _norm_check(x, groups, weight, bias, offsets, activation)
+    _check_like("dy", dy, x.shape, x.dtype, x.device)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _check_like(name, t, (w, groups), torch.float32, x.device)
+    dx = torch.empty_like(x) if dx is None else dx
+    _check_like("dx", dx, x.shape, x.dtype, x.device)
+    dweight, dbias = (torch.empty(C, dtype=torch.float32, device=x.device) for _ in range(2))
+    need = group_norm_workspace_bytes(n, 0 if offsets is None else w, x.dtype, C, groups, backward=True)
+    workspace, nbytes = _own_workspace(need, workspace, x.device, "sla_group_norm_backward_workspace_bytes")
+    with torch.cuda.device(x.device):
+        st = lib().sla_backward_group_norm(_ptr(offsets), n, w, _dtype_code(x.dtype), C, groups,
+                                           ACTIVATIONS[activation], _ptr(x), _ptr(weight), _ptr(bias), _ptr(dy),
+                                           _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dweight), _ptr(dbias),
+                                           _ptr(workspace), nbytes, _stream(x.device))
+    _check(st, "sla_backward_group_norm")
+    return dx, dweight, dbias
 
 
 def read_plan(plan: Plan):
