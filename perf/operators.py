@@ -198,8 +198,8 @@ def _own(s):
     if kind == "norm_forward":
         return sla.forward_group_norm(s["x"], case["groups"], weight=s["weight"], bias=s["bias"], offsets=offsets,
                                       eps=EPS, activation=case["activation"])
-    return sla.backward_group_norm(s["x"], case["groups"], s["dy"], s["mean"], s["rstd"], weight=s["weight"],
-                                   bias=s["bias"], offsets=offsets, activation=case["activation"])
+    return sla.backward_group_norm(s["x"], case["groups"], s["dy"], s["mean"].contiguous(), s["rstd"].contiguous(),
+                                   weight=s["weight"], bias=s["bias"], offsets=offsets, activation=case["activation"])
 
 
 # ------------------------------------------------------------------ the plain forms
