@@ -34,9 +34,9 @@ constexpr int kTriHalfs = 2 * kTri * kFrag;
 // T and P are kept 64 times as large (T's entries stay below 45, P's below 512): an entry's error is
 // then below 2^-31 of the diagonal's 1
 constexpr float kTriUp = 64.f;
-constexpr int kScal = 448;            // floats: 6 rows of 64 and one value
-// rows of the per-chunk scalars
-enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kLast = 384 };
+constexpr int kScal = 512;            // 4-byte values: 6 rows of 64, one value, padding to 2 KB
+// rows of the per-chunk scalars; kRow: original rows (int32)
+enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow = 320, kLast = 384 };
 
 struct Args {
   const int32_t* offsets;
@@ -206,7 +206,25 @@ __device__ __forceinline__ half8_t image_cols(const _Float16* img, int t, int p,
 // number of the triangle's operand for row tile tau and column block s
 __device__ __forceinline__ constexpr int tri_at(int tau, int s) { return tau < 2 ? tau : 2 * tau - 2 + s; }
 
+// ------------------------------------------------------------------ staging
+// `bytes` (a multiple of 1,024) from global memory into LDS without passing registers, split over the
+// workgroup's waves: one instruction moves 64 x 16 bytes in lane order.  Complete at the next
+// __syncthreads().
+__device__ __forceinline__ void stage(void* lds, const void* src, int bytes, int wave, int waves, int lane) {
+  for (int at = wave * 1024; at < bytes; at += waves * 1024)
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(static_cast<const char*>(src) + at + lane * 16),
+        (__attribute__((address_space(3))) void*)(static_cast<char*>(lds) + at), 16, 0, 0);
+}
+
 // ------------------------------------------------------------------ storage types
+template <typename T>
+using Bits = std::conditional_t<std::is_same<T, float>::value, float, unsigned short>;
+template <typename T>
+__device__ __forceinline__ float widen(Bits<T> x) {
+  if constexpr (std::is_same<T, float>::value) return x;
+  else return u16_to_f32<T>(x);
+}
 template <typename T>
 __device__ __forceinline__ float load1(const T* p) {
   if constexpr (std::is_same<T, float>::value) return *p;

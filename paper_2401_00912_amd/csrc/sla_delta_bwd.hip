@@ -57,71 +57,55 @@ BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int
 // ------------------------------------------------------------------ the walk back
 // As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
 template <typename T, int DK>
-__global__ __launch_bounds__(256) void k_delta_back(Args a, const T* __restrict__ dout, const float* __restrict__ dstate,
+__global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict__ dout, const float* __restrict__ dstate,
                                                     const _Float16* __restrict__ images,
                                                     const _Float16* __restrict__ tri, const float* __restrict__ scal,
                                                     const float* __restrict__ states, float* __restrict__ lam,
                                                     float* __restrict__ dstates, float* __restrict__ dmax,
                                                     float* __restrict__ start, float* __restrict__ dstate_in) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG];
-  __shared__ __attribute__((aligned(16))) _Float16 s_tri[2 * kTriHalfs];
-  __shared__ __attribute__((aligned(16))) float s_scal[kScal];
+  constexpr bool TWICE = kTwice<T, DK>;
+  __shared__ Stage<T, DK> s_a;
+  __shared__ std::conditional_t<TWICE, Stage<T, DK>, char> s_b;
 
   const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-  const int threads = blockDim.x;
-  const int cg = blockIdx.z * (threads >> 6) + (tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+  const int cg = blockIdx.z * waves + wave;
   const bool live = 16 * cg < a.dv;
   const int col = 16 * cg + i;
   const Win win = window(a, w);
   const uint32_t slot0 = first_slot(win.begin, w);
+  const int chunks = (win.rows + kChunk - 1) / kChunk;
+  const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
 
   floatx4 S[ST];
-#pragma unroll
-  for (int t = 0; t < ST; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
-      S[t][r] = dstate != nullptr && live && d < a.dk ? dstate[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] : 0.f;
-    }
+  load_state(S, a, dstate, w, h, col, live, g);
   bool carried = dstate != nullptr;
-
-  for (int c = (win.rows + kChunk - 1) / kChunk - 1; c >= 0; --c) {
-    const uint32_t slot = slot0 + c;
-    const int rows = min(kChunk, win.rows - c * kChunk);
-    const size_t sh = (size_t)slot * a.H + h;
-    __syncthreads();
-    {
-      const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
-      uint4* dst = reinterpret_cast<uint4*>(s_img);
-      for (int x = tid; x < 2 * NT * IMG / 8; x += threads) dst[x] = src[x];
-      const uint4* st = reinterpret_cast<const uint4*>(tri + (sh * 4 + 2) * kTriHalfs);
-      uint4* dt = reinterpret_cast<uint4*>(s_tri);
-      for (int x = tid; x < 2 * kTriHalfs / 8; x += threads) dt[x] = st[x];
-      const uint4* ss = reinterpret_cast<const uint4*>(scal + sh * kScal);
-      uint4* ds = reinterpret_cast<uint4*>(s_scal);
-      for (int x = tid; x < kScal / 4; x += threads) ds[x] = ss[x];
+  Column<T> oc, on;
+  Places pn;   // of the chunk before the one in work
+  // the transposed triangles are the third and fourth of a chunk
+  const _Float16* tri_t = tri + 2 * kTriHalfs;
+  if (chunks > 0) {
+    const int c = chunks - 1;
+    if constexpr (TWICE) stage_chunk<T, DK>(s_a, a, slot0 + c, hk, h, images, tri_t, 4, scal, wave, waves, lane);
+    if (live) {
+      pn.ask(a, win.begin + c * kChunk, rows_of(c), g);
+      oc.ask(a, dout, pn, h, col);
+      if (c > 0) pn.ask(a, win.begin + (c - 1) * kChunk, rows_of(c - 1), g);
     }
-    floatx4 Y[4];
-#pragma unroll
-    for (int tau = 0; tau < 4; ++tau)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * tau + 4 * g + r;
-        Y[tau][r] = 0.f;
-        if (live && row < rows) {
-          const size_t at = (size_t)row_at(a, win.begin + c * kChunk + row) * a.H + h;
-          Y[tau][r] = load1(dout + at * a.dv + col);
-        }
-      }
-    __syncthreads();
-    if (!live) continue;
-    const _Float16 *qi = s_img, *ki = s_img + NT * IMG, *st = s_tri, *sp = s_tri + kTriHalfs;
+  }
+
+  const auto work = [&](const Stage<T, DK>& s, int c) {
+    const int rows = rows_of(c);
+    const size_t sh = (size_t)(slot0 + c) * a.H + h;
+    const _Float16 *qi = s.img, *ki = s.img + NT * IMG, *st = s.tri, *sp = s.tri + kTriHalfs;
     auto row4 = [&](int what, int tau) {
-      return *reinterpret_cast<const floatx4*>(s_scal + what + 16 * tau + 4 * g);
+      return *reinterpret_cast<const floatx4*>(s.scal + what + 16 * tau + 4 * g);
     };
     const size_t sgrp = sh * (a.dv / 16) + cg;
+    if (c > 0) on.ask(a, dout, pn, h, col);
+    if (c > 1) pn.ask(a, win.begin + (c - 2) * kChunk, rows_of(c - 2), g);
 
     uint32_t top = 0;
     {
@@ -136,27 +120,27 @@ __global__ __launch_bounds__(256) void k_delta_back(Args a, const T* __restrict_
       if (lane == 0) dmax[sgrp] = __uint_as_float(top);
     }
     // du = P^T do' + until k' dS
-    floatx4 X[4];
+    floatx4 X[4], Y[4];
     {
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         const floatx4 os = row4(kOScale, tau);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) Y[tau][r] *= os[r];
+        for (int r = 0; r < 4; ++r) Y[tau][r] = oc.get(tau, r, g, rows) * os[r];
       }
       const Scale sy = scale_for(Y);
       const float ydown = sy.down * (1.f / kTriUp);
       Pair Yp[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) Yp[s] = split(Y[2 * s], Y[2 * s + 1], sy.up);
+      for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = tau / 2; s < 2; ++s) {
-          const _Float16* at = sp + 2 * tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
+        for (int s2 = tau / 2; s2 < 2; ++s2) {
+          const _Float16* at = sp + 2 * tri_at(3 - tau, 1 - s2) * kFrag + lane * 8;
           const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          x = mma2(t, Yp[s], x);
+          x = mma2(t, Yp[s2], x);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) X[tau][r] = x[r] * ydown;
@@ -181,21 +165,24 @@ __global__ __launch_bounds__(256) void k_delta_back(Args a, const T* __restrict_
         for (int r = 0; r < 4; ++r) X[tau][r] += un[r] * (x[r] * sc.down);
       }
     }
+    floatx4 s0[ST];   // the state before the chunk, for the end
+#pragma unroll
+    for (int t = 0; t < ST; ++t) s0[t] = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
     // lam, then -since mu in X and since do' in Y
     {
       const Scale sx = scale_for(X);
       const float xdown = sx.down * (1.f / kTriUp);
       Pair Xp[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) Xp[s] = split(X[2 * s], X[2 * s + 1], sx.up);
+      for (int s2 = 0; s2 < 2; ++s2) Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sx.up);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = tau / 2; s < 2; ++s) {
-          const _Float16* at = st + 2 * tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
+        for (int s2 = tau / 2; s2 < 2; ++s2) {
+          const _Float16* at = st + 2 * tri_at(3 - tau, 1 - s2) * kFrag + lane * 8;
           const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          x = mma2(t, Xp[s], x);
+          x = mma2(t, Xp[s2], x);
         }
         const floatx4 be = row4(kBeta, tau), since = row4(kSince, tau);
 #pragma unroll
@@ -217,35 +204,54 @@ __global__ __launch_bounds__(256) void k_delta_back(Args a, const T* __restrict_
       const Scale sc = scale_of(wave_max_bits(m));
       Pair Xp[2], Yp[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        Xp[s] = split(X[2 * s], X[2 * s + 1], sc.up);
-        Yp[s] = split(Y[2 * s], Y[2 * s + 1], sc.up);
+      for (int s2 = 0; s2 < 2; ++s2) {
+        Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sc.up);
+        Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sc.up);
       }
-      const float last = s_scal[kLast];
+      const float last = s.scal[kLast];
       float dot = 0.f;
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
-        const floatx4 s0 = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s2 = 0; s2 < 2; ++s2) {
           if constexpr (NT == 2) {
-            x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s, i, g), Xp[s].hi, x);
-            x = mma(image_cols<DK>(qi + IMG, t >> 1, t & 1, s, i, g), Yp[s].hi, x);
+            x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s2, i, g), Xp[s2].hi, x);
+            x = mma(image_cols<DK>(qi + IMG, t >> 1, t & 1, s2, i, g), Yp[s2].hi, x);
           }
-          x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s, i, g), Xp[s], x);
-          x = mma1(image_cols<DK>(qi, t >> 1, t & 1, s, i, g), Yp[s], x);
+          x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s2, i, g), Xp[s2], x);
+          x = mma1(image_cols<DK>(qi, t >> 1, t & 1, s2, i, g), Yp[s2], x);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           S[t][r] = last * S[t][r] + sc.down * x[r];
-          dot += s0[r] * S[t][r];
+          dot += s0[t][r] * S[t][r];
         }
       }
 #pragma unroll
       for (int m2 = 1; m2 < 64; m2 *= 2) dot += __shfl_xor(dot, m2);
       if (lane == 0) start[sgrp] = dot;
       carried = true;
+    }
+    oc = on;
+  };
+
+  if constexpr (TWICE) {
+    const auto turn = [&](const Stage<T, DK>& s, Stage<T, DK>& other, int c) {
+      __syncthreads();   // chunk c is there, and no wave reads the other buffer any more
+      if (c > 0) stage_chunk<T, DK>(other, a, slot0 + c - 1, hk, h, images, tri_t, 4, scal, wave, waves, lane);
+      if (live) work(s, c);
+    };
+    for (int c = chunks - 1; c >= 0; c -= 2) {
+      turn(s_a, s_b, c);
+      if (c > 0) turn(s_b, s_a, c - 1);
+    }
+  } else {
+    for (int c = chunks - 1; c >= 0; --c) {
+      __syncthreads();
+      stage_chunk<T, DK>(s_a, a, slot0 + c, hk, h, images, tri_t, 4, scal, wave, waves, lane);
+      __syncthreads();
+      if (live) work(s_a, c);
     }
   }
   if (dstate_in != nullptr && live)
@@ -644,7 +650,7 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
   const auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   float* scal = at(sp.base.scal);
   const T *v = static_cast<const T*>(b.v), *dout = static_cast<const T*>(b.dout);
-  const int groups = a.dv / 16, waves = groups < 4 ? groups : 4;
+  const int groups = a.dv / 16, waves = walk_waves(a);
   const dim3 walk(a.W, a.H, (groups + waves - 1) / waves);
   if (a.n > 0) {
     k_delta_prep<T, DK, true><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(

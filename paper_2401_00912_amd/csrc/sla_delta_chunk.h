@@ -2,6 +2,7 @@
 // chunks.  Included by the forward and by the backward, which makes the states again.
 #pragma once
 
+#include <cstdlib>
 #include "sla_delta.h"
 
 namespace sla {
@@ -237,6 +238,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
       sc[kUntil + lane] = real && cut == lcut ? expf((float)(last - gam)) : 0.f;
       sc[kVScale + lane] = vs;
       sc[kOScale + lane] = s_os[lane] * a.scale;
+      sc[kRow + lane] = __int_as_float(real ? row_at(a, base + lane) : 0);
       if (lane == 0) sc[kLast] = lcut == 0 ? expf((float)last) : 0.f;
     }
     __syncthreads();
@@ -291,6 +293,11 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
 // of lane (i, g) is state row 32 t + 8 g + 4 p + r, column i.  Two tiles are then an operand of the
 // products with k' and q' without moving a value, and so are the chunk's r and u (16 rows a tile);
 // the columns are independent of each other, so no wave waits for another but for the staging.
+//
+// The chunks of a window depend on each other, so their latency counts: a chunk's images, triangles
+// and scalars (58 KB at dk = 128 in 16 bits) are moved into the second of two LDS buffers while the
+// first one's chunk is worked on, with one barrier a chunk, and its v is loaded ahead into registers.
+// fp32 rows of dk = 128 (90 KB) do not fit twice and are staged between two barriers.
 struct WalkOut {
   float* state_out;    // final states or null
   float* states;       // the states before every chunk [slot][H][dv / 16], in register order, or null
@@ -299,71 +306,135 @@ struct WalkOut {
   float* odo;          // sums over 16 columns of o dout [slot][H][dv / 16][64], or null
 };
 
-template <typename T, int DK, bool KEEP>
-__global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict__ v, const float* __restrict__ state_in,
-                                                    const _Float16* __restrict__ images,
-                                                    const _Float16* __restrict__ tri, int tris,
-                                                    const float* __restrict__ scal, T* __restrict__ o,
-                                                    const T* __restrict__ dout, WalkOut out) {
-  constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG];
-  __shared__ __attribute__((aligned(16))) _Float16 s_tri[2 * kTriHalfs];
-  __shared__ __attribute__((aligned(16))) float s_scal[kScal];
+template <typename T, int DK>
+struct Stage {
+  static constexpr int kImages = 2 * kTerms<T> * kChunk * DK;   // halfs
+  __attribute__((aligned(16))) _Float16 img[kImages];
+  __attribute__((aligned(16))) _Float16 tri[2 * kTriHalfs];
+  __attribute__((aligned(16))) float scal[kScal];
+};
+template <typename T, int DK>
+constexpr bool kTwice = 2 * sizeof(Stage<T, DK>) <= 158 * 1024;
 
-  const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
-  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-  const int threads = blockDim.x;
-  const int cg = blockIdx.z * (threads >> 6) + (tid >> 6);
-  const bool live = 16 * cg < a.dv;
-  const int col = 16 * cg + i;
-  const Win win = window(a, w);
-  const uint32_t slot0 = first_slot(win.begin, w);
+// Chunk `slot` into a buffer: `tri` is the first triangle wanted, of `tris` kept a chunk.
+template <typename T, int DK>
+__device__ __forceinline__ void stage_chunk(Stage<T, DK>& b, const Args& a, size_t slot, int hk, int h,
+                                            const _Float16* images, const _Float16* tri, int tris, const float* scal,
+                                            int wave, int waves, int lane) {
+  const size_t sh = slot * a.H + h;
+  stage(b.img, images + (slot * a.Hk + hk) * Stage<T, DK>::kImages, sizeof(b.img), wave, waves, lane);
+  stage(b.tri, tri + sh * (size_t)tris * kTriHalfs, sizeof(b.tri), wave, waves, lane);
+  stage(b.scal, scal + sh * kScal, sizeof(b.scal), wave, waves, lane);
+}
 
-  floatx4 S[ST];
+// A chunk's 16 columns of a wave as four tiles of 16 rows.  Loads are unconditional (a row past the
+// chunk's end reads the chunk's first and is dropped when it is used), so that all of them are in
+// flight at once; the rows' places are asked for a chunk earlier than their values.
+struct Places {
+  int row[4][4];
+  __device__ __forceinline__ void ask(const Args& a, int base, int rows, int g) {
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int p = 16 * tau + 4 * g + r;
+        row[tau][r] = base + (p < rows ? p : 0);
+      }
+    if (a.order != nullptr) {
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) row[tau][r] = a.order[row[tau][r]];
+    }
+  }
+};
+template <typename T>
+struct Column {
+  Bits<T> x[4][4];
+  __device__ __forceinline__ void ask(const Args& a, const T* src, const Places& at, int h, int col) {
+    const Bits<T>* p = reinterpret_cast<const Bits<T>*>(src) + (size_t)h * a.dv + col;
+    const size_t step = (size_t)a.H * a.dv;
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int o = at.row[tau][r] < 0 ? 0 : at.row[tau][r] >= a.n ? a.n - 1 : at.row[tau][r];
+        x[tau][r] = p[o * step];
+      }
+  }
+  __device__ __forceinline__ float get(int tau, int r, int g, int rows) const {
+    return 16 * tau + 4 * g + r < rows ? widen<T>(x[tau][r]) : 0.f;
+  }
+};
+// 16 columns of a window's state as result tiles, zero for a null pointer and beyond dk.
+template <int ST>
+__device__ __forceinline__ void load_state(floatx4 (&S)[ST], const Args& a, const float* state, int w, int h, int col,
+                                           bool live, int g) {
+#pragma unroll
+  for (int t = 0; t < ST; ++t) S[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (state == nullptr || !live) return;
+  const float* p = state + (((size_t)w * a.H + h) * a.dk) * a.dv + col;
 #pragma unroll
   for (int t = 0; t < ST; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
-      S[t][r] = state_in != nullptr && live && d < a.dk ? state_in[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] : 0.f;
+      S[t][r] = p[(size_t)(d < a.dk ? d : 0) * a.dv];
     }
+#pragma unroll
+  for (int t = 0; t < ST; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (32 * (t >> 1) + 8 * g + 4 * (t & 1) + r >= a.dk) S[t][r] = 0.f;
+}
+
+template <typename T, int DK, bool KEEP>
+__global__ __launch_bounds__(512) void k_delta_walk(Args a, const T* __restrict__ v, const float* __restrict__ state_in,
+                                                    const _Float16* __restrict__ images,
+                                                    const _Float16* __restrict__ tri, int tris,
+                                                    const float* __restrict__ scal, T* __restrict__ o,
+                                                    const T* __restrict__ dout, WalkOut out) {
+  constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
+  constexpr bool TWICE = kTwice<T, DK>;
+  __shared__ Stage<T, DK> s_a;
+  __shared__ std::conditional_t<TWICE, Stage<T, DK>, char> s_b;
+
+  const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+  const int cg = blockIdx.z * waves + wave;
+  const bool live = 16 * cg < a.dv;
+  const int col = 16 * cg + i;
+  const Win win = window(a, w);
+  const uint32_t slot0 = first_slot(win.begin, w);
+  const int chunks = (win.rows + kChunk - 1) / kChunk;
+
+  floatx4 S[ST];
+  load_state(S, a, state_in, w, h, col, live, g);
   bool carried = state_in != nullptr;   // no products with a state that is zero
-
-  for (int c0 = 0; c0 < win.rows; c0 += kChunk) {
-    const uint32_t slot = slot0 + c0 / kChunk;
-    const int rows = min(kChunk, win.rows - c0);
-    const size_t sh = (size_t)slot * a.H + h;
-    __syncthreads();
-    {
-      const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
-      uint4* dst = reinterpret_cast<uint4*>(s_img);
-      for (int x = tid; x < 2 * NT * IMG / 8; x += threads) dst[x] = src[x];
-      const uint4* st = reinterpret_cast<const uint4*>(tri + sh * (size_t)tris * kTriHalfs);
-      uint4* dt = reinterpret_cast<uint4*>(s_tri);
-      for (int x = tid; x < 2 * kTriHalfs / 8; x += threads) dt[x] = st[x];
-      const uint4* ss = reinterpret_cast<const uint4*>(scal + sh * kScal);
-      uint4* ds = reinterpret_cast<uint4*>(s_scal);
-      for (int x = tid; x < kScal / 4; x += threads) ds[x] = ss[x];
+  Column<T> vc, vn;
+  Places pn;   // of the chunk after the one in work
+  const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
+  if (chunks > 0) {
+    if constexpr (TWICE) stage_chunk<T, DK>(s_a, a, slot0, hk, h, images, tri, tris, scal, wave, waves, lane);
+    if (live) {
+      pn.ask(a, win.begin, rows_of(0), g);
+      vc.ask(a, v, pn, h, col);
+      if (chunks > 1) pn.ask(a, win.begin + kChunk, rows_of(1), g);
     }
-    floatx4 Y[4];
-#pragma unroll
-    for (int tau = 0; tau < 4; ++tau)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * tau + 4 * g + r;
-        Y[tau][r] = 0.f;
-        if (live && row < rows) {
-          const size_t at = (size_t)row_at(a, win.begin + c0 + row) * a.H + h;
-          Y[tau][r] = load1(v + at * a.dv + col);
-        }
-      }
-    __syncthreads();
-    if (!live) continue;
-    const _Float16 *qi = s_img, *ki = s_img + NT * IMG, *st = s_tri, *sp = s_tri + kTriHalfs;
-    auto row4 = [&](int what, int tau) {
-      return *reinterpret_cast<const floatx4*>(s_scal + what + 16 * tau + 4 * g);
-    };
+  }
 
+  // chunk c, staged in `s`
+  const auto work = [&](const Stage<T, DK>& s, int c) {
+    const int rows = rows_of(c);
+    const size_t sh = (size_t)(slot0 + c) * a.H + h;
+    const _Float16 *qi = s.img, *ki = s.img + NT * IMG, *st = s.tri, *sp = s.tri + kTriHalfs;
+    auto row4 = [&](int what, int tau) {
+      return *reinterpret_cast<const floatx4*>(s.scal + what + 16 * tau + 4 * g);
+    };
+    const bool next = c + 1 < chunks;
+    if (next) vn.ask(a, v, pn, h, col);
+    if (c + 2 < chunks) pn.ask(a, win.begin + (c + 2) * kChunk, rows_of(c + 2), g);
     if constexpr (KEEP) {
       float* at = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
 #pragma unroll
@@ -371,13 +442,14 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
       if (!carried && lane == 0) out.smax[sh * (a.dv / 16) + cg] = 0.f;
     }
     // y = 2^-kap v - exp(gam) k' S
+    floatx4 Y[4];
     Pair Sp[KB];
     Scale sc = {1.f, 1.f};
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau) {
       const floatx4 vs = row4(kVScale, tau);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) Y[tau][r] *= vs[r];
+      for (int r = 0; r < 4; ++r) Y[tau][r] = vc.get(tau, r, g, rows) * vs[r];
     }
     if (carried) {
       float m = 0.f;
@@ -405,6 +477,16 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
         for (int r = 0; r < 4; ++r) Y[tau][r] -= since[r] * (x[r] * sc.down);
       }
     }
+    u16x4 dn[KEEP ? 4 : 1];
+    floatx4 df[KEEP ? 4 : 1];
+    if constexpr (KEEP)
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) {
+        const int row = __float_as_int(s.scal[kRow + 16 * tau + i]);
+        const T* at = dout + ((size_t)row * a.H + h) * a.dv + 16 * cg + 4 * g;   // row 0 where there is none
+        if constexpr (NT == 2) df[tau] = *reinterpret_cast<const floatx4*>(at);
+        else dn[tau] = *reinterpret_cast<const u16x4*>(at);
+      }
     // r = T y, u = beta' r
     floatx4 U[4];
     {
@@ -412,15 +494,15 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
       const float ydown = sy.down * (1.f / kTriUp);
       Pair Yp[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) Yp[s] = split(Y[2 * s], Y[2 * s + 1], sy.up);
+      for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s <= tau / 2; ++s) {
-          const _Float16* at = st + 2 * tri_at(tau, s) * kFrag + lane * 8;
+        for (int s2 = 0; s2 <= tau / 2; ++s2) {
+          const _Float16* at = st + 2 * tri_at(tau, s2) * kFrag + lane * 8;
           const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          x = mma2(t, Yp[s], x);
+          x = mma2(t, Yp[s2], x);
         }
         const floatx4 be = row4(kBeta, tau);
 #pragma unroll
@@ -437,7 +519,7 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
       const float udown = su.down * (1.f / kTriUp);
       Pair Up[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) Up[s] = split(U[2 * s], U[2 * s + 1], su.up);
+      for (int s2 = 0; s2 < 2; ++s2) Up[s2] = split(U[2 * s2], U[2 * s2 + 1], su.up);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
@@ -450,31 +532,30 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
           }
         }
 #pragma unroll
-        for (int s = 0; s <= tau / 2; ++s) {
-          const _Float16* at = sp + 2 * tri_at(tau, s) * kFrag + lane * 8;
+        for (int s2 = 0; s2 <= tau / 2; ++s2) {
+          const _Float16* at = sp + 2 * tri_at(tau, s2) * kFrag + lane * 8;
           const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          y = mma2(Up[s], t, y);
+          y = mma2(Up[s2], t, y);
         }
-        const int row = 16 * tau + i;
-        const float since = s_scal[kSince + row] * sc.down, os = s_scal[kOScale + row];
+        const int p = 16 * tau + i;
+        const float since = s.scal[kSince + p] * sc.down, os = s.scal[kOScale + p];
         floatx4 z;
 #pragma unroll
         for (int r = 0; r < 4; ++r) z[r] = os * (since * x[r] + udown * y[r]);
         if constexpr (!KEEP) {
-          if (row < rows) {
-            const size_t at = (size_t)row_at(a, win.begin + c0 + row) * a.H + h;
-            store4(o + at * a.dv + 16 * cg + 4 * g, z);
-          }
+          const int row = __float_as_int(s.scal[kRow + p]);
+          if (p < rows) store4(o + ((size_t)row * a.H + h) * a.dv + 16 * cg + 4 * g, z);
         } else {
           float dot = 0.f;
-          if (row < rows) {
-            const size_t at = (size_t)row_at(a, win.begin + c0 + row) * a.H + h;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dot += z[r] * load1(dout + at * a.dv + 16 * cg + 4 * g + r);
+          for (int r = 0; r < 4; ++r) {
+            if constexpr (NT == 2) dot += z[r] * df[tau][r];
+            else dot += z[r] * widen<T>(dn[tau][r]);
           }
+          dot = p < rows ? dot : 0.f;
           dot += __shfl_xor(dot, 16);
           dot += __shfl_xor(dot, 32);
-          if (g == 0) out.odo[(sh * (a.dv / 16) + cg) * kChunk + row] = dot;
+          if (g == 0) out.odo[(sh * (a.dv / 16) + cg) * kChunk + p] = dot;
         }
       }
     }
@@ -489,20 +570,40 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
       const Scale su = scale_for(U);
       Pair Up[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) Up[s] = split(U[2 * s], U[2 * s + 1], su.up);
-      const float last = s_scal[kLast];
+      for (int s2 = 0; s2 < 2; ++s2) Up[s2] = split(U[2 * s2], U[2 * s2 + 1], su.up);
+      const float last = s.scal[kLast];
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if constexpr (NT == 2) x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s, i, g), Up[s].hi, x);
-          x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s, i, g), Up[s], x);
+        for (int s2 = 0; s2 < 2; ++s2) {
+          if constexpr (NT == 2) x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s2, i, g), Up[s2].hi, x);
+          x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s2, i, g), Up[s2], x);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[t][r] = last * S[t][r] + su.down * x[r];
       }
       carried = true;
+    }
+    vc = vn;
+  };
+
+  if constexpr (TWICE) {
+    const auto turn = [&](const Stage<T, DK>& s, Stage<T, DK>& other, int c) {
+      __syncthreads();   // chunk c is there, and no wave reads the other buffer any more
+      if (c + 1 < chunks) stage_chunk<T, DK>(other, a, slot0 + c + 1, hk, h, images, tri, tris, scal, wave, waves, lane);
+      if (live) work(s, c);
+    };
+    for (int c = 0; c < chunks; c += 2) {
+      turn(s_a, s_b, c);
+      if (c + 1 < chunks) turn(s_b, s_a, c + 1);
+    }
+  } else {
+    for (int c = 0; c < chunks; ++c) {
+      __syncthreads();
+      stage_chunk<T, DK>(s_a, a, slot0 + c, hk, h, images, tri, tris, scal, wave, waves, lane);
+      __syncthreads();
+      if (live) work(s_a, c);
     }
   }
   if (out.state_out != nullptr && live)
@@ -513,6 +614,14 @@ __global__ __launch_bounds__(256) void k_delta_walk(Args a, const T* __restrict_
         const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
         if (d < a.dk) out.state_out[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] = S[t][r];
       }
+}
+
+// Waves of a walk's workgroup.
+inline int walk_waves(const Args& a) {
+  const int groups = a.dv / 16;
+  int most = 8;
+  if (const char* e = getenv("SLA_WAVES")) most = atoi(e);
+  return groups < most ? groups : most;
 }
 
 }  // namespace delta
