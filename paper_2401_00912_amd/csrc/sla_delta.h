@@ -113,17 +113,26 @@ __device__ __forceinline__ floatx4 mma1(const Pair& a, half8_t b, floatx4 c) {
   return mma(a.hi, b, c);
 }
 
-// x scaled by s as two fp16 terms
+// x scaled by s as two fp16 terms.  The product is hidden from the compiler, which would make it
+// twice, once for each term.
 __device__ __forceinline__ Pair split(const floatx4& x0, const floatx4& x1, float s) {
   Pair p;
+  float y[8];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const float y0 = x0[r] * s, y1 = x1[r] * s;
-    p.hi[r] = (_Float16)y0;
-    p.hi[4 + r] = (_Float16)y1;
-    p.lo[r] = (_Float16)(y0 - (float)p.hi[r]);
-    p.lo[4 + r] = (_Float16)(y1 - (float)p.hi[4 + r]);
+  for (int r = 0; r < 4; ++r) y[r] = x0[r] * s, y[4 + r] = x1[r] * s;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    asm("" : "+v"(y[e]));
+    p.hi[e] = (_Float16)y[e];
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p.lo[e] = (_Float16)(y[e] - (float)p.hi[e]);
+  return p;
+}
+__device__ __forceinline__ half8_t narrow(const floatx4& x0, const floatx4& x1, float s) {
+  half8_t p;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) p[r] = (_Float16)(x0[r] * s), p[4 + r] = (_Float16)(x1[r] * s);
   return p;
 }
 
@@ -203,7 +212,8 @@ __device__ __forceinline__ half8_t image_cols(const _Float16* img, int t, int p,
   }
   return x;
 }
-// number of the triangle's operand for row tile tau and column block s
+// Operands of a triangle: the six first terms, then the six second ones; number of row tile tau's
+// operand for column block s:
 __device__ __forceinline__ constexpr int tri_at(int tau, int s) { return tau < 2 ? tau : 2 * tau - 2 + s; }
 
 // ------------------------------------------------------------------ staging

@@ -19,10 +19,12 @@ hipError_t forward_impl(const Args& a, int dtype, const void* q, const void* k, 
   if (a.n > 0)
     k_delta_prep<T, DK, false><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
         a, static_cast<const T*>(q), static_cast<const T*>(k), g, beta, images, tri, scal);
-  const int groups = a.dv / 16, waves = walk_waves(a);
-  k_delta_walk<T, DK, false><<<dim3(a.W, a.H, (groups + waves - 1) / waves), 64 * waves, 0, stream>>>(
-      a, static_cast<const T*>(v), state_in, images, tri, 2, scal, static_cast<T*>(o), nullptr,
-      WalkOut{state_out, nullptr, nullptr, nullptr, nullptr});
+  with_walk<T>(a, [&](auto nw, dim3 grid) {
+    constexpr int NW = decltype(nw)::value;
+    k_delta_walk<T, DK, false, NW><<<grid, 64 * NW, 0, stream>>>(
+        a, static_cast<const T*>(v), state_in, images, tri, 2, scal, static_cast<T*>(o), nullptr,
+        WalkOut{state_out, nullptr, nullptr, nullptr, nullptr});
+  });
   return hipGetLastError();
 }
 

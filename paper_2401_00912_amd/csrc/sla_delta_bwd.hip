@@ -56,22 +56,24 @@ BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int
 
 // ------------------------------------------------------------------ the walk back
 // As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
-template <typename T, int DK>
-__global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict__ dout, const float* __restrict__ dstate,
-                                                    const _Float16* __restrict__ images,
-                                                    const _Float16* __restrict__ tri, const float* __restrict__ scal,
-                                                    const float* __restrict__ states, float* __restrict__ lam,
-                                                    float* __restrict__ dstates, float* __restrict__ dmax,
-                                                    float* __restrict__ start, float* __restrict__ dstate_in) {
+template <typename T, int DK, int NW>
+__global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restrict__ dout,
+                                                        const float* __restrict__ dstate,
+                                                        const _Float16* __restrict__ images,
+                                                        const _Float16* __restrict__ tri,
+                                                        const float* __restrict__ scal,
+                                                        const float* __restrict__ states, float* __restrict__ lam,
+                                                        float* __restrict__ dstates, float* __restrict__ dmax,
+                                                        float* __restrict__ start, float* __restrict__ dstate_in) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  constexpr bool TWICE = kTwice<T, DK>;
-  __shared__ Stage<T, DK> s_a;
-  __shared__ std::conditional_t<TWICE, Stage<T, DK>, char> s_b;
+  constexpr bool TWICE = kTwice<T, DK, NW>;
+  __shared__ Stage<T, DK, NW> s_a;
+  __shared__ std::conditional_t<TWICE, Stage<T, DK, NW>, char> s_b;
 
   const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-  const int cg = blockIdx.z * waves + wave;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = blockIdx.z * NW + wave;
   const bool live = 16 * cg < a.dv;
   const int col = 16 * cg + i;
   const Win win = window(a, w);
@@ -82,21 +84,19 @@ __global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict_
   floatx4 S[ST];
   load_state(S, a, dstate, w, h, col, live, g);
   bool carried = dstate != nullptr;
-  Column<T> oc, on;
-  Places pn;   // of the chunk before the one in work
-  // the transposed triangles are the third and fourth of a chunk
-  const _Float16* tri_t = tri + 2 * kTriHalfs;
+  Places<T> at;
+  const auto fetch = [&](Stage<T, DK, NW>& s, int c) {   // at: chunk c's places, then chunk c - 1's
+    // the transposed triangles are the third and fourth of a chunk
+    stage_chunk<T, DK, NW, false>(s, a, slot0 + c, hk, h, cg, live, images, tri + 2 * kTriHalfs, 4, scal, dout, at,
+                                  wave, lane);
+    if (c > 0) at.ask(a, win.begin + (c - 1) * kChunk, rows_of(c - 1), lane);
+  };
   if (chunks > 0) {
-    const int c = chunks - 1;
-    if constexpr (TWICE) stage_chunk<T, DK>(s_a, a, slot0 + c, hk, h, images, tri_t, 4, scal, wave, waves, lane);
-    if (live) {
-      pn.ask(a, win.begin + c * kChunk, rows_of(c), g);
-      oc.ask(a, dout, pn, h, col);
-      if (c > 0) pn.ask(a, win.begin + (c - 1) * kChunk, rows_of(c - 1), g);
-    }
+    at.ask(a, win.begin + (chunks - 1) * kChunk, rows_of(chunks - 1), lane);
+    if constexpr (TWICE) fetch(s_a, chunks - 1);
   }
 
-  const auto work = [&](const Stage<T, DK>& s, int c) {
+  const auto work = [&](const Stage<T, DK, NW>& s, int c) {
     const int rows = rows_of(c);
     const size_t sh = (size_t)(slot0 + c) * a.H + h;
     const _Float16 *qi = s.img, *ki = s.img + NT * IMG, *st = s.tri, *sp = s.tri + kTriHalfs;
@@ -104,70 +104,38 @@ __global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict_
       return *reinterpret_cast<const floatx4*>(s.scal + what + 16 * tau + 4 * g);
     };
     const size_t sgrp = sh * (a.dv / 16) + cg;
-    if (c > 0) on.ask(a, dout, pn, h, col);
-    if (c > 1) pn.ask(a, win.begin + (c - 2) * kChunk, rows_of(c - 2), g);
-
-    uint32_t top = 0;
-    {
-      float m = 0.f;
+    floatx4 s0[ST];   // the state before the chunk, for the end
 #pragma unroll
-      for (int t = 0; t < ST; ++t) {
-        *reinterpret_cast<floatx4*>(dstates + sgrp * ST * 256 + t * 256 + lane * 4) = S[t];
+    for (int t = 0; t < ST; ++t) s0[t] = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[t][r]));
-      }
-      top = wave_max_bits(m);
-      if (lane == 0) dmax[sgrp] = __uint_as_float(top);
-    }
+    for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(dstates + sgrp * ST * 256 + t * 256 + lane * 4) = S[t];
+    const uint32_t top = wave_max_bits(max_of(S));
+    if (lane == 0) dmax[sgrp] = __uint_as_float(top);
     // du = P^T do' + until k' dS
     floatx4 X[4], Y[4];
+    rows_in(s.rows[wave], Y, rows, i, g);
     {
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-        const floatx4 os = row4(kOScale, tau);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) Y[tau][r] = oc.get(tau, r, g, rows) * os[r];
-      }
+      for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kOScale, tau);
       const Scale sy = scale_for(Y);
       const float ydown = sy.down * (1.f / kTriUp);
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
+      tri_times<true>(sp, Yp, X, lane);
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s2 = tau / 2; s2 < 2; ++s2) {
-          const _Float16* at = sp + 2 * tri_at(3 - tau, 1 - s2) * kFrag + lane * 8;
-          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          x = mma2(t, Yp[s2], x);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) X[tau][r] = x[r] * ydown;
-      }
+      for (int tau = 0; tau < 4; ++tau) X[tau] *= ydown;
     }
     if (carried) {
       const Scale sc = scale_of(top);
       Pair Sp[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
+      floatx4 x[4];
+      rows_times<NT, DK>(ki, Sp, x, i, g);
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const half8_t kr = image_rows<DK>(ki, tau, kb, i, g);
-          if constexpr (NT == 2) x = mma(image_rows<DK>(ki + IMG, tau, kb, i, g), Sp[kb].hi, x);
-          x = mma1(kr, Sp[kb], x);
-        }
-        const floatx4 un = row4(kUntil, tau);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) X[tau][r] += un[r] * (x[r] * sc.down);
-      }
+      for (int tau = 0; tau < 4; ++tau) X[tau] += (row4(kUntil, tau) * sc.down) * x[tau];
     }
-    floatx4 s0[ST];   // the state before the chunk, for the end
-#pragma unroll
-    for (int t = 0; t < ST; ++t) s0[t] = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
     // lam, then -since mu in X and since do' in Y
     {
       const Scale sx = scale_for(X);
@@ -175,33 +143,20 @@ __global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict_
       Pair Xp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sx.up);
+      tri_times<true>(st, Xp, X, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+        const floatx4 since = row4(kSince, tau);
+        X[tau] *= xdown;
 #pragma unroll
-        for (int s2 = tau / 2; s2 < 2; ++s2) {
-          const _Float16* at = st + 2 * tri_at(3 - tau, 1 - s2) * kFrag + lane * 8;
-          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          x = mma2(t, Xp[s2], x);
-        }
-        const floatx4 be = row4(kBeta, tau), since = row4(kSince, tau);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float y = x[r] * xdown;
-          lam[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = y;
-          X[tau][r] = -since[r] * (be[r] * y);
-          Y[tau][r] *= since[r];
-        }
+        for (int r = 0; r < 4; ++r) lam[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = X[tau][r];
+        X[tau] *= -since * row4(kBeta, tau);
+        Y[tau] *= since;
       }
     }
     // dS = exp(gam_last) dS + q'^T (since do') - k'^T (since mu)
     {
-      float m = 0.f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) m = fmaxf(m, fmaxf(fabsf(X[t][r]), fabsf(Y[t][r])));
-      const Scale sc = scale_of(wave_max_bits(m));
+      const Scale sc = scale_of(wave_max_bits(fmaxf(max_of(X), max_of(Y))));
       Pair Xp[2], Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
@@ -222,24 +177,21 @@ __global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict_
           x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s2, i, g), Xp[s2], x);
           x = mma1(image_cols<DK>(qi, t >> 1, t & 1, s2, i, g), Yp[s2], x);
         }
+        S[t] = last * S[t] + sc.down * x;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          S[t][r] = last * S[t][r] + sc.down * x[r];
-          dot += s0[t][r] * S[t][r];
-        }
+        for (int r = 0; r < 4; ++r) dot += s0[t][r] * S[t][r];
       }
 #pragma unroll
       for (int m2 = 1; m2 < 64; m2 *= 2) dot += __shfl_xor(dot, m2);
       if (lane == 0) start[sgrp] = dot;
       carried = true;
     }
-    oc = on;
   };
 
   if constexpr (TWICE) {
-    const auto turn = [&](const Stage<T, DK>& s, Stage<T, DK>& other, int c) {
+    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) {
       __syncthreads();   // chunk c is there, and no wave reads the other buffer any more
-      if (c > 0) stage_chunk<T, DK>(other, a, slot0 + c - 1, hk, h, images, tri_t, 4, scal, wave, waves, lane);
+      if (c > 0) fetch(other, c - 1);
       if (live) work(s, c);
     };
     for (int c = chunks - 1; c >= 0; c -= 2) {
@@ -249,19 +201,12 @@ __global__ __launch_bounds__(512) void k_delta_back(Args a, const T* __restrict_
   } else {
     for (int c = chunks - 1; c >= 0; --c) {
       __syncthreads();
-      stage_chunk<T, DK>(s_a, a, slot0 + c, hk, h, images, tri_t, 4, scal, wave, waves, lane);
+      fetch(s_a, c);
       __syncthreads();
       if (live) work(s_a, c);
     }
   }
-  if (dstate_in != nullptr && live)
-#pragma unroll
-    for (int t = 0; t < ST; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
-        if (d < a.dk) dstate_in[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] = S[t][r];
-      }
+  store_state(S, a, dstate_in, w, h, col, live, g);
 }
 
 // ------------------------------------------------------------------ the rest, all chunks at once
@@ -650,23 +595,24 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
   const auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   float* scal = at(sp.base.scal);
   const T *v = static_cast<const T*>(b.v), *dout = static_cast<const T*>(b.dout);
-  const int groups = a.dv / 16, waves = walk_waves(a);
-  const dim3 walk(a.W, a.H, (groups + waves - 1) / waves);
-  if (a.n > 0) {
+  if (a.n > 0)
     k_delta_prep<T, DK, true><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
         a, static_cast<const T*>(b.q), static_cast<const T*>(b.k), b.g, b.beta, images, tri, scal);
-    k_delta_walk<T, DK, true><<<walk, 64 * waves, 0, stream>>>(
-        a, v, b.state_in, images, tri, 4, scal, nullptr, dout,
-        WalkOut{nullptr, at(sp.states), at(sp.smax), at(sp.resid), at(sp.odo)});
-  }
-  k_delta_back<T, DK><<<walk, 64 * waves, 0, stream>>>(a, dout, b.dstate_out, images, tri, scal, at(sp.states),
-                                                       at(sp.lam), at(sp.dstates), at(sp.dmax), at(sp.start),
-                                                       b.dstate_in);
+  with_walk<T>(a, [&](auto nw, dim3 grid) {
+    constexpr int NW = decltype(nw)::value;
+    if (a.n > 0)
+      k_delta_walk<T, DK, true, NW><<<grid, 64 * NW, 0, stream>>>(
+          a, v, b.state_in, images, tri, 4, scal, nullptr, dout,
+          WalkOut{nullptr, at(sp.states), at(sp.smax), at(sp.resid), at(sp.odo)});
+    k_delta_back<T, DK, NW><<<grid, 64 * NW, 0, stream>>>(a, dout, b.dstate_out, images, tri, scal, at(sp.states),
+                                                          at(sp.lam), at(sp.dstates), at(sp.dmax), at(sp.start),
+                                                          b.dstate_in);
+  });
   if (a.n > 0)
     k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
         a, v, dout, b.g, images, scal, at(sp.states), at(sp.dstates), at(sp.smax), at(sp.dmax), at(sp.resid),
-        at(sp.lam), at(sp.odo), at(sp.start), b.state_in != nullptr, b.dstate_out != nullptr, static_cast<T*>(b.dq), static_cast<T*>(b.dk),
-        static_cast<T*>(b.dv), b.dg, b.dbeta);
+        at(sp.lam), at(sp.odo), at(sp.start), b.state_in != nullptr, b.dstate_out != nullptr, static_cast<T*>(b.dq),
+        static_cast<T*>(b.dk), static_cast<T*>(b.dv), b.dg, b.dbeta);
   return hipGetLastError();
 }
 

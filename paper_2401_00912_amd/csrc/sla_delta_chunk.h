@@ -80,9 +80,9 @@ __device__ __forceinline__ void put_tri(const float* m, _Float16* out, int tau, 
     const floatx4 x0 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 4 * g);
     const floatx4 x1 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 16 + 4 * g);
     const Pair p = split(x0, x1, kTriUp);
-    _Float16* at = out + 2 * tri_at(tau, s) * kFrag + lane * 8;
+    _Float16* at = out + tri_at(tau, s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(at) = p.hi;
-    *reinterpret_cast<half8_t*>(at + kFrag) = p.lo;
+    *reinterpret_cast<half8_t*>(at + kTri * kFrag) = p.lo;
   }
 }
 // The transposed matrix's operands of tile row `tau`: upper triangular, kept under the mirrored
@@ -96,9 +96,9 @@ __device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, int tau
       x1[r] = m[(32 * s + 16 + 4 * g + r) * kLd + 16 * tau + i];
     }
     const Pair p = split(x0, x1, kTriUp);
-    _Float16* at = out + 2 * tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
+    _Float16* at = out + tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(at) = p.hi;
-    *reinterpret_cast<half8_t*>(at + kFrag) = p.lo;
+    *reinterpret_cast<half8_t*>(at + kTri * kFrag) = p.lo;
   }
 }
 
@@ -294,10 +294,10 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
 // products with k' and q' without moving a value, and so are the chunk's r and u (16 rows a tile);
 // the columns are independent of each other, so no wave waits for another but for the staging.
 //
-// The chunks of a window depend on each other, so their latency counts: a chunk's images, triangles
-// and scalars (58 KB at dk = 128 in 16 bits) are moved into the second of two LDS buffers while the
-// first one's chunk is worked on, with one barrier a chunk, and its v is loaded ahead into registers.
-// fp32 rows of dk = 128 (90 KB) do not fit twice and are staged between two barriers.
+// The chunks of a window depend on each other, so their latency counts: a chunk's images, triangles,
+// scalars and the waves' columns of v are moved into the second of two LDS buffers while the first
+// one's chunk is worked on, with one barrier a chunk.  fp32 rows of dk = 128 do not fit twice and are
+// staged between two barriers.
 struct WalkOut {
   float* state_out;    // final states or null
   float* states;       // the states before every chunk [slot][H][dv / 16], in register order, or null
@@ -306,66 +306,88 @@ struct WalkOut {
   float* odo;          // sums over 16 columns of o dout [slot][H][dv / 16][64], or null
 };
 
-template <typename T, int DK>
+// P needs its second terms where o is kept to more than bf16's 8 bits (one fp16 term is off by 2^-11).
+template <typename T, bool KEEP>
+constexpr bool kShortOut = std::is_same<T, bf16_t>::value && !KEEP;
+
+template <typename T, int DK, int NW>
 struct Stage {
   static constexpr int kImages = 2 * kTerms<T> * kChunk * DK;   // halfs
   __attribute__((aligned(16))) _Float16 img[kImages];
   __attribute__((aligned(16))) _Float16 tri[2 * kTriHalfs];
   __attribute__((aligned(16))) float scal[kScal];
+  __attribute__((aligned(16))) T rows[NW][kChunk * 16];         // 16 columns of v (or dout) a wave
 };
-template <typename T, int DK>
-constexpr bool kTwice = 2 * sizeof(Stage<T, DK>) <= 158 * 1024;
+template <typename T, int DK, int NW>
+constexpr bool kTwice = 2 * sizeof(Stage<T, DK, NW>) <= 160 * 1024;
 
-// Chunk `slot` into a buffer: `tri` is the first triangle wanted, of `tris` kept a chunk.
-template <typename T, int DK>
-__device__ __forceinline__ void stage_chunk(Stage<T, DK>& b, const Args& a, size_t slot, int hk, int h,
-                                            const _Float16* images, const _Float16* tri, int tris, const float* scal,
-                                            int wave, int waves, int lane) {
-  const size_t sh = slot * a.H + h;
-  stage(b.img, images + (slot * a.Hk + hk) * Stage<T, DK>::kImages, sizeof(b.img), wave, waves, lane);
-  stage(b.tri, tri + sh * (size_t)tris * kTriHalfs, sizeof(b.tri), wave, waves, lane);
-  stage(b.scal, scal + sh * kScal, sizeof(b.scal), wave, waves, lane);
-}
-
-// A chunk's 16 columns of a wave as four tiles of 16 rows.  Loads are unconditional (a row past the
-// chunk's end reads the chunk's first and is dropped when it is used), so that all of them are in
-// flight at once; the rows' places are asked for a chunk earlier than their values.
+// Places of the rows whose 16 bytes this lane moves: kMoves instructions move a wave's 64 rows of 16
+// columns.  They are asked for a chunk earlier than the rows.
+template <typename T>
+constexpr int kMoves = sizeof(T);   // 64 rows x 16 columns / 1,024 bytes
+template <typename T>
 struct Places {
-  int row[4][4];
-  __device__ __forceinline__ void ask(const Args& a, int base, int rows, int g) {
+  int row[kMoves<T>];
+  __device__ __forceinline__ void ask(const Args& a, int base, int rows, int lane) {
 #pragma unroll
-    for (int tau = 0; tau < 4; ++tau)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int p = 16 * tau + 4 * g + r;
-        row[tau][r] = base + (p < rows ? p : 0);
-      }
+    for (int n = 0; n < kMoves<T>; ++n) {
+      const int p = (n * 64 + lane) / kMoves<T>;
+      row[n] = base + (p < rows ? p : 0);   // a row past the end: the first one, dropped when it is used
+    }
     if (a.order != nullptr) {
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) row[tau][r] = a.order[row[tau][r]];
+      for (int n = 0; n < kMoves<T>; ++n) row[n] = a.order[row[n]];
     }
   }
 };
+
+// Chunk `slot` into a buffer: `tri` is the first of two triangles in a row, of `tris` kept a chunk; the
+// wave's columns of `src` if it has any.
+template <typename T, int DK, int NW, bool SHORT>
+__device__ __forceinline__ void stage_chunk(Stage<T, DK, NW>& b, const Args& a, size_t slot, int hk, int h, int cg,
+                                            bool live, const _Float16* images, const _Float16* tri, int tris,
+                                            const float* scal, const T* src, const Places<T>& at, int wave, int lane) {
+  const size_t sh = slot * a.H + h;
+  if (live) {
+#pragma unroll
+    for (int n = 0; n < kMoves<T>; ++n) {
+      const int o = at.row[n] < 0 ? 0 : at.row[n] >= a.n ? a.n - 1 : at.row[n];
+      const T* p = src + ((size_t)o * a.H + h) * a.dv + 16 * cg + (lane % kMoves<T>) * (16 / (int)sizeof(T));
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                       (__attribute__((address_space(3))) void*)(b.rows[wave] + n * (1024 / sizeof(T))),
+                                       16, 0, 0);
+    }
+  }
+  stage(b.img, images + (slot * a.Hk + hk) * Stage<T, DK, NW>::kImages, sizeof(b.img), wave, NW, lane);
+  stage(b.tri, tri + sh * (size_t)tris * kTriHalfs, sizeof(b.tri) - (SHORT ? kTriHalfs : 0), wave, NW, lane);
+  stage(b.scal, scal + sh * kScal, sizeof(b.scal), wave, NW, lane);
+}
+
+// The wave's columns of a staged chunk as result tiles, rows from `rows` on zero.
 template <typename T>
-struct Column {
-  Bits<T> x[4][4];
-  __device__ __forceinline__ void ask(const Args& a, const T* src, const Places& at, int h, int col) {
-    const Bits<T>* p = reinterpret_cast<const Bits<T>*>(src) + (size_t)h * a.dv + col;
-    const size_t step = (size_t)a.H * a.dv;
+__device__ __forceinline__ void rows_in(const T* at, floatx4 (&x)[4], int rows, int i, int g) {
+#pragma unroll
+  for (int tau = 0; tau < 4; ++tau) {
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[tau][r] = at[(16 * tau + 4 * g + r) * 16 + i];
+    } else {
+      const unsigned short* p = reinterpret_cast<const unsigned short*>(at) + (16 * tau + 4 * g + (i >> 2)) * 16 + 4 * (i & 3);
+      const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) short4v*)(const_cast<unsigned short*>(p)));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[tau][r] = u16_to_f32<T>((unsigned short)y[r]);
+    }
+  }
+  if (rows < kChunk) {
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int o = at.row[tau][r] < 0 ? 0 : at.row[tau][r] >= a.n ? a.n - 1 : at.row[tau][r];
-        x[tau][r] = p[o * step];
-      }
+      for (int r = 0; r < 4; ++r)
+        if (16 * tau + 4 * g + r >= rows) x[tau][r] = 0.f;
   }
-  __device__ __forceinline__ float get(int tau, int r, int g, int rows) const {
-    return 16 * tau + 4 * g + r < rows ? widen<T>(x[tau][r]) : 0.f;
-  }
-};
+}
+
 // 16 columns of a window's state as result tiles, zero for a null pointer and beyond dk.
 template <int ST>
 __device__ __forceinline__ void load_state(floatx4 (&S)[ST], const Args& a, const float* state, int w, int h, int col,
@@ -387,106 +409,135 @@ __device__ __forceinline__ void load_state(floatx4 (&S)[ST], const Args& a, cons
     for (int r = 0; r < 4; ++r)
       if (32 * (t >> 1) + 8 * g + 4 * (t & 1) + r >= a.dk) S[t][r] = 0.f;
 }
+template <int ST>
+__device__ __forceinline__ void store_state(const floatx4 (&S)[ST], const Args& a, float* state, int w, int h, int col,
+                                            bool live, int g) {
+  if (state == nullptr || !live) return;
+  float* p = state + (((size_t)w * a.H + h) * a.dk) * a.dv + col;
+#pragma unroll
+  for (int t = 0; t < ST; ++t) {
+    const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1);   // dk is a multiple of 16
+    if (d < a.dk)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[(size_t)(d + r) * a.dv] = S[t][r];
+  }
+}
+template <int N>
+__device__ __forceinline__ float max_of(const floatx4 (&x)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[t][r]));
+  return m;
+}
 
-template <typename T, int DK, bool KEEP>
-__global__ __launch_bounds__(512) void k_delta_walk(Args a, const T* __restrict__ v, const float* __restrict__ state_in,
-                                                    const _Float16* __restrict__ images,
-                                                    const _Float16* __restrict__ tri, int tris,
-                                                    const float* __restrict__ scal, T* __restrict__ o,
-                                                    const T* __restrict__ dout, WalkOut out) {
+// x[tau] = triangle times y, lower (UPPER: the transposed triangle under its mirrored numbers)
+template <bool UPPER>
+__device__ __forceinline__ void tri_times(const _Float16* tri, const Pair (&y)[2], floatx4 (&x)[4], int lane) {
+#pragma unroll
+  for (int tau = 0; tau < 4; ++tau) x[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau) {
+      if (UPPER ? s < tau / 2 : s > tau / 2) continue;
+      const _Float16* at = tri + (UPPER ? tri_at(3 - tau, 1 - s) : tri_at(tau, s)) * kFrag + lane * 8;
+      const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kTri * kFrag)};
+      x[tau] = mma2(t, y[s], x[tau]);
+    }
+}
+// x[tau] = rows of the image times the state's columns
+template <int NT, int DK>
+__device__ __forceinline__ void rows_times(const _Float16* img, const Pair (&S)[DK / 32], floatx4 (&x)[4], int i, int g) {
+#pragma unroll
+  for (int tau = 0; tau < 4; ++tau) x[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kb = 0; kb < DK / 32; ++kb)
+#pragma unroll
+    for (int tau = 0; tau < 4; ++tau) {
+      const half8_t r = image_rows<DK>(img, tau, kb, i, g);
+      if constexpr (NT == 2) x[tau] = mma(image_rows<DK>(img + kChunk * DK, tau, kb, i, g), S[kb].hi, x[tau]);
+      x[tau] = mma1(r, S[kb], x[tau]);
+    }
+}
+
+template <typename T, int DK, bool KEEP, int NW>
+__global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restrict__ v,
+                                                        const float* __restrict__ state_in,
+                                                        const _Float16* __restrict__ images,
+                                                        const _Float16* __restrict__ tri, int tris,
+                                                        const float* __restrict__ scal, T* __restrict__ o,
+                                                        const T* __restrict__ dout, WalkOut out) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  constexpr bool TWICE = kTwice<T, DK>;
-  __shared__ Stage<T, DK> s_a;
-  __shared__ std::conditional_t<TWICE, Stage<T, DK>, char> s_b;
+  constexpr bool TWICE = kTwice<T, DK, NW>, SHORT = kShortOut<T, KEEP>;
+  __shared__ Stage<T, DK, NW> s_a;
+  __shared__ std::conditional_t<TWICE, Stage<T, DK, NW>, char> s_b;
 
   const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-  const int cg = blockIdx.z * waves + wave;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = blockIdx.z * NW + wave;
   const bool live = 16 * cg < a.dv;
   const int col = 16 * cg + i;
   const Win win = window(a, w);
   const uint32_t slot0 = first_slot(win.begin, w);
   const int chunks = (win.rows + kChunk - 1) / kChunk;
+  const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
 
   floatx4 S[ST];
   load_state(S, a, state_in, w, h, col, live, g);
   bool carried = state_in != nullptr;   // no products with a state that is zero
-  Column<T> vc, vn;
-  Places pn;   // of the chunk after the one in work
-  const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
+  Places<T> at;
+  const auto fetch = [&](Stage<T, DK, NW>& s, int c) {   // at: chunk c's places, then chunk c + 1's
+    stage_chunk<T, DK, NW, SHORT>(s, a, slot0 + c, hk, h, cg, live, images, tri, tris, scal, v, at, wave, lane);
+    if (c + 1 < chunks) at.ask(a, win.begin + (c + 1) * kChunk, rows_of(c + 1), lane);
+  };
   if (chunks > 0) {
-    if constexpr (TWICE) stage_chunk<T, DK>(s_a, a, slot0, hk, h, images, tri, tris, scal, wave, waves, lane);
-    if (live) {
-      pn.ask(a, win.begin, rows_of(0), g);
-      vc.ask(a, v, pn, h, col);
-      if (chunks > 1) pn.ask(a, win.begin + kChunk, rows_of(1), g);
-    }
+    at.ask(a, win.begin, rows_of(0), lane);
+    if constexpr (TWICE) fetch(s_a, 0);
   }
 
   // chunk c, staged in `s`
-  const auto work = [&](const Stage<T, DK>& s, int c) {
+  const auto work = [&](const Stage<T, DK, NW>& s, int c) {
     const int rows = rows_of(c);
     const size_t sh = (size_t)(slot0 + c) * a.H + h;
     const _Float16 *qi = s.img, *ki = s.img + NT * IMG, *st = s.tri, *sp = s.tri + kTriHalfs;
     auto row4 = [&](int what, int tau) {
       return *reinterpret_cast<const floatx4*>(s.scal + what + 16 * tau + 4 * g);
     };
-    const bool next = c + 1 < chunks;
-    if (next) vn.ask(a, v, pn, h, col);
-    if (c + 2 < chunks) pn.ask(a, win.begin + (c + 2) * kChunk, rows_of(c + 2), g);
-    if constexpr (KEEP) {
-      float* at = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
+    int place[4];   // this lane's row of every tile
 #pragma unroll
-      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(at + t * 256) = S[t];
+    for (int tau = 0; tau < 4; ++tau) place[tau] = __float_as_int(s.scal[kRow + 16 * tau + i]);
+    Raw<T, 4> dn[KEEP ? 4 : 1];
+    if constexpr (KEEP) {
+      float* to = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t];
       if (!carried && lane == 0) out.smax[sh * (a.dv / 16) + cg] = 0.f;
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau)   // row 0 where there is none
+        dn[tau] = *reinterpret_cast<const Raw<T, 4>*>(dout + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g);
     }
     // y = 2^-kap v - exp(gam) k' S
     floatx4 Y[4];
     Pair Sp[KB];
     Scale sc = {1.f, 1.f};
+    rows_in(s.rows[wave], Y, rows, i, g);
 #pragma unroll
-    for (int tau = 0; tau < 4; ++tau) {
-      const floatx4 vs = row4(kVScale, tau);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) Y[tau][r] = vc.get(tau, r, g, rows) * vs[r];
-    }
+    for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kVScale, tau);
     if (carried) {
-      float m = 0.f;
-#pragma unroll
-      for (int t = 0; t < ST; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[t][r]));
-      const uint32_t top = wave_max_bits(m);
+      const uint32_t top = wave_max_bits(max_of(S));
       sc = scale_of(top);
       if constexpr (KEEP)
         if (lane == 0) out.smax[sh * (a.dv / 16) + cg] = __uint_as_float(top);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
+      floatx4 x[4];
+      rows_times<NT, DK>(ki, Sp, x, i, g);
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const half8_t kr = image_rows<DK>(ki, tau, kb, i, g);
-          if constexpr (NT == 2) x = mma(image_rows<DK>(ki + IMG, tau, kb, i, g), Sp[kb].hi, x);
-          x = mma1(kr, Sp[kb], x);
-        }
-        const floatx4 since = row4(kSince, tau);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) Y[tau][r] -= since[r] * (x[r] * sc.down);
-      }
+      for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSince, tau) * sc.down) * x[tau];
     }
-    u16x4 dn[KEEP ? 4 : 1];
-    floatx4 df[KEEP ? 4 : 1];
-    if constexpr (KEEP)
-#pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-        const int row = __float_as_int(s.scal[kRow + 16 * tau + i]);
-        const T* at = dout + ((size_t)row * a.H + h) * a.dv + 16 * cg + 4 * g;   // row 0 where there is none
-        if constexpr (NT == 2) df[tau] = *reinterpret_cast<const floatx4*>(at);
-        else dn[tau] = *reinterpret_cast<const u16x4*>(at);
-      }
     // r = T y, u = beta' r
     floatx4 U[4];
     {
@@ -495,63 +546,58 @@ __global__ __launch_bounds__(512) void k_delta_walk(Args a, const T* __restrict_
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
+      tri_times<false>(st, Yp, U, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (KEEP) {
 #pragma unroll
-        for (int s2 = 0; s2 <= tau / 2; ++s2) {
-          const _Float16* at = st + 2 * tri_at(tau, s2) * kFrag + lane * 8;
-          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          x = mma2(t, Yp[s2], x);
+          for (int r = 0; r < 4; ++r)
+            out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = U[tau][r] * ydown;
         }
-        const floatx4 be = row4(kBeta, tau);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float y = x[r] * ydown;
-          if constexpr (KEEP) out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = y;
-          U[tau][r] = be[r] * y;
-        }
+        U[tau] *= row4(kBeta, tau) * ydown;
       }
     }
     // o, transposed: a lane holds 4 columns of one row
     {
       const Scale su = scale_for(U);
       const float udown = su.down * (1.f / kTriUp);
-      Pair Up[2];
+      floatx4 x[4], y[4];
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) Up[s2] = split(U[2 * s2], U[2 * s2 + 1], su.up);
+      for (int tau = 0; tau < 4; ++tau) x[tau] = y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (carried) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int tau = 0; tau < 4; ++tau) {
+            const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
+            if constexpr (NT == 2) x[tau] = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), x[tau]);
+            x[tau] = SHORT ? mma(Sp[kb].hi, qr, x[tau]) : mma1(Sp[kb], qr, x[tau]);
+          }
+      }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const half8_t un = narrow(U[2 * s2], U[2 * s2 + 1], su.up);
+        const Pair up = SHORT ? Pair{un, un} : split(U[2 * s2], U[2 * s2 + 1], su.up);
+#pragma unroll
+        for (int tau = 2 * s2; tau < 4; ++tau) {
+          const _Float16* p = sp + tri_at(tau, s2) * kFrag + lane * 8;
+          const half8_t hi = *reinterpret_cast<const half8_t*>(p);
+          if constexpr (SHORT) y[tau] = mma(un, hi, y[tau]);
+          else y[tau] = mma2(up, Pair{hi, *reinterpret_cast<const half8_t*>(p + kTri * kFrag)}, y[tau]);
+        }
+      }
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
-        if (carried) {
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb) {
-            const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
-            if constexpr (NT == 2) x = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), x);
-            x = mma1(Sp[kb], qr, x);
-          }
-        }
-#pragma unroll
-        for (int s2 = 0; s2 <= tau / 2; ++s2) {
-          const _Float16* at = sp + 2 * tri_at(tau, s2) * kFrag + lane * 8;
-          const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kFrag)};
-          y = mma2(Up[s2], t, y);
-        }
         const int p = 16 * tau + i;
-        const float since = s.scal[kSince + p] * sc.down, os = s.scal[kOScale + p];
-        floatx4 z;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) z[r] = os * (since * x[r] + udown * y[r]);
+        const float os = s.scal[kOScale + p], since = os * s.scal[kSince + p] * sc.down;
+        const floatx4 z = since * x[tau] + (os * udown) * y[tau];
         if constexpr (!KEEP) {
-          const int row = __float_as_int(s.scal[kRow + p]);
-          if (p < rows) store4(o + ((size_t)row * a.H + h) * a.dv + 16 * cg + 4 * g, z);
+          if (p < rows) store4(o + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g, z);
         } else {
-          float dot = 0.f;
+          float d4[4], dot = 0.f;
+          Frag<T, 4>::to_f32(dn[tau], d4);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if constexpr (NT == 2) dot += z[r] * df[tau][r];
-            else dot += z[r] * widen<T>(dn[tau][r]);
-          }
+          for (int r = 0; r < 4; ++r) dot += z[r] * d4[r];
           dot = p < rows ? dot : 0.f;
           dot += __shfl_xor(dot, 16);
           dot += __shfl_xor(dot, 32);
@@ -562,11 +608,7 @@ __global__ __launch_bounds__(512) void k_delta_walk(Args a, const T* __restrict_
     // S = exp(gam_last) S + k'^T (until u)
     {
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) {
-        const floatx4 un = row4(kUntil, tau);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) U[tau][r] *= un[r];
-      }
+      for (int tau = 0; tau < 4; ++tau) U[tau] *= row4(kUntil, tau);
       const Scale su = scale_for(U);
       Pair Up[2];
 #pragma unroll
@@ -580,18 +622,16 @@ __global__ __launch_bounds__(512) void k_delta_walk(Args a, const T* __restrict_
           if constexpr (NT == 2) x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s2, i, g), Up[s2].hi, x);
           x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s2, i, g), Up[s2], x);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = last * S[t][r] + su.down * x[r];
+        S[t] = last * S[t] + su.down * x;
       }
       carried = true;
     }
-    vc = vn;
   };
 
   if constexpr (TWICE) {
-    const auto turn = [&](const Stage<T, DK>& s, Stage<T, DK>& other, int c) {
+    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) {
       __syncthreads();   // chunk c is there, and no wave reads the other buffer any more
-      if (c + 1 < chunks) stage_chunk<T, DK>(other, a, slot0 + c + 1, hk, h, images, tri, tris, scal, wave, waves, lane);
+      if (c + 1 < chunks) fetch(other, c + 1);
       if (live) work(s, c);
     };
     for (int c = 0; c < chunks; c += 2) {
@@ -601,27 +641,33 @@ __global__ __launch_bounds__(512) void k_delta_walk(Args a, const T* __restrict_
   } else {
     for (int c = 0; c < chunks; ++c) {
       __syncthreads();
-      stage_chunk<T, DK>(s_a, a, slot0 + c, hk, h, images, tri, tris, scal, wave, waves, lane);
+      fetch(s_a, c);
       __syncthreads();
       if (live) work(s_a, c);
     }
   }
-  if (out.state_out != nullptr && live)
-#pragma unroll
-    for (int t = 0; t < ST; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
-        if (d < a.dk) out.state_out[(((size_t)w * a.H + h) * a.dk + d) * a.dv + col] = S[t][r];
-      }
+  store_state(S, a, out.state_out, w, h, col, live, g);
 }
 
-// Waves of a walk's workgroup.
+// Waves of a walk's workgroup.  Eight share a chunk's staging among 128 columns, four leave a SIMD to a
+// wave.  33 sequences x 16 heads of 128 (bf16): 1,087 us with eight, 1,225 with four; 7 sequences x 8 heads:
+// 599 and 442 (two: 468).  So eight where that still fills the 256 CUs.  fp32 rows have room for four.
+template <typename T>
 inline int walk_waves(const Args& a) {
   const int groups = a.dv / 16;
-  int most = 8;
-  if (const char* e = getenv("SLA_WAVES")) most = atoi(e);
-  return groups < most ? groups : most;
+  if (groups <= 2) return 2;
+  if (groups <= 4 || sizeof(T) == 4) return 4;
+  if (const char* e = getenv("SLA_WAVES")) return atoi(e);
+  return (int64_t)a.W * a.H * ((groups + 7) / 8) >= 256 ? 8 : 4;
+}
+// f(integral_constant<waves>, grid)
+template <typename T, class F>
+inline void with_walk(const Args& a, F f) {
+  const int waves = walk_waves<T>(a);
+  const dim3 grid(a.W, a.H, (a.dv / 16 + waves - 1) / waves);
+  if (waves == 2) f(std::integral_constant<int, 2>{}, grid);
+  else if (waves == 4) f(std::integral_constant<int, 4>{}, grid);
+  else if constexpr (sizeof(T) == 2) f(std::integral_constant<int, 8>{}, grid);
 }
 
 }  // namespace delta
