@@ -34,9 +34,18 @@ constexpr int kTriHalfs = 2 * kTri * kFrag;
 // T and P are kept 64 times as large (T's entries stay below 45, P's below 512): an entry's error is
 // then below 2^-31 of the diagonal's 1
 constexpr float kTriUp = 64.f;
-constexpr int kScal = 512;            // 4-byte values: 6 rows of 64, one value, padding to 2 KB
-// rows of the per-chunk scalars; kRow: original rows (int32)
-enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow = 320, kLast = 384 };
+constexpr int kScal = 768;            // 4-byte values: 8 rows of 64, one value, padding to 3 KB
+// Rows of a chunk's scalars.  kRow, kNext, kPrev: the original rows (int32) of the chunk and of its
+// window's next and previous chunk, whose rows are asked for while this one is in work.
+enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow = 320, kNext = 384, kPrev = 448,
+       kLast = 512 };
+// What a chunk has for each value head, in halfs: P's second and first terms, T's first and second,
+// the scalars, and for the backward the transposed inverse and the transposed P, two terms each.
+// The walk forward reads up to the scalars (bf16 outputs: from P's first terms), the walk back from there.
+constexpr int kTerm = kTriHalfs / 2;
+enum { kPLo = 0, kPHi = kTerm, kTHi = 2 * kTerm, kScalAt = 4 * kTerm, kBackT = kScalAt + 2 * kScal,
+       kBackP = kBackT + 2 * kTerm };
+constexpr int kRecord = kBackT, kRecordBack = kBackP + 2 * kTerm;
 
 struct Args {
   const int32_t* offsets;
@@ -46,10 +55,10 @@ struct Args {
   uint32_t slots;                     // n / 64 + W
 };
 
-// Workspace of the chunk form: per chunk slot and query/key head the images of k' and q', per
-// slot and value head T, P and the scalars.
+// Workspace of the chunk form: per chunk slot and query/key head the images of q' and k', per slot and
+// value head a record.
 struct Space {
-  size_t image, images, tri, scal, total;   // halfs of one image; byte offsets
+  size_t image, images, records, total;   // halfs of one image; byte offsets
 };
 
 __host__ __device__ inline int pad_dk(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
@@ -57,14 +66,13 @@ __host__ __device__ inline int pad_dk(int dk) { return dk <= 32 ? 32 : dk <= 64 
 __host__ __device__ inline size_t slots_of(int64_t n, int32_t W) { return (size_t)(n / kChunk + W); }
 
 __host__ __device__ inline Space space_of(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk,
-                                          int tris) {
+                                          int record) {
   Space s;
   const size_t ns = slots_of(n, W);
   s.image = (size_t)(dtype == 0 ? 2 : 1) * kChunk * pad_dk(dk);
   s.images = 0;
-  s.tri = align_up(s.images + ns * Hk * 2 * s.image * 2, 256);
-  s.scal = align_up(s.tri + ns * H * tris * kTriHalfs * 2, 256);
-  s.total = align_up(s.scal + ns * H * kScal * 4, 256);
+  s.records = align_up(s.images + ns * Hk * 2 * s.image * 2, 256);
+  s.total = align_up(s.records + ns * H * record * 2, 256);
   return s;
 }
 
@@ -113,20 +121,24 @@ __device__ __forceinline__ floatx4 mma1(const Pair& a, half8_t b, floatx4 c) {
   return mma(a.hi, b, c);
 }
 
-// x scaled by s as two fp16 terms.  The product is hidden from the compiler, which would make it
-// twice, once for each term.
+// x scaled by s as two fp16 terms, two instructions a value: each term is one multiply-add that
+// rounds to fp16, the second one's addend the first term.  (The first terms are hidden from the
+// compiler once they are there: it would make them again for the second.)
 __device__ __forceinline__ Pair split(const floatx4& x0, const floatx4& x1, float s) {
+  typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
   Pair p;
-  float y[8];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) y[r] = x0[r] * s, y[4 + r] = x1[r] * s;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    asm("" : "+v"(y[e]));
-    p.hi[e] = (_Float16)y[e];
+  for (int e = 0; e < 8; e += 2) {
+    const float a = e < 4 ? x0[e] : x1[e - 4], b = e < 4 ? x0[e + 1] : x1[e - 3];
+    half2_t h = {(_Float16)__builtin_fmaf(a, s, 0.f), (_Float16)__builtin_fmaf(b, s, 0.f)};
+    uint32_t u = __builtin_bit_cast(uint32_t, h);
+    asm("" : "+v"(u));
+    h = __builtin_bit_cast(half2_t, u);
+    p.hi[e] = h[0];
+    p.hi[e + 1] = h[1];
+    p.lo[e] = (_Float16)__builtin_fmaf(a, s, -(float)h[0]);
+    p.lo[e + 1] = (_Float16)__builtin_fmaf(b, s, -(float)h[1]);
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) p.lo[e] = (_Float16)(y[e] - (float)p.hi[e]);
   return p;
 }
 __device__ __forceinline__ half8_t narrow(const floatx4& x0, const floatx4& x1, float s) {
@@ -162,6 +174,7 @@ struct Scale {
   float up, down;
 };
 __device__ __forceinline__ Scale scale_of(uint32_t max_bits) {
+  if (max_bits == 0) return {1.f, 1.f};
   const int e = (int)(max_bits >> 23);
   const int s = 267 - e < 240 ? 267 - e : 240;
   return {__uint_as_float((uint32_t)s << 23), __uint_as_float((uint32_t)(254 - s) << 23)};
@@ -212,19 +225,24 @@ __device__ __forceinline__ half8_t image_cols(const _Float16* img, int t, int p,
   }
   return x;
 }
-// Operands of a triangle: the six first terms, then the six second ones; number of row tile tau's
-// operand for column block s:
+// Number of row tile tau's operand for column block s in a triangle's term:
 __device__ __forceinline__ constexpr int tri_at(int tau, int s) { return tau < 2 ? tau : 2 * tau - 2 + s; }
 
 // ------------------------------------------------------------------ staging
-// `bytes` (a multiple of 1,024) from global memory into LDS without passing registers, split over the
-// workgroup's waves: one instruction moves 64 x 16 bytes in lane order.  Complete at the next
-// __syncthreads().
-__device__ __forceinline__ void stage(void* lds, const void* src, int bytes, int wave, int waves, int lane) {
-  for (int at = wave * 1024; at < bytes; at += waves * 1024)
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(static_cast<const char*>(src) + at + lane * 16),
-        (__attribute__((address_space(3))) void*)(static_cast<char*>(lds) + at), 16, 0, 0);
+// 64 x 16 bytes from every lane's address in global memory into LDS at `lds`, in lane order, without
+// passing registers.  Counted with the wave's vector memory operations.
+__device__ __forceinline__ void to_lds(void* lds, const void* src) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+// Barrier of the workgroup that waits for the wave's LDS operations and for all of its vector memory
+// operations but the LATER last ones.
+template <int LATER>
+__device__ __forceinline__ void barrier_after() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | LATER);   // vmcnt(LATER) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // ------------------------------------------------------------------ storage types

@@ -11,18 +11,17 @@ template <typename T, int DK>
 hipError_t forward_impl(const Args& a, int dtype, const void* q, const void* k, const void* v, const float* g,
                         const float* beta, const float* state_in, void* o, float* state_out, void* workspace,
                         hipStream_t stream) {
-  const Space sp = space_of(a.n, a.W, dtype, a.Hk, a.H, a.dk, 2);
+  const Space sp = space_of(a.n, a.W, dtype, a.Hk, a.H, a.dk, kRecord);
   char* ws = static_cast<char*>(workspace);
   _Float16* images = reinterpret_cast<_Float16*>(ws + sp.images);
-  _Float16* tri = reinterpret_cast<_Float16*>(ws + sp.tri);
-  float* scal = reinterpret_cast<float*>(ws + sp.scal);
+  _Float16* records = reinterpret_cast<_Float16*>(ws + sp.records);
   if (a.n > 0)
     k_delta_prep<T, DK, false><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
-        a, static_cast<const T*>(q), static_cast<const T*>(k), g, beta, images, tri, scal);
+        a, static_cast<const T*>(q), static_cast<const T*>(k), g, beta, images, records);
   with_walk<T>(a, [&](auto nw, dim3 grid) {
     constexpr int NW = decltype(nw)::value;
     k_delta_walk<T, DK, false, NW><<<grid, 64 * NW, 0, stream>>>(
-        a, static_cast<const T*>(v), state_in, images, tri, 2, scal, static_cast<T*>(o), nullptr,
+        a, static_cast<const T*>(v), state_in, images, records, kRecord, static_cast<T*>(o), nullptr,
         WalkOut{state_out, nullptr, nullptr, nullptr, nullptr});
   });
   return hipGetLastError();
@@ -43,7 +42,7 @@ hipError_t forward_dk(const Args& a, int dtype, const void* q, const void* k, co
 
 size_t delta_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv) {
   (void)dv;
-  return space_of(n, W, dtype, Hk, H, dk, 2).total;
+  return space_of(n, W, dtype, Hk, H, dk, kRecord).total;
 }
 
 hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,

@@ -34,7 +34,7 @@ struct BackSpace {
 };
 BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv) {
   BackSpace s;
-  s.base = space_of(n, W, dtype, Hk, H, dk, 4);
+  s.base = space_of(n, W, dtype, Hk, H, dk, kRecordBack);
   const size_t sh = slots_of(n, W) * H, groups = dv / 16;
   size_t at = s.base.total;
   const auto take = [&](size_t floats) {
@@ -60,8 +60,7 @@ template <typename T, int DK, int NW>
 __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restrict__ dout,
                                                         const float* __restrict__ dstate,
                                                         const _Float16* __restrict__ images,
-                                                        const _Float16* __restrict__ tri,
-                                                        const float* __restrict__ scal,
+                                                        const _Float16* __restrict__ records,
                                                         const float* __restrict__ states, float* __restrict__ lam,
                                                         float* __restrict__ dstates, float* __restrict__ dmax,
                                                         float* __restrict__ start, float* __restrict__ dstate_in) {
@@ -84,25 +83,40 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
   floatx4 S[ST];
   load_state(S, a, dstate, w, h, col, live, g);
   bool carried = dstate != nullptr;
-  Places<T> at;
-  const auto fetch = [&](Stage<T, DK, NW>& s, int c) {   // at: chunk c's places, then chunk c - 1's
-    // the transposed triangles are the third and fourth of a chunk
-    stage_chunk<T, DK, NW, false>(s, a, slot0 + c, hk, h, cg, live, images, tri + 2 * kTriHalfs, 4, scal, dout, at,
-                                  wave, lane);
-    if (c > 0) at.ask(a, win.begin + (c - 1) * kChunk, rows_of(c - 1), lane);
+  using F = Fetch<T, DK, NW, kScalAt, kRecordBack, kScalAt>;
+  F fetch;
+  const auto begin = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) {
+    fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, kRecordBack, dout, at, wave, lane);
   };
+  Places<T> at;
   if (chunks > 0) {
     at.ask(a, win.begin + (chunks - 1) * kChunk, rows_of(chunks - 1), lane);
-    if constexpr (TWICE) fetch(s_a, chunks - 1);
+    if constexpr (TWICE) {
+      begin(s_a, chunks - 1, at);
+      fetch.template jobs<0, F::kJobs>(s_a, wave);
+    }
   }
 
-  const auto work = [&](const Stage<T, DK, NW>& s, int c) {
-    const int rows = rows_of(c);
-    const size_t sh = (size_t)(slot0 + c) * a.H + h;
-    const _Float16 *qi = s.img, *ki = s.img + NT * IMG, *st = s.tri, *sp = s.tri + kTriHalfs;
-    auto row4 = [&](int what, int tau) {
-      return *reinterpret_cast<const floatx4*>(s.scal + what + 16 * tau + 4 * g);
+  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) {
+    const float* scal = reinterpret_cast<const float*>(s.rec);
+    const auto jobs = [&](auto from, auto to) {
+      if constexpr (TWICE)
+        if (c > 0) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
     };
+    using std::integral_constant;
+    floatx4 X[4], Y[4];
+    rows_in(s.rows[wave], Y, rows_of(c), i, g);
+    if constexpr (TWICE)
+      if (c > 0) {
+        Places<T> to;
+        to.take(scal + kPrev, lane);
+        begin(other, c - 1, to);
+      }
+    jobs(integral_constant<int, 0>{}, integral_constant<int, 2>{});
+    const size_t sh = (size_t)(slot0 + c) * a.H + h;
+    const _Float16 *qi = s.img, *ki = s.img + NT * IMG;
+    const _Float16 *bt = s.rec + kBackT - kScalAt, *bp = s.rec + kBackP - kScalAt;
+    auto row4 = [&](int what, int tau) { return *reinterpret_cast<const floatx4*>(scal + what + 16 * tau + 4 * g); };
     const size_t sgrp = sh * (a.dv / 16) + cg;
     floatx4 s0[ST];   // the state before the chunk, for the end
 #pragma unroll
@@ -112,8 +126,6 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     const uint32_t top = wave_max_bits(max_of(S));
     if (lane == 0) dmax[sgrp] = __uint_as_float(top);
     // du = P^T do' + until k' dS
-    floatx4 X[4], Y[4];
-    rows_in(s.rows[wave], Y, rows, i, g);
     {
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kOScale, tau);
@@ -122,7 +134,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
-      tri_times<true>(sp, Yp, X, lane);
+      tri_times<true>(bp, bp + kTerm, Yp, X, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) X[tau] *= ydown;
     }
@@ -136,6 +148,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) X[tau] += (row4(kUntil, tau) * sc.down) * x[tau];
     }
+    jobs(integral_constant<int, 2>{}, integral_constant<int, 5>{});
     // lam, then -since mu in X and since do' in Y
     {
       const Scale sx = scale_for(X);
@@ -143,7 +156,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
       Pair Xp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sx.up);
-      tri_times<true>(st, Xp, X, lane);
+      tri_times<true>(bt, bt + kTerm, Xp, X, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         const floatx4 since = row4(kSince, tau);
@@ -154,6 +167,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
         Y[tau] *= since;
       }
     }
+    jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});
     // dS = exp(gam_last) dS + q'^T (since do') - k'^T (since mu)
     {
       const Scale sc = scale_of(wave_max_bits(fmaxf(max_of(X), max_of(Y))));
@@ -163,7 +177,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
         Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sc.up);
         Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sc.up);
       }
-      const float last = s.scal[kLast];
+      const float last = scal[kLast];
       float dot = 0.f;
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
@@ -190,9 +204,13 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 
   if constexpr (TWICE) {
     const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) {
-      __syncthreads();   // chunk c is there, and no wave reads the other buffer any more
-      if (c > 0) fetch(other, c - 1);
-      if (live) work(s, c);
+      barrier_after<0>();   // chunk c is there, and no wave reads the other buffer any more
+      if (live) {
+        work(s, other, c);
+      } else if (c > 0) {
+        begin(other, c - 1, at);   // moves no rows
+        fetch.template jobs<0, F::kJobs>(other, wave);
+      }
     };
     for (int c = chunks - 1; c >= 0; c -= 2) {
       turn(s_a, s_b, c);
@@ -200,10 +218,12 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     }
   } else {
     for (int c = chunks - 1; c >= 0; --c) {
-      __syncthreads();
-      fetch(s_a, c);
-      __syncthreads();
-      if (live) work(s_a, c);
+      if (c + 1 < chunks) at.take(reinterpret_cast<const float*>(s_a.rec) + kPrev, lane);
+      barrier_after<0>();
+      begin(s_a, c, at);
+      fetch.template jobs<0, F::kJobs>(s_a, wave);
+      barrier_after<0>();
+      if (live) work(s_a, s_a, c);
     }
   }
   store_state(S, a, dstate_in, w, h, col, live, g);
@@ -253,7 +273,8 @@ template <typename T, int DK>
 __global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
                                                     const float* __restrict__ gin,
                                                     const _Float16* __restrict__ images,
-                                                    const float* __restrict__ scal, const float* __restrict__ states,
+                                                    const _Float16* __restrict__ records,
+                                                    const float* __restrict__ states,
                                                     const float* __restrict__ dstates, const float* __restrict__ smax,
                                                     const float* __restrict__ dmax, const float* __restrict__ resid,
                                                     const float* __restrict__ lam, const float* __restrict__ odo,
@@ -310,7 +331,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict_
     const size_t sh = (size_t)slot * a.H + h;
     __syncthreads();
     for (int x = tid; x < kScal / 4; x += 256)
-      reinterpret_cast<uint4*>(s_scal)[x] = reinterpret_cast<const uint4*>(scal + sh * kScal)[x];
+      reinterpret_cast<uint4*>(s_scal)[x] = reinterpret_cast<const uint4*>(records + sh * kRecordBack + kScalAt)[x];
     if (wave == 0) {   // the decay sums, as k_delta_prep makes them
       const bool r1 = lane < rows;
       const float g1 = r1 ? gin[(size_t)row_at(a, base + lane) * a.H + h] : 0.f;
@@ -591,26 +612,25 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
   const BackSpace sp = back_space(a.n, a.W, dtype, a.Hk, a.H, a.dk, a.dv);
   char* ws = static_cast<char*>(workspace);
   _Float16* images = reinterpret_cast<_Float16*>(ws + sp.base.images);
-  _Float16* tri = reinterpret_cast<_Float16*>(ws + sp.base.tri);
+  _Float16* records = reinterpret_cast<_Float16*>(ws + sp.base.records);
   const auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
-  float* scal = at(sp.base.scal);
   const T *v = static_cast<const T*>(b.v), *dout = static_cast<const T*>(b.dout);
   if (a.n > 0)
     k_delta_prep<T, DK, true><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
-        a, static_cast<const T*>(b.q), static_cast<const T*>(b.k), b.g, b.beta, images, tri, scal);
+        a, static_cast<const T*>(b.q), static_cast<const T*>(b.k), b.g, b.beta, images, records);
   with_walk<T>(a, [&](auto nw, dim3 grid) {
     constexpr int NW = decltype(nw)::value;
     if (a.n > 0)
       k_delta_walk<T, DK, true, NW><<<grid, 64 * NW, 0, stream>>>(
-          a, v, b.state_in, images, tri, 4, scal, nullptr, dout,
+          a, v, b.state_in, images, records, kRecordBack, nullptr, dout,
           WalkOut{nullptr, at(sp.states), at(sp.smax), at(sp.resid), at(sp.odo)});
-    k_delta_back<T, DK, NW><<<grid, 64 * NW, 0, stream>>>(a, dout, b.dstate_out, images, tri, scal, at(sp.states),
+    k_delta_back<T, DK, NW><<<grid, 64 * NW, 0, stream>>>(a, dout, b.dstate_out, images, records, at(sp.states),
                                                           at(sp.lam), at(sp.dstates), at(sp.dmax), at(sp.start),
                                                           b.dstate_in);
   });
   if (a.n > 0)
     k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
-        a, v, dout, b.g, images, scal, at(sp.states), at(sp.dstates), at(sp.smax), at(sp.dmax), at(sp.resid),
+        a, v, dout, b.g, images, records, at(sp.states), at(sp.dstates), at(sp.smax), at(sp.dmax), at(sp.resid),
         at(sp.lam), at(sp.odo), at(sp.start), b.state_in != nullptr, b.dstate_out != nullptr, static_cast<T*>(b.dq),
         static_cast<T*>(b.dk), static_cast<T*>(b.dv), b.dg, b.dbeta);
   return hipGetLastError();

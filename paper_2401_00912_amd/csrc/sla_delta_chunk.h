@@ -75,14 +75,14 @@ __device__ __forceinline__ void invert(PrepShared& s, int wave, int i, int g) {
 
 // The triangle's operands of tile row `tau` out of a matrix in LDS: rows as operand rows, columns
 // in the order of two stacked result tiles.
-__device__ __forceinline__ void put_tri(const float* m, _Float16* out, int tau, int lane, int i, int g) {
+__device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* lo, int tau, int lane, int i, int g) {
   for (int s = 0; s <= tau / 2; ++s) {
     const floatx4 x0 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 4 * g);
     const floatx4 x1 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 16 + 4 * g);
     const Pair p = split(x0, x1, kTriUp);
-    _Float16* at = out + tri_at(tau, s) * kFrag + lane * 8;
-    *reinterpret_cast<half8_t*>(at) = p.hi;
-    *reinterpret_cast<half8_t*>(at + kTri * kFrag) = p.lo;
+    const int at = tri_at(tau, s) * kFrag + lane * 8;
+    *reinterpret_cast<half8_t*>(hi + at) = p.hi;
+    *reinterpret_cast<half8_t*>(lo + at) = p.lo;
   }
 }
 // The transposed matrix's operands of tile row `tau`: upper triangular, kept under the mirrored
@@ -105,8 +105,8 @@ __device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, int tau
 template <typename T, int DK, bool REV>
 __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict__ q, const T* __restrict__ k,
                                                     const float* __restrict__ gin, const float* __restrict__ beta,
-                                                    _Float16* __restrict__ images, _Float16* __restrict__ tri,
-                                                    float* __restrict__ scal) {
+                                                    _Float16* __restrict__ images,
+                                                    _Float16* __restrict__ records) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK;
   constexpr size_t kImages = (size_t)2 * NT * IMG * 2;
   __shared__ __attribute__((aligned(16))) char s_mem[kImages > sizeof(PrepShared) ? kImages : sizeof(PrepShared)];
@@ -210,6 +210,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
   for (int hv = 0; hv < group; ++hv) {
     const int h = hk * group + hv;
     const size_t sh = (size_t)slot * a.H + h;
+    _Float16* out = records + sh * (REV ? kRecordBack : kRecord);
     if (wave == 0) {
       // log decays summed in 64 bits: their differences are small where they are large.  A decay of
       // zero (g below -104, -infinity) starts a new stretch, over which nothing is carried.
@@ -232,13 +233,17 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
       s_beta[lane] = bp;
       const double last = __shfl(gam, 63);
       const int lcut = __shfl(cut, 63);
-      float* sc = scal + sh * kScal;
+      float* sc = reinterpret_cast<float*>(out + kScalAt);
       sc[kSince + lane] = real && cut == 0 ? expf((float)gam) : 0.f;
       sc[kBeta + lane] = bp;
       sc[kUntil + lane] = real && cut == lcut ? expf((float)(last - gam)) : 0.f;
       sc[kVScale + lane] = vs;
       sc[kOScale + lane] = s_os[lane] * a.scale;
+      // a row that is none reads row 0 (or its chunk's first row) and is dropped when it is used
+      const int p1 = base + kChunk + lane, p0 = base - kChunk + lane, end = win.begin + win.rows;
       sc[kRow + lane] = __int_as_float(real ? row_at(a, base + lane) : 0);
+      sc[kNext + lane] = __int_as_float(base + kChunk < end ? row_at(a, p1 < end ? p1 : base + kChunk) : 0);
+      sc[kPrev + lane] = __int_as_float(p0 >= win.begin ? row_at(a, p0) : 0);
       if (lane == 0) sc[kLast] = lcut == 0 ? expf((float)last) : 0.f;
     }
     __syncthreads();
@@ -261,8 +266,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
     }
     __syncthreads();
     invert(sm, wave, i, g);
-    _Float16* out = tri + sh * (size_t)((REV ? 4 : 2) * kTriHalfs);
-    put_tri(sm.x, out, wave, lane, i, g);
+    put_tri(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
     if constexpr (REV) {
       __syncthreads();
 #pragma unroll
@@ -274,7 +278,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
         }
       __syncthreads();
       invert(sm, wave, i, g);
-      put_tri_t(sm.x, out + 2 * kTriHalfs, wave, lane, i, g);
+      put_tri_t(sm.x, out + kBackT, wave, lane, i, g);
     }
     // every wave is past its reads of n (the inverse's last barrier)
 #pragma unroll
@@ -282,8 +286,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
 #pragma unroll
       for (int r = 0; r < 4; ++r) sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = p[j][r];
     __syncthreads();
-    put_tri(sm.n, out + kTriHalfs, wave, lane, i, g);
-    if constexpr (REV) put_tri_t(sm.n, out + 3 * kTriHalfs, wave, lane, i, g);
+    put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
+    if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
     __syncthreads();
   }
 }
@@ -314,54 +318,70 @@ template <typename T, int DK, int NW>
 struct Stage {
   static constexpr int kImages = 2 * kTerms<T> * kChunk * DK;   // halfs
   __attribute__((aligned(16))) _Float16 img[kImages];
-  __attribute__((aligned(16))) _Float16 tri[2 * kTriHalfs];
-  __attribute__((aligned(16))) float scal[kScal];
+  __attribute__((aligned(16))) _Float16 rec[kRecord];           // as the walk forward or back reads it
   __attribute__((aligned(16))) T rows[NW][kChunk * 16];         // 16 columns of v (or dout) a wave
 };
 template <typename T, int DK, int NW>
 constexpr bool kTwice = 2 * sizeof(Stage<T, DK, NW>) <= 160 * 1024;
 
-// Places of the rows whose 16 bytes this lane moves: kMoves instructions move a wave's 64 rows of 16
-// columns.  They are asked for a chunk earlier than the rows.
+// Instructions that move a wave's 64 rows of 16 columns: 16 bytes a lane.
 template <typename T>
-constexpr int kMoves = sizeof(T);   // 64 rows x 16 columns / 1,024 bytes
+constexpr int kMoves = sizeof(T);
+// Rows whose 16 bytes this lane moves.
 template <typename T>
 struct Places {
   int row[kMoves<T>];
+  __device__ __forceinline__ static int position(int n, int lane) { return (n * 64 + lane) / kMoves<T>; }
+  // of the chunk from position `base` on: a row past its end stands for the first one
   __device__ __forceinline__ void ask(const Args& a, int base, int rows, int lane) {
 #pragma unroll
-    for (int n = 0; n < kMoves<T>; ++n) {
-      const int p = (n * 64 + lane) / kMoves<T>;
-      row[n] = base + (p < rows ? p : 0);   // a row past the end: the first one, dropped when it is used
-    }
-    if (a.order != nullptr) {
+    for (int n = 0; n < kMoves<T>; ++n) row[n] = row_at(a, base + (position(n, lane) < rows ? position(n, lane) : 0));
+  }
+  __device__ __forceinline__ void take(const float* rows, int lane) {
 #pragma unroll
-      for (int n = 0; n < kMoves<T>; ++n) row[n] = a.order[row[n]];
-    }
+    for (int n = 0; n < kMoves<T>; ++n) row[n] = __float_as_int(rows[position(n, lane)]);
   }
 };
 
-// Chunk `slot` into a buffer: `tri` is the first of two triangles in a row, of `tris` kept a chunk; the
-// wave's columns of `src` if it has any.
-template <typename T, int DK, int NW, bool SHORT>
-__device__ __forceinline__ void stage_chunk(Stage<T, DK, NW>& b, const Args& a, size_t slot, int hk, int h, int cg,
-                                            bool live, const _Float16* images, const _Float16* tri, int tris,
-                                            const float* scal, const T* src, const Places<T>& at, int wave, int lane) {
-  const size_t sh = slot * a.H + h;
-  if (live) {
+// A chunk on its way into a buffer: kJobs moves a wave, issued in parts between the steps of the chunk
+// in work (all at once, they hold up the wave that issues them, and its stores behind them).  FROM, TO:
+// the part of the record that is wanted, in halfs; it goes to the same place of the buffer's record less
+// SHIFT.
+template <typename T, int DK, int NW, int FROM, int TO, int SHIFT>
+struct Fetch {
+  using S = Stage<T, DK, NW>;
+  static constexpr int kImg = S::kImages * 2 / 1024, kRec = (TO - FROM) * 2 / 1024;
+  static constexpr int kJobs = kImg / NW + (kRec + NW - 1) / NW;
+  static_assert(kImg % NW == 0 && (TO - FROM) * 2 % 1024 == 0, "whole pieces");
+  const char *img, *rec;
+
+  __device__ __forceinline__ void start(S& b, const Args& a, size_t slot, int hk, int h, int cg, bool live,
+                                        const _Float16* images, const _Float16* records, int record, const T* src,
+                                        const Places<T>& at, int wave, int lane) {
+    const size_t sh = slot * a.H + h;
+    img = reinterpret_cast<const char*>(images + (slot * a.Hk + hk) * S::kImages) + wave * 1024 + lane * 16;
+    rec = reinterpret_cast<const char*>(records + sh * record + FROM) + wave * 1024 + lane * 16;
+    if (live) {   // the wave's columns of src
 #pragma unroll
-    for (int n = 0; n < kMoves<T>; ++n) {
-      const int o = at.row[n] < 0 ? 0 : at.row[n] >= a.n ? a.n - 1 : at.row[n];
-      const T* p = src + ((size_t)o * a.H + h) * a.dv + 16 * cg + (lane % kMoves<T>) * (16 / (int)sizeof(T));
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                       (__attribute__((address_space(3))) void*)(b.rows[wave] + n * (1024 / sizeof(T))),
-                                       16, 0, 0);
+      for (int n = 0; n < kMoves<T>; ++n)
+        to_lds(b.rows[wave] + n * (1024 / sizeof(T)),
+               src + ((size_t)at.row[n] * a.H + h) * a.dv + 16 * cg + (lane % kMoves<T>) * (16 / (int)sizeof(T)));
     }
   }
-  stage(b.img, images + (slot * a.Hk + hk) * Stage<T, DK, NW>::kImages, sizeof(b.img), wave, NW, lane);
-  stage(b.tri, tri + sh * (size_t)tris * kTriHalfs, sizeof(b.tri) - (SHORT ? kTriHalfs : 0), wave, NW, lane);
-  stage(b.scal, scal + sh * kScal, sizeof(b.scal), wave, NW, lane);
-}
+  template <int J0, int J1>
+  __device__ __forceinline__ void jobs(S& b, int wave) const {
+#pragma unroll
+    for (int j = J0; j < J1; ++j) {
+      if (j < kImg / NW) {
+        to_lds(b.img + (wave + j * NW) * 512, img + j * NW * 1024);
+      } else {
+        const int p = j - kImg / NW;
+        if ((p + 1) * NW <= kRec || wave + p * NW < kRec)
+          to_lds(b.rec + FROM - SHIFT + (wave + p * NW) * 512, rec + p * NW * 1024);
+      }
+    }
+  }
+};
 
 // The wave's columns of a staged chunk as result tiles, rows from `rows` on zero.
 template <typename T>
@@ -434,7 +454,8 @@ __device__ __forceinline__ float max_of(const floatx4 (&x)[N]) {
 
 // x[tau] = triangle times y, lower (UPPER: the transposed triangle under its mirrored numbers)
 template <bool UPPER>
-__device__ __forceinline__ void tri_times(const _Float16* tri, const Pair (&y)[2], floatx4 (&x)[4], int lane) {
+__device__ __forceinline__ void tri_times(const _Float16* hi, const _Float16* lo, const Pair (&y)[2], floatx4 (&x)[4],
+                                          int lane) {
 #pragma unroll
   for (int tau = 0; tau < 4; ++tau) x[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -442,8 +463,8 @@ __device__ __forceinline__ void tri_times(const _Float16* tri, const Pair (&y)[2
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau) {
       if (UPPER ? s < tau / 2 : s > tau / 2) continue;
-      const _Float16* at = tri + (UPPER ? tri_at(3 - tau, 1 - s) : tri_at(tau, s)) * kFrag + lane * 8;
-      const Pair t = {*reinterpret_cast<const half8_t*>(at), *reinterpret_cast<const half8_t*>(at + kTri * kFrag)};
+      const int at = (UPPER ? tri_at(3 - tau, 1 - s) : tri_at(tau, s)) * kFrag + lane * 8;
+      const Pair t = {*reinterpret_cast<const half8_t*>(hi + at), *reinterpret_cast<const half8_t*>(lo + at)};
       x[tau] = mma2(t, y[s], x[tau]);
     }
 }
@@ -466,11 +487,12 @@ template <typename T, int DK, bool KEEP, int NW>
 __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restrict__ v,
                                                         const float* __restrict__ state_in,
                                                         const _Float16* __restrict__ images,
-                                                        const _Float16* __restrict__ tri, int tris,
-                                                        const float* __restrict__ scal, T* __restrict__ o,
+                                                        const _Float16* __restrict__ records, int record,
+                                                        T* __restrict__ o,
                                                         const T* __restrict__ dout, WalkOut out) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
   constexpr bool TWICE = kTwice<T, DK, NW>, SHORT = kShortOut<T, KEEP>;
+  using F = Fetch<T, DK, NW, SHORT ? kPHi : 0, kRecord, 0>;
   __shared__ Stage<T, DK, NW> s_a;
   __shared__ std::conditional_t<TWICE, Stage<T, DK, NW>, char> s_b;
 
@@ -485,112 +507,136 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   const int chunks = (win.rows + kChunk - 1) / kChunk;
   const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
 
+  // the state is `unit` times S: after a chunk S stays in the units of the products it was summed with
   floatx4 S[ST];
+  float unit = 1.f;
   load_state(S, a, state_in, w, h, col, live, g);
   bool carried = state_in != nullptr;   // no products with a state that is zero
-  Places<T> at;
-  const auto fetch = [&](Stage<T, DK, NW>& s, int c) {   // at: chunk c's places, then chunk c + 1's
-    stage_chunk<T, DK, NW, SHORT>(s, a, slot0 + c, hk, h, cg, live, images, tri, tris, scal, v, at, wave, lane);
-    if (c + 1 < chunks) at.ask(a, win.begin + (c + 1) * kChunk, rows_of(c + 1), lane);
+  F fetch;
+  const auto start = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) {
+    fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, record, v, at, wave, lane);
   };
+  Places<T> at;
   if (chunks > 0) {
     at.ask(a, win.begin, rows_of(0), lane);
-    if constexpr (TWICE) fetch(s_a, 0);
+    if constexpr (TWICE) {
+      start(s_a, 0, at);
+      fetch.template jobs<0, F::kJobs>(s_a, wave);
+    }
   }
 
-  // chunk c, staged in `s`
-  const auto work = [&](const Stage<T, DK, NW>& s, int c) {
+  // chunk c, staged in `s`; the next one's moves go into `other` in between
+  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) {
     const int rows = rows_of(c);
     const size_t sh = (size_t)(slot0 + c) * a.H + h;
-    const _Float16 *qi = s.img, *ki = s.img + NT * IMG, *st = s.tri, *sp = s.tri + kTriHalfs;
-    auto row4 = [&](int what, int tau) {
-      return *reinterpret_cast<const floatx4*>(s.scal + what + 16 * tau + 4 * g);
+    const _Float16 *qi = s.img, *ki = s.img + NT * IMG;
+    const float* scal = reinterpret_cast<const float*>(s.rec + kScalAt);
+    auto row4 = [&](int what, int tau) { return *reinterpret_cast<const floatx4*>(scal + what + 16 * tau + 4 * g); };
+    const bool next = TWICE && c + 1 < chunks;
+    const auto jobs = [&](auto from, auto to) {
+      if constexpr (TWICE)
+        if (next) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
     };
+    using std::integral_constant;
+    floatx4 Y[4], qs[4];
+    rows_in(s.rows[wave], Y, rows, i, g);   // before any move: the compiler makes transposed reads wait for those
+    if constexpr (TWICE)
+      if (next) {
+        Places<T> to;
+        to.take(scal + kNext, lane);
+        start(other, c + 1, to);
+      }
+    jobs(integral_constant<int, 0>{}, integral_constant<int, 2>{});
     int place[4];   // this lane's row of every tile
 #pragma unroll
-    for (int tau = 0; tau < 4; ++tau) place[tau] = __float_as_int(s.scal[kRow + 16 * tau + i]);
+    for (int tau = 0; tau < 4; ++tau) place[tau] = __float_as_int(scal[kRow + 16 * tau + i]);
     Raw<T, 4> dn[KEEP ? 4 : 1];
     if constexpr (KEEP) {
       float* to = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
 #pragma unroll
-      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t];
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t] * unit;
       if (!carried && lane == 0) out.smax[sh * (a.dv / 16) + cg] = 0.f;
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau)   // row 0 where there is none
         dn[tau] = *reinterpret_cast<const Raw<T, 4>*>(dout + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g);
     }
-    // y = 2^-kap v - exp(gam) k' S
-    floatx4 Y[4];
-    Pair Sp[KB];
-    Scale sc = {1.f, 1.f};
-    rows_in(s.rows[wave], Y, rows, i, g);
+    // y = 2^-kap v - exp(gam) k' S, and q' S for later
+    uint32_t top = 0;   // of the state, in S's units
+    float qdown = 0.f;
 #pragma unroll
-    for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kVScale, tau);
+    for (int tau = 0; tau < 4; ++tau) {
+      Y[tau] *= row4(kVScale, tau);
+      qs[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
     if (carried) {
-      const uint32_t top = wave_max_bits(max_of(S));
-      sc = scale_of(top);
+      top = wave_max_bits(max_of(S));
+      const Scale sc = scale_of(top);
       if constexpr (KEEP)
-        if (lane == 0) out.smax[sh * (a.dv / 16) + cg] = __uint_as_float(top);
+        if (lane == 0) out.smax[sh * (a.dv / 16) + cg] = __uint_as_float(top) * unit;
+      Pair Sp[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
+      qdown = sc.down * unit;
       floatx4 x[4];
       rows_times<NT, DK>(ki, Sp, x, i, g);
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSince, tau) * sc.down) * x[tau];
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int tau = 0; tau < 4; ++tau) {
+          const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
+          if constexpr (NT == 2) qs[tau] = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), qs[tau]);
+          qs[tau] = SHORT ? mma(Sp[kb].hi, qr, qs[tau]) : mma1(Sp[kb], qr, qs[tau]);
+        }
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSince, tau) * qdown) * x[tau];
     }
-    // r = T y, u = beta' r
+    jobs(integral_constant<int, 2>{}, integral_constant<int, 5>{});
+    // r = T y, u = beta' r; both times uunit
     floatx4 U[4];
+    float uunit;
     {
       const Scale sy = scale_for(Y);
-      const float ydown = sy.down * (1.f / kTriUp);
+      uunit = sy.down * (1.f / kTriUp);
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
-      tri_times<false>(st, Yp, U, lane);
+      tri_times<false>(s.rec + kTHi, s.rec + kTHi + kTerm, Yp, U, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         if constexpr (KEEP) {
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = U[tau][r] * ydown;
+            out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = U[tau][r] * uunit;
         }
-        U[tau] *= row4(kBeta, tau) * ydown;
+        U[tau] *= row4(kBeta, tau);
       }
     }
+    jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});
     // o, transposed: a lane holds 4 columns of one row
     {
       const Scale su = scale_for(U);
-      const float udown = su.down * (1.f / kTriUp);
-      floatx4 x[4], y[4];
+      const float udown = su.down * uunit * (1.f / kTriUp);
+      floatx4 y[4];
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) x[tau] = y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (carried) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int tau = 0; tau < 4; ++tau) {
-            const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
-            if constexpr (NT == 2) x[tau] = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), x[tau]);
-            x[tau] = SHORT ? mma(Sp[kb].hi, qr, x[tau]) : mma1(Sp[kb], qr, x[tau]);
-          }
-      }
+      for (int tau = 0; tau < 4; ++tau) y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        const half8_t un = narrow(U[2 * s2], U[2 * s2 + 1], su.up);
-        const Pair up = SHORT ? Pair{un, un} : split(U[2 * s2], U[2 * s2 + 1], su.up);
+        Pair up;
+        if constexpr (SHORT) up.hi = narrow(U[2 * s2], U[2 * s2 + 1], su.up);
+        else up = split(U[2 * s2], U[2 * s2 + 1], su.up);
 #pragma unroll
         for (int tau = 2 * s2; tau < 4; ++tau) {
-          const _Float16* p = sp + tri_at(tau, s2) * kFrag + lane * 8;
-          const half8_t hi = *reinterpret_cast<const half8_t*>(p);
-          if constexpr (SHORT) y[tau] = mma(un, hi, y[tau]);
-          else y[tau] = mma2(up, Pair{hi, *reinterpret_cast<const half8_t*>(p + kTri * kFrag)}, y[tau]);
+          const int p = tri_at(tau, s2) * kFrag + lane * 8;
+          const half8_t hi = *reinterpret_cast<const half8_t*>(s.rec + kPHi + p);
+          if constexpr (SHORT) y[tau] = mma(up.hi, hi, y[tau]);
+          else y[tau] = mma2(up, Pair{hi, *reinterpret_cast<const half8_t*>(s.rec + kPLo + p)}, y[tau]);
         }
       }
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         const int p = 16 * tau + i;
-        const float os = s.scal[kOScale + p], since = os * s.scal[kSince + p] * sc.down;
-        const floatx4 z = since * x[tau] + (os * udown) * y[tau];
+        const float os = scal[kOScale + p], since = os * scal[kSince + p] * qdown;
+        const floatx4 z = since * qs[tau] + (os * udown) * y[tau];
         if constexpr (!KEEP) {
           if (p < rows) store4(o + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g, z);
         } else {
@@ -605,34 +651,46 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
         }
       }
     }
-    // S = exp(gam_last) S + k'^T (until u)
+    // S = exp(gam_last) S + k'^T (until u), summed in the units of the products.  Where u is so small
+    // beside the state that the state would overflow there, its units follow the state's size.
     {
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) U[tau] *= row4(kUntil, tau);
-      const Scale su = scale_for(U);
+      uint32_t ubits = wave_max_bits(max_of(U));
+      const uint32_t least = __float_as_uint(__uint_as_float(top) * unit / uunit * 0x1p-60f);
+      ubits = least < 0x7f800000u && least > ubits ? least : ubits;
+      const Scale su = scale_of(ubits);
       Pair Up[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Up[s2] = split(U[2 * s2], U[2 * s2 + 1], su.up);
-      const float last = s.scal[kLast];
+      const float newunit = su.down * uunit, keep = scal[kLast] * (unit / newunit);
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+        floatx4 x = S[t] * keep;
 #pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
           if constexpr (NT == 2) x = mma(image_cols<DK>(ki + IMG, t >> 1, t & 1, s2, i, g), Up[s2].hi, x);
           x = mma1(image_cols<DK>(ki, t >> 1, t & 1, s2, i, g), Up[s2], x);
         }
-        S[t] = last * S[t] + su.down * x;
+        S[t] = x;
       }
+      unit = newunit;
       carried = true;
     }
   };
 
   if constexpr (TWICE) {
     const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) {
-      __syncthreads();   // chunk c is there, and no wave reads the other buffer any more
-      if (c + 1 < chunks) fetch(other, c + 1);
-      if (live) work(s, c);
+      // chunk c is there, and no wave reads the other buffer any more.  The four stores of o of the chunk
+      // before come after all its moves and need not be waited for.
+      if (!KEEP && live && c > 0) barrier_after<4>();
+      else barrier_after<0>();
+      if (live) {
+        work(s, other, c);
+      } else if (c + 1 < chunks) {
+        start(other, c + 1, at);   // moves no rows
+        fetch.template jobs<0, F::kJobs>(other, wave);
+      }
     };
     for (int c = 0; c < chunks; c += 2) {
       turn(s_a, s_b, c);
@@ -640,12 +698,16 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     }
   } else {
     for (int c = 0; c < chunks; ++c) {
-      __syncthreads();
-      fetch(s_a, c);
-      __syncthreads();
-      if (live) work(s_a, c);
+      if (c > 0) at.take(reinterpret_cast<const float*>(s_a.rec + kScalAt) + kNext, lane);
+      barrier_after<0>();
+      start(s_a, c, at);
+      fetch.template jobs<0, F::kJobs>(s_a, wave);
+      barrier_after<0>();
+      if (live) work(s_a, s_a, c);
     }
   }
+#pragma unroll
+  for (int t = 0; t < ST; ++t) S[t] *= unit;
   store_state(S, a, out.state_out, w, h, col, live, g);
 }
 
