@@ -91,6 +91,24 @@ __device__ __forceinline__ Win window(const Args& a, int w) {
 // the windows is needed to place them.
 __device__ __forceinline__ uint32_t first_slot(int begin, int w) { return (uint32_t)begin / kChunk + (uint32_t)w; }
 
+// The window whose chunk `slot` is, if any is: first slots grow with the window, so each step of the
+// search probes 64 windows at once (a lane each) and one of a few thousand is found in two loads.
+__device__ __forceinline__ int window_of(const Args& a, uint32_t slot, int lane) {
+  int lo = 0, hi = a.W;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, w = lo + lane * step;
+    bool at_most = false;
+    if (w < hi) {
+      const int b = a.offsets[w];
+      at_most = first_slot(b < 0 ? 0 : b > a.n ? a.n : b, w) <= slot;
+    }
+    const int count = __popcll(__ballot(at_most));
+    lo += (count > 0 ? count - 1 : 0) * step;
+    hi = min(lo + step, hi);
+  }
+  return lo;
+}
+
 // Original row of position p (order: the caller's, clamped so that nothing is read out of range).
 __device__ __forceinline__ int row_at(const Args& a, int p) {
   if (a.order == nullptr) return p;

@@ -78,14 +78,14 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
   const Win win = window(a, w);
   const uint32_t slot0 = first_slot(win.begin, w);
   const int chunks = (win.rows + kChunk - 1) / kChunk;
-  const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
+  const auto rows_of = [&](int c) __attribute__((always_inline)) { return min(kChunk, win.rows - c * kChunk); };
 
   floatx4 S[ST];
   load_state(S, a, dstate, w, h, col, live, g);
   bool carried = dstate != nullptr;
   using F = Fetch<T, DK, NW, kScalAt, kRecordBack, kScalAt>;
   F fetch;
-  const auto begin = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) {
+  const auto begin = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) __attribute__((always_inline)) {
     fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, kRecordBack, dout, at, wave, lane);
   };
   Places<T> at;
@@ -97,9 +97,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     }
   }
 
-  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) {
+  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) __attribute__((always_inline)) {
     const float* scal = reinterpret_cast<const float*>(s.rec);
-    const auto jobs = [&](auto from, auto to) {
+    const auto jobs = [&](auto from, auto to) __attribute__((always_inline)) {
       if constexpr (TWICE)
         if (c > 0) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
     };
@@ -202,15 +202,29 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     }
   };
 
-  if constexpr (TWICE) {
-    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) {
-      barrier_after<0>();   // chunk c is there, and no wave reads the other buffer any more
-      if (live) {
-        work(s, other, c);
-      } else if (c > 0) {
-        begin(other, c - 1, at);   // moves no rows
-        fetch.template jobs<0, F::kJobs>(other, wave);
+  if (!live) {   // beyond dv: a share of the moves
+    for (int c = chunks - 1; c >= 0; --c) {
+      barrier_after<0>();
+      if constexpr (TWICE) {
+        if (c == 0) break;
+        begin(s_b, c - 1, at);
+        fetch.template jobs<0, F::kJobs>(s_b, wave);
+        barrier_after<0>();
+        if (--c == 0) break;
+        begin(s_a, c - 1, at);
+        fetch.template jobs<0, F::kJobs>(s_a, wave);
+      } else {
+        begin(s_a, c, at);
+        fetch.template jobs<0, F::kJobs>(s_a, wave);
+        barrier_after<0>();
       }
+    }
+    return;
+  }
+  if constexpr (TWICE) {
+    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) __attribute__((always_inline)) {
+      barrier_after<0>();   // chunk c is there, and no wave reads the other buffer any more
+      work(s, other, c);
     };
     for (int c = chunks - 1; c >= 0; c -= 2) {
       turn(s_a, s_b, c);
@@ -223,7 +237,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
       begin(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
       barrier_after<0>();
-      if (live) work(s_a, s_a, c);
+      work(s_a, s_a, c);
     }
   }
   store_state(S, a, dstate_in, w, h, col, live, g);
@@ -270,7 +284,7 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {
 }
 
 template <typename T, int DK>
-__global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
+__global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
                                                     const float* __restrict__ gin,
                                                     const _Float16* __restrict__ images,
                                                     const _Float16* __restrict__ records,
@@ -295,12 +309,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict_
 
   const uint32_t slot = blockIdx.x;
   const int hk = blockIdx.y;
-  int lo = 0, hi = a.W;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first_slot(window(a, mid).begin, mid) <= slot) lo = mid;
-    else hi = mid;
-  }
+  const int lo = window_of(a, slot, threadIdx.x & 63);
   const Win win = window(a, lo);
   const uint32_t f = first_slot(win.begin, lo);
   if (slot < f || (int64_t)(slot - f) * kChunk >= win.rows) return;
@@ -308,7 +317,8 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict_
   const int rows = min(kChunk, win.rows - (int)(slot - f) * kChunk);
   const bool more = (int64_t)(slot - f + 1) * kChunk < win.rows;   // the window has a chunk after this one
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int own = 16 * wave + i;
   const bool real = own < rows;
   const int orig = real ? row_at(a, base + own) : 0;
@@ -460,7 +470,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args a, const T* __restrict_
           DKc[t][r] += vs * (fk0 * y[r] + fk1 * z[r]);
         }
       }
-      const auto rows_of = [&](auto& rows, auto& x, int j) {
+      const auto rows_of = [&](auto& rows, auto& x, int j) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < (int)(sizeof(x.t) / sizeof(x.t[0])); ++n)
           x.t[n] = *reinterpret_cast<const half8_t*>(&rows[j][n][lane * 8]);

@@ -34,14 +34,24 @@ __device__ __forceinline__ floatx4 mma_f32(const floatx4& a, const floatx4& b, f
 // x = (I + n)^-1 for strictly lower n; upper blocks of x that the operands read become zero.
 __device__ __forceinline__ void invert(PrepShared& s, int wave, int i, int g) {
   {
+    // column i of the inverse: row after row is finished and taken out of those below it
     float col[16];
 #pragma unroll
-    for (int a = 0; a < 16; ++a) {
-      const float* row = s.n + (16 * wave + a) * kLd + 16 * wave;
-      float sum = a == i ? 1.f : 0.f;
+    for (int a = 0; a < 16; ++a) col[a] = a == i ? 1.f : 0.f;
 #pragma unroll
-      for (int b = 0; b < a; ++b) sum -= row[b] * col[b];
-      col[a] = sum;
+    for (int b4 = 0; b4 < 4; ++b4) {
+#pragma unroll
+      for (int a4 = b4; a4 < 4; ++a4) {   // rows 4 a4 .. + 3 less what rows 4 b4 .. + 3 have of them
+        floatx4 row[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+          row[a] = *reinterpret_cast<const floatx4*>(s.n + (16 * wave + 4 * a4 + a) * kLd + 16 * wave + 4 * b4);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            if (a4 > b4 || a > b) col[4 * a4 + a] -= row[a][b] * col[4 * b4 + b];
+      }
     }
 #pragma unroll
     for (int a = 0; a < 16; ++a)
@@ -103,7 +113,7 @@ __device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, int tau
 }
 
 template <typename T, int DK, bool REV>
-__global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict__ q, const T* __restrict__ k,
+__global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restrict__ q, const T* __restrict__ k,
                                                     const float* __restrict__ gin, const float* __restrict__ beta,
                                                     _Float16* __restrict__ images,
                                                     _Float16* __restrict__ records) {
@@ -118,20 +128,15 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
 
   const uint32_t slot = blockIdx.x;
   const int hk = blockIdx.y;
-  // the window of this slot: first slots grow with the window
-  int lo = 0, hi = a.W;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first_slot(window(a, mid).begin, mid) <= slot) lo = mid;
-    else hi = mid;
-  }
+  const int lo = window_of(a, slot, threadIdx.x & 63);
   const Win win = window(a, lo);
   const uint32_t f = first_slot(win.begin, lo);
   if (slot < f || (int64_t)(slot - f) * kChunk >= win.rows) return;
   const int base = win.begin + (int)(slot - f) * kChunk;
   const int rows = min(kChunk, win.rows - (int)(slot - f) * kChunk);
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   {
     const int row = tid >> 2, gg = tid & 3;
     const bool real = row < rows;
@@ -247,7 +252,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
       if (lane == 0) sc[kLast] = lcut == 0 ? expf((float)last) : 0.f;
     }
     __syncthreads();
-    floatx4 p[4], b[4];
+    floatx4 d[4];   // decays between the rows, zero above the diagonal
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int col = 16 * j + i;
@@ -258,10 +263,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * wave + 4 * g + r;
         const bool low = j <= wave && row >= col && s_cut[row] == cc;
-        const float d = low ? expf((float)(s_gam[row] - gc)) : 0.f;
-        p[j][r] = low ? d * qk[j][r] : 0.f;
-        b[j][r] = low && row > col ? d * kk[j][r] : 0.f;
-        sm.n[row * kLd + col] = b[j][r] * bc;
+        d[j][r] = low ? expf((float)(s_gam[row] - gc)) : 0.f;
+        sm.n[row * kLd + col] = low && row > col ? d[j][r] * kk[j][r] * bc : 0.f;
       }
     }
     __syncthreads();
@@ -273,8 +276,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = 16 * wave + 4 * g + r;
-          sm.n[row * kLd + 16 * j + i] = b[j][r] * s_beta[row];
+          const int row = 16 * wave + 4 * g + r, col = 16 * j + i;
+          sm.n[row * kLd + col] = row > col ? d[j][r] * kk[j][r] * s_beta[row] : 0.f;
         }
       __syncthreads();
       invert(sm, wave, i, g);
@@ -284,7 +287,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args a, const T* __restrict_
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = p[j][r];
+      for (int r = 0; r < 4; ++r)
+        sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = d[j][r] == 0.f ? 0.f : d[j][r] * qk[j][r];
     __syncthreads();
     put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
     if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
@@ -505,7 +509,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   const Win win = window(a, w);
   const uint32_t slot0 = first_slot(win.begin, w);
   const int chunks = (win.rows + kChunk - 1) / kChunk;
-  const auto rows_of = [&](int c) { return min(kChunk, win.rows - c * kChunk); };
+  const auto rows_of = [&](int c) __attribute__((always_inline)) { return min(kChunk, win.rows - c * kChunk); };
 
   // the state is `unit` times S: after a chunk S stays in the units of the products it was summed with
   floatx4 S[ST];
@@ -513,7 +517,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   load_state(S, a, state_in, w, h, col, live, g);
   bool carried = state_in != nullptr;   // no products with a state that is zero
   F fetch;
-  const auto start = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) {
+  const auto start = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) __attribute__((always_inline)) {
     fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, record, v, at, wave, lane);
   };
   Places<T> at;
@@ -526,14 +530,14 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   }
 
   // chunk c, staged in `s`; the next one's moves go into `other` in between
-  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) {
+  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) __attribute__((always_inline)) {
     const int rows = rows_of(c);
     const size_t sh = (size_t)(slot0 + c) * a.H + h;
     const _Float16 *qi = s.img, *ki = s.img + NT * IMG;
     const float* scal = reinterpret_cast<const float*>(s.rec + kScalAt);
     auto row4 = [&](int what, int tau) { return *reinterpret_cast<const floatx4*>(scal + what + 16 * tau + 4 * g); };
     const bool next = TWICE && c + 1 < chunks;
-    const auto jobs = [&](auto from, auto to) {
+    const auto jobs = [&](auto from, auto to) __attribute__((always_inline)) {
       if constexpr (TWICE)
         if (next) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
     };
@@ -679,18 +683,32 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     }
   };
 
+  if (!live) {   // beyond dv: a share of the moves
+    for (int c = 0; c < chunks; ++c) {
+      barrier_after<0>();
+      if constexpr (TWICE) {
+        if (c + 1 >= chunks) break;
+        start(s_b, c + 1, at);
+        fetch.template jobs<0, F::kJobs>(s_b, wave);
+        barrier_after<0>();
+        if (++c + 1 >= chunks) break;
+        start(s_a, c + 1, at);
+        fetch.template jobs<0, F::kJobs>(s_a, wave);
+      } else {
+        start(s_a, c, at);
+        fetch.template jobs<0, F::kJobs>(s_a, wave);
+        barrier_after<0>();
+      }
+    }
+    return;
+  }
   if constexpr (TWICE) {
-    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) {
+    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) __attribute__((always_inline)) {
       // chunk c is there, and no wave reads the other buffer any more.  The four stores of o of the chunk
       // before come after all its moves and need not be waited for.
-      if (!KEEP && live && c > 0) barrier_after<4>();
+      if (!KEEP && c > 0) barrier_after<4>();
       else barrier_after<0>();
-      if (live) {
-        work(s, other, c);
-      } else if (c + 1 < chunks) {
-        start(other, c + 1, at);   // moves no rows
-        fetch.template jobs<0, F::kJobs>(other, wave);
-      }
+      work(s, other, c);
     };
     for (int c = 0; c < chunks; c += 2) {
       turn(s_a, s_b, c);
@@ -703,7 +721,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       start(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
       barrier_after<0>();
-      if (live) work(s_a, s_a, c);
+      work(s_a, s_a, c);
     }
   }
 #pragma unroll
