@@ -253,12 +253,10 @@ __device__ __forceinline__ void to_lds(void* lds, const void* src) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
-// Barrier of the workgroup that waits for the wave's LDS operations and for all of its vector memory
-// operations but the LATER last ones.
-template <int LATER>
-__device__ __forceinline__ void barrier_after() {
+// Barrier of the workgroup, after the wave's own LDS and vector memory operations.
+__device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070 | LATER);   // vmcnt(LATER) lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }

@@ -204,26 +204,26 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 
   if (!live) {   // beyond dv: a share of the moves
     for (int c = chunks - 1; c >= 0; --c) {
-      barrier_after<0>();
+      barrier();
       if constexpr (TWICE) {
         if (c == 0) break;
         begin(s_b, c - 1, at);
         fetch.template jobs<0, F::kJobs>(s_b, wave);
-        barrier_after<0>();
+        barrier();
         if (--c == 0) break;
         begin(s_a, c - 1, at);
         fetch.template jobs<0, F::kJobs>(s_a, wave);
       } else {
         begin(s_a, c, at);
         fetch.template jobs<0, F::kJobs>(s_a, wave);
-        barrier_after<0>();
+        barrier();
       }
     }
     return;
   }
   if constexpr (TWICE) {
     const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) __attribute__((always_inline)) {
-      barrier_after<0>();   // chunk c is there, and no wave reads the other buffer any more
+      barrier();   // chunk c is there, and no wave reads the other buffer any more
       work(s, other, c);
     };
     for (int c = chunks - 1; c >= 0; c -= 2) {
@@ -233,10 +233,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
   } else {
     for (int c = chunks - 1; c >= 0; --c) {
       if (c + 1 < chunks) at.take(reinterpret_cast<const float*>(s_a.rec) + kPrev, lane);
-      barrier_after<0>();
+      barrier();
       begin(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
-      barrier_after<0>();
+      barrier();
       work(s_a, s_a, c);
     }
   }

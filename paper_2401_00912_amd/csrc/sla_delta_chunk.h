@@ -511,6 +511,17 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   const int chunks = (win.rows + kChunk - 1) / kChunk;
   const auto rows_of = [&](int c) __attribute__((always_inline)) { return min(kChunk, win.rows - c * kChunk); };
 
+  // o of the chunk before: stored when the next one starts, so that no barrier waits for it
+  Raw<T, 4> held[4];
+  int held_place[4], held_rows = 0;
+  const auto put = [&]() __attribute__((always_inline)) {
+    if constexpr (!KEEP)
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau)
+        if (16 * tau + i < held_rows)
+          *reinterpret_cast<Raw<T, 4>*>(o + ((size_t)held_place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g) = held[tau];
+  };
+
   // the state is `unit` times S: after a chunk S stays in the units of the products it was summed with
   floatx4 S[ST];
   float unit = 1.f;
@@ -544,6 +555,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     using std::integral_constant;
     floatx4 Y[4], qs[4];
     rows_in(s.rows[wave], Y, rows, i, g);   // before any move: the compiler makes transposed reads wait for those
+    put();
     if constexpr (TWICE)
       if (next) {
         Places<T> to;
@@ -642,7 +654,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
         const float os = scal[kOScale + p], since = os * scal[kSince + p] * qdown;
         const floatx4 z = since * qs[tau] + (os * udown) * y[tau];
         if constexpr (!KEEP) {
-          if (p < rows) store4(o + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g, z);
+          const float z4[4] = {z[0], z[1], z[2], z[3]};
+          held[tau] = Frag<T, 4>::from_f32(z4);
+          held_place[tau] = place[tau];
         } else {
           float d4[4], dot = 0.f;
           Frag<T, 4>::to_f32(dn[tau], d4);
@@ -681,33 +695,31 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       unit = newunit;
       carried = true;
     }
+    held_rows = rows;
   };
 
   if (!live) {   // beyond dv: a share of the moves
     for (int c = 0; c < chunks; ++c) {
-      barrier_after<0>();
+      barrier();
       if constexpr (TWICE) {
         if (c + 1 >= chunks) break;
         start(s_b, c + 1, at);
         fetch.template jobs<0, F::kJobs>(s_b, wave);
-        barrier_after<0>();
+        barrier();
         if (++c + 1 >= chunks) break;
         start(s_a, c + 1, at);
         fetch.template jobs<0, F::kJobs>(s_a, wave);
       } else {
         start(s_a, c, at);
         fetch.template jobs<0, F::kJobs>(s_a, wave);
-        barrier_after<0>();
+        barrier();
       }
     }
     return;
   }
   if constexpr (TWICE) {
     const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) __attribute__((always_inline)) {
-      // chunk c is there, and no wave reads the other buffer any more.  The four stores of o of the chunk
-      // before come after all its moves and need not be waited for.
-      if (!KEEP && c > 0) barrier_after<4>();
-      else barrier_after<0>();
+      barrier();   // chunk c is there, and no wave reads the other buffer any more
       work(s, other, c);
     };
     for (int c = 0; c < chunks; c += 2) {
@@ -717,13 +729,14 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   } else {
     for (int c = 0; c < chunks; ++c) {
       if (c > 0) at.take(reinterpret_cast<const float*>(s_a.rec + kScalAt) + kNext, lane);
-      barrier_after<0>();
+      barrier();
       start(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
-      barrier_after<0>();
+      barrier();
       work(s_a, s_a, c);
     }
   }
+  put();
 #pragma unroll
   for (int t = 0; t < ST; ++t) S[t] *= unit;
   store_state(S, a, out.state_out, w, h, col, live, g);
