@@ -28,15 +28,26 @@ constexpr int kMaxVectors = 1024;          // channels / 4 at most
 
 enum Act { kNone = 0, kRelu = 1, kSilu = 2 };
 
+// 1 / (1 + e^-z) from the hardware's 2^x and 1 / x (each within one step): -z log2 e in two terms, so
+// that a large exponent loses nothing.  With expf and a division the activation took more time than
+// the memory (240,011 x 256 bf16 values: 56 us, 47 for the bytes).
+__device__ __forceinline__ float sigmoid(float z) {
+  constexpr float kHi = -1.44269502f, kLo = -1.92596299e-8f;   // -log2 e
+  z = __builtin_amdgcn_fmed3f(z, -87.f, 87.f);   // 1e-38 and 1 beyond; a NaN is the caller's factor too
+  const float t = z * kHi;
+  const float r = __builtin_fmaf(z, kHi, -t) + z * kLo;
+  const float e = __builtin_amdgcn_exp2f(t);
+  return __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, r * 0.693147181f, e));
+}
 __device__ __forceinline__ float act(int a, float z) {
   if (a == kRelu) return z > 0.f ? z : (z != z ? z : 0.f);
-  if (a == kSilu) return z / (1.f + expf(-z));
+  if (a == kSilu) return z * sigmoid(z);
   return z;
 }
 __device__ __forceinline__ float slope(int a, float z) {
   if (a == kRelu) return z > 0.f ? 1.f : 0.f;
   if (a == kSilu) {
-    const float s = 1.f / (1.f + expf(-z));
+    const float s = sigmoid(z);
     return s * (1.f + z * (1.f - s));
   }
   return 1.f;
@@ -90,6 +101,37 @@ struct GroupSum {
   float* table;   // kMaxVectors floats and kMaxVectors results
   bool fast;
   int tid, r, cv;
+
+  // two sums at once
+  template <bool ROW>
+  __device__ __forceinline__ void sum(const NormArgs& a, bool live, float (&x)[NV], float (&z)[NV]) const {
+    if (NV == 1 && fast) {
+      const int lane = tid & 63, wave = tid >> 6;
+      float y0 = live ? x[0] : 0.f, y1 = live ? z[0] : 0.f;
+      const int in = a.cgv < 64 ? a.cgv : 64;
+      for (int m = 1; m < in; m *= 2) y0 += __shfl_xor(y0, m), y1 += __shfl_xor(y1, m);
+      if constexpr (!ROW)
+        for (int m = a.tpr; m < 64; m *= 2) y0 += __shfl_xor(y0, m), y1 += __shfl_xor(y1, m);
+      if (ROW ? a.cgv > 64 : true) {
+        const int nw = a.tpr > 64 ? a.tpr / 64 : 1, bpg = a.cgv > 64 ? a.cgv / 64 : 1;
+        const int mine = wave % nw / bpg;
+        const int at = (lane % (a.tpr < 64 ? a.tpr : 64)) / in;
+        __syncthreads();
+        if (lane % in == 0) table[wave * 64 + at] = y0, table[256 + wave * 64 + at] = y1;
+        __syncthreads();
+        y0 = y1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWavesN; ++w)
+          if (w % nw / bpg == mine && (!ROW || w / nw == wave / nw))
+            y0 += table[w * 64 + at], y1 += table[256 + w * 64 + at];
+      }
+      x[0] = y0;
+      z[0] = y1;
+      return;
+    }
+    sum<ROW>(a, live, x);
+    sum<ROW>(a, live, z);
+  }
 
   template <bool ROW>
   __device__ __forceinline__ void sum(const NormArgs& a, bool live, float (&x)[NV]) const {
@@ -212,6 +254,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormArgs a, const T* __re
     params<VEC>(a.weight, c, 1.f, w[j]);
     params<VEC>(a.bias, c, 0.f, b[j]);
   }
+  // rows: the next row's vectors are asked for before this one's sums
+  Raw<T, VEC> ahead[ROWS ? NV : 1];
+  const auto ask = [&](int s) __attribute__((always_inline)) {
+    if constexpr (ROWS)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        ahead[j] = *reinterpret_cast<const Raw<T, VEC>*>(x + (size_t)min(s, a.S - 1) * a.C +
+                                                         min(gs.cv + kThreads * j, a.cv - 1) * VEC);
+  };
+  ask(blockIdx.x * step + gs.r);
   for (int s0 = blockIdx.x * step; s0 < a.S; s0 += gridDim.x * step) {
     const int s = ROWS ? s0 + gs.r : s0;
     const bool live = in && (!ROWS || s < a.S);
@@ -229,8 +281,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormArgs a, const T* __re
     const float inv = 1.f / ((float)seg.rows * (float)(a.cgv * VEC));
     Moments<VEC> mo[NV];
     int k = 0;
-    if (live)
-      for (int r = first; r < seg.rows; r += ROWS ? 1 : a.rp, ++k)
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        Frag<T, VEC>::to_f32(ahead[j], v[j]);
+        mo[j].add(v[j], 0);
+      }
+      k = 1;
+      ask(s + gridDim.x * step);
+    } else if (live) {
+      for (int r = first; r < seg.rows; r += a.rp, ++k)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           const int c = gs.cv + kThreads * j;
@@ -238,6 +298,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormArgs a, const T* __re
           load<T, VEC>(x + (size_t)(seg.begin + r) * a.C + c * VEC, v[j]);
           mo[j].add(v[j], k);
         }
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) total[j] = mo[j].mean * ((float)k * VEC);
     gs.template sum<ROWS>(a, live, total);
@@ -361,8 +422,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a, const T* __re
             sb[j] += dz[j][e] * w[j][e] * hat[j][e];
           }
         }
-    gs.template sum<ROWS>(a, live, sa);
-    gs.template sum<ROWS>(a, live, sb);
+    gs.template sum<ROWS>(a, live, sa, sb);
     if (!live) continue;
     for (int r = first; r < seg.rows; r += ROWS ? 1 : a.rp)
 #pragma unroll
@@ -425,37 +485,41 @@ __global__ __launch_bounds__(kThreads) void k_norm_part(NormArgs a, const T* __r
     }
 }
 
-__device__ __forceinline__ float wave_sum(float y) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) y += __shfl_xor(y, m);
-  return y;
-}
-
-// a wave for each window and group: the blocks' means and squares joined
+// A workgroup for each window and 8 groups, 32 threads a group: the blocks' means and squares joined.
 __global__ __launch_bounds__(kThreads) void k_norm_join(NormArgs a, const float* __restrict__ part,
                                                         float* __restrict__ mean, float* __restrict__ rstd) {
-  const int64_t id = (int64_t)blockIdx.x * kWavesN + (threadIdx.x >> 6);
-  if (id >= (int64_t)a.S * a.G) return;
-  const int s = (int)(id / a.G), q = (int)(id % a.G), lane = threadIdx.x & 63;
+  __shared__ float s_sum[2][32][9];
+  const int s = blockIdx.x, t = threadIdx.x & 7, q = blockIdx.y * 8 + t, l = threadIdx.x >> 3;
   const Seg seg = segment(a, s);
-  if (seg.rows == 0) {
-    if (lane == 0) mean[id] = 0.f, rstd[id] = 1.f / sqrtf(a.eps);
-    return;
-  }
-  const float* p = part + ((size_t)(seg.begin / a.rows_per + s) * a.G + q) * 2;
+  const bool live = q < a.G;
+  const float2* p = reinterpret_cast<const float2*>(part) + (size_t)(seg.begin / a.rows_per + s) * a.G + min(q, a.G - 1);
   const int blocks = (seg.rows + a.rows_per - 1) / a.rows_per, cg = a.C / a.G;
-  const float inv = 1.f / ((float)seg.rows * (float)cg);
+  const float inv = seg.rows ? 1.f / ((float)seg.rows * (float)cg) : 0.f;
+  const auto total = [&](int which, float x) __attribute__((always_inline)) {
+    s_sum[which][l][t] = x;
+    __syncthreads();
+    float y = 0.f;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) y += s_sum[which][r][t];
+    return y;
+  };
   float sum = 0.f;
-  for (int b = lane; b < blocks; b += 64)
-    sum += p[(size_t)b * a.G * 2] * (float)(min(a.rows_per, seg.rows - b * a.rows_per) * cg);
-  const float m = wave_sum(sum) * inv;
+#pragma unroll 8
+  for (int b = l; b < blocks; b += 32)
+    sum += p[(size_t)b * a.G].x * (float)(min(a.rows_per, seg.rows - b * a.rows_per) * cg);
+  const float m = total(0, sum) * inv;
   float sq = 0.f;
-  for (int b = lane; b < blocks; b += 64) {
-    const float d = p[(size_t)b * a.G * 2] - m;
-    sq += p[(size_t)b * a.G * 2 + 1] + d * d * (float)(min(a.rows_per, seg.rows - b * a.rows_per) * cg);
+#pragma unroll 8
+  for (int b = l; b < blocks; b += 32) {
+    const float2 v = p[(size_t)b * a.G];
+    const float d = v.x - m;
+    sq += v.y + d * d * (float)(min(a.rows_per, seg.rows - b * a.rows_per) * cg);
   }
-  sq = wave_sum(sq);
-  if (lane == 0) mean[id] = m, rstd[id] = 1.f / sqrtf(sq * inv + a.eps);
+  sq = total(1, sq);
+  if (l == 0 && live) {
+    mean[(size_t)s * a.G + q] = m;
+    rstd[(size_t)s * a.G + q] = 1.f / sqrtf(sq * inv + a.eps);
+  }
 }
 
 template <typename T, int VEC, int NV>
@@ -524,45 +588,40 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_part(NormArgs a, const T*
   put_channels<VEC, NV>(a, gs, db, dw, s_table, part + (size_t)blockIdx.x * 2 * a.C);
 }
 
-// A workgroup for each window and 32 of the C x 2 values: the blocks' sums, to seg[S][C][2].
-__global__ __launch_bounds__(1024) void k_norm_bwd_join(NormArgs a, const float* __restrict__ part,
-                                                        float* __restrict__ seg) {
-  __shared__ float s_sum[32][33];
-  const int s = blockIdx.x, col = blockIdx.y * 32 + (threadIdx.x & 31), rr = threadIdx.x >> 5;
-  const Seg g = segment(a, s);
-  const int blocks = (g.rows + a.rows_per - 1) / a.rows_per;
-  float y = 0.f;
-  if (col < 2 * a.C)
-#pragma unroll 4
-    for (int b = rr; b < blocks; b += 32) y += part[((size_t)(g.begin / a.rows_per + s + b) * a.C) * 2 + col];
-  s_sum[rr][threadIdx.x & 31] = y;
-  __syncthreads();
-  if (threadIdx.x < 32 && col < 2 * a.C) {
-    y = 0.f;
-#pragma unroll
-    for (int r = 0; r < 32; ++r) y += s_sum[r][threadIdx.x];
-    seg[(size_t)s * a.C * 2 + col] = y;
-  }
-}
-
-// dbias and dweight: `count` rows of C x 2 values summed
-__global__ __launch_bounds__(1024) void k_norm_channels(const float* __restrict__ rows, int count, int C,
-                                                        float* __restrict__ dweight, float* __restrict__ dbias) {
-  __shared__ float s_sum[32][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), rr = threadIdx.x >> 5;
+// 16 columns of `count` rows of C x 2 values summed by a workgroup, 64 threads a column, each row's
+// values in the same order whatever the count: to out[C x 2], or, where that is null, dbias and dweight.
+__device__ __forceinline__ void sum_columns(const float* rows, int count, int C, float* out, float* dweight,
+                                            float* dbias) {
+  __shared__ float s_sum[64][17];
+  const int t = threadIdx.x & 15, col = blockIdx.y * 16 + t, rr = threadIdx.x >> 4;
   float y = 0.f;
   if (col < 2 * C)
-#pragma unroll 4
-    for (int b = rr; b < count; b += 32) y += rows[(size_t)b * C * 2 + col];
-  s_sum[rr][threadIdx.x & 31] = y;
+#pragma unroll 8
+    for (int b = rr; b < count; b += 64) y += rows[(size_t)b * C * 2 + col];
+  s_sum[rr][t] = y;
   __syncthreads();
-  if (threadIdx.x < 32 && col < 2 * C) {
+  if (rr == 0 && col < 2 * C) {
     y = 0.f;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) y += s_sum[r][threadIdx.x];
+    for (int r = 0; r < 64; ++r) y += s_sum[r][t];
+    if (out != nullptr) out[col] = y;
     float* to = col & 1 ? dweight : dbias;
     if (to != nullptr) to[col >> 1] = y;
   }
+}
+// The blocks' sums of every window, to seg[S][C][2]; with one window they are dbias and dweight too.
+__global__ __launch_bounds__(1024) void k_norm_bwd_join(NormArgs a, const float* __restrict__ part,
+                                                        float* __restrict__ seg, float* __restrict__ dweight,
+                                                        float* __restrict__ dbias) {
+  const int s = blockIdx.x;
+  const Seg g = segment(a, s);
+  const int blocks = (g.rows + a.rows_per - 1) / a.rows_per;
+  sum_columns(part + (size_t)(g.begin / a.rows_per + s) * a.C * 2, blocks, a.C, seg + (size_t)s * a.C * 2, dweight,
+              dbias);
+}
+__global__ __launch_bounds__(1024) void k_norm_channels(const float* __restrict__ rows, int count, int C,
+                                                        float* __restrict__ dweight, float* __restrict__ dbias) {
+  sum_columns(rows, count, C, nullptr, dweight, dbias);
 }
 
 // dx of a block of rows.  A and B come from the window's channel sums, summed by the block itself.
@@ -593,8 +652,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_apply(NormArgs a, const T
     if (gs.r != 0) sa[j] = sb[j] = 0.f;   // a channel's sums once
   }
   const bool live = gs.r < a.rp;
-  gs.template sum<false>(a, live, sa);
-  gs.template sum<false>(a, live, sb);
+  gs.template sum<false>(a, live, sa, sb);
   if (!live) return;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -624,7 +682,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_apply(NormArgs a, const T
 // ------------------------------------------------------------------ host
 constexpr int kShortRows = 256;    // rows of a window on average, up to which a workgroup takes it whole
 constexpr int kGroups = 2048;      // workgroups of the rows and windows forms (8 a CU)
-constexpr int kBlocks = 2048;      // blocks of rows the long form aims at
+constexpr int kBlocks = 1024;      // blocks of rows the long form aims at (4 a CU)
 
 enum Form { kRowsForm, kWindowsForm, kLongForm };
 struct Shape {
@@ -666,8 +724,7 @@ void forward_impl(const Shape& s, const void* xv, void* yv, float* mean, float* 
     k_norm_fwd<T, VEC, NV, false><<<s.grid, kThreads, 0, stream>>>(s.a, x, y, mean, rstd);
   } else {
     k_norm_part<T, VEC, NV><<<s.grid, kThreads, 0, stream>>>(s.a, x, part);
-    const int64_t pairs = (int64_t)s.a.S * s.a.G;
-    k_norm_join<<<(uint32_t)((pairs + kWavesN - 1) / kWavesN), kThreads, 0, stream>>>(s.a, part, mean, rstd);
+    k_norm_join<<<dim3(s.a.S, (s.a.G + 7) / 8), kThreads, 0, stream>>>(s.a, part, mean, rstd);
     k_norm_apply<T, VEC, NV><<<s.grid, kThreads, 0, stream>>>(s.a, x, mean, rstd, y);
   }
 }
@@ -688,13 +745,16 @@ void backward_impl(const Shape& s, const void* xv, const void* dyv, const float*
   } else {
     float* seg = part + (size_t)s.grid * s.a.C * 2;
     k_norm_bwd_part<T, VEC, NV><<<s.grid, kThreads, 0, stream>>>(s.a, x, dy, mean, rstd, part);
-    k_norm_bwd_join<<<dim3(s.a.S, (2 * s.a.C + 31) / 32), 1024, 0, stream>>>(s.a, part, seg);
+    const bool one = s.a.S == 1;
+    k_norm_bwd_join<<<dim3(s.a.S, (2 * s.a.C + 15) / 16), 1024, 0, stream>>>(s.a, part, seg, one ? dweight : nullptr,
+                                                                            one ? dbias : nullptr);
     k_norm_bwd_apply<T, VEC, NV><<<s.grid, kThreads, 0, stream>>>(s.a, x, dy, mean, rstd, seg, dx);
+    if (one) return;
     rows = seg;
     count = s.a.S;
   }
   if (dweight != nullptr || dbias != nullptr)
-    k_norm_channels<<<(2 * s.a.C + 31) / 32, 1024, 0, stream>>>(rows, count, s.a.C, dweight, dbias);
+    k_norm_channels<<<dim3(1, (2 * s.a.C + 15) / 16), 1024, 0, stream>>>(rows, count, s.a.C, dweight, dbias);
 }
 
 template <class F>
