@@ -304,7 +304,6 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
   __shared__ float s_scale[3][4];
   __shared__ __attribute__((aligned(16))) float s_scal[kScal];
   __shared__ double s_gam[kChunk];
-  __shared__ int s_cut[kChunk];
   __shared__ float s_dot[kChunk];
 
   const uint32_t slot = blockIdx.x;
@@ -345,17 +344,13 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
     if (wave == 0) {   // the decay sums, as k_delta_prep makes them
       const bool r1 = lane < rows;
       const float g1 = r1 ? gin[(size_t)row_at(a, base + lane) * a.H + h] : 0.f;
-      const bool cut1 = g1 < -104.f;
-      double gam = cut1 ? 0.0 : (double)g1;
-      int cut = cut1 ? 1 : 0;
+      double gam = g1 < -104.f ? -65536.0 : (double)g1 * 1.4426950408889634;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
-        const double og = __shfl_up(gam, d);
-        const int oc = __shfl_up(cut, d);
-        if (lane >= d) gam += og, cut += oc;
+        const double o = __shfl_up(gam, d);
+        if (lane >= d) gam += o;
       }
       s_gam[lane] = gam;
-      s_cut[lane] = cut;
     }
     // one power of two for all of a state: the largest of its column groups
     uint32_t sbits = 0, dbits = 0;
@@ -507,16 +502,15 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
     // the decays between own row and the others, then the products over the chunk's rows
     floatx4 A[4], B[4], C[4];   // for dq from k; dk from k; dk from q
     const double go = s_gam[own];
-    const int co = s_cut[own];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int o = 16 * j + 4 * g + r;   // the other row
-        const bool joined = s_cut[o] == co;
         const bool before = o <= own, after = o >= own;
-        const float db = joined && before ? expf((float)(go - s_gam[o])) : 0.f;
-        const float da = joined && after ? expf((float)(s_gam[o] - go)) : 0.f;
+        const float diff = (float)(go - s_gam[o]);
+        const float db = before ? __builtin_amdgcn_exp2f(diff) : 0.f;
+        const float da = after ? __builtin_amdgcn_exp2f(-diff) : 0.f;
         A[j][r] = before ? a.scale * db * M[0][j][r] : 0.f;
         B[j][r] = o < own ? -db * M[1][j][r] : o > own ? -da * M[3][j][r] : 0.f;
         C[j][r] = after ? da * M[2][j][r] * s_scal[kOScale + o] : 0.f;

@@ -120,9 +120,8 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK;
   constexpr size_t kImages = (size_t)2 * NT * IMG * 2;
   __shared__ __attribute__((aligned(16))) char s_mem[kImages > sizeof(PrepShared) ? kImages : sizeof(PrepShared)];
-  __shared__ double s_gam[kChunk];
-  __shared__ int s_cut[kChunk];
-  __shared__ float s_beta[kChunk], s_vs[kChunk], s_os[kChunk];
+  __shared__ double s_gam[2][kChunk];
+  __shared__ float s_beta[2][kChunk], s_ks[kChunk], s_os[kChunk];
   _Float16* s_img = reinterpret_cast<_Float16*>(s_mem);
   PrepShared& sm = *reinterpret_cast<PrepShared*>(s_mem);
 
@@ -137,6 +136,24 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // wave 0, a row a lane: where the rows are, and one head ahead their log decays and betas
+  const int group = a.H / a.Hk;
+  const bool mine = wave == 0 && lane < rows;
+  int place = 0, place_next = 0, place_prev = 0;
+  float g1 = 0.f, b1 = 0.f;
+  const auto ask = [&](int hv) __attribute__((always_inline)) {
+    const size_t at = (size_t)place * a.H + hk * group + hv;
+    g1 = mine ? gin[at] : 0.f;
+    b1 = mine ? beta[at] : 0.f;
+  };
+  if (wave == 0) {
+    // a row that is none: row 0, or its chunk's first row; it is dropped when it is used
+    const int p1 = base + kChunk + lane, p0 = base - kChunk + lane, end = win.begin + win.rows;
+    if (mine) place = row_at(a, base + lane);
+    if (base + kChunk < end) place_next = row_at(a, p1 < end ? p1 : base + kChunk);
+    if (p0 >= win.begin) place_prev = row_at(a, p0);
+    ask(0);
+  }
   {
     const int row = tid >> 2, gg = tid & 3;
     const bool real = row < rows;
@@ -180,11 +197,26 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
         }
       }
       if (gg == 0) {
-        if (which) s_vs[row] = down;
-        else s_os[row] = up;
+        (which ? s_ks : s_os)[row] = up;
       }
     }
   }
+  // Decay sums of head hv, in powers of two and in 64 bits: their differences are small where they are
+  // large, and as an exponent a difference is exact enough in fp32 (2^t's own step is 2^-24 t).  A decay
+  // that is zero in fp32 (g below -104, -infinity) counts as 2^-65536, so that no power across it is left.
+  const auto sums = [&](int hv) __attribute__((always_inline)) {
+    if (wave != 0) return;
+    double gam = g1 < -104.f ? -65536.0 : (double)g1 * 1.4426950408889634;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const double o = __shfl_up(gam, d);
+      if (lane >= d) gam += o;
+    }
+    s_gam[hv & 1][lane] = gam;
+    s_beta[hv & 1][lane] = b1;
+    if (hv + 1 < group) ask(hv + 1);
+  };
+  sums(0);
   __syncthreads();
 
   // lower tiles of k'k'^T and q'k'^T, tile row `wave`
@@ -211,61 +243,48 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
   }
   __syncthreads();   // the images' place is the matrices' from here
 
-  const int group = a.H / a.Hk;
   for (int hv = 0; hv < group; ++hv) {
     const int h = hk * group + hv;
     const size_t sh = (size_t)slot * a.H + h;
     _Float16* out = records + sh * (REV ? kRecordBack : kRecord);
+    const double* gam = s_gam[hv & 1];
+    const float* bet = s_beta[hv & 1];
     if (wave == 0) {
-      // log decays summed in 64 bits: their differences are small where they are large.  A decay of
-      // zero (g below -104, -infinity) starts a new stretch, over which nothing is carried.
       const bool real = lane < rows;
-      const size_t at = real ? (size_t)row_at(a, base + lane) * a.H + h : 0;
-      const float g1 = real ? gin[at] : 0.f, b1 = real ? beta[at] : 0.f;
-      const bool cut1 = g1 < -104.f;
-      double gam = cut1 ? 0.0 : (double)g1;
-      int cut = cut1 ? 1 : 0;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const double og = __shfl_up(gam, d);
-        const int oc = __shfl_up(cut, d);
-        if (lane >= d) gam += og, cut += oc;
-      }
-      const float vs = s_vs[lane];
-      const float bp = b1 / vs / vs;   // powers of two
-      s_gam[lane] = gam;
-      s_cut[lane] = cut;
-      s_beta[lane] = bp;
-      const double last = __shfl(gam, 63);
-      const int lcut = __shfl(cut, 63);
+      const double gl = gam[lane], last = gam[63];
+      const float ks = s_ks[lane];
       float* sc = reinterpret_cast<float*>(out + kScalAt);
-      sc[kSince + lane] = real && cut == 0 ? expf((float)gam) : 0.f;
-      sc[kBeta + lane] = bp;
-      sc[kUntil + lane] = real && cut == lcut ? expf((float)(last - gam)) : 0.f;
-      sc[kVScale + lane] = vs;
+      sc[kSince + lane] = real ? __builtin_amdgcn_exp2f((float)gl) : 0.f;
+      sc[kBeta + lane] = bet[lane] * ks * ks;
+      sc[kUntil + lane] = real ? __builtin_amdgcn_exp2f((float)(last - gl)) : 0.f;
+      sc[kVScale + lane] = 1.f / ks;   // a power of two
       sc[kOScale + lane] = s_os[lane] * a.scale;
-      // a row that is none reads row 0 (or its chunk's first row) and is dropped when it is used
-      const int p1 = base + kChunk + lane, p0 = base - kChunk + lane, end = win.begin + win.rows;
-      sc[kRow + lane] = __int_as_float(real ? row_at(a, base + lane) : 0);
-      sc[kNext + lane] = __int_as_float(base + kChunk < end ? row_at(a, p1 < end ? p1 : base + kChunk) : 0);
-      sc[kPrev + lane] = __int_as_float(p0 >= win.begin ? row_at(a, p0) : 0);
-      if (lane == 0) sc[kLast] = lcut == 0 ? expf((float)last) : 0.f;
+      sc[kRow + lane] = __int_as_float(place);
+      sc[kNext + lane] = __int_as_float(place_next);
+      sc[kPrev + lane] = __int_as_float(place_prev);
+      if (lane == 0) sc[kLast] = __builtin_amdgcn_exp2f((float)last);
     }
-    __syncthreads();
     floatx4 d[4];   // decays between the rows, zero above the diagonal
+    double gr[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) gr[r] = gam[16 * wave + 4 * g + r];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int col = 16 * j + i;
-      const double gc = s_gam[col];
-      const int cc = s_cut[col];
-      const float bc = s_beta[col];
+      d[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+      floatx4 n = d[j];
+      if (j <= wave) {
+        const double gc = gam[col];
+        const float bc = bet[col] * s_ks[col] * s_ks[col];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * wave + 4 * g + r;
-        const bool low = j <= wave && row >= col && s_cut[row] == cc;
-        d[j][r] = low ? expf((float)(s_gam[row] - gc)) : 0.f;
-        sm.n[row * kLd + col] = low && row > col ? d[j][r] * kk[j][r] * bc : 0.f;
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * wave + 4 * g + r;
+          d[j][r] = row >= col ? __builtin_amdgcn_exp2f((float)(gr[r] - gc)) : 0.f;
+          n[r] = row > col ? d[j][r] * kk[j][r] * bc : 0.f;
+        }
       }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sm.n[(16 * wave + 4 * g + r) * kLd + col] = n[r];
     }
     __syncthreads();
     invert(sm, wave, i, g);
@@ -277,7 +296,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = 16 * wave + 4 * g + r, col = 16 * j + i;
-          sm.n[row * kLd + col] = row > col ? d[j][r] * kk[j][r] * s_beta[row] : 0.f;
+          sm.n[row * kLd + col] = row > col ? d[j][r] * kk[j][r] * (bet[row] * s_ks[row] * s_ks[row]) : 0.f;
         }
       __syncthreads();
       invert(sm, wave, i, g);
@@ -292,6 +311,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     __syncthreads();
     put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
     if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
+    if (hv + 1 < group) sums(hv + 1);
     __syncthreads();
   }
 }
