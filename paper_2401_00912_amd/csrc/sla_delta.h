@@ -53,6 +53,7 @@ struct Args {
   int32_t n, W, Hk, H, dk, dv;
   float scale;
   uint32_t slots;                     // n / 64 + W
+  int32_t part;                       // chunks of a part of a window; 0: windows are not parted
 };
 
 // Workspace of the chunk form: per chunk slot and query/key head the images of q' and k', per slot and
@@ -89,18 +90,21 @@ __device__ __forceinline__ Win window(const Args& a, int w) {
 // First chunk slot of a window: chunks of different windows never share a slot, since a window of
 // m rows from row b has at most floor((b + m) / 64) - floor(b / 64) + 1 chunks, and no scan over
 // the windows is needed to place them.
-__device__ __forceinline__ uint32_t first_slot(int begin, int w) { return (uint32_t)begin / kChunk + (uint32_t)w; }
+__device__ __forceinline__ uint32_t first_slot(int begin, int w, uint32_t rows = kChunk) {
+  return (uint32_t)begin / rows + (uint32_t)w;
+}
 
 // The window whose chunk `slot` is, if any is: first slots grow with the window, so each step of the
 // search probes 64 windows at once (a lane each) and one of a few thousand is found in two loads.
-__device__ __forceinline__ int window_of(const Args& a, uint32_t slot, int lane) {
+// (Parts of `rows` rows have slots in the same way.)
+__device__ __forceinline__ int window_of(const Args& a, uint32_t slot, int lane, uint32_t rows = kChunk) {
   int lo = 0, hi = a.W;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) / 64, w = lo + lane * step;
     bool at_most = false;
     if (w < hi) {
       const int b = a.offsets[w];
-      at_most = first_slot(b < 0 ? 0 : b > a.n ? a.n : b, w) <= slot;
+      at_most = first_slot(b < 0 ? 0 : b > a.n ? a.n : b, w, rows) <= slot;
     }
     const int count = __popcll(__ballot(at_most));
     lo += (count > 0 ? count - 1 : 0) * step;

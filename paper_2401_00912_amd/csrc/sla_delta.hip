@@ -18,10 +18,13 @@ hipError_t forward_impl(const Args& a, int dtype, const void* q, const void* k, 
   if (a.n > 0)
     k_delta_prep<T, DK, false><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
         a, static_cast<const T*>(q), static_cast<const T*>(k), g, beta, images, records);
+  float* ends = reinterpret_cast<float*>(ws + align_up(sp.total, 256));
+  _Float16* maps = reinterpret_cast<_Float16*>(ends) + (a.part ? ends_halfs(a, DK) : 0);
+  if (a.n > 0) launch_ends<T, DK>(a, static_cast<const T*>(v), state_in, images, records, kRecord, ends, maps, stream);
   with_walk<T>(a, [&](auto nw, dim3 grid) {
     constexpr int NW = decltype(nw)::value;
-    k_delta_walk<T, DK, false, NW><<<grid, 64 * NW, 0, stream>>>(
-        a, static_cast<const T*>(v), state_in, images, records, kRecord, static_cast<T*>(o), nullptr,
+    k_delta_walk<T, DK, kOut, NW><<<grid, 64 * NW, 0, stream>>>(
+        a, static_cast<const T*>(v), state_in, images, records, kRecord, ends, maps, static_cast<T*>(o), nullptr,
         WalkOut{state_out, nullptr, nullptr, nullptr, nullptr});
   });
   return hipGetLastError();
@@ -41,8 +44,8 @@ hipError_t forward_dk(const Args& a, int dtype, const void* q, const void* k, co
 }  // namespace
 
 size_t delta_workspace_bytes(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv) {
-  (void)dv;
-  return space_of(n, W, dtype, Hk, H, dk, kRecord).total;
+  const Args a = args_of(nullptr, n, W, nullptr, Hk, H, dk, dv, 1.f);
+  return space_of(n, W, dtype, Hk, H, dk, kRecord).total + parts_bytes(a);
 }
 
 hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype,
@@ -50,7 +53,7 @@ hipError_t launch_forward_delta(const int32_t* offsets, int32_t n, int32_t W, co
                                 const void* k, const void* v, const float* g, const float* beta,
                                 const float* state_in, void* o, float* state_out, void* workspace,
                                 hipStream_t stream) {
-  const Args a{offsets, order, n, W, Hk, H, dk, dv, scale, (uint32_t)slots_of(n, W)};
+  const Args a = args_of(offsets, n, W, order, Hk, H, dk, dv, scale);
   if (dtype == 0)
     return forward_dk<float>(a, dtype, q, k, v, g, beta, state_in, o, state_out, workspace, stream);
   if (dtype == 1)

@@ -30,7 +30,7 @@ using namespace delta;
 // Workspace behind the chunk form's: byte offsets.
 struct BackSpace {
   Space base;
-  size_t states, dstates, resid, lam, odo, smax, dmax, start, total;
+  size_t states, dstates, resid, lam, odo, smax, dmax, start, ends, maps, back_ends, total;
 };
 BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int32_t dk, int32_t dv) {
   BackSpace s;
@@ -50,64 +50,86 @@ BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int
   s.smax = take(sh * groups);
   s.dmax = take(sh * groups);
   s.start = take(sh * groups);
+  const Args a = args_of(nullptr, n, W, nullptr, Hk, H, dk, dv, 1.f);
+  s.ends = s.maps = s.back_ends = at;
+  if (a.part) {
+    s.ends = take(ends_halfs(a, pad_dk(dk)) / 2);
+    s.maps = take(maps_halfs(a, pad_dk(dk)) / 2);
+    s.back_ends = take(ends_halfs(a, pad_dk(dk)) / 2);
+  }
   s.total = at;
   return s;
 }
 
 // ------------------------------------------------------------------ the walk back
 // As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
+// ENDS: only the state gradients at the parts' starts, from none at their ends (the last part: from dstate).
 template <typename T, int DK, int NW>
+using BackStage = Stage<T, DK, NW, 0, kScalAt, kRecordBack>;
+
+template <typename T, int DK, int NW, bool ENDS>
 __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restrict__ dout,
                                                         const float* __restrict__ dstate,
                                                         const _Float16* __restrict__ images,
-                                                        const _Float16* __restrict__ records,
+                                                        const _Float16* __restrict__ records, float* ends,
                                                         const float* __restrict__ states, float* __restrict__ lam,
                                                         float* __restrict__ dstates, float* __restrict__ dmax,
                                                         float* __restrict__ start, float* __restrict__ dstate_in) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  constexpr bool TWICE = kTwice<T, DK, NW>;
-  __shared__ Stage<T, DK, NW> s_a;
-  __shared__ std::conditional_t<TWICE, Stage<T, DK, NW>, char> s_b;
+  using SG = BackStage<T, DK, NW>;
+  constexpr bool TWICE = kTwice<SG>;
+  __shared__ SG s_a;
+  __shared__ std::conditional_t<TWICE, SG, char> s_b;
 
-  const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int cg = blockIdx.z * NW + wave;
-  const bool live = 16 * cg < a.dv;
+  const Part part = part_of(a, blockIdx.x, lane);
+  if (part.none || (ENDS && part.lo == 0)) return;
+  const int w = part.w, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int cg = blockIdx.z * NW + wave, groups = a.dv / 16;
+  const bool live = cg < groups;
   const int col = 16 * cg + i;
   const Win win = window(a, w);
   const uint32_t slot0 = first_slot(win.begin, w);
-  const int chunks = (win.rows + kChunk - 1) / kChunk;
+  const int first = part.lo;   // the last chunk of this part's walk
   const auto rows_of = [&](int c) __attribute__((always_inline)) { return min(kChunk, win.rows - c * kChunk); };
 
   floatx4 S[ST];
-  load_state(S, a, dstate, w, h, col, live, g);
-  bool carried = dstate != nullptr;
-  using F = Fetch<T, DK, NW, kScalAt, kRecordBack, kScalAt>;
+  bool carried = true;
+  if (part.hi == part.chunks || ENDS) {
+    const float* from = part.hi == part.chunks ? dstate : nullptr;
+    load_state(S, a, from, w, h, col, live, g);
+    carried = from != nullptr;
+  } else if (live) {
+    const float* from = ends + (((size_t)(part.slot + 1) * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+#pragma unroll
+    for (int t = 0; t < ST; ++t) S[t] = *reinterpret_cast<const floatx4*>(from + t * 256);
+  }
+  using F = Fetch<SG, T, kScalAt>;
   F fetch;
-  const auto begin = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) __attribute__((always_inline)) {
+  const auto begin = [&](SG& s, int c, const Places<T>& at) __attribute__((always_inline)) {
     fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, kRecordBack, dout, at, wave, lane);
   };
   Places<T> at;
-  if (chunks > 0) {
-    at.ask(a, win.begin + (chunks - 1) * kChunk, rows_of(chunks - 1), lane);
+  if (part.hi > first) {
+    at.ask(a, win.begin + (part.hi - 1) * kChunk, rows_of(part.hi - 1), lane);
     if constexpr (TWICE) {
-      begin(s_a, chunks - 1, at);
+      begin(s_a, part.hi - 1, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
     }
   }
 
-  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) __attribute__((always_inline)) {
+  const auto work = [&](const SG& s, auto& other, int c) __attribute__((always_inline)) {
     const float* scal = reinterpret_cast<const float*>(s.rec);
     const auto jobs = [&](auto from, auto to) __attribute__((always_inline)) {
       if constexpr (TWICE)
-        if (c > 0) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
+        if (c > first) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
     };
     using std::integral_constant;
     floatx4 X[4], Y[4];
     rows_in(s.rows[wave], Y, rows_of(c), i, g);
     if constexpr (TWICE)
-      if (c > 0) {
+      if (c > first) {
         Places<T> to;
         to.take(scal + kPrev, lane);
         begin(other, c - 1, to);
@@ -118,13 +140,16 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     const _Float16 *bt = s.rec + kBackT - kScalAt, *bp = s.rec + kBackP - kScalAt;
     auto row4 = [&](int what, int tau) { return *reinterpret_cast<const floatx4*>(scal + what + 16 * tau + 4 * g); };
     const size_t sgrp = sh * (a.dv / 16) + cg;
-    floatx4 s0[ST];   // the state before the chunk, for the end
+    floatx4 s0[ENDS ? 1 : ST];   // the state before the chunk, for the end
+    if constexpr (!ENDS)
 #pragma unroll
-    for (int t = 0; t < ST; ++t) s0[t] = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
-#pragma unroll
-    for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(dstates + sgrp * ST * 256 + t * 256 + lane * 4) = S[t];
+      for (int t = 0; t < ST; ++t) s0[t] = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
     const uint32_t top = wave_max_bits(max_of(S));
-    if (lane == 0) dmax[sgrp] = __uint_as_float(top);
+    if constexpr (!ENDS) {
+#pragma unroll
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(dstates + sgrp * ST * 256 + t * 256 + lane * 4) = S[t];
+      if (lane == 0) dmax[sgrp] = __uint_as_float(top);
+    }
     // du = P^T do' + until k' dS
     {
 #pragma unroll
@@ -161,8 +186,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
       for (int tau = 0; tau < 4; ++tau) {
         const floatx4 since = row4(kSince, tau);
         X[tau] *= xdown;
+        if constexpr (!ENDS)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) lam[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = X[tau][r];
+          for (int r = 0; r < 4; ++r) lam[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = X[tau][r];
         X[tau] *= -since * row4(kBeta, tau);
         Y[tau] *= since;
       }
@@ -192,25 +218,28 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
           x = mma1(image_cols<DK>(qi, t >> 1, t & 1, s2, i, g), Yp[s2], x);
         }
         S[t] = last * S[t] + sc.down * x;
+        if constexpr (!ENDS)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) dot += s0[t][r] * S[t][r];
+          for (int r = 0; r < 4; ++r) dot += s0[t][r] * S[t][r];
       }
+      if constexpr (!ENDS) {
 #pragma unroll
-      for (int m2 = 1; m2 < 64; m2 *= 2) dot += __shfl_xor(dot, m2);
-      if (lane == 0) start[sgrp] = dot;
+        for (int m2 = 1; m2 < 64; m2 *= 2) dot += __shfl_xor(dot, m2);
+        if (lane == 0) start[sgrp] = dot;
+      }
       carried = true;
     }
   };
 
   if (!live) {   // beyond dv: a share of the moves
-    for (int c = chunks - 1; c >= 0; --c) {
+    for (int c = part.hi - 1; c >= first; --c) {
       barrier();
       if constexpr (TWICE) {
-        if (c == 0) break;
+        if (c == first) break;
         begin(s_b, c - 1, at);
         fetch.template jobs<0, F::kJobs>(s_b, wave);
         barrier();
-        if (--c == 0) break;
+        if (--c == first) break;
         begin(s_a, c - 1, at);
         fetch.template jobs<0, F::kJobs>(s_a, wave);
       } else {
@@ -222,17 +251,17 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     return;
   }
   if constexpr (TWICE) {
-    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) __attribute__((always_inline)) {
+    const auto turn = [&](const SG& s, SG& other, int c) __attribute__((always_inline)) {
       barrier();   // chunk c is there, and no wave reads the other buffer any more
       work(s, other, c);
     };
-    for (int c = chunks - 1; c >= 0; c -= 2) {
+    for (int c = part.hi - 1; c >= first; c -= 2) {
       turn(s_a, s_b, c);
-      if (c > 0) turn(s_b, s_a, c - 1);
+      if (c > first) turn(s_b, s_a, c - 1);
     }
   } else {
-    for (int c = chunks - 1; c >= 0; --c) {
-      if (c + 1 < chunks) at.take(reinterpret_cast<const float*>(s_a.rec) + kPrev, lane);
+    for (int c = part.hi - 1; c >= first; --c) {
+      if (c + 1 < part.hi) at.take(reinterpret_cast<const float*>(s_a.rec) + kPrev, lane);
       barrier();
       begin(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
@@ -240,7 +269,13 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
       work(s_a, s_a, c);
     }
   }
-  store_state(S, a, dstate_in, w, h, col, live, g);
+  if constexpr (ENDS) {
+    float* to = ends + (((size_t)part.slot * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+#pragma unroll
+    for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t];
+  } else if (part.lo == 0) {
+    store_state(S, a, dstate_in, w, h, col, live, g);
+  }
 }
 
 // ------------------------------------------------------------------ the rest, all chunks at once
@@ -622,15 +657,25 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
   if (a.n > 0)
     k_delta_prep<T, DK, true><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
         a, static_cast<const T*>(b.q), static_cast<const T*>(b.k), b.g, b.beta, images, records);
+  _Float16* maps = reinterpret_cast<_Float16*>(ws + sp.maps);
+  if (a.n > 0)
+    launch_ends<T, DK>(a, v, b.state_in, images, records, kRecordBack, at(sp.ends), maps, stream);
   with_walk<T>(a, [&](auto nw, dim3 grid) {
     constexpr int NW = decltype(nw)::value;
     if (a.n > 0)
-      k_delta_walk<T, DK, true, NW><<<grid, 64 * NW, 0, stream>>>(
-          a, v, b.state_in, images, records, kRecordBack, nullptr, dout,
+      k_delta_walk<T, DK, kKeep, NW><<<grid, 64 * NW, 0, stream>>>(
+          a, v, b.state_in, images, records, kRecordBack, at(sp.ends), maps, nullptr, dout,
           WalkOut{nullptr, at(sp.states), at(sp.smax), at(sp.resid), at(sp.odo)});
-    k_delta_back<T, DK, NW><<<grid, 64 * NW, 0, stream>>>(a, dout, b.dstate_out, images, records, at(sp.states),
-                                                          at(sp.lam), at(sp.dstates), at(sp.dmax), at(sp.start),
-                                                          b.dstate_in);
+    const auto back = [&](auto ends) {
+      k_delta_back<T, DK, NW, decltype(ends)::value><<<grid, 64 * NW, 0, stream>>>(
+          a, dout, b.dstate_out, images, records, at(sp.back_ends), at(sp.states), at(sp.lam), at(sp.dstates),
+          at(sp.dmax), at(sp.start), b.dstate_in);
+    };
+    if (a.part != 0 && a.n > 0) {
+      back(std::true_type{});
+      k_delta_join<DK, true><<<dim3(a.W, a.H, (a.dv / 16 + 3) / 4), 256, 0, stream>>>(a, at(sp.back_ends), maps);
+    }
+    back(std::false_type{});
   });
   if (a.n > 0)
     k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
@@ -662,7 +707,7 @@ hipError_t launch_backward_delta(const int32_t* offsets, int32_t n, int32_t W, c
                                  const float* state_in, const void* dout, const float* dstate_out, void* dq,
                                  void* dk_out, void* dv_out, float* dg, float* dbeta, float* dstate_in,
                                  void* workspace, hipStream_t stream) {
-  const Args a{offsets, order, n, W, Hk, H, dk, dv, scale, (uint32_t)slots_of(n, W)};
+  const Args a = args_of(offsets, n, W, order, Hk, H, dk, dv, scale);
   const BackArgs b{q, k, v, dout, g, beta, state_in, dstate_out, dq, dk_out, dv_out, dg, dbeta, dstate_in};
   if (dtype == 0) return backward_dk<float>(a, dtype, b, workspace, stream);
   if (dtype == 1) return backward_dk<_Float16>(a, dtype, b, workspace, stream);

@@ -338,15 +338,17 @@ struct WalkOut {
 template <typename T, bool KEEP>
 constexpr bool kShortOut = std::is_same<T, bf16_t>::value && !KEEP;
 
-template <typename T, int DK, int NW>
+// What a walk reads of a chunk: the images from kImgAt on and the record from kRecAt (or later) to kRecTo.
+template <typename T, int DK, int NW, int kImgAt_, int kRecAt_, int kRecTo_>
 struct Stage {
-  static constexpr int kImages = 2 * kTerms<T> * kChunk * DK;   // halfs
-  __attribute__((aligned(16))) _Float16 img[kImages];
-  __attribute__((aligned(16))) _Float16 rec[kRecord];           // as the walk forward or back reads it
+  static constexpr int kImages = 2 * kTerms<T> * kChunk * DK;   // halfs of both images
+  static constexpr int kImgAt = kImgAt_, kRecAt = kRecAt_, kRecTo = kRecTo_, kWaves = NW;
+  __attribute__((aligned(16))) _Float16 img[kImages - kImgAt];
+  __attribute__((aligned(16))) _Float16 rec[kRecTo - kRecAt];
   __attribute__((aligned(16))) T rows[NW][kChunk * 16];         // 16 columns of v (or dout) a wave
 };
-template <typename T, int DK, int NW>
-constexpr bool kTwice = 2 * sizeof(Stage<T, DK, NW>) <= 160 * 1024;
+template <class S>
+constexpr bool kTwice = 2 * sizeof(S) <= 160 * 1024;
 
 // Instructions that move a wave's 64 rows of 16 columns: 16 bytes a lane.
 template <typename T>
@@ -368,24 +370,23 @@ struct Places {
 };
 
 // A chunk on its way into a buffer: kJobs moves a wave, issued in parts between the steps of the chunk
-// in work (all at once, they hold up the wave that issues them, and its stores behind them).  FROM, TO:
-// the part of the record that is wanted, in halfs; it goes to the same place of the buffer's record less
-// SHIFT.
-template <typename T, int DK, int NW, int FROM, int TO, int SHIFT>
+// in work (all at once, they hold up the wave that issues them, and its stores behind them).  FROM: the
+// first part of the record that is wanted.
+template <class S, typename T, int FROM>
 struct Fetch {
-  using S = Stage<T, DK, NW>;
-  static constexpr int kImg = S::kImages * 2 / 1024, kRec = (TO - FROM) * 2 / 1024;
-  static constexpr int kJobs = kImg / NW + (kRec + NW - 1) / NW;
-  static_assert(kImg % NW == 0 && (TO - FROM) * 2 % 1024 == 0, "whole pieces");
+  static constexpr int NW = S::kWaves, kImg = (S::kImages - S::kImgAt) * 2 / 1024, kRec = (S::kRecTo - FROM) * 2 / 1024;
+  static constexpr int kImgJobs = (kImg + NW - 1) / NW, kJobs = kImgJobs + (kRec + NW - 1) / NW;
+  static_assert((S::kRecTo - FROM) * 2 % 1024 == 0 && FROM >= S::kRecAt, "whole pieces");
   const char *img, *rec;
 
-  __device__ __forceinline__ void start(S& b, const Args& a, size_t slot, int hk, int h, int cg, bool live,
+  // rows: the wave has columns of src to move
+  __device__ __forceinline__ void start(S& b, const Args& a, size_t slot, int hk, int h, int cg, bool rows,
                                         const _Float16* images, const _Float16* records, int record, const T* src,
                                         const Places<T>& at, int wave, int lane) {
     const size_t sh = slot * a.H + h;
-    img = reinterpret_cast<const char*>(images + (slot * a.Hk + hk) * S::kImages) + wave * 1024 + lane * 16;
+    img = reinterpret_cast<const char*>(images + (slot * a.Hk + hk) * S::kImages + S::kImgAt) + wave * 1024 + lane * 16;
     rec = reinterpret_cast<const char*>(records + sh * record + FROM) + wave * 1024 + lane * 16;
-    if (live) {   // the wave's columns of src
+    if (rows) {
 #pragma unroll
       for (int n = 0; n < kMoves<T>; ++n)
         to_lds(b.rows[wave] + n * (1024 / sizeof(T)),
@@ -396,16 +397,76 @@ struct Fetch {
   __device__ __forceinline__ void jobs(S& b, int wave) const {
 #pragma unroll
     for (int j = J0; j < J1; ++j) {
-      if (j < kImg / NW) {
-        to_lds(b.img + (wave + j * NW) * 512, img + j * NW * 1024);
+      if (j < kImgJobs) {
+        if ((j + 1) * NW <= kImg || wave + j * NW < kImg) to_lds(b.img + (wave + j * NW) * 512, img + j * NW * 1024);
       } else {
-        const int p = j - kImg / NW;
+        const int p = j - kImgJobs;
         if ((p + 1) * NW <= kRec || wave + p * NW < kRec)
-          to_lds(b.rec + FROM - SHIFT + (wave + p * NW) * 512, rec + p * NW * 1024);
+          to_lds(b.rec + (FROM - S::kRecAt) + (wave + p * NW) * 512, rec + p * NW * 1024);
       }
     }
   }
 };
+
+// ------------------------------------------------------------------ parts
+// The chunks of one window are a chain, and a few long windows leave most of the chip idle.  Then
+// windows are cut into parts of a.part chunks.  Across a part a state is mapped linearly, S' = M S + Z,
+// with M the part's walk of the unit matrix without values and Z its walk of no state: a first walk
+// makes them for all parts at once (M: dk more columns), a short chain per window joins them, and the
+// walk proper starts every part from its state.  The walk back does the same with M^T.
+// Part slots are numbered like chunk slots, with parts of 64 a.part rows.
+struct Part {
+  int w, lo, hi, chunks;   // window, its part's chunks [lo, hi), all of its chunks
+  uint32_t slot;           // the part's
+  bool none;
+};
+__device__ __forceinline__ int chunks_of(const Win& win) { return (int)(((int64_t)win.rows + kChunk - 1) / kChunk); }
+__device__ __forceinline__ Part part_of(const Args& a, uint32_t slot, int lane) {
+  Part p;
+  p.slot = slot;
+  if (a.part == 0) {
+    p.w = (int)slot;
+    p.lo = 0;
+    p.hi = p.chunks = chunks_of(window(a, p.w));
+    p.none = false;
+    return p;
+  }
+  const uint32_t rows = (uint32_t)a.part * kChunk;
+  p.w = window_of(a, slot, lane, rows);
+  const Win win = window(a, p.w);
+  const uint32_t f = first_slot(win.begin, p.w, rows);
+  p.chunks = chunks_of(win);
+  const int64_t lo = (int64_t)(slot - f) * a.part;
+  // a window without rows has a first part without chunks
+  p.none = slot < f || (slot > f && lo >= p.chunks);
+  p.lo = p.none ? 0 : (int)lo;
+  p.hi = min(p.lo + a.part, p.chunks);
+  return p;
+}
+__host__ __device__ inline size_t part_slots(const Args& a) {
+  return a.part == 0 ? (size_t)a.W : (size_t)(a.n / (a.part * kChunk)) + a.W;
+}
+// Parts of 8 to 32 chunks where that gives the chip some 512 workgroups of 64 columns; none where the
+// windows do by themselves, or where they are short (256 rows on average).
+inline int part_chunks(int64_t n, int32_t W, int32_t H, int32_t dv) {
+  if (const char* e = getenv("SLA_PART")) return atoi(e);
+  const int64_t blocks = (int64_t)H * ((dv + 63) / 64), most = (n * blocks + 512 * kChunk - 1) / (512 * kChunk);
+  const int64_t part = most < 8 ? 8 : most;
+  if (part > 32 || n < 256 * (int64_t)W || n < 2 * part * kChunk) return 0;
+  return (int)part;
+}
+inline Args args_of(const int32_t* offsets, int64_t n, int32_t W, const int32_t* order, int32_t Hk, int32_t H,
+                    int32_t dk, int32_t dv, float scale) {
+  return Args{offsets, order, (int32_t)n, W, Hk, H, dk, dv, scale, (uint32_t)slots_of(n, W), part_chunks(n, W, H, dv)};
+}
+// Halfs of the parts' ends (dk x dv states, in register order) and of their maps (M^T as an image in two terms).
+__host__ __device__ inline size_t ends_halfs(const Args& a, int DK) { return part_slots(a) * a.H * (size_t)DK * a.dv * 2; }
+__host__ __device__ inline size_t maps_halfs(const Args& a, int DK) { return part_slots(a) * a.H * (size_t)DK * DK * 2; }
+inline size_t parts_bytes(const Args& a) {
+  if (a.part == 0) return 0;
+  const int DK = pad_dk(a.dk);
+  return align_up((ends_halfs(a, DK) + maps_halfs(a, DK)) * 2, 256);
+}
 
 // The wave's columns of a staged chunk as result tiles, rows from `rows` on zero.
 template <typename T>
@@ -507,35 +568,48 @@ __device__ __forceinline__ void rows_times(const _Float16* img, const Pair (&S)[
     }
 }
 
-template <typename T, int DK, bool KEEP, int NW>
+// kOut: o and the final states; kKeep: for the backward, what WalkOut names; kEnds: the parts' Z (value
+// columns) and M (dk more columns).
+enum WalkKind { kOut, kKeep, kEnds };
+template <typename T, int DK, int KIND, int NW>
+using WalkStage = std::conditional_t<KIND == kEnds, Stage<T, DK, NW, kTerms<T> * kChunk * DK, kTHi, kRecord>,
+                                     Stage<T, DK, NW, 0, 0, kRecord>>;
+
+template <typename T, int DK, int KIND, int NW>
 __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restrict__ v,
                                                         const float* __restrict__ state_in,
                                                         const _Float16* __restrict__ images,
                                                         const _Float16* __restrict__ records, int record,
-                                                        T* __restrict__ o,
-                                                        const T* __restrict__ dout, WalkOut out) {
+                                                        float* ends, _Float16* __restrict__ maps,
+                                                        T* __restrict__ o, const T* __restrict__ dout, WalkOut out) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  constexpr bool TWICE = kTwice<T, DK, NW>, SHORT = kShortOut<T, KEEP>;
-  using F = Fetch<T, DK, NW, SHORT ? kPHi : 0, kRecord, 0>;
-  __shared__ Stage<T, DK, NW> s_a;
-  __shared__ std::conditional_t<TWICE, Stage<T, DK, NW>, char> s_b;
+  constexpr bool KEEP = KIND == kKeep, ENDS = KIND == kEnds, SHORT = kShortOut<T, KEEP>;
+  using SG = WalkStage<T, DK, KIND, NW>;
+  constexpr bool TWICE = kTwice<SG>;
+  using F = Fetch<SG, T, ENDS ? kTHi : SHORT ? kPHi : 0>;
+  __shared__ SG s_a;
+  __shared__ std::conditional_t<TWICE, SG, char> s_b;
 
-  const int w = blockIdx.x, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int cg = blockIdx.z * NW + wave;
-  const bool live = 16 * cg < a.dv;
+  const Part part = part_of(a, blockIdx.x, lane);
+  if (part.none || (ENDS && part.hi >= part.chunks)) return;
+  const int w = part.w, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int cg = blockIdx.z * NW + wave, groups = a.dv / 16;
+  const bool map = ENDS && cg >= groups;   // columns of M
+  if (ENDS && part.lo == 0 && (int)blockIdx.z * NW >= groups) return;   // a window's first part needs no M
+  const bool live = ENDS ? cg < (part.lo == 0 ? groups : groups + ST) : cg < groups;
   const int col = 16 * cg + i;
   const Win win = window(a, w);
   const uint32_t slot0 = first_slot(win.begin, w);
-  const int chunks = (win.rows + kChunk - 1) / kChunk;
+  const int last_chunk = part.hi;   // this part's chunks end before it
   const auto rows_of = [&](int c) __attribute__((always_inline)) { return min(kChunk, win.rows - c * kChunk); };
 
   // o of the chunk before: stored when the next one starts, so that no barrier waits for it
   Raw<T, 4> held[4];
   int held_place[4], held_rows = 0;
   const auto put = [&]() __attribute__((always_inline)) {
-    if constexpr (!KEEP)
+    if constexpr (KIND == kOut)
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau)
         if (16 * tau + i < held_rows)
@@ -545,36 +619,57 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   // the state is `unit` times S: after a chunk S stays in the units of the products it was summed with
   floatx4 S[ST];
   float unit = 1.f;
-  load_state(S, a, state_in, w, h, col, live, g);
-  bool carried = state_in != nullptr;   // no products with a state that is zero
+  bool carried = true;   // no products with a state that is zero
+  if (map) {
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        S[t][r] = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r == 16 * (cg - groups) + i ? 1.f : 0.f;
+  } else if (part.lo == 0 || ENDS) {
+    const float* from = part.lo == 0 ? state_in : nullptr;
+    load_state(S, a, from, w, h, col, live, g);
+    carried = from != nullptr;
+  } else if (live) {
+    const float* from = ends + (((size_t)(part.slot - 1) * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+#pragma unroll
+    for (int t = 0; t < ST; ++t) S[t] = *reinterpret_cast<const floatx4*>(from + t * 256);
+  }
   F fetch;
-  const auto start = [&](Stage<T, DK, NW>& s, int c, const Places<T>& at) __attribute__((always_inline)) {
-    fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, record, v, at, wave, lane);
+  const auto start = [&](SG& s, int c, const Places<T>& at) __attribute__((always_inline)) {
+    fetch.start(s, a, slot0 + c, hk, h, cg, live && !map, images, records, record, v, at, wave, lane);
   };
   Places<T> at;
-  if (chunks > 0) {
-    at.ask(a, win.begin, rows_of(0), lane);
+  if (part.lo < last_chunk) {
+    at.ask(a, win.begin + part.lo * kChunk, rows_of(part.lo), lane);
     if constexpr (TWICE) {
-      start(s_a, 0, at);
+      start(s_a, part.lo, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
     }
   }
 
   // chunk c, staged in `s`; the next one's moves go into `other` in between
-  const auto work = [&](const Stage<T, DK, NW>& s, auto& other, int c) __attribute__((always_inline)) {
+  const auto work = [&](const SG& s, auto& other, int c) __attribute__((always_inline)) {
     const int rows = rows_of(c);
     const size_t sh = (size_t)(slot0 + c) * a.H + h;
-    const _Float16 *qi = s.img, *ki = s.img + NT * IMG;
-    const float* scal = reinterpret_cast<const float*>(s.rec + kScalAt);
+    const _Float16 *qi = s.img, *ki = s.img + (NT * IMG - SG::kImgAt);
+    const auto rec = [&](int from) __attribute__((always_inline)) { return s.rec + (from - SG::kRecAt); };
+    const float* scal = reinterpret_cast<const float*>(rec(kScalAt));
     auto row4 = [&](int what, int tau) { return *reinterpret_cast<const floatx4*>(scal + what + 16 * tau + 4 * g); };
-    const bool next = TWICE && c + 1 < chunks;
+    const bool next = TWICE && c + 1 < last_chunk;
     const auto jobs = [&](auto from, auto to) __attribute__((always_inline)) {
       if constexpr (TWICE)
         if (next) fetch.template jobs<decltype(from)::value * F::kJobs / 8, decltype(to)::value * F::kJobs / 8>(other, wave);
     };
     using std::integral_constant;
     floatx4 Y[4], qs[4];
-    rows_in(s.rows[wave], Y, rows, i, g);   // before any move: the compiler makes transposed reads wait for those
+    // (before any move: the compiler makes transposed reads wait for those)
+    if (map) {
+#pragma unroll
+      for (int tau = 0; tau < 4; ++tau) Y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+    } else {
+      rows_in(s.rows[wave], Y, rows, i, g);
+    }
     put();
     if constexpr (TWICE)
       if (next) {
@@ -615,14 +710,15 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       qdown = sc.down * unit;
       floatx4 x[4];
       rows_times<NT, DK>(ki, Sp, x, i, g);
+      if constexpr (!ENDS)
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int tau = 0; tau < 4; ++tau) {
-          const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
-          if constexpr (NT == 2) qs[tau] = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), qs[tau]);
-          qs[tau] = SHORT ? mma(Sp[kb].hi, qr, qs[tau]) : mma1(Sp[kb], qr, qs[tau]);
-        }
+          for (int tau = 0; tau < 4; ++tau) {
+            const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
+            if constexpr (NT == 2) qs[tau] = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), qs[tau]);
+            qs[tau] = SHORT ? mma(Sp[kb].hi, qr, qs[tau]) : mma1(Sp[kb], qr, qs[tau]);
+          }
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSince, tau) * qdown) * x[tau];
     }
@@ -636,7 +732,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
-      tri_times<false>(s.rec + kTHi, s.rec + kTHi + kTerm, Yp, U, lane);
+      tri_times<false>(rec(kTHi), rec(kTHi + kTerm), Yp, U, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         if constexpr (KEEP) {
@@ -649,7 +745,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     }
     jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});
     // o, transposed: a lane holds 4 columns of one row
-    {
+    if constexpr (!ENDS) {
       const Scale su = scale_for(U);
       const float udown = su.down * uunit * (1.f / kTriUp);
       floatx4 y[4];
@@ -663,9 +759,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
 #pragma unroll
         for (int tau = 2 * s2; tau < 4; ++tau) {
           const int p = tri_at(tau, s2) * kFrag + lane * 8;
-          const half8_t hi = *reinterpret_cast<const half8_t*>(s.rec + kPHi + p);
+          const half8_t hi = *reinterpret_cast<const half8_t*>(rec(kPHi) + p);
           if constexpr (SHORT) y[tau] = mma(up.hi, hi, y[tau]);
-          else y[tau] = mma2(up, Pair{hi, *reinterpret_cast<const half8_t*>(s.rec + kPLo + p)}, y[tau]);
+          else y[tau] = mma2(up, Pair{hi, *reinterpret_cast<const half8_t*>(rec(kPLo) + p)}, y[tau]);
         }
       }
 #pragma unroll
@@ -696,8 +792,12 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       for (int tau = 0; tau < 4; ++tau) U[tau] *= row4(kUntil, tau);
       uint32_t ubits = wave_max_bits(max_of(U));
       const uint32_t least = __float_as_uint(__uint_as_float(top) * unit / uunit * 0x1p-60f);
-      ubits = least < 0x7f800000u && least > ubits ? least : ubits;
-      const Scale su = scale_of(ubits);
+      ubits = max(ubits, min(least, 0x7f000000u));
+      Scale su = scale_of(ubits);
+      if (su.down * uunit < 0x1p-120f) {   // values below some 2^-100 lose their low bits, and no unit is zero
+        su.down = 0x1p-120f / uunit;
+        su.up = 1.f / su.down;
+      }
       Pair Up[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Up[s2] = split(U[2 * s2], U[2 * s2 + 1], su.up);
@@ -718,15 +818,15 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     held_rows = rows;
   };
 
-  if (!live) {   // beyond dv: a share of the moves
-    for (int c = 0; c < chunks; ++c) {
+  if (!live) {   // beyond the columns: a share of the moves
+    for (int c = part.lo; c < last_chunk; ++c) {
       barrier();
       if constexpr (TWICE) {
-        if (c + 1 >= chunks) break;
+        if (c + 1 >= last_chunk) break;
         start(s_b, c + 1, at);
         fetch.template jobs<0, F::kJobs>(s_b, wave);
         barrier();
-        if (++c + 1 >= chunks) break;
+        if (++c + 1 >= last_chunk) break;
         start(s_a, c + 1, at);
         fetch.template jobs<0, F::kJobs>(s_a, wave);
       } else {
@@ -738,17 +838,17 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     return;
   }
   if constexpr (TWICE) {
-    const auto turn = [&](const Stage<T, DK, NW>& s, Stage<T, DK, NW>& other, int c) __attribute__((always_inline)) {
+    const auto turn = [&](const SG& s, SG& other, int c) __attribute__((always_inline)) {
       barrier();   // chunk c is there, and no wave reads the other buffer any more
       work(s, other, c);
     };
-    for (int c = 0; c < chunks; c += 2) {
+    for (int c = part.lo; c < last_chunk; c += 2) {
       turn(s_a, s_b, c);
-      if (c + 1 < chunks) turn(s_b, s_a, c + 1);
+      if (c + 1 < last_chunk) turn(s_b, s_a, c + 1);
     }
   } else {
-    for (int c = 0; c < chunks; ++c) {
-      if (c > 0) at.take(reinterpret_cast<const float*>(s_a.rec + kScalAt) + kNext, lane);
+    for (int c = part.lo; c < last_chunk; ++c) {
+      if (c > part.lo) at.take(reinterpret_cast<const float*>(s_a.rec + (kScalAt - SG::kRecAt)) + kNext, lane);
       barrier();
       start(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
@@ -759,7 +859,103 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   put();
 #pragma unroll
   for (int t = 0; t < ST; ++t) S[t] *= unit;
-  store_state(S, a, out.state_out, w, h, col, live, g);
+  if constexpr (ENDS) {
+    if (map) {   // a lane has a column of M: a row of the image of M^T, 8 neighbouring columns from two tiles
+      _Float16* to = maps + ((size_t)part.slot * a.H + h) * (2 * DK * DK);
+#pragma unroll
+      for (int t = 0; t < KB; ++t) {
+        const Pair p = split(S[2 * t], S[2 * t + 1], kTriUp);
+        const int at2 = image_at<DK>(16 * (cg - groups) + i, t, g);
+        *reinterpret_cast<half8_t*>(to + at2) = p.hi;
+        *reinterpret_cast<half8_t*>(to + DK * DK + at2) = p.lo;
+      }
+    } else {
+      float* to = ends + (((size_t)part.slot * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t];
+    }
+  } else if (part.hi == part.chunks) {
+    store_state(S, a, out.state_out, w, h, col, live, g);
+  }
+}
+
+// ------------------------------------------------------------------ the parts' states joined
+// A wave for 16 columns of a window's states: after the first part's end, which is there, S = M S + Z part
+// after part, each written over its Z.  BACK: from the last part's start to the second one's, with M^T.
+template <int DK, bool BACK>
+__global__ __launch_bounds__(256) void k_delta_join(Args a, float* ends, const _Float16* __restrict__ maps) {
+  constexpr int ST = DK / 16, KB = DK / 32, kMap = 2 * DK * DK;
+  __shared__ __attribute__((aligned(16))) _Float16 s_a[kMap];
+  __shared__ __attribute__((aligned(16))) _Float16 s_b[kMap];
+  const int w = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), groups = a.dv / 16;
+  const int cg = blockIdx.z * 4 + wave;
+  const bool live = cg < groups;
+  const Win win = window(a, w);
+  const uint32_t f = first_slot(win.begin, w, (uint32_t)a.part * kChunk);
+  const int parts = (chunks_of(win) + a.part - 1) / a.part;
+  if (parts < 3) return;   // one end at most, and no map
+  const auto part = [&](int n) { return f + (BACK ? parts - 1 - n : n); };   // n-th in the order of the walk
+  const auto end = [&](int n) { return ends + (((size_t)part(n) * a.H + h) * groups + (live ? cg : 0)) * ST * 256 + lane * 4; };
+  const auto fetch = [&](_Float16* to, int n) __attribute__((always_inline)) {
+    const char* from = reinterpret_cast<const char*>(maps + ((size_t)part(n) * a.H + h) * kMap) + lane * 16;
+#pragma unroll
+    for (int j = 0; j < kMap * 2 / 4096; ++j) to_lds(to + (wave + 4 * j) * 512, from + (wave + 4 * j) * 1024);
+  };
+  floatx4 S[ST];
+#pragma unroll
+  for (int t = 0; t < ST; ++t) S[t] = *reinterpret_cast<const floatx4*>(end(0) + t * 256);
+  const auto step = [&](const _Float16* m, _Float16* other, int n) __attribute__((always_inline)) {
+    floatx4 Z[ST];
+#pragma unroll
+    for (int t = 0; t < ST; ++t) Z[t] = *reinterpret_cast<const floatx4*>(end(n) + t * 256);
+    barrier();
+    if (n + 1 < parts - 1) fetch(other, n + 1);
+    const Scale sc = scale_for(S);
+    const float down = sc.down * (1.f / kTriUp);
+    Pair Sp[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
+#pragma unroll
+    for (int t = 0; t < ST; ++t) {
+      floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        Pair p;
+#pragma unroll
+        for (int term = 0; term < 2; ++term) {
+          const _Float16* at = m + term * DK * DK;
+          half8_t y;
+          if constexpr (BACK) {   // rows of M^T in the order of the state's rows, contraction over columns
+            y = *reinterpret_cast<const half8_t*>(at + image_at<DK>(32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3), kb, g));
+          } else {                // columns as rows, contraction over rows 32 kb + 8 g + e
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+              const _Float16* q = at + image_at<DK>(32 * kb + 8 * g + 4 * hh + (i >> 2), t >> 1, i & 3) + 4 * (t & 1);
+              const short4v z = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(q)));
+#pragma unroll
+              for (int r = 0; r < 4; ++r) y[4 * hh + r] = __builtin_bit_cast(_Float16, (short)z[r]);
+            }
+          }
+          if (term == 0) p.hi = y;
+          else p.lo = y;
+        }
+        x = mma2(p, Sp[kb], x);
+      }
+      Z[t] += down * x;
+    }
+#pragma unroll
+    for (int t = 0; t < ST; ++t) {
+      S[t] = Z[t];
+      if (live) *reinterpret_cast<floatx4*>(end(n) + t * 256) = S[t];
+    }
+  };
+  fetch(s_a, 1);
+  for (int n = 1; n < parts - 1; n += 2) {
+    step(s_a, s_b, n);
+    if (n + 1 < parts - 1) step(s_b, s_a, n + 1);
+  }
 }
 
 // Waves of a walk's workgroup.  Eight share a chunk's staging among 128 columns, four leave a SIMD to a
@@ -771,16 +967,26 @@ inline int walk_waves(const Args& a) {
   if (groups <= 2) return 2;
   if (groups <= 4 || sizeof(T) == 4) return 4;
   if (const char* e = getenv("SLA_WAVES")) return atoi(e);
-  return (int64_t)a.W * a.H * ((groups + 7) / 8) >= 256 ? 8 : 4;
+  return a.part == 0 && (int64_t)a.W * a.H * ((groups + 7) / 8) >= 256 ? 8 : 4;
 }
 // f(integral_constant<waves>, grid)
 template <typename T, class F>
 inline void with_walk(const Args& a, F f) {
   const int waves = walk_waves<T>(a);
-  const dim3 grid(a.W, a.H, (a.dv / 16 + waves - 1) / waves);
+  const dim3 grid((uint32_t)part_slots(a), a.H, (a.dv / 16 + waves - 1) / waves);
   if (waves == 2) f(std::integral_constant<int, 2>{}, grid);
   else if (waves == 4) f(std::integral_constant<int, 4>{}, grid);
   else if constexpr (sizeof(T) == 2) f(std::integral_constant<int, 8>{}, grid);
+}
+// The states at the parts' starts, where windows are parted.
+template <typename T, int DK>
+inline void launch_ends(const Args& a, const T* v, const float* state_in, const _Float16* images,
+                        const _Float16* records, int record, float* ends, _Float16* maps, hipStream_t stream) {
+  if (a.part == 0) return;
+  const int groups = a.dv / 16 + DK / 16;
+  k_delta_walk<T, DK, kEnds, 4><<<dim3((uint32_t)part_slots(a), a.H, (groups + 3) / 4), 256, 0, stream>>>(
+      a, v, state_in, images, records, record, ends, maps, nullptr, nullptr, WalkOut{});
+  k_delta_join<DK, false><<<dim3(a.W, a.H, (a.dv / 16 + 3) / 4), 256, 0, stream>>>(a, ends, maps);
 }
 
 }  // namespace delta

@@ -124,6 +124,17 @@ def test_forward_order(sla, dtype):
     check_forward(sla, Case([40, 0, 90, 7, 64], 2, 4, 64, 32, dtype, seed=5, state=True, behind=6, order=True))
 
 
+LONG = [[1100], [1024, 0, 1], [2500, 3, 1], [513, 1, 0, 2049, 512]]   # cut into parts of 512 rows
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lengths", LONG)
+@pytest.mark.parametrize("hk,h,dk,dv", [(1, 2, 32, 32), (1, 1, 128, 80), (1, 1, 48, 16)])
+def test_forward_long(sla, lengths, hk, h, dk, dv, dtype):
+    check_forward(sla, Case(lengths, hk, h, dk, dv, dtype, seed=sum(lengths) + dk, state=len(lengths) > 1, behind=2,
+                            order=dk == 48))
+
+
 def test_forward_of_a_plan(sla):
     """Rows in any order with a window id each: a plan's offsets and perm."""
     import torch
@@ -265,6 +276,14 @@ def test_backward_widths(sla, hk, h, dk, dv, dtype):
 def test_backward_lengths(sla, lengths, dtype):
     check_backward(sla, Case(lengths, 1, 2, 32, 32, dtype, seed=len(lengths) + sum(lengths), state=len(lengths) % 2 == 0,
                              behind=3, grads=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lengths", LONG)
+@pytest.mark.parametrize("hk,h,dk,dv", [(1, 2, 32, 32), (1, 1, 128, 80), (1, 1, 48, 16)])
+def test_backward_long(sla, lengths, hk, h, dk, dv, dtype):
+    check_backward(sla, Case(lengths, hk, h, dk, dv, dtype, seed=sum(lengths) + dk, state=len(lengths) > 1, behind=2,
+                             order=dk == 48, grads=True))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
