@@ -280,9 +280,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 
 // ------------------------------------------------------------------ the rest, all chunks at once
 // A workgroup per chunk and query/key head, its value heads one after the other, their dq and dk
-// summed in registers (in head order: deterministic).  Wave w owns rows 16w .. 16w + 15, one a lane
-// (i) and four lane groups over the columns, and makes the transposed dq and dk tiles: a lane ends
-// with 8 neighbouring columns of its row.  The value columns go by in blocks of 32.
+// summed in registers (in head order: deterministic).  Waves 0 to 3 make dq, waves 4 to 7 dk: wave w
+// owns rows 16 (w mod 4) .. + 15, one a lane (i) and four lane groups over the columns, and makes the
+// transposed tiles: a lane ends with 8 neighbouring columns of its row.  The value columns go by in
+// blocks of 32.
 //
 // Computed operands (states, mu, u, the products over columns) have two fp16 terms, and one, 2^-11
 // of a value, where dq and dk are bf16, whose own rounding is 8 times as coarse; dg and dbeta, which
@@ -319,7 +320,7 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {
 }
 
 template <typename T, int DK>
-__global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
+__global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
                                                     const float* __restrict__ gin,
                                                     const _Float16* __restrict__ images,
                                                     const _Float16* __restrict__ records,
@@ -352,31 +353,35 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
   const bool more = (int64_t)(slot - f + 1) * kChunk < win.rows;   // the window has a chunk after this one
 
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 & 3;
+  const bool for_k = wave8 > 3;   // dk's waves; the others are dq's
   const int own = 16 * wave + i;
   const bool real = own < rows;
   const int orig = real ? row_at(a, base + own) : 0;
   {
     const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
     uint4* dst = reinterpret_cast<uint4*>(s_img);
-    for (int x = tid; x < 2 * NT * IMG / 8; x += 256) dst[x] = src[x];
+    for (int x = tid; x < 2 * NT * IMG / 8; x += 512) dst[x] = src[x];
   }
   const _Float16 *qi = s_img, *ki = s_img + NT * IMG;
-  floatx4 DQ[ST], DKc[ST];
+  floatx4 D[ST];   // dq or dk, transposed
 #pragma unroll
-  for (int t = 0; t < ST; ++t) {
-    DQ[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    DKc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int t = 0; t < ST; ++t) D[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  const int group = a.H / a.Hk, groups = a.dv / 16;
+  const int group = a.H / a.Hk, groups = a.dv / 16, tid0 = tid, lane0 = lane;
   for (int hv = 0; hv < group; ++hv) {
+    // the lane's numbers anew for every head: their many comparisons and addresses are made where they
+    // are used, and not kept in registers over the loop
+    int tid = tid0, lane = lane0;
+    asm volatile("" : "+v"(tid), "+v"(lane));
+    const int i = lane & 15, g = lane >> 4, own = 16 * wave + i;
+    const bool real = own < rows;
     const int h = hk * group + hv;
     const size_t sh = (size_t)slot * a.H + h;
     __syncthreads();
-    for (int x = tid; x < kScal / 4; x += 256)
+    for (int x = tid; x < kScal / 4; x += 512)
       reinterpret_cast<uint4*>(s_scal)[x] = reinterpret_cast<const uint4*>(records + sh * kRecordBack + kScalAt)[x];
-    if (wave == 0) {   // the decay sums, as k_delta_prep makes them
+    if (wave8 == 7) {   // the decay sums, as k_delta_prep makes them
       const bool r1 = lane < rows;
       const float g1 = r1 ? gin[(size_t)row_at(a, base + lane) * a.H + h] : 0.f;
       double gam = g1 < -104.f ? -65536.0 : (double)g1 * 1.4426950408889634;
@@ -398,12 +403,12 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
     const float since = s_scal[kSince + own], until = s_scal[kUntil + own], be = s_scal[kBeta + own];
     const float vs = s_scal[kVScale + own];
 
-    // products over the value columns: M[.][j], transposed tiles with this wave's rows in the lanes;
-    // 0: do of own rows with u of tile j, 1: mu of own rows with u of tile j (j <= wave),
-    // 2: u of own rows with do of tile j, 3: with mu of tile j (j >= wave)
-    floatx4 M[4][4];
+    // products over the value columns: M[.][j], transposed tiles with this wave's rows in the lanes.
+    // dq: 0: do of own rows with u of tile j (j <= wave).  dk: 0: mu of own rows with u of tile j
+    // (j <= wave), 1: u of own rows with do of tile j, 2: with mu of tile j (j >= wave)
+    floatx4 M[3][4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int x = 0; x < 3; ++x)
 #pragma unroll
       for (int j = 0; j < 4; ++j) M[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     float lr = 0.f, vdv = 0.f;
@@ -411,19 +416,21 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
       // own rows of the block: 8 columns a lane
       const int col = c0 + 8 * g;
       const bool here = real && col < a.dv;
+      const size_t at = ((size_t)orig * a.H + h) * a.dv + col;
       float xo[8], xm[8], xu[8];
-      {
-        Raw<T, 8> ro = Frag<T, 8>::zero(), rv = Frag<T, 8>::zero();
+      if (!for_k) {
+        Raw<T, 8> ro = Frag<T, 8>::zero();
+        if (here) ro = *reinterpret_cast<const Raw<T, 8>*>(dout + at);
+        Frag<T, 8>::to_f32(ro, xo);
+      } else {
+        Raw<T, 8> rv = Frag<T, 8>::zero();
         f32x8 rl = {}, rr = {};
-        const size_t at = ((size_t)orig * a.H + h) * a.dv + col;
         if (here) {
-          ro = *reinterpret_cast<const Raw<T, 8>*>(dout + at);
           rv = *reinterpret_cast<const Raw<T, 8>*>(v + at);
           rl = *reinterpret_cast<const f32x8*>(lam + (sh * kChunk + own) * a.dv + col);
           rr = *reinterpret_cast<const f32x8*>(resid + (sh * kChunk + own) * a.dv + col);
         }
         float xv[8], xd[8];
-        Frag<T, 8>::to_f32(ro, xo);
         Frag<T, 8>::to_f32(rv, xv);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -435,35 +442,50 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
         }
         if (here) *reinterpret_cast<Raw<T, 8>*>(dv + at) = Frag<T, 8>::from_f32(xd);
       }
-      __syncthreads();   // the last block's reads are done
-      const Scale so = scale_of(wave_max_bits(max8(xo))), sm = scale_of(wave_max_bits(max8(xm)));
-      const Scale su = scale_of(wave_max_bits(max8(xu)));
-      const Op<NT> oo = op_of<NT>(xo, so.up);
-      const Op<NC> om = op_of<NC>(xm, sm.up), ou = op_of<NC>(xu, su.up);
+      // S0 and dS1 of the block's two column groups, as the walks left them
+      constexpr int kLoads = 2 * 2 * ST * 64 / 512;
+      floatx4 z[kLoads];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) *reinterpret_cast<half8_t*>(&s_do[wave][t][lane * 8]) = oo.t[t];
-#pragma unroll
-      for (int t = 0; t < NC; ++t) {
-        *reinterpret_cast<half8_t*>(&s_mu[wave][t][lane * 8]) = om.t[t];
-        *reinterpret_cast<half8_t*>(&s_u[wave][t][lane * 8]) = ou.t[t];
-      }
-      if (lane == 0) {
-        s_scale[0][wave] = so.down;
-        s_scale[1][wave] = sm.down;
-        s_scale[2][wave] = su.down;
-      }
-      // S0 and dS1 of the block's two column groups, as the walks left them, in 16-bit terms
-      for (int x = tid; x < 2 * 2 * ST * 64; x += 256) {
-        const int which = x / (2 * ST * 64), y = x % (2 * ST * 64), cgl = y / (ST * 64);
-        floatx4 z = {0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < kLoads; ++n) {
+        const int x = tid + 512 * n, which = x / (2 * ST * 64), y = x % (2 * ST * 64), cgl = y / (ST * 64);
+        z[n] = floatx4{0.f, 0.f, 0.f, 0.f};
         if (c0 + 16 * cgl < a.dv)
-          z = *reinterpret_cast<const floatx4*>((which ? dstates : states) +
-                                                (sh * groups + c0 / 16) * (size_t)(ST * 256) + (size_t)y * 4);
+          z[n] = *reinterpret_cast<const floatx4*>((which ? dstates : states) +
+                                                   (sh * groups + c0 / 16) * (size_t)(ST * 256) + (size_t)y * 4);
+      }
+      __syncthreads();   // the last block's reads are done
+      Op<NT> oo;
+      Op<NC> om, ou;
+      Scale so, sm, su;
+      if (!for_k) {
+        so = scale_of(wave_max_bits(max8(xo)));
+        oo = op_of<NT>(xo, so.up);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *reinterpret_cast<half8_t*>(&s_do[wave][t][lane * 8]) = oo.t[t];
+        if (lane == 0) s_scale[0][wave] = so.down;
+      } else {
+        sm = scale_of(wave_max_bits(max8(xm)));
+        su = scale_of(wave_max_bits(max8(xu)));
+        om = op_of<NC>(xm, sm.up);
+        ou = op_of<NC>(xu, su.up);
+#pragma unroll
+        for (int t = 0; t < NC; ++t) {
+          *reinterpret_cast<half8_t*>(&s_mu[wave][t][lane * 8]) = om.t[t];
+          *reinterpret_cast<half8_t*>(&s_u[wave][t][lane * 8]) = ou.t[t];
+        }
+        if (lane == 0) {
+          s_scale[1][wave] = sm.down;
+          s_scale[2][wave] = su.down;
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        const int x = tid + 512 * n, which = x / (2 * ST * 64), y = x % (2 * ST * 64);
         const float up = which ? sd.up : ss.up;
         half4_t p, l;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float u = z[r] * up;
+          const float u = z[n][r] * up;
           p[r] = (_Float16)u;
           l[r] = (_Float16)(u - (float)p[r]);
         }
@@ -472,134 +494,135 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
       }
       __syncthreads();
       // rows of the block's states as operand rows: tile t's 16 state rows, contraction over 32 columns
-      const auto state_rows = [&](int which, int t) {
+      const auto state_rows = [&](int which, int t) __attribute__((always_inline)) {
         Op<NC> x;
 #pragma unroll
         for (int n = 0; n < NC; ++n)
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
             const int c = 8 * g + 4 * hh;   // the columns' place in the block
-            const _Float16* at = &s_state[which][n][(((c >> 4) * ST + t) * 64 + (i & 3) * 16 + (c & 15) + (i >> 2)) * 4];
+            const _Float16* at2 = &s_state[which][n][(((c >> 4) * ST + t) * 64 + (i & 3) * 16 + (c & 15) + (i >> 2)) * 4];
             const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(at)));
+                (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(at2)));
 #pragma unroll
             for (int r = 0; r < 4; ++r) x.t[n][4 * hh + r] = __builtin_bit_cast(_Float16, (short)y[r]);
           }
         return x;
       };
-      const float fq = a.scale * since * (ss.down * so.down), fk0 = -since * (ss.down * sm.down);
-      const float fk1 = until * (sd.down * su.down);
-#pragma unroll
-      for (int t = 0; t < ST; ++t) {
-        const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-        const Op<NC> s0 = state_rows(0, t), d1 = state_rows(1, t);
-        const floatx4 x = mma_op(s0, oo, zero), y = mma_op(s0, om, zero), z = mma_op(d1, ou, zero);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          DQ[t][r] += fq * x[r];
-          DKc[t][r] += vs * (fk0 * y[r] + fk1 * z[r]);
-        }
-      }
       const auto rows_of = [&](auto& rows, auto& x, int j) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < (int)(sizeof(x.t) / sizeof(x.t[0])); ++n)
           x.t[n] = *reinterpret_cast<const half8_t*>(&rows[j][n][lane * 8]);
       };
+      const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+      if (!for_k) {
+        const float fq = a.scale * since * (ss.down * so.down);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-        if (j <= wave) {
-          Op<NC> u;
-          rows_of(s_u, u, j);
-          const floatx4 x = mma_op(u, oo, zero), y = mma_op(u, om, zero);
-          const float d = s_scale[2][j];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            M[0][j][r] += d * so.down * x[r];
-            M[1][j][r] += d * sm.down * y[r];
-          }
+        for (int t = 0; t < ST; ++t) {
+          if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+          D[t] += fq * mma_op(state_rows(0, t), oo, zero);
         }
-        if (j >= wave) {
-          Op<NT> o;
-          Op<NC> m;
-          rows_of(s_do, o, j);
-          rows_of(s_mu, m, j);
-          const floatx4 x = mma_op(o, ou, zero), y = mma_op(m, ou, zero);
-          const float d0 = s_scale[0][j], d1 = s_scale[1][j];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            M[2][j][r] += d0 * su.down * x[r];
-            M[3][j][r] += d1 * su.down * y[r];
+        for (int j = 0; j < 4; ++j)
+          if (j <= wave) {
+            Op<NC> u;
+            rows_of(s_u, u, j);
+            M[0][j] += (s_scale[2][j] * so.down) * mma_op(u, oo, zero);
+          }
+      } else {
+        const float fk0 = -vs * since * (ss.down * sm.down), fk1 = vs * until * (sd.down * su.down);
+#pragma unroll
+        for (int t = 0; t < ST; ++t) {
+          if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);   // two tiles' operands in registers
+          D[t] += fk0 * mma_op(state_rows(0, t), om, zero);
+          D[t] += fk1 * mma_op(state_rows(1, t), ou, zero);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (j <= wave) {
+            Op<NC> u;
+            rows_of(s_u, u, j);
+            M[0][j] += (s_scale[2][j] * sm.down) * mma_op(u, om, zero);
+          }
+          if (j >= wave) {
+            Op<NT> o;
+            Op<NC> m;
+            rows_of(s_do, o, j);
+            rows_of(s_mu, m, j);
+            M[1][j] += (s_scale[0][j] * su.down) * mma_op(o, ou, zero);
+            M[2][j] += (s_scale[1][j] * su.down) * mma_op(m, ou, zero);
           }
         }
       }
     }
-    // the decays between own row and the others, then the products over the chunk's rows
-    floatx4 A[4], B[4], C[4];   // for dq from k; dk from k; dk from q
+    // the decays between own row and the others, then the products over the chunk's rows: M[0] becomes
+    // what k is multiplied with, for dk M[1] what q is
     const double go = s_gam[own];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int o = 16 * j + 4 * g + r;   // the other row
-        const bool before = o <= own, after = o >= own;
         const float diff = (float)(go - s_gam[o]);
-        const float db = before ? __builtin_amdgcn_exp2f(diff) : 0.f;
-        const float da = after ? __builtin_amdgcn_exp2f(-diff) : 0.f;
-        A[j][r] = before ? a.scale * db * M[0][j][r] : 0.f;
-        B[j][r] = o < own ? -db * M[1][j][r] : o > own ? -da * M[3][j][r] : 0.f;
-        C[j][r] = after ? da * M[2][j][r] * s_scal[kOScale + o] : 0.f;
-      }
-    const Scale sa = scale_for(A), sb = scale_for(B), sc = scale_for(C);
-    Op<NC> Ap[2], Bp[2], Cp[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float xa[8], xb[8], xc[8];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        xa[r] = A[2 * s][r], xa[4 + r] = A[2 * s + 1][r];
-        xb[r] = B[2 * s][r], xb[4 + r] = B[2 * s + 1][r];
-        xc[r] = C[2 * s][r], xc[4 + r] = C[2 * s + 1][r];
-      }
-      Ap[s] = op_of<NC>(xa, sa.up);
-      Bp[s] = op_of<NC>(xb, sb.up);
-      Cp[s] = op_of<NC>(xc, sc.up);
-    }
-    const float vsb = vs * sb.down, vsc = vs * sc.down;
-#pragma unroll
-    for (int t = 0; t < ST; ++t) {
-      floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f}, z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        Op<NT> kc, qc;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          kc.t[n] = image_cols<DK>(ki + n * IMG, t >> 1, t & 1, s, i, g);
-          qc.t[n] = image_cols<DK>(qi + n * IMG, t >> 1, t & 1, s, i, g);
+        // decay from the other row to the own one if it is before, else from the own to the other
+        const float d = __builtin_amdgcn_exp2f(o <= own ? diff : -diff);
+        if (!for_k) {
+          M[0][j][r] = o <= own ? a.scale * d * M[0][j][r] : 0.f;
+        } else {
+          M[0][j][r] = o < own ? -d * M[0][j][r] : o > own ? -d * M[2][j][r] : 0.f;
+          M[1][j][r] = o >= own ? d * M[1][j][r] * s_scal[kOScale + o] : 0.f;
         }
-        x = mma_op(kc, Ap[s], x);
-        y = mma_op(kc, Bp[s], y);
-        z = mma_op(qc, Cp[s], z);
       }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const auto ops_of = [&](const floatx4 (&m)[4], Op<NC> (&p)[2]) __attribute__((always_inline)) {
+      const Scale s = scale_for(m);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        DQ[t][r] += sa.down * x[r];
-        DKc[t][r] += vsb * y[r] + vsc * z[r];
+      for (int s2 = 0; s2 < 2; ++s2) {
+        float x[8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = m[2 * s2][r], x[4 + r] = m[2 * s2 + 1][r];
+        p[s2] = op_of<NC>(x, s.up);
       }
+      return s.down;
+    };
+    const auto add = [&](const _Float16* img, const Op<NC> (&p)[2], float f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          Op<NT> c;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) c.t[n] = image_cols<DK>(img + n * IMG, t >> 1, t & 1, s2, i, g);
+          x = mma_op(c, p[s2], x);
+        }
+        D[t] += f * x;
+      }
+    };
+    Op<NC> P[2];
+    const float down0 = ops_of(M[0], P);
+    add(ki, P, for_k ? vs * down0 : down0);
+    if (for_k) {
+      const float down1 = ops_of(M[1], P);
+      add(qi, P, vs * down1);
     }
     // dbeta = lam . r and the terms of dg: sums over the lane groups
     lr += __shfl_xor(lr, 16);
     lr += __shfl_xor(lr, 32);
     vdv += __shfl_xor(vdv, 16);
     vdv += __shfl_xor(vdv, 32);
-    if (g == 0) {
+    if (for_k && g == 0) {
       if (real) dbeta[(size_t)orig * a.H + h] = lr / vs / vs;
       float od = 0.f;
       for (int c = 0; c < groups; ++c) od += real ? odo[(sh * groups + c) * kChunk + own] : 0.f;
       s_dot[own] = real ? od - vdv : 0.f;
     }
     __syncthreads();
-    if (wave == 0) {
+    if (wave8 == 0) {
       float x = s_dot[lane];
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {   // sums to the end
@@ -627,15 +650,11 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
     for (int t = 0; t < ST / 2; ++t) {
       const int c = 32 * t + 8 * g;
       if (c >= a.dk) continue;
-      float x[8], y[8];
+      float x[8];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[r] = DQ[2 * t][r], x[4 + r] = DQ[2 * t + 1][r];
-        y[r] = DKc[2 * t][r], y[4 + r] = DKc[2 * t + 1][r];
-      }
-      const size_t at = ((size_t)orig * a.Hk + hk) * a.dk + c;
-      *reinterpret_cast<Raw<T, 8>*>(dq + at) = Frag<T, 8>::from_f32(x);
-      *reinterpret_cast<Raw<T, 8>*>(dk + at) = Frag<T, 8>::from_f32(y);
+      for (int r = 0; r < 4; ++r) x[r] = D[2 * t][r], x[4 + r] = D[2 * t + 1][r];
+      T* to = (for_k ? dk : dq) + ((size_t)orig * a.Hk + hk) * a.dk + c;
+      *reinterpret_cast<Raw<T, 8>*>(to) = Frag<T, 8>::from_f32(x);
     }
 }
 
@@ -678,7 +697,7 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
     back(std::false_type{});
   });
   if (a.n > 0)
-    k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
+    k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 512, 0, stream>>>(
         a, v, dout, b.g, images, records, at(sp.states), at(sp.dstates), at(sp.smax), at(sp.dmax), at(sp.resid),
         at(sp.lam), at(sp.odo), at(sp.start), b.state_in != nullptr, b.dstate_out != nullptr, static_cast<T*>(b.dq),
         static_cast<T*>(b.dk), static_cast<T*>(b.dv), b.dg, b.dbeta);

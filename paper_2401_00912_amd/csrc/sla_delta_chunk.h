@@ -243,7 +243,12 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
   }
   __syncthreads();   // the images' place is the matrices' from here
 
+  const int lane0 = lane;
   for (int hv = 0; hv < group; ++hv) {
+    // the lane's numbers anew for every head, so that what follows from them takes no registers over the loop
+    int lane = lane0;
+    asm volatile("" : "+v"(lane));
+    const int i = lane & 15, g = lane >> 4;
     const int h = hk * group + hv;
     const size_t sh = (size_t)slot * a.H + h;
     _Float16* out = records + sh * (REV ? kRecordBack : kRecord);
@@ -967,7 +972,7 @@ inline int walk_waves(const Args& a) {
   if (groups <= 2) return 2;
   if (groups <= 4 || sizeof(T) == 4) return 4;
   if (const char* e = getenv("SLA_WAVES")) return atoi(e);
-  return a.part == 0 && (int64_t)a.W * a.H * ((groups + 7) / 8) >= 256 ? 8 : 4;
+  return (int64_t)a.W * a.H * ((groups + 7) / 8) >= 256 ? 8 : 4;
 }
 // f(integral_constant<waves>, grid)
 template <typename T, class F>
