@@ -279,11 +279,13 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 }
 
 // ------------------------------------------------------------------ the rest, all chunks at once
-// A workgroup per chunk and query/key head, its value heads one after the other, their dq and dk
-// summed in registers (in head order: deterministic).  Waves 0 to 3 make dq, waves 4 to 7 dk: wave w
-// owns rows 16 (w mod 4) .. + 15, one a lane (i) and four lane groups over the columns, and makes the
-// transposed tiles: a lane ends with 8 neighbouring columns of its row.  The value columns go by in
-// blocks of 32.
+// A workgroup per chunk and query/key head, its value heads one after the other, their dq (or dk)
+// summed in registers (in head order: deterministic).  Wave w owns rows 16w .. 16w + 15, one a lane (i)
+// and four lane groups over the columns, and makes the transposed tiles: a lane ends with 8
+// neighbouring columns of its row.  The value columns go by in blocks of 32, the next block's loads in
+// flight.  dq and dk are launches of their own (FOR_K; dv, dbeta and dg come with dk): together they
+// took twice the registers and waited for memory at one workgroup a CU (16,381 bf16 rows, 8 heads of
+// 128: 426 us).
 //
 // Computed operands (states, mu, u, the products over columns) have two fp16 terms, and one, 2^-11
 // of a value, where dq and dk are bf16, whose own rounding is 8 times as coarse; dg and dbeta, which
@@ -319,8 +321,8 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {
   return m;
 }
 
-template <typename T, int DK>
-__global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
+template <typename T, int DK, bool FOR_K>
+__global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
                                                     const float* __restrict__ gin,
                                                     const _Float16* __restrict__ images,
                                                     const _Float16* __restrict__ records,
@@ -334,9 +336,12 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
   constexpr int NT = kTerms<T>, IMG = kChunk * DK, ST = DK / 16;
   constexpr int NC = std::is_same<T, bf16_t>::value ? 1 : 2;   // terms of computed operands
   constexpr int kStateHalfs = ST * 256;   // one group of 16 columns, in register order
-  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG];
-  __shared__ __attribute__((aligned(16))) _Float16 s_state[2][NC][2 * kStateHalfs];   // S0, dS1
-  __shared__ __attribute__((aligned(16))) _Float16 s_do[4][NT][kFrag], s_mu[4][NC][kFrag], s_u[4][NC][kFrag];
+  constexpr int kStates = FOR_K ? 2 : 1;   // S0, dS1
+  constexpr int kSkip = FOR_K ? 0 : NT * IMG;   // dq does not need q'
+  __shared__ __attribute__((aligned(16))) _Float16 s_img[2 * NT * IMG - kSkip];
+  __shared__ __attribute__((aligned(16))) _Float16 s_state[kStates][NC][2 * kStateHalfs];
+  __shared__ __attribute__((aligned(16))) _Float16 s_do[FOR_K ? 4 : 1][NT][kFrag], s_mu[FOR_K ? 4 : 1][NC][kFrag];
+  __shared__ __attribute__((aligned(16))) _Float16 s_u[4][NC][kFrag];
   __shared__ float s_scale[3][4];
   __shared__ __attribute__((aligned(16))) float s_scal[kScal];
   __shared__ double s_gam[kChunk];
@@ -353,17 +358,17 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
   const bool more = (int64_t)(slot - f + 1) * kChunk < win.rows;   // the window has a chunk after this one
 
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 & 3;
-  const bool for_k = wave8 > 3;   // dk's waves; the others are dq's
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int own = 16 * wave + i;
   const bool real = own < rows;
   const int orig = real ? row_at(a, base + own) : 0;
   {
-    const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG);
+    const uint4* src = reinterpret_cast<const uint4*>(images + ((size_t)slot * a.Hk + hk) * 2 * NT * IMG + kSkip);
     uint4* dst = reinterpret_cast<uint4*>(s_img);
-    for (int x = tid; x < 2 * NT * IMG / 8; x += 512) dst[x] = src[x];
+#pragma unroll 4
+    for (int x = tid; x < (2 * NT * IMG - kSkip) / 8; x += 256) dst[x] = src[x];
   }
-  const _Float16 *qi = s_img, *ki = s_img + NT * IMG;
+  const _Float16 *qi = s_img, *ki = s_img + (NT * IMG - kSkip);
   floatx4 D[ST];   // dq or dk, transposed
 #pragma unroll
   for (int t = 0; t < ST; ++t) D[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -378,10 +383,33 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
     const bool real = own < rows;
     const int h = hk * group + hv;
     const size_t sh = (size_t)slot * a.H + h;
+    // a block's own rows (8 columns a lane) and its two column groups of the states, as the walks left them
+    constexpr int kLoads = kStates * 2 * ST * 64 / 256;
+    floatx4 z[kLoads];
+    Raw<T, 8> ro, rv;
+    f32x8 rl, rr;
+    const size_t row0 = ((size_t)orig * a.H + h) * a.dv, lam0 = (sh * kChunk + own) * a.dv;
+    const auto ask = [&](int c0) __attribute__((always_inline)) {
+      const int col = c0 + 8 * g < a.dv ? c0 + 8 * g : 0;   // dropped when it is used
+      ro = *reinterpret_cast<const Raw<T, 8>*>(dout + row0 + col);
+      rr = *reinterpret_cast<const f32x8*>(resid + lam0 + col);
+      if constexpr (FOR_K) {
+        rv = *reinterpret_cast<const Raw<T, 8>*>(v + row0 + col);
+        rl = *reinterpret_cast<const f32x8*>(lam + lam0 + col);
+      }
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        const int which = n >= kLoads / kStates ? 1 : 0, y = tid + 256 * (n - which * (kLoads / kStates));
+        const int group2 = c0 + 16 * (y / (ST * 64)) < a.dv ? c0 / 16 + y / (ST * 64) : 0;
+        z[n] = *reinterpret_cast<const floatx4*>((which ? dstates : states) +
+                                                 (sh * groups + group2) * (size_t)(ST * 256) + (size_t)(y % (ST * 64)) * 4);
+      }
+    };
+    ask(0);
     __syncthreads();
-    for (int x = tid; x < kScal / 4; x += 512)
+    for (int x = tid; x < kScal / 4; x += 256)
       reinterpret_cast<uint4*>(s_scal)[x] = reinterpret_cast<const uint4*>(records + sh * kRecordBack + kScalAt)[x];
-    if (wave8 == 7) {   // the decay sums, as k_delta_prep makes them
+    if (wave == 3) {   // the decay sums, as k_delta_prep makes them
       const bool r1 = lane < rows;
       const float g1 = r1 ? gin[(size_t)row_at(a, base + lane) * a.H + h] : 0.f;
       double gam = g1 < -104.f ? -65536.0 : (double)g1 * 1.4426950408889634;
@@ -405,93 +433,75 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
 
     // products over the value columns: M[.][j], transposed tiles with this wave's rows in the lanes.
     // dq: 0: do of own rows with u of tile j (j <= wave).  dk: 0: mu of own rows with u of tile j
-    // (j <= wave), 1: u of own rows with do of tile j, 2: with mu of tile j (j >= wave)
-    floatx4 M[3][4];
+    // (j <= wave) or u of own rows with mu of tile j (j > wave; at j = wave: Mw), 1: u of own rows with
+    // do of tile j (j >= wave)
+    floatx4 M[FOR_K ? 2 : 1][4], Mw = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < 3; ++x)
+    for (int x = 0; x < (FOR_K ? 2 : 1); ++x)
 #pragma unroll
       for (int j = 0; j < 4; ++j) M[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     float lr = 0.f, vdv = 0.f;
+
     for (int c0 = 0; c0 < a.dv; c0 += kBlockCols) {
-      // own rows of the block: 8 columns a lane
       const int col = c0 + 8 * g;
       const bool here = real && col < a.dv;
-      const size_t at = ((size_t)orig * a.H + h) * a.dv + col;
       float xo[8], xm[8], xu[8];
-      if (!for_k) {
-        Raw<T, 8> ro = Frag<T, 8>::zero();
-        if (here) ro = *reinterpret_cast<const Raw<T, 8>*>(dout + at);
-        Frag<T, 8>::to_f32(ro, xo);
-      } else {
-        Raw<T, 8> rv = Frag<T, 8>::zero();
-        f32x8 rl = {}, rr = {};
-        if (here) {
-          rv = *reinterpret_cast<const Raw<T, 8>*>(v + at);
-          rl = *reinterpret_cast<const f32x8*>(lam + (sh * kChunk + own) * a.dv + col);
-          rr = *reinterpret_cast<const f32x8*>(resid + (sh * kChunk + own) * a.dv + col);
-        }
+      Frag<T, 8>::to_f32(ro, xo);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        xo[e] = here ? xo[e] : 0.f;
+        xu[e] = here ? be * rr[e] : 0.f;
+      }
+      if constexpr (FOR_K) {
         float xv[8], xd[8];
         Frag<T, 8>::to_f32(rv, xv);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          lr += rl[e] * rr[e];
-          xm[e] = be * rl[e];
-          xu[e] = be * rr[e];
+          xm[e] = here ? be * rl[e] : 0.f;
+          lr += here ? rl[e] * rr[e] : 0.f;
           xd[e] = vs * xm[e];
-          vdv += xv[e] * xd[e];
+          vdv += here ? xv[e] * xd[e] : 0.f;
         }
-        if (here) *reinterpret_cast<Raw<T, 8>*>(dv + at) = Frag<T, 8>::from_f32(xd);
+        if (here) *reinterpret_cast<Raw<T, 8>*>(dv + row0 + col) = Frag<T, 8>::from_f32(xd);
       }
-      // S0 and dS1 of the block's two column groups, as the walks left them
-      constexpr int kLoads = 2 * 2 * ST * 64 / 512;
-      floatx4 z[kLoads];
-#pragma unroll
-      for (int n = 0; n < kLoads; ++n) {
-        const int x = tid + 512 * n, which = x / (2 * ST * 64), y = x % (2 * ST * 64), cgl = y / (ST * 64);
-        z[n] = floatx4{0.f, 0.f, 0.f, 0.f};
-        if (c0 + 16 * cgl < a.dv)
-          z[n] = *reinterpret_cast<const floatx4*>((which ? dstates : states) +
-                                                   (sh * groups + c0 / 16) * (size_t)(ST * 256) + (size_t)y * 4);
+      const Scale so = scale_of(wave_max_bits(max8(xo))), su = scale_of(wave_max_bits(max8(xu)));
+      Scale sm = {1.f, 1.f};
+      const Op<NT> oo = op_of<NT>(xo, so.up);
+      const Op<NC> ou = op_of<NC>(xu, su.up);
+      Op<NC> om;
+      if constexpr (FOR_K) {
+        sm = scale_of(wave_max_bits(max8(xm)));
+        om = op_of<NC>(xm, sm.up);
       }
       __syncthreads();   // the last block's reads are done
-      Op<NT> oo;
-      Op<NC> om, ou;
-      Scale so, sm, su;
-      if (!for_k) {
-        so = scale_of(wave_max_bits(max8(xo)));
-        oo = op_of<NT>(xo, so.up);
+#pragma unroll
+      for (int t = 0; t < NC; ++t) *reinterpret_cast<half8_t*>(&s_u[wave][t][lane * 8]) = ou.t[t];
+      if constexpr (FOR_K) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) *reinterpret_cast<half8_t*>(&s_do[wave][t][lane * 8]) = oo.t[t];
-        if (lane == 0) s_scale[0][wave] = so.down;
-      } else {
-        sm = scale_of(wave_max_bits(max8(xm)));
-        su = scale_of(wave_max_bits(max8(xu)));
-        om = op_of<NC>(xm, sm.up);
-        ou = op_of<NC>(xu, su.up);
 #pragma unroll
-        for (int t = 0; t < NC; ++t) {
-          *reinterpret_cast<half8_t*>(&s_mu[wave][t][lane * 8]) = om.t[t];
-          *reinterpret_cast<half8_t*>(&s_u[wave][t][lane * 8]) = ou.t[t];
-        }
-        if (lane == 0) {
-          s_scale[1][wave] = sm.down;
-          s_scale[2][wave] = su.down;
-        }
+        for (int t = 0; t < NC; ++t) *reinterpret_cast<half8_t*>(&s_mu[wave][t][lane * 8]) = om.t[t];
+      }
+      if (lane == 0) {
+        s_scale[0][wave] = so.down;
+        s_scale[1][wave] = sm.down;
+        s_scale[2][wave] = su.down;
       }
 #pragma unroll
       for (int n = 0; n < kLoads; ++n) {
-        const int x = tid + 512 * n, which = x / (2 * ST * 64), y = x % (2 * ST * 64);
-        const float up = which ? sd.up : ss.up;
+        const int which = n >= kLoads / kStates ? 1 : 0, y = tid + 256 * (n - which * (kLoads / kStates));
+        const float up = c0 + 16 * (y / (ST * 64)) < a.dv ? (which ? sd.up : ss.up) : 0.f;
         half4_t p, l;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float u = z[n][r] * up;
+          const float u = up != 0.f ? z[n][r] * up : 0.f;
           p[r] = (_Float16)u;
           l[r] = (_Float16)(u - (float)p[r]);
         }
         *reinterpret_cast<half4_t*>(&s_state[which][0][y * 4]) = p;
         if constexpr (NC == 2) *reinterpret_cast<half4_t*>(&s_state[which][NC - 1][y * 4]) = l;
       }
+      if (c0 + kBlockCols < a.dv) ask(c0 + kBlockCols);
       __syncthreads();
       // rows of the block's states as operand rows: tile t's 16 state rows, contraction over 32 columns
       const auto state_rows = [&](int which, int t) __attribute__((always_inline)) {
@@ -501,9 +511,9 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
             const int c = 8 * g + 4 * hh;   // the columns' place in the block
-            const _Float16* at2 = &s_state[which][n][(((c >> 4) * ST + t) * 64 + (i & 3) * 16 + (c & 15) + (i >> 2)) * 4];
+            const _Float16* at = &s_state[which][n][(((c >> 4) * ST + t) * 64 + (i & 3) * 16 + (c & 15) + (i >> 2)) * 4];
             const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(at2)));
+                (__attribute__((address_space(3))) short4v*)(const_cast<_Float16*>(at)));
 #pragma unroll
             for (int r = 0; r < 4; ++r) x.t[n][4 * hh + r] = __builtin_bit_cast(_Float16, (short)y[r]);
           }
@@ -515,45 +525,38 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
           x.t[n] = *reinterpret_cast<const half8_t*>(&rows[j][n][lane * 8]);
       };
       const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-      if (!for_k) {
-        const float fq = a.scale * since * (ss.down * so.down);
+      const float fq = a.scale * since * (ss.down * so.down);
+      const float fk0 = -vs * since * (ss.down * sm.down), fk1 = vs * until * (sd.down * su.down);
 #pragma unroll
-        for (int t = 0; t < ST; ++t) {
-          if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+      for (int t = 0; t < ST; ++t) {
+        if (t % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // four tiles' operands in registers
+        if constexpr (FOR_K) {
+          D[t] += fk0 * mma_op(state_rows(0, t), om, zero);
+          D[t] += fk1 * mma_op(state_rows(kStates - 1, t), ou, zero);
+        } else {
           D[t] += fq * mma_op(state_rows(0, t), oo, zero);
         }
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j <= wave) {
-            Op<NC> u;
-            rows_of(s_u, u, j);
-            M[0][j] += (s_scale[2][j] * so.down) * mma_op(u, oo, zero);
-          }
-      } else {
-        const float fk0 = -vs * since * (ss.down * sm.down), fk1 = vs * until * (sd.down * su.down);
-#pragma unroll
-        for (int t = 0; t < ST; ++t) {
-          if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);   // two tiles' operands in registers
-          D[t] += fk0 * mma_op(state_rows(0, t), om, zero);
-          D[t] += fk1 * mma_op(state_rows(1, t), ou, zero);
+      for (int j = 0; j < 4; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (j <= wave) {
+          Op<NC> u;
+          rows_of(s_u, u, j);
+          if constexpr (FOR_K) M[0][j] += (s_scale[2][j] * sm.down) * mma_op(u, om, zero);
+          else M[0][j] += (s_scale[2][j] * so.down) * mma_op(u, oo, zero);
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          __builtin_amdgcn_sched_barrier(0);
-          if (j <= wave) {
-            Op<NC> u;
-            rows_of(s_u, u, j);
-            M[0][j] += (s_scale[2][j] * sm.down) * mma_op(u, om, zero);
-          }
+        if constexpr (FOR_K)
           if (j >= wave) {
             Op<NT> o;
             Op<NC> m;
             rows_of(s_do, o, j);
             rows_of(s_mu, m, j);
-            M[1][j] += (s_scale[0][j] * su.down) * mma_op(o, ou, zero);
-            M[2][j] += (s_scale[1][j] * su.down) * mma_op(m, ou, zero);
+            M[FOR_K][j] += (s_scale[0][j] * su.down) * mma_op(o, ou, zero);
+            const floatx4 x = (s_scale[1][j] * su.down) * mma_op(m, ou, zero);
+            if (j == wave) Mw += x;
+            else M[0][j] += x;
           }
-        }
       }
     }
     // the decays between own row and the others, then the products over the chunk's rows: M[0] becomes
@@ -562,17 +565,20 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       __builtin_amdgcn_sched_barrier(0);
+      const floatx4 os = *reinterpret_cast<const floatx4*>(&s_scal[kOScale + 16 * j + 4 * g]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int o = 16 * j + 4 * g + r;   // the other row
-        const float diff = (float)(go - s_gam[o]);
         // decay from the other row to the own one if it is before, else from the own to the other
+        const float diff = (float)(go - s_gam[o]);
         const float d = __builtin_amdgcn_exp2f(o <= own ? diff : -diff);
-        if (!for_k) {
-          M[0][j][r] = o <= own ? a.scale * d * M[0][j][r] : 0.f;
+        if constexpr (!FOR_K) {
+          const float x = a.scale * d * M[0][j][r];
+          M[0][j][r] = o <= own ? x : 0.f;
         } else {
-          M[0][j][r] = o < own ? -d * M[0][j][r] : o > own ? -d * M[2][j][r] : 0.f;
-          M[1][j][r] = o >= own ? d * M[1][j][r] * s_scal[kOScale + o] : 0.f;
+          const float x = -d * (j == wave && o > own ? Mw[r] : M[0][j][r]), y = d * M[FOR_K][j][r] * os[r];
+          M[0][j][r] = o == own ? 0.f : x;
+          M[FOR_K][j][r] = o >= own ? y : 0.f;
         }
       }
     }
@@ -591,7 +597,7 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
     const auto add = [&](const _Float16* img, const Op<NC> (&p)[2], float f) __attribute__((always_inline)) {
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
-        if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        if (t % 4 == 0) __builtin_amdgcn_sched_barrier(0);
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
@@ -605,24 +611,25 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
     };
     Op<NC> P[2];
     const float down0 = ops_of(M[0], P);
-    add(ki, P, for_k ? vs * down0 : down0);
-    if (for_k) {
-      const float down1 = ops_of(M[1], P);
+    add(ki, P, FOR_K ? vs * down0 : down0);
+    if constexpr (FOR_K) {
+      const float down1 = ops_of(M[FOR_K], P);
       add(qi, P, vs * down1);
     }
+    if constexpr (!FOR_K) continue;
     // dbeta = lam . r and the terms of dg: sums over the lane groups
     lr += __shfl_xor(lr, 16);
     lr += __shfl_xor(lr, 32);
     vdv += __shfl_xor(vdv, 16);
     vdv += __shfl_xor(vdv, 32);
-    if (for_k && g == 0) {
+    if (g == 0) {
       if (real) dbeta[(size_t)orig * a.H + h] = lr / vs / vs;
       float od = 0.f;
       for (int c = 0; c < groups; ++c) od += real ? odo[(sh * groups + c) * kChunk + own] : 0.f;
       s_dot[own] = real ? od - vdv : 0.f;
     }
     __syncthreads();
-    if (wave8 == 0) {
+    if (wave == 0) {
       float x = s_dot[lane];
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {   // sums to the end
@@ -653,7 +660,7 @@ __global__ __launch_bounds__(512, 2) void k_delta_grad(Args a, const T* __restri
       float x[8];
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[r] = D[2 * t][r], x[4 + r] = D[2 * t + 1][r];
-      T* to = (for_k ? dk : dq) + ((size_t)orig * a.Hk + hk) * a.dk + c;
+      T* to = (FOR_K ? dk : dq) + ((size_t)orig * a.Hk + hk) * a.dk + c;
       *reinterpret_cast<Raw<T, 8>*>(to) = Frag<T, 8>::from_f32(x);
     }
 }
@@ -696,11 +703,16 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
     }
     back(std::false_type{});
   });
-  if (a.n > 0)
-    k_delta_grad<T, DK><<<dim3(a.slots, a.Hk), 512, 0, stream>>>(
+  const auto grad = [&](auto for_k) {
+    k_delta_grad<T, DK, decltype(for_k)::value><<<dim3(a.slots, a.Hk), 256, 0, stream>>>(
         a, v, dout, b.g, images, records, at(sp.states), at(sp.dstates), at(sp.smax), at(sp.dmax), at(sp.resid),
         at(sp.lam), at(sp.odo), at(sp.start), b.state_in != nullptr, b.dstate_out != nullptr, static_cast<T*>(b.dq),
         static_cast<T*>(b.dk), static_cast<T*>(b.dv), b.dg, b.dbeta);
+  };
+  if (a.n > 0) {
+    grad(std::false_type{});
+    grad(std::true_type{});
+  }
   return hipGetLastError();
 }
 

@@ -2,7 +2,6 @@
 // chunks.  Included by the forward and by the backward, which makes the states again.
 #pragma once
 
-#include <cstdlib>
 #include "sla_delta.h"
 
 namespace sla {
@@ -452,9 +451,10 @@ __host__ __device__ inline size_t part_slots(const Args& a) {
   return a.part == 0 ? (size_t)a.W : (size_t)(a.n / (a.part * kChunk)) + a.W;
 }
 // Parts of 8 to 32 chunks where that gives the chip some 512 workgroups of 64 columns; none where the
-// windows do by themselves, or where they are short (256 rows on average).
+// windows do by themselves, or where they are short (256 rows on average).  Forward, no parts and parts of
+// 8, 16 and 32 chunks: 7 bf16 windows with 12,289 rows in all, 8 heads of 128: 346 us and 165, 192, 235;
+// 1 fp32 window of 8,191 rows, 4 heads of 64: 459 us and 88, 124, 208.
 inline int part_chunks(int64_t n, int32_t W, int32_t H, int32_t dv) {
-  if (const char* e = getenv("SLA_PART")) return atoi(e);
   const int64_t blocks = (int64_t)H * ((dv + 63) / 64), most = (n * blocks + 512 * kChunk - 1) / (512 * kChunk);
   const int64_t part = most < 8 ? 8 : most;
   if (part > 32 || n < 256 * (int64_t)W || n < 2 * part * kChunk) return 0;
@@ -964,15 +964,15 @@ __global__ __launch_bounds__(256) void k_delta_join(Args a, float* ends, const _
 }
 
 // Waves of a walk's workgroup.  Eight share a chunk's staging among 128 columns, four leave a SIMD to a
-// wave.  33 sequences x 16 heads of 128 (bf16): 1,087 us with eight, 1,225 with four; 7 sequences x 8 heads:
-// 599 and 442 (two: 468).  So eight where that still fills the 256 CUs.  fp32 rows have room for four.
+// wave: eight where workgroups of four would be more than the 256 CUs.  Windows of 1,024 bf16 rows, heads
+// of 128, four and eight: 64 window heads 81 and 98 us, 128: 105 and 119, 160: 166 and 132, 384: 312 and
+// 274 (gradients 378 and 432, 585 and 646, 844 and 742, 1,702 and 1,622).  fp32 rows have room for four.
 template <typename T>
 inline int walk_waves(const Args& a) {
   const int groups = a.dv / 16;
   if (groups <= 2) return 2;
   if (groups <= 4 || sizeof(T) == 4) return 4;
-  if (const char* e = getenv("SLA_WAVES")) return atoi(e);
-  return (int64_t)a.W * a.H * ((groups + 7) / 8) >= 256 ? 8 : 4;
+  return (int64_t)part_slots(a) * a.H * ((groups + 7) / 8) > 128 ? 8 : 4;
 }
 // f(integral_constant<waves>, grid)
 template <typename T, class F>
