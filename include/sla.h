@@ -461,7 +461,8 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
  * The rule is stable where beta_t |k_t|^2 <= 2 (keys are usually normalised to 1); where it is not,
  * states grow exponentially and results may not be finite.  Sums, states and decays are fp32, decay
  * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
- * held exactly down to 2^-17 of its row's largest value).  A value that is not finite reaches only its
+ * held exactly down to 2^-17 of its row's largest value), but for the two products that are summed
+ * to a bf16 o, whose computed operands hold 11.  o must not be an input.  A value that is not finite reaches only its
  * own window (v's, only its own head and column).  Deterministic.
  */
 size_t sla_delta_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t heads_qk,
@@ -482,8 +483,8 @@ sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_wi
  * The gradient of a log decay whose exp underflows is zero.  States are made again from the inputs.
  * Other arguments, limits and errors as sla_forward_delta; the outputs must not be inputs.
  * `workspace` (256-byte aligned) has at least sla_delta_backward_workspace_bytes(...) bytes:
- * the states and their gradients at every 64th row are most of it.  16-bit rows: the products that end
- * in dq and dk alone have operands of 11 bits, all others 22.  Deterministic.
+ * the states and their gradients at every 64th row are most of it.  bf16 rows: the products that end
+ * in dq and dk alone have computed operands of 11 bits, all others 22.  Deterministic.
  */
 size_t sla_delta_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                           int32_t heads_qk, int32_t heads, int32_t dim_k, int32_t dim_v);
@@ -526,7 +527,7 @@ sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t num_slots, 
  *   mean, rstd    fp32 [num_windows, groups], outputs (the backward reads them).
  *   workspace     device, 256-byte aligned, sla_group_norm_workspace_bytes() bytes (num_windows = 0
  *             there: no windows; 0 for sizes that are not supported), else SLA_E_WORKSPACE.
- * Statistics are fp32, variances summed around means.  Deterministic.  The activation of a value is
+ * Statistics are fp32, variances summed around means.  Deterministic.  y must not be x.  The activation of a value is
  * fp32, y is rounded once.
  */
 typedef enum { SLA_ACT_NONE = 0, SLA_ACT_RELU = 1, SLA_ACT_SILU = 2 } sla_activation_t;
@@ -544,7 +545,7 @@ sla_status_t sla_forward_group_norm(const int32_t* offsets, int64_t n, int32_t n
  * Backward of sla_forward_group_norm (the chain rule), from x, the forward's mean and rstd and
  * dy = dL/dy: dx in `dtype` (rows in no window are left as they were), dweight and dbias (fp32
  * [channels], each may be NULL), summed over all rows in windows in a fixed order.  relu's slope at 0
- * is 0.  Limits and errors as the forward.
+ * is 0.  Limits and errors as the forward; the outputs must not be inputs.
  */
 size_t sla_group_norm_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                                int32_t channels, int32_t groups);

@@ -500,8 +500,8 @@ sla_status_t check_delta_sizes(int64_t n, int32_t W, int dtype, int32_t heads_qk
   if (dtype < 0 || dtype > 2) return SLA_E_ARG;
   if (dim_k < 16 || dim_k > 128 || dim_k % 16 || dim_v < 16 || dim_v > 256 || dim_v % 16) return SLA_E_UNSUPPORTED;
   if (heads > 65535) return SLA_E_UNSUPPORTED;
-  // HIP bounds a grid at 2^32 - 1 threads in x
-  if (n / 64 + (int64_t)W > UINT32_MAX / 256 || n > UINT32_MAX / 256) return SLA_E_UNSUPPORTED;
+  // HIP bounds a grid at 2^32 - 1 threads in x (a walk's workgroup has up to 512)
+  if (n / 64 + (int64_t)W > UINT32_MAX / 512 || n > UINT32_MAX / 256) return SLA_E_UNSUPPORTED;
   return SLA_OK;
 }
 
@@ -596,6 +596,7 @@ sla_status_t check_norm_sizes(int64_t n, int32_t num_windows, int dtype, int32_t
   if (n < 0 || n >= INT32_MAX || num_windows < 0 || channels < 1 || groups < 1 || channels % groups) return SLA_E_ARG;
   if (dtype < 0 || dtype > 2) return SLA_E_ARG;
   if (channels > 4096 || channels / groups % 4) return SLA_E_UNSUPPORTED;
+  if (n > INT32_MAX - (1 << 24)) return SLA_E_UNSUPPORTED;   // a launch's stride past the last row stays below 2^31
   // HIP bounds a grid at 2^32 - 1 threads in x (the joining launch has 1,024 a window)
   if (num_windows > (int32_t)(UINT32_MAX / 1024) - 4096) return SLA_E_UNSUPPORTED;
   return SLA_OK;

@@ -120,6 +120,12 @@ __device__ __forceinline__ int row_at(const Args& a, int p) {
   return r < 0 ? 0 : r >= a.n ? a.n - 1 : r;
 }
 
+// A row out of a chunk's record.  Where offsets are not as they should be no launch may have written that
+// record, so a row is bounded here again.
+__device__ __forceinline__ int kept_row(const Args& a, float x) {
+  return (int)min(__float_as_uint(x), (uint32_t)a.n - 1u);
+}
+
 // ------------------------------------------------------------------ operands
 struct Pair {
   half8_t hi, lo;

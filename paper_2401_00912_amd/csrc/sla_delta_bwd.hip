@@ -96,12 +96,21 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 
   floatx4 S[ST];
   bool carried = true;
-  if (part.hi == part.chunks || ENDS) {
+  // A parted window's last gradient is read once, by the walk of the ends, which keeps it where the first
+  // part's would be: dstate_in, which the first part's workgroup writes, may be dstate.
+  const bool kept = part.hi == part.chunks && part.lo > 0 && dstate != nullptr;
+  const uint32_t from_slot = kept ? part.slot - (uint32_t)(part.lo / a.part) : part.slot + 1;
+  if (ENDS || (part.hi == part.chunks && !kept)) {
     const float* from = part.hi == part.chunks ? dstate : nullptr;
     load_state(S, a, from, w, h, col, live, g);
     carried = from != nullptr;
+    if (ENDS && kept && live) {
+      float* to = ends + (((size_t)from_slot * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t];
+    }
   } else if (live) {
-    const float* from = ends + (((size_t)(part.slot + 1) * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+    const float* from = ends + (((size_t)from_slot * a.H + h) * groups + cg) * ST * 256 + lane * 4;
 #pragma unroll
     for (int t = 0; t < ST; ++t) S[t] = *reinterpret_cast<const floatx4*>(from + t * 256);
   }
@@ -131,7 +140,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     if constexpr (TWICE)
       if (c > first) {
         Places<T> to;
-        to.take(scal + kPrev, lane);
+        to.take(a, scal + kPrev, lane);
         begin(other, c - 1, to);
       }
     jobs(integral_constant<int, 0>{}, integral_constant<int, 2>{});
@@ -261,7 +270,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     }
   } else {
     for (int c = part.hi - 1; c >= first; --c) {
-      if (c + 1 < part.hi) at.take(reinterpret_cast<const float*>(s_a.rec) + kPrev, lane);
+      if (c + 1 < part.hi) at.take(a, reinterpret_cast<const float*>(s_a.rec) + kPrev, lane);
       barrier();
       begin(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);

@@ -367,9 +367,9 @@ struct Places {
 #pragma unroll
     for (int n = 0; n < kMoves<T>; ++n) row[n] = row_at(a, base + (position(n, lane) < rows ? position(n, lane) : 0));
   }
-  __device__ __forceinline__ void take(const float* rows, int lane) {
+  __device__ __forceinline__ void take(const Args& a, const float* rows, int lane) {
 #pragma unroll
-    for (int n = 0; n < kMoves<T>; ++n) row[n] = __float_as_int(rows[position(n, lane)]);
+    for (int n = 0; n < kMoves<T>; ++n) row[n] = kept_row(a, rows[position(n, lane)]);
   }
 };
 
@@ -625,18 +625,27 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   floatx4 S[ST];
   float unit = 1.f;
   bool carried = true;   // no products with a state that is zero
+  // A parted window's first state is read once, by the walk of the ends, which keeps it where the last part's
+  // end would be: state_out, which the last part's workgroup writes, may be state_in.
+  const bool kept = part.lo == 0 && part.hi < part.chunks && state_in != nullptr;
+  const uint32_t from_slot = kept ? part.slot + (uint32_t)((part.chunks - 1) / a.part) : part.slot - 1;
   if (map) {
 #pragma unroll
     for (int t = 0; t < ST; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         S[t][r] = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r == 16 * (cg - groups) + i ? 1.f : 0.f;
-  } else if (part.lo == 0 || ENDS) {
+  } else if (ENDS || (part.lo == 0 && !kept)) {
     const float* from = part.lo == 0 ? state_in : nullptr;
     load_state(S, a, from, w, h, col, live, g);
     carried = from != nullptr;
+    if (ENDS && kept && live) {
+      float* to = ends + (((size_t)from_slot * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(to + t * 256) = S[t];
+    }
   } else if (live) {
-    const float* from = ends + (((size_t)(part.slot - 1) * a.H + h) * groups + cg) * ST * 256 + lane * 4;
+    const float* from = ends + (((size_t)from_slot * a.H + h) * groups + cg) * ST * 256 + lane * 4;
 #pragma unroll
     for (int t = 0; t < ST; ++t) S[t] = *reinterpret_cast<const floatx4*>(from + t * 256);
   }
@@ -679,13 +688,13 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     if constexpr (TWICE)
       if (next) {
         Places<T> to;
-        to.take(scal + kNext, lane);
+        to.take(a, scal + kNext, lane);
         start(other, c + 1, to);
       }
     jobs(integral_constant<int, 0>{}, integral_constant<int, 2>{});
     int place[4];   // this lane's row of every tile
 #pragma unroll
-    for (int tau = 0; tau < 4; ++tau) place[tau] = __float_as_int(scal[kRow + 16 * tau + i]);
+    for (int tau = 0; tau < 4; ++tau) place[tau] = kept_row(a, scal[kRow + 16 * tau + i]);
     Raw<T, 4> dn[KEEP ? 4 : 1];
     if constexpr (KEEP) {
       float* to = out.states + ((sh * (a.dv / 16) + cg) * ST) * 256 + lane * 4;
@@ -853,7 +862,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     }
   } else {
     for (int c = part.lo; c < last_chunk; ++c) {
-      if (c > part.lo) at.take(reinterpret_cast<const float*>(s_a.rec + (kScalAt - SG::kRecAt)) + kNext, lane);
+      if (c > part.lo) at.take(a, reinterpret_cast<const float*>(s_a.rec + (kScalAt - SG::kRecAt)) + kNext, lane);
       barrier();
       start(s_a, c, at);
       fetch.template jobs<0, F::kJobs>(s_a, wave);
