@@ -117,7 +117,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
   using F = Fetch<SG, T, kScalAt>;
   F fetch;
   const auto begin = [&](SG& s, int c, const Places<T>& at) __attribute__((always_inline)) {
-    fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, kRecordBack, dout, at, wave, lane);
+    fetch.start(s, a, slot0 + c, hk, h, cg, live, images, records, kRecordBack, dout, at, wave, lane, rows_of(c));
   };
   Places<T> at;
   if (part.hi > first) {

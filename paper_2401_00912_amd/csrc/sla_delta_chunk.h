@@ -292,7 +292,8 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     }
     __syncthreads();
     invert(sm, wave, i, g);
-    put_tri(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
+    const bool here = 16 * wave < rows;   // pieces of tile rows past the last row are not written (nor moved)
+    if (here) put_tri(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
     if constexpr (REV) {
       __syncthreads();
 #pragma unroll
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
       for (int r = 0; r < 4; ++r)
         sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = d[j][r] == 0.f ? 0.f : d[j][r] * qk[j][r];
     __syncthreads();
-    put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
+    if (here) put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
     if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
     if (hv + 1 < group) sums(hv + 1);
     __syncthreads();
@@ -382,11 +383,13 @@ struct Fetch {
   static constexpr int kImgJobs = (kImg + NW - 1) / NW, kJobs = kImgJobs + (kRec + NW - 1) / NW;
   static_assert((S::kRecTo - FROM) * 2 % 1024 == 0 && FROM >= S::kRecAt, "whole pieces");
   const char *img, *rec;
+  int pieces;   // of a triangle: those with rows in them
 
-  // rows: the wave has columns of src to move
+  // rows: the wave has columns of src to move; height: the chunk's rows
   __device__ __forceinline__ void start(S& b, const Args& a, size_t slot, int hk, int h, int cg, bool rows,
                                         const _Float16* images, const _Float16* records, int record, const T* src,
-                                        const Places<T>& at, int wave, int lane) {
+                                        const Places<T>& at, int wave, int lane, int height) {
+    pieces = height > 32 ? 2 * ((height + 15) / 16) - 2 : (height + 15) / 16;
     const size_t sh = slot * a.H + h;
     img = reinterpret_cast<const char*>(images + (slot * a.Hk + hk) * S::kImages + S::kImgAt) + wave * 1024 + lane * 16;
     rec = reinterpret_cast<const char*>(records + sh * record + FROM) + wave * 1024 + lane * 16;
@@ -404,7 +407,8 @@ struct Fetch {
       if (j < kImgJobs) {
         if ((j + 1) * NW <= kImg || wave + j * NW < kImg) to_lds(b.img + (wave + j * NW) * 512, img + j * NW * 1024);
       } else {
-        const int p = j - kImgJobs;
+        const int p = j - kImgJobs, q = FROM / kFrag + wave + p * NW;
+        if (FROM < kScalAt && q < kScalAt / kFrag && q % kTri >= pieces) continue;
         if ((p + 1) * NW <= kRec || wave + p * NW < kRec)
           to_lds(b.rec + (FROM - S::kRecAt) + (wave + p * NW) * 512, rec + p * NW * 1024);
       }
@@ -651,7 +655,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   }
   F fetch;
   const auto start = [&](SG& s, int c, const Places<T>& at) __attribute__((always_inline)) {
-    fetch.start(s, a, slot0 + c, hk, h, cg, live && !map, images, records, record, v, at, wave, lane);
+    fetch.start(s, a, slot0 + c, hk, h, cg, live && !map, images, records, record, v, at, wave, lane, rows_of(c));
   };
   Places<T> at;
   if (part.lo < last_chunk) {
@@ -754,7 +758,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
           for (int r = 0; r < 4; ++r)
             out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = U[tau][r] * uunit;
         }
-        U[tau] *= row4(kBeta, tau);
+        U[tau] = 16 * tau < rows ? U[tau] * row4(kBeta, tau) : floatx4{0.f, 0.f, 0.f, 0.f};   // (what was not moved)
       }
     }
     jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});
