@@ -63,6 +63,8 @@ BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int
 
 // ------------------------------------------------------------------ the walk back
 // As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
+// Bound by the chain like it: 16,381 bf16 rows, 9 sequences, 8 heads of 128: 146 us behind 120 for the
+// parts' gradients; 1,521 fp16 windows: 93 us.
 // ENDS: only the state gradients at the parts' starts, from none at their ends (the last part: from dstate).
 template <typename T, int DK, int NW>
 using BackStage = Stage<T, DK, NW, 0, kScalAt, kRecordBack>;
@@ -293,8 +295,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 // and four lane groups over the columns, and makes the transposed tiles: a lane ends with 8
 // neighbouring columns of its row.  The value columns go by in blocks of 32, the next block's loads in
 // flight.  dq and dk are launches of their own (FOR_K; dv, dbeta and dg come with dk): together they
-// took twice the registers and waited for memory at one workgroup a CU (16,381 bf16 rows, 8 heads of
-// 128: 426 us).
+// took twice the registers and waited for memory at one workgroup a CU.  Bound by the waits of two (dk)
+// or three workgroups a CU: 16,381 bf16 rows, 8 heads of 128: 82 and 232 us (together: 426); 1,521 fp16
+// windows, 4 heads of 32: 59 and 165 us (together: 228).  Eight waves, four for dq and four for dk:
+// 345 and 366.
 //
 // Computed operands (states, mu, u, the products over columns) have two fp16 terms, and one, 2^-11
 // of a value, where dq and dk are bf16, whose own rounding is 8 times as coarse; dg and dbeta, which
@@ -331,7 +335,8 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {
 }
 
 template <typename T, int DK, bool FOR_K>
-__global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, const T* __restrict__ v, const T* __restrict__ dout,
+__global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, const T* __restrict__ v,
+                                                    const T* __restrict__ dout,
                                                     const float* __restrict__ gin,
                                                     const _Float16* __restrict__ images,
                                                     const _Float16* __restrict__ records,
