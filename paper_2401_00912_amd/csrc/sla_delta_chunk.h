@@ -9,6 +9,11 @@ namespace delta {
 
 constexpr int kLd = 68;   // floats a row of a 64 x 64 matrix in LDS: 16-byte rows, banks turned by 4
 
+// P needs its second terms where o is kept to more than bf16's 8 bits (one fp16 term is off by 2^-11): not
+// in a forward (the backward keeps sums of o dout in fp32).
+template <typename T, bool KEEP>
+constexpr bool kShortOut = std::is_same<T, bf16_t>::value && !KEEP;
+
 // ------------------------------------------------------------------ T and P
 // Per chunk and query/key head, 256 threads: k' and q' into LDS in operand order (and into the
 // workspace: the walk stages them from there as they are), k'k'^T and q'k'^T lower tiles one tile
@@ -21,7 +26,7 @@ constexpr int kLd = 68;   // floats a row of a 64 x 64 matrix in LDS: 16-byte ro
 // I + [beta_i D_ij k_i . k_j], whose rows and not columns carry beta.
 //
 // Chunks are independent here, so a batch is bound by memory: 65,536 bf16 rows, 16 heads of 128, in
-// 320 us, 1.5 GB, 4.8 TB/s (a copy reaches 5.2).  Windows of one chunk are bound by the steps between
+// 306 us, 1.4 GB, 4.7 TB/s (a copy reaches 5.2).  Windows of one chunk are bound by the steps between
 // the barriers, some 10 us a workgroup: 1,521 fp16 windows (59,837 rows, 4 heads of 32) in 74 us, 138
 // with REV.  The inverse is made here and not in the walk because there it would be part of the chain
 // from chunk to chunk.
@@ -89,7 +94,8 @@ __device__ __forceinline__ void invert(PrepShared& s, int wave, int i, int g) {
 }
 
 // The triangle's operands of tile row `tau` out of a matrix in LDS: rows as operand rows, columns
-// in the order of two stacked result tiles.
+// in the order of two stacked result tiles.  ONE: the first terms alone.
+template <bool ONE>
 __device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* lo, int tau, int lane, int i, int g) {
   for (int s = 0; s <= tau / 2; ++s) {
     const floatx4 x0 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 4 * g);
@@ -97,7 +103,7 @@ __device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* 
     const Pair p = split(x0, x1, kTriUp);
     const int at = tri_at(tau, s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(hi + at) = p.hi;
-    *reinterpret_cast<half8_t*>(lo + at) = p.lo;
+    if constexpr (!ONE) *reinterpret_cast<half8_t*>(lo + at) = p.lo;
   }
 }
 // The transposed matrix's operands of tile row `tau`: upper triangular, kept under the mirrored
@@ -299,7 +305,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     __syncthreads();
     invert(sm, wave, i, g);
     const bool here = 16 * wave < rows;   // pieces of tile rows past the last row are not written (nor moved)
-    if (here) put_tri(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
+    if (here) put_tri<false>(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
     if constexpr (REV) {
       __syncthreads();
 #pragma unroll
@@ -320,7 +326,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
       for (int r = 0; r < 4; ++r)
         sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = d[j][r] == 0.f ? 0.f : d[j][r] * qk[j][r];
     __syncthreads();
-    if (here) put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
+    if (here) put_tri<kShortOut<T, REV>>(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
     if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
     if (hv + 1 < group) sums(hv + 1);
     __syncthreads();
@@ -349,10 +355,6 @@ struct WalkOut {
   float* resid;        // r' of every chunk row [slot][H][64][dv], or null
   float* odo;          // sums over 16 columns of o dout [slot][H][dv / 16][64], or null
 };
-
-// P needs its second terms where o is kept to more than bf16's 8 bits (one fp16 term is off by 2^-11).
-template <typename T, bool KEEP>
-constexpr bool kShortOut = std::is_same<T, bf16_t>::value && !KEEP;
 
 // What a walk reads of a chunk: the images from kImgAt on and the record from kRecAt (or later) to kRecTo.
 template <typename T, int DK, int NW, int kImgAt_, int kRecAt_, int kRecTo_>
