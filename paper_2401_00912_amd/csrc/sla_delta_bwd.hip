@@ -85,9 +85,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Part part = part_of(a, blockIdx.x, lane);
+  const Place here = place_of(a, lane);
+  const Part part = here.part;
   if (part.none || (ENDS && part.lo == 0)) return;
-  const int w = part.w, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int w = part.w, h = here.h, group = a.H / a.Hk, hk = h / group;
   const int cg = blockIdx.z * NW + wave, groups = a.dv / 16;
   const bool live = cg < groups;
   const int col = 16 * cg + i;

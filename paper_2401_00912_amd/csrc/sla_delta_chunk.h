@@ -345,8 +345,8 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 // staged between two barriers.
 //
 // Bound by the chain: some 4.5 us a chunk of 128 x 128 states with eight waves a workgroup, whatever else
-// the chip does.  65,536 bf16 rows, 33 uneven sequences, 16 heads: 758 us, the longest sequence's chunks
-// one after the other (1.4 GB, 1.9 TB/s); 12,289 rows cut into parts: 48 us behind 90 for the parts'
+// the chip does.  65,536 bf16 rows, 33 uneven sequences, 16 heads: 588 us, the longest sequence's chunks
+// one after the other (1.4 GB, 2.4 TB/s); 12,289 rows cut into parts: 48 us behind 90 for the parts'
 // states; 1,521 fp16 windows of a chunk or two: 82 us, where a workgroup waits for its only chunk.
 struct WalkOut {
   float* state_out;    // final states or null
@@ -463,6 +463,27 @@ __device__ __forceinline__ Part part_of(const Args& a, uint32_t slot, int lane) 
   p.lo = p.none ? 0 : (int)lo;
   p.hi = min(p.lo + a.part, p.chunks);
   return p;
+}
+// A walk's window (or part) and value head: grid (part slots, heads, column groups).  Where whole windows are
+// walked in more workgroups than there are CUs, the longest windows' heads come first, so that none is left
+// alone at the end: a lane a window, up to 64.  65,536 bf16 rows, 33 uneven sequences, 16 heads of 128: 588 us
+// so, 758 in the order of the windows.
+struct Place {
+  Part part;
+  int h;
+};
+__device__ __forceinline__ Place place_of(const Args& a, int lane) {
+  if (a.part != 0 || a.W > 64 || (size_t)gridDim.x * gridDim.y * gridDim.z <= 256)
+    return {part_of(a, blockIdx.x, lane), (int)blockIdx.y};
+  const int rows = lane < a.W ? window(a, lane).rows : -1;
+  int before = 0;   // windows that come first: with more rows, or as many and a smaller number
+  for (int o = 0; o < a.W; ++o) {
+    const int other = __builtin_amdgcn_readlane(rows, o);
+    before += other > rows || (other == rows && o < lane) ? 1 : 0;
+  }
+  const int at = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  const uint64_t hit = __ballot(lane < a.W && before == at / a.H);
+  return {part_of(a, (uint32_t)(__ffsll((unsigned long long)hit) - 1), lane), at % a.H};
 }
 __host__ __device__ inline size_t part_slots(const Args& a) {
   return a.part == 0 ? (size_t)a.W : (size_t)(a.n / (a.part * kChunk)) + a.W;
@@ -614,9 +635,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
 
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Part part = part_of(a, blockIdx.x, lane);
+  const Place here = place_of(a, lane);
+  const Part part = here.part;
   if (part.none || (ENDS && part.hi >= part.chunks)) return;
-  const int w = part.w, h = blockIdx.y, group = a.H / a.Hk, hk = h / group;
+  const int w = part.w, h = here.h, group = a.H / a.Hk, hk = h / group;
   const int cg = blockIdx.z * NW + wave, groups = a.dv / 16;
   const bool map = ENDS && cg >= groups;   // columns of M
   if (ENDS && part.lo == 0 && (int)blockIdx.z * NW >= groups) return;   // a window's first part needs no M

@@ -12,7 +12,7 @@ import numpy as np
 import pytest
 
 from oracle import delta_ref
-from tests.test_gpu_delta import FP32_BAR, Case, close
+from tests.test_gpu_delta import FP32_BAR, Case, check_backward, check_forward, close
 
 pytestmark = pytest.mark.gpu
 
@@ -57,6 +57,17 @@ def test_long_states_in_place(sla):
                                               torch.cuda.current_stream().cuda_stream)
             assert rc == 0
             assert all(torch.equal(a, b) for a, b in zip(outs, g)) and torch.equal(ds, g[5])
+
+
+@pytest.mark.parametrize("windows", [2, 40, 63, 64, 65])
+def test_many_uneven_windows(sla, windows):
+    """More workgroups than CUs (the longest windows first, up to 64 of them), with windows of the same length
+    and without rows among them."""
+    rng = np.random.default_rng(windows)
+    lengths = rng.choice([0, 1, 17, 64, 65, 130, 200], size=windows).tolist()
+    h = 8 if windows > 2 else 130
+    check_forward(sla, Case(lengths, 2, h, 16, 16, "bf16", seed=windows, state=True, behind=3))
+    check_backward(sla, Case(lengths, 2, h, 16, 16, "f32", seed=windows, state=True, behind=3, grads=True))
 
 
 WRONG = ([0, 200, 100, 300, 250, 700], [-5, 300, 900, 10, 10, 2000], [700, 600, 500, 400, 0, 700],
