@@ -21,9 +21,9 @@ hipError_t forward_impl(const Args& a, int dtype, const void* q, const void* k, 
   float* ends = reinterpret_cast<float*>(ws + align_up(sp.total, 256));
   _Float16* maps = reinterpret_cast<_Float16*>(ends) + (a.part ? ends_halfs(a, DK) : 0);
   if (a.n > 0) launch_ends<T, DK>(a, static_cast<const T*>(v), state_in, images, records, kRecord, ends, maps, stream);
-  with_walk<T>(a, [&](auto nw, dim3 grid) {
+  with_walk<T, DK>(a, [&](auto nw, auto ahead, dim3 grid) {
     constexpr int NW = decltype(nw)::value;
-    k_delta_walk<T, DK, kOut, NW><<<grid, 64 * NW, 0, stream>>>(
+    k_delta_walk<T, DK, kOut, NW, decltype(ahead)::value><<<grid, 64 * NW, 0, stream>>>(
         a, static_cast<const T*>(v), state_in, images, records, kRecord, ends, maps, static_cast<T*>(o), nullptr,
         WalkOut{state_out, nullptr, nullptr, nullptr, nullptr});
   });

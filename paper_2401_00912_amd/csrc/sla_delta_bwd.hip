@@ -64,12 +64,12 @@ BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int
 // ------------------------------------------------------------------ the walk back
 // As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
 // Bound by the chain like it: 16,381 bf16 rows, 9 sequences, 8 heads of 128: 146 us behind 120 for the
-// parts' gradients; 1,521 fp16 windows: 93 us.
+// parts' gradients; 1,521 fp16 windows: 85 us.
 // ENDS: only the state gradients at the parts' starts, from none at their ends (the last part: from dstate).
 template <typename T, int DK, int NW>
 using BackStage = Stage<T, DK, NW, 0, kScalAt, kRecordBack>;
 
-template <typename T, int DK, int NW, bool ENDS>
+template <typename T, int DK, int NW, bool ENDS, bool AHEAD>
 __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restrict__ dout,
                                                         const float* __restrict__ dstate,
                                                         const _Float16* __restrict__ images,
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
                                                         float* __restrict__ start, float* __restrict__ dstate_in) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
   using SG = BackStage<T, DK, NW>;
-  constexpr bool TWICE = kTwice<SG>;
+  constexpr bool TWICE = AHEAD && kTwice<SG>;
   __shared__ SG s_a;
   __shared__ std::conditional_t<TWICE, SG, char> s_b;
 
@@ -701,14 +701,14 @@ hipError_t backward_impl(const Args& a, int dtype, const BackArgs& b, void* work
   _Float16* maps = reinterpret_cast<_Float16*>(ws + sp.maps);
   if (a.n > 0)
     launch_ends<T, DK>(a, v, b.state_in, images, records, kRecordBack, at(sp.ends), maps, stream);
-  with_walk<T>(a, [&](auto nw, dim3 grid) {
+  with_walk<T, DK>(a, [&](auto nw, auto ahead, dim3 grid) {
     constexpr int NW = decltype(nw)::value;
     if (a.n > 0)
-      k_delta_walk<T, DK, kKeep, NW><<<grid, 64 * NW, 0, stream>>>(
+      k_delta_walk<T, DK, kKeep, NW, decltype(ahead)::value><<<grid, 64 * NW, 0, stream>>>(
           a, v, b.state_in, images, records, kRecordBack, at(sp.ends), maps, nullptr, dout,
           WalkOut{nullptr, at(sp.states), at(sp.smax), at(sp.resid), at(sp.odo)});
     const auto back = [&](auto ends) {
-      k_delta_back<T, DK, NW, decltype(ends)::value><<<grid, 64 * NW, 0, stream>>>(
+      k_delta_back<T, DK, NW, decltype(ends)::value, decltype(ahead)::value><<<grid, 64 * NW, 0, stream>>>(
           a, dout, b.dstate_out, images, records, at(sp.back_ends), at(sp.states), at(sp.lam), at(sp.dstates),
           at(sp.dmax), at(sp.start), b.dstate_in);
     };

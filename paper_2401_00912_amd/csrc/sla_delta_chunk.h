@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 // Bound by the chain: some 4.5 us a chunk of 128 x 128 states with eight waves a workgroup, whatever else
 // the chip does.  65,536 bf16 rows, 33 uneven sequences, 16 heads: 588 us, the longest sequence's chunks
 // one after the other (1.4 GB, 2.4 TB/s); 12,289 rows cut into parts: 48 us behind 90 for the parts'
-// states; 1,521 fp16 windows of a chunk or two: 82 us, where a workgroup waits for its only chunk.
+// states; 1,521 fp16 windows of a chunk or two: 60 us, where a workgroup waits for its only chunk.
 struct WalkOut {
   float* state_out;    // final states or null
   float* states;       // the states before every chunk [slot][H][dv / 16], in register order, or null
@@ -618,7 +618,7 @@ template <typename T, int DK, int KIND, int NW>
 using WalkStage = std::conditional_t<KIND == kEnds, Stage<T, DK, NW, kTerms<T> * kChunk * DK, kTHi, kRecord>,
                                      Stage<T, DK, NW, 0, 0, kRecord>>;
 
-template <typename T, int DK, int KIND, int NW>
+template <typename T, int DK, int KIND, int NW, bool AHEAD>
 __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restrict__ v,
                                                         const float* __restrict__ state_in,
                                                         const _Float16* __restrict__ images,
@@ -628,7 +628,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
   constexpr bool KEEP = KIND == kKeep, ENDS = KIND == kEnds, SHORT = kShortOut<T, KEEP>;
   using SG = WalkStage<T, DK, KIND, NW>;
-  constexpr bool TWICE = kTwice<SG>;
+  constexpr bool TWICE = AHEAD && kTwice<SG>;
   using F = Fetch<SG, T, ENDS ? kTHi : SHORT ? kPHi : 0>;
   __shared__ SG s_a;
   __shared__ std::conditional_t<TWICE, SG, char> s_b;
@@ -1024,14 +1024,25 @@ inline int walk_waves(const Args& a) {
   if (groups <= 4 || sizeof(T) == 4) return 4;
   return (int64_t)part_slots(a) * a.H * ((groups + 7) / 8) > 128 ? 8 : 4;
 }
-// f(integral_constant<waves>, grid)
-template <typename T, class F>
+// Whether the walks stage a chunk ahead.  Not where three workgroups a CU and more are there to wait for
+// each other and the second buffer would keep some of them off it, which is at 32 state rows: 60,000 fp16
+// rows, 4 heads of 32, with and without, forward and gradients: windows of 40 rows 136 + 452 and 115 + 432
+// us, 128: 87 + 301 and 78 + 279, 256: 87 + 307 and 81 + 289; but 24,000 bf16 rows, 8 heads of 128: windows
+// of 40 238 + 1,190 and 240 + 1,194, 256: 163 + 859 and 188 + 878.
+inline bool walks_ahead(dim3 grid) { return (int64_t)grid.x * grid.y * grid.z < 768; }
+// f(integral_constant<waves>, bool_constant<ahead>, grid)
+template <typename T, int DK, class F>
 inline void with_walk(const Args& a, F f) {
   const int waves = walk_waves<T>(a);
   const dim3 grid((uint32_t)part_slots(a), a.H, (a.dv / 16 + waves - 1) / waves);
-  if (waves == 2) f(std::integral_constant<int, 2>{}, grid);
-  else if (waves == 4) f(std::integral_constant<int, 4>{}, grid);
-  else if constexpr (sizeof(T) == 2) f(std::integral_constant<int, 8>{}, grid);
+  const auto by_waves = [&](auto ahead) {
+    if (waves == 2) f(std::integral_constant<int, 2>{}, ahead, grid);
+    else if (waves == 4) f(std::integral_constant<int, 4>{}, ahead, grid);
+    else if constexpr (sizeof(T) == 2) f(std::integral_constant<int, 8>{}, ahead, grid);
+  };
+  if constexpr (DK == 32)
+    if (!walks_ahead(grid)) return by_waves(std::false_type{});
+  by_waves(std::true_type{});
 }
 // The states at the parts' starts, where windows are parted.
 template <typename T, int DK>
@@ -1039,7 +1050,7 @@ inline void launch_ends(const Args& a, const T* v, const float* state_in, const 
                         const _Float16* records, int record, float* ends, _Float16* maps, hipStream_t stream) {
   if (a.part == 0) return;
   const int groups = a.dv / 16 + DK / 16;
-  k_delta_walk<T, DK, kEnds, 4><<<dim3((uint32_t)part_slots(a), a.H, (groups + 3) / 4), 256, 0, stream>>>(
+  k_delta_walk<T, DK, kEnds, 4, true><<<dim3((uint32_t)part_slots(a), a.H, (groups + 3) / 4), 256, 0, stream>>>(
       a, v, state_in, images, records, record, ends, maps, nullptr, nullptr, WalkOut{});
   k_delta_join<DK, false><<<dim3(a.W, a.H, (a.dv / 16 + 3) / 4), 256, 0, stream>>>(a, ends, maps);
 }

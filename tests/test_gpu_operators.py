@@ -70,6 +70,13 @@ def test_many_uneven_windows(sla, windows):
     check_backward(sla, Case(lengths, 2, h, 16, 16, "f32", seed=windows, state=True, behind=3, grads=True))
 
 
+def test_many_windows_of_several_chunks(sla):
+    """32 state rows and many workgroups: walks of several chunks that stage none ahead."""
+    lengths = [200, 0, 129, 64, 65, 7] * 60
+    check_forward(sla, Case(lengths, 3, 3, 32, 32, "f16", seed=1, state=True, order=True, behind=3))
+    check_backward(sla, Case(lengths, 1, 3, 16, 80, "bf16", seed=2, state=True, order=True, behind=3, grads=True))
+
+
 WRONG = ([0, 200, 100, 300, 250, 700], [-5, 300, 900, 10, 10, 2000], [700, 600, 500, 400, 0, 700],
          [0, 2000, 0, 2000, 0, 2000])
 
