@@ -458,7 +458,7 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
  *   states   fp32 [num_windows, heads, dim_k, dim_v].  state_out may be state_in.
  *   workspace  device, 256-byte aligned, at least sla_delta_workspace_bytes(...) bytes (0 for
  *            sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
- * The rule is stable where beta_t |k_t|^2 <= 2 (keys are usually normalised to 1); where it is not,
+ * Entries of q and k are below 2^75 (fp32).  The rule is stable where beta_t |k_t|^2 <= 2 (keys are usually normalised to 1); where it is not,
  * states grow exponentially and results may not be finite.  Sums, states and decays are fp32, decay
  * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
  * held exactly down to 2^-17 of its row's largest value), but for the two products that are summed
@@ -480,7 +480,7 @@ sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_wi
  * given dout = dL/do and dstate_out = dL/d(state_out) (NULL: zero), writes dq, dk (summed over the
  * value heads that share them, in head order), dv in `dtype`, dg, dbeta (fp32 [n, heads]) and, if not
  * NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  Rows in no window are left as they were.
- * The gradient of a log decay whose exp underflows is zero.  States are made again from the inputs.
+ * The gradient of a log decay below -104, whose exp underflows, is zero.  States are made again from the inputs.
  * Other arguments, limits and errors as sla_forward_delta; the outputs must not be inputs.
  * `workspace` (256-byte aligned) has at least sla_delta_backward_workspace_bytes(...) bytes:
  * the states and their gradients at every 64th row are most of it.  bf16 rows: the products that end
@@ -502,7 +502,8 @@ sla_status_t sla_backward_delta(const int32_t* offsets, int64_t n, int32_t num_w
  * [num_slots, heads, dim_k, dim_v] (fp32, 16-byte aligned), row b of the batch belongs to the
  * sequence in slot slots[b] (int32 [n], device), whose state it updates in place, and o[b] receives
  * its output.  Rows with the same slot are successive rows of one sequence, in row order.  A slot
- * outside [0, num_slots) marks a padding row: it touches neither o nor a state.  Other arguments as
+ * outside [0, num_slots) marks a padding row: it touches neither o nor a state.  n up to 65,536, else
+ * SLA_E_UNSUPPORTED (many rows of one sequence belong into sla_forward_delta).  Other arguments as
  * sla_forward_delta; all arithmetic is fp32.
  */
 sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,

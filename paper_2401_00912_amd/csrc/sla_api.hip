@@ -579,6 +579,7 @@ SLA_EXPORT sla_status_t sla_step_delta(const int32_t* slots, int64_t n, int32_t 
                                        const float* beta, void* o, sla_stream_t stream) {
   const sla_status_t st = check_delta_sizes(n, num_slots, (int)dtype, heads_qk, heads, dim_k, dim_v);
   if (st != SLA_OK) return st;
+  if (n > 65536) return SLA_E_UNSUPPORTED;   // each row's workgroups look through the slots of all rows
   if (!finite(scale)) return SLA_E_ARG;
   if (n == 0) return SLA_OK;
   if (!slots || !state || !q || !k || !v || !g || !beta || !o) return SLA_E_ARG;

@@ -87,6 +87,10 @@ def test_delta_pointers(L):
     assert call(L.sla_step_delta, STEP, DELTA, dict(n=0, q=None, o=None)) == sla.SLA_OK
 
 
+def test_step_rows(L):
+    assert call(L.sla_step_delta, STEP, DELTA, dict(n=65537)) == sla.SLA_E_UNSUPPORTED
+
+
 NORM = dict(offsets=FAKE, n=100, W=3, dtype=2, C=64, G=4, eps=1e-5, act=2, x=FAKE, w=FAKE, b=FAKE, y=FAKE, dy=FAKE,
             mean=FAKE, rstd=FAKE, dx=FAKE, dw=FAKE, db=FAKE, ws=FAKE, nbytes=BIG, stream=None)
 NORM_FORWARD = ["offsets", "n", "W", "dtype", "C", "G", "eps", "act", "x", "w", "b", "y", "mean", "rstd", "ws", "nbytes",
