@@ -295,10 +295,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 // summed in registers (in head order: deterministic).  Wave w owns rows 16w .. 16w + 15, one a lane (i)
 // and four lane groups over the columns, and makes the transposed tiles: a lane ends with 8
 // neighbouring columns of its row.  The value columns go by in blocks of 32, the next block's loads in
-// flight.  dq and dk are launches of their own (FOR_K; dv, dbeta and dg come with dk): together they
+// flight (not at 32 state rows, where a third workgroup a CU is worth more than they are).  dq and dk are launches of their own (FOR_K; dv, dbeta and dg come with dk): together they
 // took twice the registers and waited for memory at one workgroup a CU.  Bound by the waits of two (dk)
-// or three workgroups a CU: 16,381 bf16 rows, 8 heads of 128: 82 and 232 us (together: 426); 1,521 fp16
-// windows, 4 heads of 32: 59 and 165 us (together: 228).  Eight waves, four for dq and four for dk:
+// to four workgroups a CU: 16,381 bf16 rows, 8 heads of 128: 74 and 170 us (together: 426); 1,521 fp16
+// windows, 4 heads of 32: 58 and 152 us (together: 228).  Eight waves, four for dq and four for dk:
 // 345 and 366.
 //
 // Computed operands (states, mu, u, the products over columns) have two fp16 terms, and one, 2^-11
@@ -336,7 +336,7 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {
 }
 
 template <typename T, int DK, bool FOR_K>
-__global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, const T* __restrict__ v,
+__global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, const T* __restrict__ v,
                                                     const T* __restrict__ dout,
                                                     const float* __restrict__ gin,
                                                     const _Float16* __restrict__ images,
@@ -458,6 +458,7 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
     float lr = 0.f, vdv = 0.f;
 
     for (int c0 = 0; c0 < a.dv; c0 += kBlockCols) {
+      if (DK == 32 && c0 > 0) ask(c0);
       const int col = c0 + 8 * g;
       const bool here = real && col < a.dv;
       float xo[8], xm[8], xu[8];
@@ -516,7 +517,7 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
         *reinterpret_cast<half4_t*>(&s_state[which][0][y * 4]) = p;
         if constexpr (NC == 2) *reinterpret_cast<half4_t*>(&s_state[which][NC - 1][y * 4]) = l;
       }
-      if (c0 + kBlockCols < a.dv) ask(c0 + kBlockCols);
+      if (DK != 32 && c0 + kBlockCols < a.dv) ask(c0 + kBlockCols);
       __syncthreads();
       // rows of the block's states as operand rows: tile t's 16 state rows, contraction over 32 columns
       const auto state_rows = [&](int which, int t) __attribute__((always_inline)) {
@@ -553,26 +554,24 @@ __global__ __launch_bounds__(256, DK == 128 ? 1 : 2) void k_delta_grad(Args a, c
         }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 4; ++j) {   // (tiles that the decays will clear are made too: fewer registers than branches)
         __builtin_amdgcn_sched_barrier(0);
-        if (j <= wave) {
+        if constexpr (FOR_K) {
+          const bool before = j <= wave;
+          Op<NC> x, own;
+          rows_of(before ? s_u : s_mu, x, j);
+          rows_of(before ? s_mu : s_u, own, wave);
+          M[0][j] += (s_scale[before ? 2 : 1][j] * (before ? sm.down : su.down)) * mma_op(x, own, zero);
+          Op<NT> o;
+          rows_of(s_do, o, j);
+          M[FOR_K][j] += (s_scale[0][j] * su.down) * mma_op(o, ou, zero);
+        } else {
           Op<NC> u;
           rows_of(s_u, u, j);
-          if constexpr (FOR_K) M[0][j] += (s_scale[2][j] * sm.down) * mma_op(u, om, zero);
-          else M[0][j] += (s_scale[2][j] * so.down) * mma_op(u, oo, zero);
+          M[0][j] += (s_scale[2][j] * so.down) * mma_op(u, oo, zero);
         }
-        if constexpr (FOR_K)
-          if (j >= wave) {
-            Op<NT> o;
-            Op<NC> m;
-            rows_of(s_do, o, j);
-            rows_of(s_mu, m, j);
-            M[FOR_K][j] += (s_scale[0][j] * su.down) * mma_op(o, ou, zero);
-            const floatx4 x = (s_scale[1][j] * su.down) * mma_op(m, ou, zero);
-            if (j == wave) Mw += x;
-            else M[0][j] += x;
-          }
       }
+      if constexpr (FOR_K) Mw += (sm.down * su.down) * mma_op(om, ou, zero);
     }
     // the decays between own row and the others, then the products over the chunk's rows: M[0] becomes
     // what k is multiplied with, for dk M[1] what q is
