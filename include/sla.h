@@ -461,9 +461,8 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
  * Entries of q and k are below 2^75 (fp32).  The rule is stable where beta_t |k_t|^2 <= 2 (keys are usually normalised to 1); where it is not,
  * states grow exponentially and results may not be finite.  Sums, states and decays are fp32, decay
  * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
- * held exactly down to 2^-17 of its row's largest value), but for the two products that are summed
- * to a bf16 o, whose computed operands hold 11.  o must not be an input.  A value that is not finite reaches only its
- * own window (v's, only its own head and column).  Deterministic.
+ * held exactly down to 2^-17 of its row's largest value).  o must not be an input.  A value that is
+ * not finite reaches only its own window (v's, only its own head and column).  Deterministic.
  */
 size_t sla_delta_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t heads_qk,
                                  int32_t heads, int32_t dim_k, int32_t dim_v);
@@ -483,8 +482,7 @@ sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_wi
  * The gradient of a log decay below -104, whose exp underflows, is zero.  States are made again from the inputs.
  * Other arguments, limits and errors as sla_forward_delta; the outputs must not be inputs.
  * `workspace` (256-byte aligned) has at least sla_delta_backward_workspace_bytes(...) bytes:
- * the states and their gradients at every 64th row are most of it.  bf16 rows: the products that end
- * in dq and dk alone have computed operands of 11 bits, all others 22.  Deterministic.
+ * the states and their gradients at every 64th row are most of it.  Deterministic.
  */
 size_t sla_delta_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                           int32_t heads_qk, int32_t heads, int32_t dim_k, int32_t dim_v);

@@ -41,7 +41,7 @@ enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow 
        kLast = 512 };
 // What a chunk has for each value head, in halfs: P's second and first terms, T's first and second,
 // the scalars, and for the backward the transposed inverse and the transposed P, two terms each.
-// The walk forward reads up to the scalars (bf16 outputs: from P's first terms), the walk back from there.
+// The walk forward reads up to the scalars, the walk back from there.
 constexpr int kTerm = kTriHalfs / 2;
 enum { kPLo = 0, kPHi = kTerm, kTHi = 2 * kTerm, kScalAt = 4 * kTerm, kBackT = kScalAt + 2 * kScal,
        kBackP = kBackT + 2 * kTerm };
@@ -167,12 +167,6 @@ __device__ __forceinline__ Pair split(const floatx4& x0, const floatx4& x1, floa
     p.lo[e] = (_Float16)__builtin_fmaf(a, s, -(float)h[0]);
     p.lo[e + 1] = (_Float16)__builtin_fmaf(b, s, -(float)h[1]);
   }
-  return p;
-}
-__device__ __forceinline__ half8_t narrow(const floatx4& x0, const floatx4& x1, float s) {
-  half8_t p;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) p[r] = (_Float16)(x0[r] * s), p[4 + r] = (_Float16)(x1[r] * s);
   return p;
 }
 

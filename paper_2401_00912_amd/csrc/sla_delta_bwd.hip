@@ -301,10 +301,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 // windows, 4 heads of 32: 58 and 152 us (together: 228).  Eight waves, four for dq and four for dk:
 // 345 and 366.
 //
-// Computed operands (states, mu, u, the products over columns) have two fp16 terms, and one, 2^-11
-// of a value, where dq and dk are bf16, whose own rounding is 8 times as coarse; dg and dbeta, which
-// are fp32, take nothing from these products.  With one term for fp16 rows too their dq and dk were
-// off by 3.7e-4 of their norm, where rounding alone is 2.1e-4.
+// Computed operands (states, mu, u, the products over columns) have two fp16 terms whatever the rows'
+// type: with one, 2^-11 of the largest value, small entries of dq and dk were off by many of their own
+// steps, bf16's too.
 constexpr int kBlockCols = 32;
 
 template <int NT>
@@ -349,7 +348,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
                                                     T* __restrict__ dq, T* __restrict__ dk, T* __restrict__ dv,
                                                     float* __restrict__ dg, float* __restrict__ dbeta) {
   constexpr int NT = kTerms<T>, IMG = kChunk * DK, ST = DK / 16;
-  constexpr int NC = std::is_same<T, bf16_t>::value ? 1 : 2;   // terms of computed operands
+  constexpr int NC = 2;   // terms of computed operands
   constexpr int kStateHalfs = ST * 256;   // one group of 16 columns, in register order
   constexpr int kStates = FOR_K ? 2 : 1;   // S0, dS1
   constexpr int kSkip = FOR_K ? 0 : NT * IMG;   // dq does not need q'
@@ -515,7 +514,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
           l[r] = (_Float16)(u - (float)p[r]);
         }
         *reinterpret_cast<half4_t*>(&s_state[which][0][y * 4]) = p;
-        if constexpr (NC == 2) *reinterpret_cast<half4_t*>(&s_state[which][NC - 1][y * 4]) = l;
+        *reinterpret_cast<half4_t*>(&s_state[which][1][y * 4]) = l;
       }
       if (DK != 32 && c0 + kBlockCols < a.dv) ask(c0 + kBlockCols);
       __syncthreads();

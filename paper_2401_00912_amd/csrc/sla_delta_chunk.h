@@ -9,11 +9,6 @@ namespace delta {
 
 constexpr int kLd = 68;   // floats a row of a 64 x 64 matrix in LDS: 16-byte rows, banks turned by 4
 
-// P needs its second terms where o is kept to more than bf16's 8 bits (one fp16 term is off by 2^-11): not
-// in a forward (the backward keeps sums of o dout in fp32).
-template <typename T, bool KEEP>
-constexpr bool kShortOut = std::is_same<T, bf16_t>::value && !KEEP;
-
 // ------------------------------------------------------------------ T and P
 // Per chunk and query/key head, 256 threads: k' and q' into LDS in operand order (and into the
 // workspace: the walk stages them from there as they are), k'k'^T and q'k'^T lower tiles one tile
@@ -94,8 +89,7 @@ __device__ __forceinline__ void invert(PrepShared& s, int wave, int i, int g) {
 }
 
 // The triangle's operands of tile row `tau` out of a matrix in LDS: rows as operand rows, columns
-// in the order of two stacked result tiles.  ONE: the first terms alone.
-template <bool ONE>
+// in the order of two stacked result tiles.
 __device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* lo, int tau, int lane, int i, int g) {
   for (int s = 0; s <= tau / 2; ++s) {
     const floatx4 x0 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 4 * g);
@@ -103,7 +97,7 @@ __device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* 
     const Pair p = split(x0, x1, kTriUp);
     const int at = tri_at(tau, s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(hi + at) = p.hi;
-    if constexpr (!ONE) *reinterpret_cast<half8_t*>(lo + at) = p.lo;
+    *reinterpret_cast<half8_t*>(lo + at) = p.lo;
   }
 }
 // The transposed matrix's operands of tile row `tau`: upper triangular, kept under the mirrored
@@ -305,7 +299,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     __syncthreads();
     invert(sm, wave, i, g);
     const bool here = 16 * wave < rows;   // pieces of tile rows past the last row are not written (nor moved)
-    if (here) put_tri<false>(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
+    if (here) put_tri(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
     if constexpr (REV) {
       __syncthreads();
 #pragma unroll
@@ -326,7 +320,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
       for (int r = 0; r < 4; ++r)
         sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = d[j][r] == 0.f ? 0.f : d[j][r] * qk[j][r];
     __syncthreads();
-    if (here) put_tri<kShortOut<T, REV>>(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
+    if (here) put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
     if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
     if (hv + 1 < group) sums(hv + 1);
     __syncthreads();
@@ -626,10 +620,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
                                                         float* ends, _Float16* __restrict__ maps,
                                                         T* __restrict__ o, const T* __restrict__ dout, WalkOut out) {
   constexpr int NT = kTerms<T>, KB = DK / 32, IMG = kChunk * DK, ST = DK / 16;
-  constexpr bool KEEP = KIND == kKeep, ENDS = KIND == kEnds, SHORT = kShortOut<T, KEEP>;
+  constexpr bool KEEP = KIND == kKeep, ENDS = KIND == kEnds;
   using SG = WalkStage<T, DK, KIND, NW>;
   constexpr bool TWICE = AHEAD && kTwice<SG>;
-  using F = Fetch<SG, T, ENDS ? kTHi : SHORT ? kPHi : 0>;
+  using F = Fetch<SG, T, ENDS ? kTHi : 0>;
   __shared__ SG s_a;
   __shared__ std::conditional_t<TWICE, SG, char> s_b;
 
@@ -770,7 +764,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
           for (int tau = 0; tau < 4; ++tau) {
             const half8_t qr = image_rows<DK>(qi, tau, kb, i, g);
             if constexpr (NT == 2) qs[tau] = mma(Sp[kb].hi, image_rows<DK>(qi + IMG, tau, kb, i, g), qs[tau]);
-            qs[tau] = SHORT ? mma(Sp[kb].hi, qr, qs[tau]) : mma1(Sp[kb], qr, qs[tau]);
+            qs[tau] = mma1(Sp[kb], qr, qs[tau]);
           }
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSince, tau) * qdown) * x[tau];
@@ -806,15 +800,13 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       for (int tau = 0; tau < 4; ++tau) y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        Pair up;
-        if constexpr (SHORT) up.hi = narrow(U[2 * s2], U[2 * s2 + 1], su.up);
-        else up = split(U[2 * s2], U[2 * s2 + 1], su.up);
+        const Pair up = split(U[2 * s2], U[2 * s2 + 1], su.up);
 #pragma unroll
         for (int tau = 2 * s2; tau < 4; ++tau) {
           const int p = tri_at(tau, s2) * kFrag + lane * 8;
-          const half8_t hi = *reinterpret_cast<const half8_t*>(rec(kPHi) + p);
-          if constexpr (SHORT) y[tau] = mma(up.hi, hi, y[tau]);
-          else y[tau] = mma2(up, Pair{hi, *reinterpret_cast<const half8_t*>(rec(kPLo) + p)}, y[tau]);
+          const Pair t = {*reinterpret_cast<const half8_t*>(rec(kPHi) + p),
+                          *reinterpret_cast<const half8_t*>(rec(kPLo) + p)};
+          y[tau] = mma2(up, t, y[tau]);
         }
       }
 #pragma unroll
