@@ -16,10 +16,16 @@
 // the sum of hi hi, hi lo and lo hi in fp32.  A 16-bit input needs no second term: its row is
 // scaled by a power of two that puts the row's largest value into [1, 2), and then fp16 holds
 // fp16 and bf16 values exactly down to 2^-17 of the row's largest (below that, to 2^-25 of it).
-// With k = 2^kap k' and q = 2^rho q' the rule reads the same for k', v' = 2^-kap v,
-// beta' = 2^(2 kap) beta, r' = 2^-kap r, u' = 2^kap u and o' = 2^-rho o: the scales cost one
-// factor a row, and wherever beta |k|^2 <= 2 (where the rule is stable) T's entries stay below
-// 2 sqrt(4 dk).
+// With k = 2^kap k' and q = 2^rho q' the rule reads the same for k', u' = 2^kap u, o' = 2^-rho o and
+// r' = s r with any s of a row's own:
+//     r' = T' (s v - t exp(gam) k' S0),   t = 2^kap s,   u' = (b / t) r',   b = 2^(2 kap) beta,
+//     T' = (I + [t_i D_ij (k'_i . k'_j) b_j / t_j]_{j < i})^-1,
+// so the scales cost one factor a row.  A column of r' has one power of two for its two terms, so no row
+// may be large there that writes little: s = min(2^-kap, c) with c the largest min(1, b) 2^-kap of the
+// chunk, which is what a row's v is worth to the state (and at least the smallest 2^-kap, where betas are
+// small).  With s = 2^-kap alone a key of 1e-9 among keys of 1 put its v' 2^30 above theirs, and their r'
+// were lost.  b / t is at most max(1, b), and wherever beta |k|^2 <= 2 (where the rule is stable) the
+// entries of T' stay below 4 dk and those of the transposed inverse (rows with b) below 2 sqrt(4 dk).
 #pragma once
 
 #include "sla_common.h"
@@ -31,14 +37,15 @@ constexpr int kChunk = 64;
 constexpr int kFrag = 512;            // halfs of one 16 x 32 operand: 64 lanes x 8
 constexpr int kTri = 6;               // 16 x 32 operands of a lower triangular 64 x 64 matrix
 constexpr int kTriHalfs = 2 * kTri * kFrag;
-// T and P are kept 64 times as large (T's entries stay below 45, P's below 512): an entry's error is
+// T and P are kept 64 times as large (T's and P's entries stay below 512): an entry's error is
 // then below 2^-31 of the diagonal's 1
 constexpr float kTriUp = 64.f;
-constexpr int kScal = 768;            // 4-byte values: 8 rows of 64, one value, padding to 3 KB
-// Rows of a chunk's scalars.  kRow, kNext, kPrev: the original rows (int32) of the chunk and of its
-// window's next and previous chunk, whose rows are asked for while this one is in work.
-enum { kSince = 0, kBeta = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow = 320, kNext = 384, kPrev = 448,
-       kLast = 512 };
+constexpr int kScal = 768;            // 4-byte values: 12 rows of 64, one of them with a single value
+// Rows of a chunk's scalars: exp(gam), b / t, exp(gam_last - gam), s, 2^rho scale; the original rows
+// (int32) of the chunk and of its window's next and previous chunk, which are asked for while this one is in
+// work; exp(gam_last); t exp(gam), b and 2^-kap.
+enum { kSince = 0, kWrite = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow = 320, kNext = 384, kPrev = 448,
+       kLast = 512, kSinceK = 576, kBeta = 640, kKScale = 704 };
 // What a chunk has for each value head, in halfs: P's second and first terms, T's first and second,
 // the scalars, and for the backward the transposed inverse and the transposed P, two terms each.
 // The walk forward reads up to the scalars, the walk back from there.
@@ -195,6 +202,7 @@ __device__ __forceinline__ uint32_t wave_max_bits(float m) {
 struct Scale {
   float up, down;
 };
+__device__ __forceinline__ float inverse_pow2(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 __device__ __forceinline__ Scale scale_of(uint32_t max_bits) {
   if (max_bits == 0) return {1.f, 1.f};
   const int e = (int)(max_bits >> 23);

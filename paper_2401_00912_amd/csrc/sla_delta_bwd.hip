@@ -6,7 +6,7 @@
 //     du  = P^T (scale do) + exp(gam_last - gam) k dS1,
 //     lam = (I + [beta_i D_ij k_i . k_j]_{j < i})^-T du,   mu = beta lam  (= dv),
 //     dS0 = exp(gam_last) dS1 + scale (exp(gam) q)^T do - (exp(gam) k)^T mu,
-//     dbeta_j = lam_j . r_j,
+//     dbeta_j = lam_j . r_j   (lam' . r' 2^kap / s),
 //     dq_i = scale (exp(gam_i) S0 do_i + sum_{j <= i} D_ij (do_i . u_j) k_j),
 //     dk_j = exp(gam_last - gam_j) dS1 u_j - exp(gam_j) S0 mu_j - sum_{i < j} D_ji (mu_j . u_i) k_i
 //            - sum_{i > j} D_ij (mu_i . u_j) k_i + scale sum_{i >= j} D_ij (do_i . u_j) q_i.
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
     const Scale ss = scale_of(sbits), sd = scale_of(dbits);
     __syncthreads();
     const float since = s_scal[kSince + own], until = s_scal[kUntil + own], be = s_scal[kBeta + own];
-    const float vs = s_scal[kVScale + own];
+    const float vs = s_scal[kKScale + own], write = s_scal[kWrite + own];
 
     // products over the value columns: M[.][j], transposed tiles with this wave's rows in the lanes.
     // dq: 0: do of own rows with u of tile j (j <= wave).  dk: 0: mu of own rows with u of tile j
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         xo[e] = here ? xo[e] : 0.f;
-        xu[e] = here ? be * rr[e] : 0.f;
+        xu[e] = here ? write * rr[e] : 0.f;
       }
       if constexpr (FOR_K) {
         float xv[8], xd[8];
@@ -636,7 +636,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
     vdv += __shfl_xor(vdv, 16);
     vdv += __shfl_xor(vdv, 32);
     if (g == 0) {
-      if (real) dbeta[(size_t)orig * a.H + h] = lr / vs / vs;
+      if (real) dbeta[(size_t)orig * a.H + h] = lr / vs / s_scal[kVScale + own];
       float od = 0.f;
       for (int c = 0; c < groups; ++c) od += real ? odo[(sh * groups + c) * kChunk + own] : 0.f;
       s_dot[own] = real ? od - vdv : 0.f;

@@ -126,7 +126,8 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
   constexpr size_t kImages = (size_t)2 * NT * IMG * 2;
   __shared__ __attribute__((aligned(16))) char s_mem[kImages > sizeof(PrepShared) ? kImages : sizeof(PrepShared)];
   __shared__ double s_gam[2][kChunk];
-  __shared__ float s_beta[2][kChunk], s_ks[kChunk], s_os[kChunk];
+  __shared__ __attribute__((aligned(16))) float s_t[2][kChunk];
+  __shared__ float s_write[2][kChunk], s_b[2][kChunk], s_ks[kChunk], s_os[kChunk];
   _Float16* s_img = reinterpret_cast<_Float16*>(s_mem);
   PrepShared& sm = *reinterpret_cast<PrepShared*>(s_mem);
 
@@ -218,11 +219,18 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
       if (lane >= d) gam += o;
     }
     s_gam[hv & 1][lane] = gam;
-    s_beta[hv & 1][lane] = b1;
+    // the scales of r' (sla_delta.h); a beta that is no number does not count
+    const float ks = s_ks[lane], b = b1 * ks * ks, worth = b == b ? fminf(1.f, fabsf(b)) * inverse_pow2(ks) : 0.f;
+    const float top = __uint_as_float(wave_max_bits(lane < rows ? ks : 0.f));
+    const float c = __uint_as_float((wave_max_bits(worth) + 0x7fffffu) & 0x7f800000u);   // the next power of two
+    const float s = fminf(inverse_pow2(ks), fmaxf(c, inverse_pow2(top)));
+    s_write[hv & 1][lane] = b1 * ks * inverse_pow2(s);
+    s_t[hv & 1][lane] = s * ks;
+    s_b[hv & 1][lane] = b;
     if (hv + 1 < group) ask(hv + 1);
   };
-  sums(0);
   __syncthreads();
+  sums(0);
 
   // lower tiles of k'k'^T and q'k'^T, tile row `wave`
   floatx4 kk[4], qk[4];
@@ -258,16 +266,19 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     const size_t sh = (size_t)slot * a.H + h;
     _Float16* out = records + sh * (REV ? kRecordBack : kRecord);
     const double* gam = s_gam[hv & 1];
-    const float* bet = s_beta[hv & 1];
+    const float *write = s_write[hv & 1], *t = s_t[hv & 1], *b = s_b[hv & 1];
     if (wave == 0) {
       const bool real = lane < rows;
       const double gl = gam[lane], last = gam[63];
-      const float ks = s_ks[lane];
+      const float kd = inverse_pow2(s_ks[lane]), since = real ? __builtin_amdgcn_exp2f((float)gl) : 0.f;
       float* sc = reinterpret_cast<float*>(out + kScalAt);
-      sc[kSince + lane] = real ? __builtin_amdgcn_exp2f((float)gl) : 0.f;
-      sc[kBeta + lane] = bet[lane] * ks * ks;
+      sc[kSince + lane] = since;
+      sc[kWrite + lane] = write[lane];
       sc[kUntil + lane] = real ? __builtin_amdgcn_exp2f((float)(last - gl)) : 0.f;
-      sc[kVScale + lane] = 1.f / ks;   // a power of two
+      sc[kVScale + lane] = t[lane] * kd;
+      sc[kSinceK + lane] = t[lane] * since;
+      sc[kBeta + lane] = b[lane];
+      sc[kKScale + lane] = kd;
       sc[kOScale + lane] = s_os[lane] * a.scale;
       sc[kRow + lane] = __int_as_float(place);
       sc[kNext + lane] = __int_as_float(place_next);
@@ -276,6 +287,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     }
     floatx4 d[4];   // decays between the rows, zero above the diagonal
     double gr[4];
+    const floatx4 tr = *reinterpret_cast<const floatx4*>(t + 16 * wave + 4 * g);
 #pragma unroll
     for (int r = 0; r < 4; ++r) gr[r] = gam[16 * wave + 4 * g + r];
 #pragma unroll
@@ -285,12 +297,12 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
       floatx4 n = d[j];
       if (j <= wave) {
         const double gc = gam[col];
-        const float bc = bet[col] * s_ks[col] * s_ks[col];
+        const float bc = write[col];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = 16 * wave + 4 * g + r;
           d[j][r] = row >= col ? __builtin_amdgcn_exp2f((float)(gr[r] - gc)) : 0.f;
-          n[r] = row > col ? d[j][r] * kk[j][r] * bc : 0.f;
+          n[r] = row > col ? d[j][r] * kk[j][r] * (tr[r] * bc) : 0.f;
         }
       }
 #pragma unroll
@@ -307,7 +319,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = 16 * wave + 4 * g + r, col = 16 * j + i;
-          sm.n[row * kLd + col] = row > col ? d[j][r] * kk[j][r] * (bet[row] * s_ks[row] * s_ks[row]) : 0.f;
+          sm.n[row * kLd + col] = row > col ? d[j][r] * kk[j][r] * b[row] : 0.f;
         }
       __syncthreads();
       invert(sm, wave, i, g);
@@ -738,7 +750,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       for (int tau = 0; tau < 4; ++tau)   // row 0 where there is none
         dn[tau] = *reinterpret_cast<const Raw<T, 4>*>(dout + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g);
     }
-    // y = 2^-kap v - exp(gam) k' S, and q' S for later
+    // y = s v - t exp(gam) k' S, and q' S for later
     uint32_t top = 0;   // of the state, in S's units
     float qdown = 0.f;
 #pragma unroll
@@ -767,10 +779,10 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
             qs[tau] = mma1(Sp[kb], qr, qs[tau]);
           }
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSince, tau) * qdown) * x[tau];
+      for (int tau = 0; tau < 4; ++tau) Y[tau] -= (row4(kSinceK, tau) * qdown) * x[tau];
     }
     jobs(integral_constant<int, 2>{}, integral_constant<int, 5>{});
-    // r = T y, u = beta' r; both times uunit
+    // r = T y, u = (b / t) r; both times uunit
     floatx4 U[4];
     float uunit;
     {
@@ -787,7 +799,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
           for (int r = 0; r < 4; ++r)
             out.resid[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = U[tau][r] * uunit;
         }
-        U[tau] = 16 * tau < rows ? U[tau] * row4(kBeta, tau) : floatx4{0.f, 0.f, 0.f, 0.f};   // (what was not moved)
+        U[tau] = 16 * tau < rows ? U[tau] * row4(kWrite, tau) : floatx4{0.f, 0.f, 0.f, 0.f};   // (what was not moved)
       }
     }
     jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});

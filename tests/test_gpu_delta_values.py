@@ -54,3 +54,82 @@ def test_bf16_results_are_rounded_once(sla, hk, h, dk, dv, lengths):
     close(o, c.forward_ref()[0], "bf16", "o")
     for name, got, ref in gradients(sla, c):
         close(got, ref, out_type(c, name), name)
+
+
+# ------------------------------------------------------------------ keys of many sizes
+def close_rows(got, ref, dtype, name, rows, bar=FP32_BAR):
+    """Rows of one kind held to the largest among them."""
+    close(got[rows.tolist()], ref[rows], dtype, name, bar)
+
+
+# windows of a chunk and some, and one that is cut into parts of 512 rows
+SMALL_KEYS = [("f32", 1e-6), ("f32", 1e-9), ("f32", 1e-12), ("f32", 1e-30), ("bf16", 1e-6), ("bf16", 1e-9),
+              ("bf16", 1e-12), ("bf16", 1e-30), ("f16", 1e-4), ("f16", 1e-6)]
+
+
+def small_keys(dtype, x, lengths, **kw):
+    """A few keys x times as long as the others, whose betas are as ever: they write x times as much."""
+    c = Case(lengths, 1, 2, 32, 32, dtype, seed=31, **kw)
+    few = np.zeros(c.n, bool)
+    few[[3, 40, 63, 66, 90, c.n - 2]] = True
+    k = c.k.float()
+    k[few] *= x
+    c.k = k.to(c.k.dtype)
+    return c, few
+
+
+@pytest.mark.parametrize("lengths", [[70, 64], [1100, 70]])
+@pytest.mark.parametrize("dtype,x", SMALL_KEYS)
+def test_forward_with_a_small_key(sla, dtype, x, lengths):
+    c, _ = small_keys(dtype, x, lengths, state=lengths[0] > 100)
+    o, st = c.forward(sla)
+    ro, rs = c.forward_ref()
+    close(o, ro, dtype, "o")
+    close(st, rs, "f32", "state")
+
+
+@pytest.mark.parametrize("lengths", [[70, 64], [1100, 70]])
+@pytest.mark.parametrize("dtype,x", SMALL_KEYS)
+def test_backward_with_a_small_key(sla, dtype, x, lengths):
+    c, few = small_keys(dtype, x, lengths, grads=True)
+    for name, got, ref in gradients(sla, c):
+        close_rows(got, ref, out_type(c, name), name, ~few)
+
+
+def mixed_keys(dtype, lengths, **kw):
+    """Keys of three sizes with betas that make up for it (beta |k|^2 as with keys of 1), so that every row
+    writes as much as any other; the sizes' rows."""
+    import torch
+
+    c = Case(lengths, 1, 2, 64, 32, dtype, seed=32, **kw)
+    sizes = (1.0, 256.0 if dtype == "f16" else 2.0 ** 20, 1.0 / 16)
+    size = torch.tensor(sizes)[torch.arange(c.n) % 3]
+    c.k = (c.k.float() * size[:, None, None]).to(c.k.dtype)
+    c.beta = c.beta / size[:, None].square()
+    c.beta[7] = 0
+    c.k[11] = 0
+    return c, [np.flatnonzero(size.numpy() == s) for s in sizes]
+
+
+@pytest.mark.parametrize("lengths", [[150, 64], [1100, 70]])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_forward_with_keys_of_many_sizes(sla, dtype, lengths):
+    c, _ = mixed_keys(dtype, lengths, state=True)
+    o, st = c.forward(sla)
+    ro, rs = c.forward_ref()
+    close(o, ro, dtype, "o")
+    close(st, rs, "f32", "state")
+
+
+def test_betas_of_zero(sla):
+    """Nothing is written, in a chunk or in a whole window: what is read and the betas' own gradients are as good
+    as ever."""
+    c = Case([200, 70], 1, 2, 32, 32, "f32", seed=33, state=True, grads=True)
+    c.beta[64:128] = 0
+    c.beta[200:] = 0
+    o, st = c.forward(sla)
+    ro, rs = c.forward_ref()
+    close(o, ro, "f32", "o")
+    close(st, rs, "f32", "state")
+    for name, got, ref in gradients(sla, c):
+        close(got, ref, "f32", name)
