@@ -196,6 +196,17 @@ __device__ __forceinline__ uint32_t wave_max_bits(float m) {
   return x > y ? x : y;
 }
 
+// Largest value of the four lanes that have a column (or row) i of a tile between them, of their non-negative
+// m; infinities and NaN as above.
+__device__ __forceinline__ uint32_t column_max_bits(float m) {
+  uint32_t b = __float_as_uint(m);
+  b = b >= 0x7f800000u ? 0u : b;
+  const auto x = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  b = x[0] > x[1] ? x[0] : x[1];
+  const auto y = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return y[0] > y[1] ? y[0] : y[1];
+}
+
 // The power of two that puts a largest value with these bits into [2^13, 2^14), and its inverse.
 // At 2^14 the products of 64 terms stay far inside fp32, and a value has its 22 bits down to 2^-17
 // of the largest.
@@ -211,13 +222,17 @@ __device__ __forceinline__ Scale scale_of(uint32_t max_bits) {
 }
 
 template <int N>
-__device__ __forceinline__ Scale scale_for(const floatx4 (&x)[N]) {
+__device__ __forceinline__ float max_of(const floatx4 (&x)[N]) {
   float m = 0.f;
 #pragma unroll
   for (int t = 0; t < N; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[t][r]));
-  return scale_of(wave_max_bits(m));
+  return m;
+}
+template <int N>
+__device__ __forceinline__ Scale scale_for(const floatx4 (&x)[N]) {
+  return scale_of(wave_max_bits(max_of(x)));
 }
 
 // ------------------------------------------------------------------ images

@@ -303,7 +303,8 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 //
 // Computed operands (states, mu, u, the products over columns) have two fp16 terms whatever the rows'
 // type: with one, 2^-11 of the largest value, small entries of dq and dk were off by many of their own
-// steps, bf16's too.
+// steps, bf16's too.  Every row has powers of two of its own (a lane's own row one, the other rows' out of
+// s_scale): mu' and u' of a small key are small beside its neighbours', but its dk is not.
 constexpr int kBlockCols = 32;
 
 template <int NT>
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
   __shared__ __attribute__((aligned(16))) _Float16 s_state[kStates][NC][2 * kStateHalfs];
   __shared__ __attribute__((aligned(16))) _Float16 s_do[FOR_K ? 4 : 1][NT][kFrag], s_mu[FOR_K ? 4 : 1][NC][kFrag];
   __shared__ __attribute__((aligned(16))) _Float16 s_u[4][NC][kFrag];
-  __shared__ float s_scale[3][4];
+  __shared__ __attribute__((aligned(16))) float s_scale[3][kChunk];   // of do, mu', u' of every row
   __shared__ __attribute__((aligned(16))) float s_scal[kScal];
   __shared__ double s_gam[kChunk];
   __shared__ float s_dot[kChunk];
@@ -479,13 +480,13 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
         }
         if (here) *reinterpret_cast<Raw<T, 8>*>(dv + row0 + col) = Frag<T, 8>::from_f32(xd);
       }
-      const Scale so = scale_of(wave_max_bits(max8(xo))), su = scale_of(wave_max_bits(max8(xu)));
+      const Scale so = scale_of(column_max_bits(max8(xo))), su = scale_of(column_max_bits(max8(xu)));
       Scale sm = {1.f, 1.f};
       const Op<NT> oo = op_of<NT>(xo, so.up);
       const Op<NC> ou = op_of<NC>(xu, su.up);
       Op<NC> om;
       if constexpr (FOR_K) {
-        sm = scale_of(wave_max_bits(max8(xm)));
+        sm = scale_of(column_max_bits(max8(xm)));
         om = op_of<NC>(xm, sm.up);
       }
       __syncthreads();   // the last block's reads are done
@@ -497,10 +498,10 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
 #pragma unroll
         for (int t = 0; t < NC; ++t) *reinterpret_cast<half8_t*>(&s_mu[wave][t][lane * 8]) = om.t[t];
       }
-      if (lane == 0) {
-        s_scale[0][wave] = so.down;
-        s_scale[1][wave] = sm.down;
-        s_scale[2][wave] = su.down;
+      if (g == 0) {
+        s_scale[0][own] = so.down;
+        s_scale[1][own] = sm.down;
+        s_scale[2][own] = su.down;
       }
 #pragma unroll
       for (int n = 0; n < kLoads; ++n) {
@@ -540,8 +541,11 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
           x.t[n] = *reinterpret_cast<const half8_t*>(&rows[j][n][lane * 8]);
       };
       const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-      const float fq = a.scale * since * (ss.down * so.down);
-      const float fk0 = -vs * since * (ss.down * sm.down), fk1 = vs * until * (sd.down * su.down);
+      const auto scale4 = [&](int which, int j) __attribute__((always_inline)) {   // of tile j's rows
+        return *reinterpret_cast<const floatx4*>(&s_scale[which][16 * j + 4 * g]);
+      };
+      const float fq = (a.scale * since * ss.down) * so.down;
+      const float fk0 = -(vs * sm.down) * (since * ss.down), fk1 = (vs * su.down) * (until * sd.down);
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
         if (t % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // four tiles' operands in registers
@@ -560,17 +564,17 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
           Op<NC> x, own;
           rows_of(before ? s_u : s_mu, x, j);
           rows_of(before ? s_mu : s_u, own, wave);
-          M[0][j] += (s_scale[before ? 2 : 1][j] * (before ? sm.down : su.down)) * mma_op(x, own, zero);
+          M[0][j] += (scale4(before ? 2 : 1, j) * (before ? sm.down : su.down)) * mma_op(x, own, zero);
           Op<NT> o;
           rows_of(s_do, o, j);
-          M[FOR_K][j] += (s_scale[0][j] * su.down) * mma_op(o, ou, zero);
+          M[FOR_K][j] += (scale4(0, j) * su.down) * mma_op(o, ou, zero);
         } else {
           Op<NC> u;
           rows_of(s_u, u, j);
-          M[0][j] += (s_scale[2][j] * so.down) * mma_op(u, oo, zero);
+          M[0][j] += (scale4(2, j) * so.down) * mma_op(u, oo, zero);
         }
       }
-      if constexpr (FOR_K) Mw += (sm.down * su.down) * mma_op(om, ou, zero);
+      if constexpr (FOR_K) Mw += (scale4(1, wave) * su.down) * mma_op(om, ou, zero);
     }
     // the decays between own row and the others, then the products over the chunk's rows: M[0] becomes
     // what k is multiplied with, for dk M[1] what q is
@@ -597,7 +601,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
     }
     __builtin_amdgcn_sched_barrier(0);
     const auto ops_of = [&](const floatx4 (&m)[4], Op<NC> (&p)[2]) __attribute__((always_inline)) {
-      const Scale s = scale_for(m);
+      const Scale s = scale_of(column_max_bits(max_of(m)));
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
         float x[8];

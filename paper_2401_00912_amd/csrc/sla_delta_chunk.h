@@ -576,15 +576,6 @@ __device__ __forceinline__ void store_state(const floatx4 (&S)[ST], const Args& 
       for (int r = 0; r < 4; ++r) p[(size_t)(d + r) * a.dv] = S[t][r];
   }
 }
-template <int N>
-__device__ __forceinline__ float max_of(const floatx4 (&x)[N]) {
-  float m = 0.f;
-#pragma unroll
-  for (int t = 0; t < N; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[t][r]));
-  return m;
-}
 
 // x[tau] = triangle times y, lower (UPPER: the transposed triangle under its mirrored numbers)
 template <bool UPPER>

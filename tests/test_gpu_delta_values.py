@@ -59,7 +59,9 @@ def test_bf16_results_are_rounded_once(sla, hk, h, dk, dv, lengths):
 # ------------------------------------------------------------------ keys of many sizes
 def close_rows(got, ref, dtype, name, rows, bar=FP32_BAR):
     """Rows of one kind held to the largest among them."""
-    close(got[rows.tolist()], ref[rows], dtype, name, bar)
+    import torch
+
+    close(got[torch.from_numpy(rows)], ref[rows], dtype, name, bar)
 
 
 # windows of a chunk and some, and one that is cut into parts of 512 rows
@@ -133,3 +135,28 @@ def test_betas_of_zero(sla):
     close(st, rs, "f32", "state")
     for name, got, ref in gradients(sla, c):
         close(got, ref, "f32", name)
+
+
+@pytest.mark.parametrize("lengths", [[70, 64], [1100, 70]])
+@pytest.mark.parametrize("dtype,x", SMALL_KEYS)
+def test_gradients_of_a_small_key(sla, dtype, x, lengths):
+    """dk of the few small keys, which is as large as the others', and their dv and dbeta, which are x times as
+    large (keys are scaled up to 2^60 times: at 1e-30 those two are not worth a bit beside the others)."""
+    c, few = small_keys(dtype, x, lengths, grads=True)
+    for name, got, ref in gradients(sla, c):
+        if name == "dk" or (name in ("dv", "dbeta") and x > 1e-30 and dtype != "f16"):
+            close_rows(got, ref, out_type(c, name), name, few)
+
+
+@pytest.mark.parametrize("lengths", [[150, 64], [1100, 70]])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gradients_with_keys_of_many_sizes(sla, dtype, lengths):
+    """Each size's rows by themselves: dk is smaller and dbeta larger the larger a key is.  fp16's dk has steps of
+    2^-24 whatever its size, and the row without a key has no size."""
+    c, kinds = mixed_keys(dtype, lengths, state=True, grads=True)
+    for name, got, ref in gradients(sla, c):
+        if name == "dstate_in":
+            close(got, ref, "f32", name)
+            continue
+        for rows in kinds:
+            close_rows(got, ref, out_type(c, name), name, np.setdiff1d(rows, [11]))
