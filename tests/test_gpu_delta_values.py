@@ -160,3 +160,29 @@ def test_gradients_with_keys_of_many_sizes(sla, dtype, lengths):
             continue
         for rows in kinds:
             close_rows(got, ref, out_type(c, name), name, np.setdiff1d(rows, [11]))
+
+
+# ------------------------------------------------------------------ parts that forget
+@pytest.mark.parametrize("dk,dv", [(32, 32), (48, 64), (128, 16)])
+def test_parts_that_forget_keep_their_bits(sla, dk, dv):
+    """A window cut into parts of 512 rows, across each of which the state falls to e^-15 of itself and nothing is
+    written: what is left of the state, its reads on the way and the gradient that comes back are as good, for
+    their own size, as at the start."""
+    import torch
+
+    n, gam = 2100, -0.03
+    c = Case([n], 1, 1, dk, dv, "f32", seed=35, state=True, grads=True)
+    c.g[:] = gam
+    c.beta[:] = 0
+    c.dout[:] = 0
+    o, st = c.forward(sla)
+    ro, rs = c.forward_ref()
+    up = np.exp(-gam * np.arange(1, n + 1))[:, None, None]
+    close(o.double().cpu() * torch.from_numpy(up), ro * up, "f32", "o")
+    close(st, rs, "f32", "state")
+    for name, got, ref in gradients(sla, c):
+        if name == "dstate_in":
+            close(got, ref, "f32", name)
+        if name == "dbeta":
+            down = up[::-1, :, 0].copy()
+            close(got.double().cpu() * torch.from_numpy(down), ref * down, "f32", name)
