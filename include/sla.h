@@ -458,8 +458,11 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
  *   states   fp32 [num_windows, heads, dim_k, dim_v].  state_out may be state_in.
  *   workspace  device, 256-byte aligned, at least sla_delta_workspace_bytes(...) bytes (0 for
  *            sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
- * Entries of q and k are below 2^75 (fp32).  The rule is stable where beta_t |k_t|^2 <= 2 (keys are usually normalised to 1); where it is not,
- * states grow exponentially and results may not be finite.  Sums, states and decays are fp32, decay
+ * Entries of q and k are below 2^75 (fp32).  The rule is stable where g <= 0 and beta_t |k_t|^2 <= 2 (keys
+ * are usually normalised to 1); where it is not, states grow exponentially and results may not be finite.
+ * With g > 0 the chunk form (64 rows) sums products that are up to e^(the chunk's sum of g) times the
+ * results they cancel to, and results have that many bits less; the sum over a chunk, and over the up to
+ * 2,048 rows of a part of a long window, has to stay below 88.  Sums, states and decays are fp32, decay
  * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
  * held exactly down to 2^-17 of its row's largest value).  o must not be an input.  A value that is
  * not finite reaches only its own window (v's, only its own head and column).  Deterministic.

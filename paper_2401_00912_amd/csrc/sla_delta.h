@@ -37,15 +37,15 @@ constexpr int kChunk = 64;
 constexpr int kFrag = 512;            // halfs of one 16 x 32 operand: 64 lanes x 8
 constexpr int kTri = 6;               // 16 x 32 operands of a lower triangular 64 x 64 matrix
 constexpr int kTriHalfs = 2 * kTri * kFrag;
-// T and P are kept 64 times as large (T's and P's entries stay below 512): an entry's error is
-// then below 2^-31 of the diagonal's 1
-constexpr float kTriUp = 64.f;
-constexpr int kScal = 768;            // 4-byte values: 12 rows of 64, one of them with a single value
+constexpr int kScal = 768;            // 4-byte values: 11 rows of 64, and single ones
 // Rows of a chunk's scalars: exp(gam), b / t, exp(gam_last - gam), s, 2^rho scale; the original rows
 // (int32) of the chunk and of its window's next and previous chunk, which are asked for while this one is in
-// work; exp(gam_last); t exp(gam), b and 2^-kap.
+// work; exp(gam_last); the factors that the four tile rows of T, P and their transposes are to be multiplied
+// with (powers of two: rows of a growing state, g > 0, are far from each other's size, and one factor for all
+// had them overflow); t exp(gam), b and 2^-kap.
 enum { kSince = 0, kWrite = 64, kUntil = 128, kVScale = 192, kOScale = 256, kRow = 320, kNext = 384, kPrev = 448,
-       kLast = 512, kSinceK = 576, kBeta = 640, kKScale = 704 };
+       kLast = 512, kTDown = 516, kPDown = 520, kBackTDown = 524, kBackPDown = 528, kSinceK = 576, kBeta = 640,
+       kKScale = 704 };
 // What a chunk has for each value head, in halfs: P's second and first terms, T's first and second,
 // the scalars, and for the backward the transposed inverse and the transposed P, two terms each.
 // The walk forward reads up to the scalars, the walk back from there.

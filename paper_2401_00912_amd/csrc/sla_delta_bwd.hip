@@ -167,13 +167,13 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kOScale, tau);
       const Scale sy = scale_for(Y);
-      const float ydown = sy.down * (1.f / kTriUp);
+      const floatx4 ydown = *reinterpret_cast<const floatx4*>(scal + kBackPDown) * sy.down;
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
       tri_times<true>(bp, bp + kTerm, Yp, X, lane);
 #pragma unroll
-      for (int tau = 0; tau < 4; ++tau) X[tau] *= ydown;
+      for (int tau = 0; tau < 4; ++tau) X[tau] *= ydown[tau];
     }
     if (carried) {
       const Scale sc = scale_of(top);
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     // lam, then -since mu in X and since do' in Y
     {
       const Scale sx = scale_for(X);
-      const float xdown = sx.down * (1.f / kTriUp);
+      const floatx4 xdown = *reinterpret_cast<const floatx4*>(scal + kBackTDown) * sx.down;
       Pair Xp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sx.up);
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         const floatx4 since = row4(kSince, tau);
-        X[tau] *= xdown;
+        X[tau] *= xdown[tau];
         if constexpr (!ENDS)
 #pragma unroll
           for (int r = 0; r < 4; ++r) lam[(sh * kChunk + 16 * tau + 4 * g + r) * a.dv + col] = X[tau][r];

@@ -89,12 +89,21 @@ __device__ __forceinline__ void invert(PrepShared& s, int wave, int i, int g) {
 }
 
 // The triangle's operands of tile row `tau` out of a matrix in LDS: rows as operand rows, columns
-// in the order of two stacked result tiles.
-__device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* lo, int tau, int lane, int i, int g) {
-  for (int s = 0; s <= tau / 2; ++s) {
-    const floatx4 x0 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 4 * g);
-    const floatx4 x1 = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 32 * s + 16 + 4 * g);
-    const Pair p = split(x0, x1, kTriUp);
+// in the order of two stacked result tiles, and to `down` the factor that belongs to the tile row.
+__device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* lo, float* down, int tau, int lane,
+                                        int i, int g) {
+  floatx4 x[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (j / 2 <= tau / 2) x[j] = *reinterpret_cast<const floatx4*>(m + (16 * tau + i) * kLd + 16 * j + 4 * g);
+  }
+  const Scale sc = scale_for(x);
+  if (lane == 0) down[tau] = sc.down;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (s > tau / 2) continue;
+    const Pair p = split(x[2 * s], x[2 * s + 1], sc.up);
     const int at = tri_at(tau, s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(hi + at) = p.hi;
     *reinterpret_cast<half8_t*>(lo + at) = p.lo;
@@ -102,15 +111,21 @@ __device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* 
 }
 // The transposed matrix's operands of tile row `tau`: upper triangular, kept under the mirrored
 // numbers (row tile 3 - tau, column block 1 - s).
-__device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, int tau, int lane, int i, int g) {
-  for (int s = tau / 2; s < 2; ++s) {
-    floatx4 x0, x1;
+__device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, float* down, int tau, int lane, int i, int g) {
+  floatx4 x[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      x0[r] = m[(32 * s + 4 * g + r) * kLd + 16 * tau + i];
-      x1[r] = m[(32 * s + 16 + 4 * g + r) * kLd + 16 * tau + i];
-    }
-    const Pair p = split(x0, x1, kTriUp);
+  for (int j = 0; j < 4; ++j) {
+    x[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (j / 2 >= tau / 2)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[j][r] = m[(16 * j + 4 * g + r) * kLd + 16 * tau + i];
+  }
+  const Scale sc = scale_for(x);
+  if (lane == 0) down[tau] = sc.down;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (s < tau / 2) continue;
+    const Pair p = split(x[2 * s], x[2 * s + 1], sc.up);
     _Float16* at = out + tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(at) = p.hi;
     *reinterpret_cast<half8_t*>(at + kTri * kFrag) = p.lo;
@@ -265,13 +280,13 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     const int h = hk * group + hv;
     const size_t sh = (size_t)slot * a.H + h;
     _Float16* out = records + sh * (REV ? kRecordBack : kRecord);
+    float* sc = reinterpret_cast<float*>(out + kScalAt);
     const double* gam = s_gam[hv & 1];
     const float *write = s_write[hv & 1], *t = s_t[hv & 1], *b = s_b[hv & 1];
     if (wave == 0) {
       const bool real = lane < rows;
       const double gl = gam[lane], last = gam[63];
       const float kd = inverse_pow2(s_ks[lane]), since = real ? __builtin_amdgcn_exp2f((float)gl) : 0.f;
-      float* sc = reinterpret_cast<float*>(out + kScalAt);
       sc[kSince + lane] = since;
       sc[kWrite + lane] = write[lane];
       sc[kUntil + lane] = real ? __builtin_amdgcn_exp2f((float)(last - gl)) : 0.f;
@@ -311,7 +326,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
     __syncthreads();
     invert(sm, wave, i, g);
     const bool here = 16 * wave < rows;   // pieces of tile rows past the last row are not written (nor moved)
-    if (here) put_tri(sm.x, out + kTHi, out + kTHi + kTerm, wave, lane, i, g);
+    if (here) put_tri(sm.x, out + kTHi, out + kTHi + kTerm, sc + kTDown, wave, lane, i, g);
     if constexpr (REV) {
       __syncthreads();
 #pragma unroll
@@ -323,7 +338,7 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
         }
       __syncthreads();
       invert(sm, wave, i, g);
-      put_tri_t(sm.x, out + kBackT, wave, lane, i, g);
+      put_tri_t(sm.x, out + kBackT, sc + kBackTDown, wave, lane, i, g);
     }
     // every wave is past its reads of n (the inverse's last barrier)
 #pragma unroll
@@ -332,8 +347,8 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
       for (int r = 0; r < 4; ++r)
         sm.n[(16 * wave + 4 * g + r) * kLd + 16 * j + i] = d[j][r] == 0.f ? 0.f : d[j][r] * qk[j][r];
     __syncthreads();
-    if (here) put_tri(sm.n, out + kPHi, out + kPLo, wave, lane, i, g);
-    if constexpr (REV) put_tri_t(sm.n, out + kBackP, wave, lane, i, g);
+    if (here) put_tri(sm.n, out + kPHi, out + kPLo, sc + kPDown, wave, lane, i, g);
+    if constexpr (REV) put_tri_t(sm.n, out + kBackP, sc + kBackPDown, wave, lane, i, g);
     if (hv + 1 < group) sums(hv + 1);
     __syncthreads();
   }
@@ -580,7 +595,8 @@ __device__ __forceinline__ void store_state(const floatx4 (&S)[ST], const Args& 
   }
 }
 
-// x[tau] = triangle times y, lower (UPPER: the transposed triangle under its mirrored numbers)
+// x[tau] = triangle times y but for the tile row's factor, lower (UPPER: the transposed triangle under its
+// mirrored numbers)
 template <bool UPPER>
 __device__ __forceinline__ void tri_times(const _Float16* hi, const _Float16* lo, const Pair (&y)[2], floatx4 (&x)[4],
                                           int lane) {
@@ -781,13 +797,15 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     float uunit;
     {
       const Scale sy = scale_for(Y);
-      uunit = sy.down * (1.f / kTriUp);
+      uunit = sy.down;
       Pair Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
       tri_times<false>(rec(kTHi), rec(kTHi + kTerm), Yp, U, lane);
+      const floatx4 tdown = *reinterpret_cast<const floatx4*>(scal + kTDown);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
+        U[tau] *= tdown[tau];
         if constexpr (KEEP) {
 #pragma unroll
           for (int r = 0; r < 4; ++r)
@@ -800,7 +818,8 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     // o, transposed: a lane holds 4 columns of one row
     if constexpr (!ENDS) {
       const Scale su = scale_for(U);
-      const float udown = su.down * uunit * (1.f / kTriUp);
+      const float udown = su.down * uunit;
+      const floatx4 pdown = *reinterpret_cast<const floatx4*>(scal + kPDown);
       floatx4 y[4];
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -819,7 +838,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       for (int tau = 0; tau < 4; ++tau) {
         const int p = 16 * tau + i;
         const float os = scal[kOScale + p], since = os * scal[kSince + p] * qdown;
-        const floatx4 z = since * qs[tau] + (os * udown) * y[tau];
+        const floatx4 z = since * qs[tau] + (os * (udown * pdown[tau])) * y[tau];
         if constexpr (!KEEP) {
           const float z4[4] = {z[0], z[1], z[2], z[3]};
           held[tau] = Frag<T, 4>::from_f32(z4);

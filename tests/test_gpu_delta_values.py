@@ -186,3 +186,28 @@ def test_parts_that_forget_keep_their_bits(sla, dk, dv):
         if name == "dbeta":
             down = up[::-1, :, 0].copy()
             close(got.double().cpu() * torch.from_numpy(down), ref * down, "f32", name)
+
+
+# ------------------------------------------------------------------ states that grow
+@pytest.mark.parametrize("lengths,g", [([150, 70], 0.1), ([1100, 70], 0.02)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_states_that_grow(sla, dtype, lengths, g):
+    """Log decays above zero: nothing overflows before the results do.  A chunk's products are up to e^(64 g) times
+    the results that they cancel to, and so is the limit."""
+    c = Case(lengths, 1, 2, 32, 32, dtype, seed=37, state=True, grads=True)
+    c.g[:] = g
+    # keys and queries of length 1 that have much in common, betas that write little of it off
+    c.q, c.k = (((1 + x.float()) / (1 + x.float()).norm(dim=-1, keepdim=True)).to(x.dtype) for x in (c.q, c.k))
+    c.beta /= 16
+    c.v, c.dout = ((x.float() * 2.0 ** -12).to(x.dtype) for x in (c.v, c.dout))
+    c.state, c.dstate = c.state * 2.0 ** -12, c.dstate * 2.0 ** -12
+    if dtype == "f16" and g < 0.1:
+        c.q /= 2.0 ** 14   # its results end at 65,504
+        c.dout /= 2.0 ** 10
+    bar = FP32_BAR * float(np.exp(64 * g))
+    o, st = c.forward(sla)
+    ro, rs = c.forward_ref()
+    close(o, ro, dtype, "o", bar)
+    close(st, rs, "f32", "state", bar)
+    for name, got, ref in gradients(sla, c):
+        close(got, ref, out_type(c, name), name, bar)
