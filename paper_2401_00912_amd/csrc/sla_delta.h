@@ -13,7 +13,11 @@
 // Two-term operands.  The matrix cores' 16-bit products are 16 times as fast as their fp32 ones,
 // and one 16-bit rounding of a state loses what fp32 states are kept for.  So an fp32 operand is
 // scaled by a power of two and split into two fp16 terms, x = hi + lo (22 bits), and a product is
-// the sum of hi hi, hi lo and lo hi in fp32.  A 16-bit input needs no second term: its row is
+// the sum of hi hi, hi lo and lo hi in fp32.  (With values under 2^-16 of the largest the second term runs
+// out of fp16's least steps, and one of 2^-38 is lost.  That is no loss in a sum that the largest one is in
+// too.  But T, P and what they are multiplied with hold rows that have nothing to do with each other, early
+// ones and a late one a billion times as large: there x = hi + 2^-11 lo, with the products of the second
+// terms summed by themselves, 22 bits down to 2^-27 of the largest and none at 2^-49.)  A 16-bit input needs no second term: its row is
 // scaled by a power of two that puts the row's largest value into [1, 2), and then fp16 holds
 // fp16 and bf16 values exactly down to 2^-17 of the row's largest (below that, to 2^-25 of it).
 // With k = 2^kap k' and q = 2^rho q' the rule reads the same for k', u' = 2^kap u, o' = 2^-rho o and
@@ -137,6 +141,13 @@ __device__ __forceinline__ int kept_row(const Args& a, float x) {
 struct Pair {
   half8_t hi, lo;
 };
+struct Far {   // second terms 2^11 times as large as what they stand for
+  half8_t hi, lo;
+};
+struct FarSum {
+  floatx4 lo = {0.f, 0.f, 0.f, 0.f}, hi = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ floatx4 all() const { return hi + lo * 0x1p-11f; }
+};
 
 __device__ __forceinline__ floatx4 mma(half8_t a, half8_t b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -147,6 +158,11 @@ __device__ __forceinline__ floatx4 mma2(const Pair& a, const Pair& b, floatx4 c)
   c = mma(a.hi, b.lo, c);
   return mma(a.hi, b.hi, c);
 }
+__device__ __forceinline__ void mma2(const Far& a, const Far& b, FarSum& c) {
+  c.lo = mma(a.lo, b.hi, c.lo);
+  c.lo = mma(a.hi, b.lo, c.lo);
+  c.hi = mma(a.hi, b.hi, c.hi);
+}
 __device__ __forceinline__ floatx4 mma1(half8_t a, const Pair& b, floatx4 c) {
   c = mma(a, b.lo, c);
   return mma(a, b.hi, c);
@@ -156,12 +172,13 @@ __device__ __forceinline__ floatx4 mma1(const Pair& a, half8_t b, floatx4 c) {
   return mma(a.hi, b, c);
 }
 
-// x scaled by s as two fp16 terms, two instructions a value: each term is one multiply-add that
-// rounds to fp16, the second one's addend the first term.  (The first terms are hidden from the
+// x scaled by s as two fp16 terms, two instructions a value (Far: three): each term is one multiply-add
+// that rounds to fp16, the second one's addend the first term.  (The first terms are hidden from the
 // compiler once they are there: it would make them again for the second.)
-__device__ __forceinline__ Pair split(const floatx4& x0, const floatx4& x1, float s) {
+template <class P = Pair>
+__device__ __forceinline__ P split(const floatx4& x0, const floatx4& x1, float s) {
   typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-  Pair p;
+  P p;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const float a = e < 4 ? x0[e] : x1[e - 4], b = e < 4 ? x0[e + 1] : x1[e - 3];
@@ -171,8 +188,13 @@ __device__ __forceinline__ Pair split(const floatx4& x0, const floatx4& x1, floa
     h = __builtin_bit_cast(half2_t, u);
     p.hi[e] = h[0];
     p.hi[e + 1] = h[1];
-    p.lo[e] = (_Float16)__builtin_fmaf(a, s, -(float)h[0]);
-    p.lo[e + 1] = (_Float16)__builtin_fmaf(b, s, -(float)h[1]);
+    if constexpr (std::is_same<P, Far>::value) {
+      p.lo[e] = (_Float16)__builtin_fmaf(__builtin_fmaf(a, s, -(float)h[0]), 0x1p11f, 0.f);
+      p.lo[e + 1] = (_Float16)__builtin_fmaf(__builtin_fmaf(b, s, -(float)h[1]), 0x1p11f, 0.f);
+    } else {
+      p.lo[e] = (_Float16)__builtin_fmaf(a, s, -(float)h[0]);
+      p.lo[e + 1] = (_Float16)__builtin_fmaf(b, s, -(float)h[1]);
+    }
   }
   return p;
 }
@@ -208,8 +230,7 @@ __device__ __forceinline__ uint32_t column_max_bits(float m) {
 }
 
 // The power of two that puts a largest value with these bits into [2^13, 2^14), and its inverse.
-// At 2^14 the products of 64 terms stay far inside fp32, and a value has its 22 bits down to 2^-17
-// of the largest.
+// At 2^14 the products of 64 terms stay far inside fp32.
 struct Scale {
   float up, down;
 };

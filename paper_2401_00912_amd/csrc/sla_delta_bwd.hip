@@ -168,9 +168,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
       for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kOScale, tau);
       const Scale sy = scale_for(Y);
       const floatx4 ydown = *reinterpret_cast<const floatx4*>(scal + kBackPDown) * sy.down;
-      Pair Yp[2];
+      Far Yp[2];
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
+      for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split<Far>(Y[2 * s2], Y[2 * s2 + 1], sy.up);
       tri_times<true>(bp, bp + kTerm, Yp, X, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) X[tau] *= ydown[tau];
@@ -190,9 +190,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     {
       const Scale sx = scale_for(X);
       const floatx4 xdown = *reinterpret_cast<const floatx4*>(scal + kBackTDown) * sx.down;
-      Pair Xp[2];
+      Far Xp[2];
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) Xp[s2] = split(X[2 * s2], X[2 * s2 + 1], sx.up);
+      for (int s2 = 0; s2 < 2; ++s2) Xp[s2] = split<Far>(X[2 * s2], X[2 * s2 + 1], sx.up);
       tri_times<true>(bt, bt + kTerm, Xp, X, lane);
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {

@@ -103,7 +103,7 @@ __device__ __forceinline__ void put_tri(const float* m, _Float16* hi, _Float16* 
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     if (s > tau / 2) continue;
-    const Pair p = split(x[2 * s], x[2 * s + 1], sc.up);
+    const Far p = split<Far>(x[2 * s], x[2 * s + 1], sc.up);
     const int at = tri_at(tau, s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(hi + at) = p.hi;
     *reinterpret_cast<half8_t*>(lo + at) = p.lo;
@@ -125,7 +125,7 @@ __device__ __forceinline__ void put_tri_t(const float* m, _Float16* out, float* 
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     if (s < tau / 2) continue;
-    const Pair p = split(x[2 * s], x[2 * s + 1], sc.up);
+    const Far p = split<Far>(x[2 * s], x[2 * s + 1], sc.up);
     _Float16* at = out + tri_at(3 - tau, 1 - s) * kFrag + lane * 8;
     *reinterpret_cast<half8_t*>(at) = p.hi;
     *reinterpret_cast<half8_t*>(at + kTri * kFrag) = p.lo;
@@ -598,19 +598,20 @@ __device__ __forceinline__ void store_state(const floatx4 (&S)[ST], const Args& 
 // x[tau] = triangle times y but for the tile row's factor, lower (UPPER: the transposed triangle under its
 // mirrored numbers)
 template <bool UPPER>
-__device__ __forceinline__ void tri_times(const _Float16* hi, const _Float16* lo, const Pair (&y)[2], floatx4 (&x)[4],
+__device__ __forceinline__ void tri_times(const _Float16* hi, const _Float16* lo, const Far (&y)[2], floatx4 (&x)[4],
                                           int lane) {
-#pragma unroll
-  for (int tau = 0; tau < 4; ++tau) x[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+  FarSum sum[4];
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau) {
       if (UPPER ? s < tau / 2 : s > tau / 2) continue;
       const int at = (UPPER ? tri_at(3 - tau, 1 - s) : tri_at(tau, s)) * kFrag + lane * 8;
-      const Pair t = {*reinterpret_cast<const half8_t*>(hi + at), *reinterpret_cast<const half8_t*>(lo + at)};
-      x[tau] = mma2(t, y[s], x[tau]);
+      const Far t = {*reinterpret_cast<const half8_t*>(hi + at), *reinterpret_cast<const half8_t*>(lo + at)};
+      mma2(t, y[s], sum[tau]);
     }
+#pragma unroll
+  for (int tau = 0; tau < 4; ++tau) x[tau] = sum[tau].all();
 }
 // x[tau] = rows of the image times the state's columns
 template <int NT, int DK>
@@ -798,9 +799,9 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     {
       const Scale sy = scale_for(Y);
       uunit = sy.down;
-      Pair Yp[2];
+      Far Yp[2];
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split(Y[2 * s2], Y[2 * s2 + 1], sy.up);
+      for (int s2 = 0; s2 < 2; ++s2) Yp[s2] = split<Far>(Y[2 * s2], Y[2 * s2 + 1], sy.up);
       tri_times<false>(rec(kTHi), rec(kTHi + kTerm), Yp, U, lane);
       const floatx4 tdown = *reinterpret_cast<const floatx4*>(scal + kTDown);
 #pragma unroll
@@ -820,25 +821,23 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       const Scale su = scale_for(U);
       const float udown = su.down * uunit;
       const floatx4 pdown = *reinterpret_cast<const floatx4*>(scal + kPDown);
-      floatx4 y[4];
-#pragma unroll
-      for (int tau = 0; tau < 4; ++tau) y[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
+      FarSum y[4];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        const Pair up = split(U[2 * s2], U[2 * s2 + 1], su.up);
+        const Far up = split<Far>(U[2 * s2], U[2 * s2 + 1], su.up);
 #pragma unroll
         for (int tau = 2 * s2; tau < 4; ++tau) {
           const int p = tri_at(tau, s2) * kFrag + lane * 8;
-          const Pair t = {*reinterpret_cast<const half8_t*>(rec(kPHi) + p),
-                          *reinterpret_cast<const half8_t*>(rec(kPLo) + p)};
-          y[tau] = mma2(up, t, y[tau]);
+          const Far t = {*reinterpret_cast<const half8_t*>(rec(kPHi) + p),
+                         *reinterpret_cast<const half8_t*>(rec(kPLo) + p)};
+          mma2(up, t, y[tau]);
         }
       }
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         const int p = 16 * tau + i;
         const float os = scal[kOScale + p], since = os * scal[kSince + p] * qdown;
-        const floatx4 z = since * qs[tau] + (os * (udown * pdown[tau])) * y[tau];
+        const floatx4 z = since * qs[tau] + (os * (udown * pdown[tau])) * y[tau].all();
         if constexpr (!KEEP) {
           const float z4[4] = {z[0], z[1], z[2], z[3]};
           held[tau] = Frag<T, 4>::from_f32(z4);

@@ -211,3 +211,22 @@ def test_states_that_grow(sla, dtype, lengths, g):
     close(st, rs, "f32", "state", bar)
     for name, got, ref in gradients(sla, c):
         close(got, ref, out_type(c, name), name, bar)
+
+
+# ------------------------------------------------------------------ rows of many sizes
+@pytest.mark.parametrize("lengths", [[150, 70], [1700, 70]])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_before_a_large_one(sla, dtype, lengths):
+    """A row's value 10^9 times the others': what came before it is as good as without it, and so are the gradients
+    of what comes behind such a row of dout.  (Its chunk's other rows have 22 bits down to 2^-27 of it, and 19 at
+    10^-9: a step of 2^-49 of it is 2e-6 of them.)"""
+    at = 60
+    c = Case(lengths, 1, 2, 64, 32, dtype, seed=38, grads=True)
+    c.v[at] *= 1e9
+    c.dout[at] *= 1e9
+    o, _ = c.forward(sla)
+    before = np.arange(c.n) < at
+    close_rows(o, c.forward_ref()[0], dtype, "o", before)
+    for name, got, ref in gradients(sla, c):
+        if name == "dv":
+            close_rows(got, ref, dtype, name, np.arange(c.n) > at)
