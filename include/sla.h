@@ -465,7 +465,8 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
  * 2,048 rows of a part of a long window, has to stay below 88.  Sums, states and decays are fp32, decay
  * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
  * held exactly down to 2^-17 of its row's largest value; rows of a chunk that differ in size have 22
- * bits down to 2^-27 of the largest, an error of 2^-49 of it below).  o must not be an input.  A value that is
+ * bits down to 2^-27 of the largest, an error of 2^-49 of it below; value columns and heads share nothing).
+ * A key's or query's own scale ends at 2^-60: entries below 2^-74 lose bits, below 2^-85 all.  o must not be an input.  A value that is
  * not finite reaches only its own window (v's, only its own head and column).  Deterministic.
  */
 size_t sla_delta_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t heads_qk,

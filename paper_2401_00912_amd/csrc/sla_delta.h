@@ -255,6 +255,17 @@ template <int N>
 __device__ __forceinline__ Scale scale_for(const floatx4 (&x)[N]) {
   return scale_of(wave_max_bits(max_of(x)));
 }
+template <int N>
+__device__ __forceinline__ Scale column_scale(const floatx4 (&x)[N]) {
+  return scale_of(column_max_bits(max_of(x)));
+}
+// of the four lane groups' columns 4g .. 4g + 3, as a transposed tile has them: x of a lane's column i
+__device__ __forceinline__ floatx4 across(float x, int g) {
+  floatx4 y;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) y[r] = __shfl(x, 4 * g + r);
+  return y;
+}
 
 // ------------------------------------------------------------------ images
 // Half index of (row, column) in the image of a 64 x DK matrix: operands of 16 rows x 32 columns

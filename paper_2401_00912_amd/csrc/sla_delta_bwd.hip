@@ -156,17 +156,18 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     if constexpr (!ENDS)
 #pragma unroll
       for (int t = 0; t < ST; ++t) s0[t] = *reinterpret_cast<const floatx4*>(states + sgrp * ST * 256 + t * 256 + lane * 4);
-    const uint32_t top = wave_max_bits(max_of(S));
+    const uint32_t top = column_max_bits(max_of(S));
     if constexpr (!ENDS) {
 #pragma unroll
       for (int t = 0; t < ST; ++t) *reinterpret_cast<floatx4*>(dstates + sgrp * ST * 256 + t * 256 + lane * 4) = S[t];
-      if (lane == 0) dmax[sgrp] = __uint_as_float(top);
+      const uint32_t all = wave_max_bits(__uint_as_float(top));
+      if (lane == 0) dmax[sgrp] = __uint_as_float(all);
     }
     // du = P^T do' + until k' dS
     {
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) Y[tau] *= row4(kOScale, tau);
-      const Scale sy = scale_for(Y);
+      const Scale sy = column_scale(Y);
       const floatx4 ydown = *reinterpret_cast<const floatx4*>(scal + kBackPDown) * sy.down;
       Far Yp[2];
 #pragma unroll
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     jobs(integral_constant<int, 2>{}, integral_constant<int, 5>{});
     // lam, then -since mu in X and since do' in Y
     {
-      const Scale sx = scale_for(X);
+      const Scale sx = column_scale(X);
       const floatx4 xdown = *reinterpret_cast<const floatx4*>(scal + kBackTDown) * sx.down;
       Far Xp[2];
 #pragma unroll
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
     jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});
     // dS = exp(gam_last) dS + q'^T (since do') - k'^T (since mu)
     {
-      const Scale sc = scale_of(wave_max_bits(fmaxf(max_of(X), max_of(Y))));
+      const Scale sc = scale_of(column_max_bits(fmaxf(max_of(X), max_of(Y))));
       Pair Xp[2], Yp[2];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
@@ -601,7 +602,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
     }
     __builtin_amdgcn_sched_barrier(0);
     const auto ops_of = [&](const floatx4 (&m)[4], Op<NC> (&p)[2]) __attribute__((always_inline)) {
-      const Scale s = scale_of(column_max_bits(max_of(m)));
+      const Scale s = column_scale(m);
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
         float x[8];

@@ -358,7 +358,9 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 // A wave holds 16 of the state's dv columns in registers, as result tiles: tile 2t + p, component r
 // of lane (i, g) is state row 32 t + 8 g + 4 p + r, column i.  Two tiles are then an operand of the
 // products with k' and q' without moving a value, and so are the chunk's r and u (16 rows a tile);
-// the columns are independent of each other, so no wave waits for another but for the staging.
+// the columns are independent of each other, so no wave waits for another but for the staging.  Each
+// column (a lane's i) has powers of two of its own for the two terms of its operands, so that a large
+// value in one costs the others nothing.
 //
 // The chunks of a window depend on each other, so their latency counts: a chunk's images, triangles,
 // scalars and the waves' columns of v are moved into the second of two LDS buffers while the first
@@ -677,7 +679,8 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
           *reinterpret_cast<Raw<T, 4>*>(o + ((size_t)held_place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g) = held[tau];
   };
 
-  // the state is `unit` times S: after a chunk S stays in the units of the products it was summed with
+  // the state is `unit` times S, a unit a column: after a chunk S stays in the units of the products it was
+  // summed with
   floatx4 S[ST];
   float unit = 1.f;
   bool carried = true;   // no products with a state that is zero
@@ -762,7 +765,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
         dn[tau] = *reinterpret_cast<const Raw<T, 4>*>(dout + ((size_t)place[tau] * a.H + h) * a.dv + 16 * cg + 4 * g);
     }
     // y = s v - t exp(gam) k' S, and q' S for later
-    uint32_t top = 0;   // of the state, in S's units
+    uint32_t top = 0;   // of the state's column, in S's units
     float qdown = 0.f;
 #pragma unroll
     for (int tau = 0; tau < 4; ++tau) {
@@ -770,10 +773,12 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
       qs[tau] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     if (carried) {
-      top = wave_max_bits(max_of(S));
+      top = column_max_bits(max_of(S));
       const Scale sc = scale_of(top);
-      if constexpr (KEEP)
-        if (lane == 0) out.smax[sh * (a.dv / 16) + cg] = __uint_as_float(top) * unit;
+      if constexpr (KEEP) {
+        const uint32_t all = wave_max_bits(__uint_as_float(top) * unit);
+        if (lane == 0) out.smax[sh * (a.dv / 16) + cg] = __uint_as_float(all);
+      }
       Pair Sp[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);
@@ -797,7 +802,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     floatx4 U[4];
     float uunit;
     {
-      const Scale sy = scale_for(Y);
+      const Scale sy = column_scale(Y);
       uunit = sy.down;
       Far Yp[2];
 #pragma unroll
@@ -818,8 +823,8 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     jobs(integral_constant<int, 5>{}, integral_constant<int, 8>{});
     // o, transposed: a lane holds 4 columns of one row
     if constexpr (!ENDS) {
-      const Scale su = scale_for(U);
-      const float udown = su.down * uunit;
+      const Scale su = column_scale(U);
+      const floatx4 udown = across(su.down * uunit, g), sdown = across(qdown, g);
       const floatx4 pdown = *reinterpret_cast<const floatx4*>(scal + kPDown);
       FarSum y[4];
 #pragma unroll
@@ -836,8 +841,8 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) {
         const int p = 16 * tau + i;
-        const float os = scal[kOScale + p], since = os * scal[kSince + p] * qdown;
-        const floatx4 z = since * qs[tau] + (os * (udown * pdown[tau])) * y[tau].all();
+        const float os = scal[kOScale + p], since = os * scal[kSince + p];
+        const floatx4 z = since * (sdown * qs[tau]) + (os * pdown[tau]) * (udown * y[tau].all());
         if constexpr (!KEEP) {
           const float z4[4] = {z[0], z[1], z[2], z[3]};
           held[tau] = Frag<T, 4>::from_f32(z4);
@@ -859,7 +864,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     {
 #pragma unroll
       for (int tau = 0; tau < 4; ++tau) U[tau] *= row4(kUntil, tau);
-      uint32_t ubits = wave_max_bits(max_of(U));
+      uint32_t ubits = column_max_bits(max_of(U));
       const uint32_t least = __float_as_uint(__uint_as_float(top) * unit / uunit * 0x1p-60f);
       ubits = max(ubits, min(least, 0x7f000000u));
       Scale su = scale_of(ubits);
@@ -930,7 +935,7 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
     if (map) {   // a lane has a column of M: a row of the image of M^T, 8 neighbouring columns from two tiles
       _Float16* to = maps + ((size_t)part.slot * a.H + h) * map_halfs(DK);
       const int m = 16 * (cg - groups) + i;
-      const Scale sc = scale_of(column_max_bits(max_of(S)));
+      const Scale sc = column_scale(S);
       if (g == 0) reinterpret_cast<float*>(to + 2 * DK * DK)[m] = sc.down * unit;
 #pragma unroll
       for (int t = 0; t < KB; ++t) {
@@ -993,7 +998,7 @@ __global__ __launch_bounds__(256) void k_delta_join(Args a, float* ends, const _
     if constexpr (!BACK)
 #pragma unroll
       for (int t = 0; t < ST; ++t) S[t] *= F[t];
-    const Scale sc = scale_for(S);
+    const Scale sc = column_scale(S);
     Pair Sp[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) Sp[kb] = split(S[2 * kb], S[2 * kb + 1], sc.up);

@@ -230,3 +230,35 @@ def test_rows_before_a_large_one(sla, dtype, lengths):
     for name, got, ref in gradients(sla, c):
         if name == "dv":
             close_rows(got, ref, dtype, name, np.arange(c.n) > at)
+
+
+# ------------------------------------------------------------------ columns of many sizes
+def close_columns(got, ref, dtype, name):
+    """Every head's columns, each held to its own largest."""
+    for h in range(ref.shape[1]):
+        for j in range(ref.shape[-1]):
+            close(got[:, h, ..., j], ref[:, h, ..., j], dtype, f"{name} of head {h}, column {j}")
+
+
+@pytest.mark.parametrize("lengths", [[150, 0, 64], [1700, 70]])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(32, 32), (64, 80), (128, 48)])
+def test_columns_of_many_sizes(sla, dk, dv, dtype, lengths):
+    """Value columns do not mix: columns 10^10 times as large or as small as their neighbours, in v, the states,
+    dout and their gradients, each as good as alone."""
+    c = Case(lengths, 1, 2, dk, dv, dtype, seed=34, state=True, grads=True)
+    for x in (c.v, c.dout):
+        x[:, 0, 5] *= 1e10
+        x[:, 0, 17] *= 1e-10
+        x[:, 1, 6] *= 1e5
+    for x in (c.state, c.dstate):
+        x[:, 0, :, 5] *= 1e10
+        x[:, 0, :, 17] *= 1e-10
+        x[:, 1, :, 9] *= 1e10
+    o, st = c.forward(sla)
+    ro, rs = c.forward_ref()
+    close_columns(o, ro, dtype, "o")
+    close_columns(st, rs, "f32", "state")
+    for name, got, ref in gradients(sla, c):
+        if name in ("dv", "dstate_in"):
+            close_columns(got, ref, out_type(c, name), name)
