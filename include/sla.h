@@ -466,8 +466,9 @@ sla_status_t sla_backward_xca_noalloc(const void* plan, size_t plan_bytes, int64
  * sums fp64; operands of the matrix cores hold 22 bits and more (two fp16 terms; a 16-bit input is
  * held exactly down to 2^-17 of its row's largest value; rows of a chunk that differ in size have 22
  * bits down to 2^-27 of the largest, an error of 2^-49 of it below; value columns and heads share nothing).
- * A key's or query's own scale ends at 2^-60: entries below 2^-74 lose bits, below 2^-85 all.  o must not be an input.  A value that is
- * not finite reaches only its own window (v's, only its own head and column).  Deterministic.
+ * A key's or query's own scale ends at 2^-60: rows whose largest entry is smaller lose bits, and all of them
+ * at 2^-85.  o must not be an input.  A value that is not finite reaches only its own window (v's, only its
+ * own head and column).  Deterministic.
  */
 size_t sla_delta_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t heads_qk,
                                  int32_t heads, int32_t dim_k, int32_t dim_v);
@@ -484,7 +485,9 @@ sla_status_t sla_forward_delta(const int32_t* offsets, int64_t n, int32_t num_wi
  * given dout = dL/do and dstate_out = dL/d(state_out) (NULL: zero), writes dq, dk (summed over the
  * value heads that share them, in head order), dv in `dtype`, dg, dbeta (fp32 [n, heads]) and, if not
  * NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  Rows in no window are left as they were.
- * The gradient of a log decay below -104, whose exp underflows, is zero.  States are made again from the inputs.
+ * The gradient of a log decay below -104, whose exp underflows, is zero; dg is a difference of sums of
+ * o . dout and v . dv over up to 64 rows, exact to 1e-5 of their largest |o| |dout| + |v| |dv| and not of
+ * itself where a fast decay makes it far smaller.  States are made again from the inputs.
  * Other arguments, limits and errors as sla_forward_delta; the outputs must not be inputs.
  * `workspace` (256-byte aligned) has at least sla_delta_backward_workspace_bytes(...) bytes:
  * the states and their gradients at every 64th row are most of it.  Deterministic.

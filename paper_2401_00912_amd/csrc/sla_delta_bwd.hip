@@ -13,7 +13,9 @@
 // The decay's gradient needs no products of its own: dg_t is the inner product of the decayed state
 // and its gradient, and from one row to the next these differ by vectors that are at hand,
 //     dg_t = dg_{t+1} + o_t . do_t - v_t . dv_t,   and at a chunk's first row dg = <dS0, S0>,
-// which starts the sum anew in every chunk, so that it never runs over more than 64 rows.
+// which starts the sum anew in every chunk, so that it never runs over more than 64 rows; it is fp64.  What
+// is left is the error of its fp32 terms: dg is as exact as the chunk's |o . do| and |v . dv| are, however
+// small it is beside them (with a fast decay it is exp(g) times as large).
 //
 // Four launches: T, P and their transposes (k_delta_prep); the forward walk, which keeps the states
 // before every chunk, r and o . do (k_delta_walk); the walk back, which keeps lam and the gradients
@@ -361,7 +363,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
   __shared__ __attribute__((aligned(16))) float s_scale[3][kChunk];   // of do, mu', u' of every row
   __shared__ __attribute__((aligned(16))) float s_scal[kScal];
   __shared__ double s_gam[kChunk];
-  __shared__ float s_dot[kChunk];
+  __shared__ double s_dot[kChunk];
 
   const uint32_t slot = blockIdx.x;
   const int hk = blockIdx.y;
@@ -456,7 +458,8 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
     for (int x = 0; x < (FOR_K ? 2 : 1); ++x)
 #pragma unroll
       for (int j = 0; j < 4; ++j) M[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    float lr = 0.f, vdv = 0.f;
+    float lr = 0.f;
+    double vdv = 0.;
 
     for (int c0 = 0; c0 < a.dv; c0 += kBlockCols) {
       if (DK == 32 && c0 > 0) ask(c0);
@@ -470,15 +473,16 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
         xu[e] = here ? write * rr[e] : 0.f;
       }
       if constexpr (FOR_K) {
-        float xv[8], xd[8];
+        float xv[8], xd[8], dot = 0.f;
         Frag<T, 8>::to_f32(rv, xv);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           xm[e] = here ? be * rl[e] : 0.f;
           lr += here ? rl[e] * rr[e] : 0.f;
           xd[e] = vs * xm[e];
-          vdv += here ? xv[e] * xd[e] : 0.f;
+          dot += here ? xv[e] * xd[e] : 0.f;
         }
+        vdv += dot;
         if (here) *reinterpret_cast<Raw<T, 8>*>(dv + row0 + col) = Frag<T, 8>::from_f32(xd);
       }
       const Scale so = scale_of(column_max_bits(max8(xo))), su = scale_of(column_max_bits(max8(xu)));
@@ -642,19 +646,19 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
     vdv += __shfl_xor(vdv, 32);
     if (g == 0) {
       if (real) dbeta[(size_t)orig * a.H + h] = lr / vs / s_scal[kVScale + own];
-      float od = 0.f;
+      double od = 0.;
       for (int c = 0; c < groups; ++c) od += real ? odo[(sh * groups + c) * kChunk + own] : 0.f;
-      s_dot[own] = real ? od - vdv : 0.f;
+      s_dot[own] = real ? od - vdv : 0.;
     }
     __syncthreads();
     if (wave == 0) {
-      float x = s_dot[lane];
+      double x = s_dot[lane];
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {   // sums to the end
-        const float y = __shfl_down(x, d);
+        const double y = __shfl_down(x, d);
         if (lane + d < 64) x += y;
       }
-      float at_end = 0.f;
+      double at_end = 0.;
       if (more || has_dstate) {
         const size_t from = more ? sh + a.H : sh;
         for (int c = 0; c < groups; ++c) at_end += start[from * groups + c];
@@ -665,7 +669,7 @@ __global__ __launch_bounds__(256, DK == 32 ? 3 : 2) void k_delta_grad(Args a, co
         const size_t at = (size_t)row_at(a, base + lane) * a.H + h;
         // nothing to decay: a decay that forgets everything, the first row without a state
         const bool none = gin[at] < -104.f || (slot == f && lane == 0 && !has_state);
-        dg[at] = none ? 0.f : x + at_end;
+        dg[at] = none ? 0.f : (float)(x + at_end);
       }
     }
   }

@@ -262,3 +262,23 @@ def test_columns_of_many_sizes(sla, dk, dv, dtype, lengths):
     for name, got, ref in gradients(sla, c):
         if name in ("dv", "dstate_in"):
             close_columns(got, ref, out_type(c, name), name)
+
+
+# ------------------------------------------------------------------ gradients of fast decays
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("g", [-1.0, -8.0, -20.0])
+def test_gradients_of_fast_decays(sla, dtype, g):
+    """Heads that forget fast all along: dg is e^g times what it is summed from, and is held to the bound that the
+    interface gives, 1e-5 of the head's own largest |o| |dout| + |v| |dv|, and to nothing of another head."""
+    import torch
+
+    c = Case([300, 70], 1, 2, 64, 64, dtype, seed=40, state=True, grads=True)
+    c.g[:, 0] = g
+    c.g[:, 1] = g * (0.5 + torch.rand(c.n, generator=torch.Generator().manual_seed(1)))
+    c.dout[:, 1] /= 1024
+    c.dstate[:, 1] /= 1024
+    ref = {name: (got.double().cpu().numpy(), want) for name, got, want in gradients(sla, c)}
+    norm = lambda x: np.sqrt((x ** 2).sum(-1))  # noqa: E731
+    bound = norm(c.forward_ref()[0]) * norm(c.wide("dout")) + norm(c.wide("v")) * norm(ref["dv"][1])
+    worst = np.abs(ref["dg"][0] - ref["dg"][1]).max(0) / (FP32_BAR * bound.max(0))
+    assert (worst <= 1).all(), worst
