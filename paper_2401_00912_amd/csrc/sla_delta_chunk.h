@@ -511,10 +511,15 @@ __device__ __forceinline__ Place place_of(const Args& a, int lane) {
 __host__ __device__ inline size_t part_slots(const Args& a) {
   return a.part == 0 ? (size_t)a.W : (size_t)(a.n / (a.part * kChunk)) + a.W;
 }
-// Parts of 8 to 32 chunks where that gives the chip some 512 workgroups of 64 columns; none where the
-// windows do by themselves, or where they are short (256 rows on average).  Forward, no parts and parts of
-// 8, 16 and 32 chunks: 7 bf16 windows with 12,289 rows in all, 8 heads of 128: 346 us and 165, 192, 235;
-// 1 fp32 window of 8,191 rows, 4 heads of 64: 459 us and 88, 124, 208.
+// Parts of 8 to 32 chunks where that gives the chip some 512 workgroups of 64 columns; none where windows have
+// under 256 rows on average, or where even parts of 32 chunks would be more than those 512 (n H dv / 64 over
+// 2^20).  Forward, no parts and parts of 8, 16 and 32 chunks: 7 bf16 windows with 12,289 rows in all, 8 heads
+// of 128: 346 us and 165, 192, 235; 1 fp32 window of 8,191 rows, 4 heads of 64: 459 us and 88, 124, 208.  The
+// aim is not sharp: one bf16 window of 16,384 rows, 16 heads of 128, with 256, 512 and 1,024 workgroups 405,
+// 431 and 411 us, gradients 1,616, 1,596 and 1,537.  Both bounds know the windows by their sum alone, and few
+// long windows past them are a chain that the chip waits for: 16 heads of 128 bf16 in one window, 32,768 rows
+// (parts) 855 us and gradients 3,025, 32,769 rows (none) 2,267 and 7,039, with parts 717 and 2,652; 16,000 rows
+// 346 and 1,384, with 100 windows of 60 rows beside them (no parts) 1,548 and 4,761.
 inline int part_chunks(int64_t n, int32_t W, int32_t H, int32_t dv) {
   const int64_t blocks = (int64_t)H * ((dv + 63) / 64), most = (n * blocks + 512 * kChunk - 1) / (512 * kChunk);
   const int64_t part = most < 8 ? 8 : most;
@@ -1056,12 +1061,13 @@ inline int walk_waves(const Args& a) {
   if (groups <= 4 || sizeof(T) == 4) return 4;
   return (int64_t)part_slots(a) * a.H * ((groups + 7) / 8) > 128 ? 8 : 4;
 }
-// Whether the walks stage a chunk ahead.  Not where three workgroups a CU and more are there to wait for
-// each other and the second buffer would keep some of them off it, which is at 32 state rows: 60,000 fp16
-// rows, 4 heads of 32, with and without, forward and gradients: windows of 40 rows 136 + 452 and 115 + 432
-// us, 128: 87 + 301 and 78 + 279, 256: 87 + 307 and 81 + 289; but 24,000 bf16 rows, 8 heads of 128: windows
-// of 40 238 + 1,190 and 240 + 1,194, 256: 163 + 859 and 188 + 878.
-inline bool walks_ahead(dim3 grid) { return (int64_t)grid.x * grid.y * grid.z < 768; }
+// Whether the walks stage a chunk ahead.  Not where two workgroups a CU and more are there to wait for
+// each other and the second buffer would keep some of them off it, which is at 32 state rows: fp16 windows of
+// 256 rows, 4 heads of 32, with and without, forward and gradients: 384 workgroups 51 + 150 and 54 + 153 us,
+// 512: 69 + 199 and 59 + 175, 768: 80 + 269 and 74 + 249, 1,536: 157 + 525 and 153 + 508 (fp32, 768: 117 + 382
+// and 91 + 329); but 24,000 bf16 rows, 8 heads of 128: windows of 40 238 + 1,190 and 240 + 1,194, 256: 163 + 859
+// and 188 + 878.
+inline bool walks_ahead(dim3 grid) { return (int64_t)grid.x * grid.y * grid.z < 512; }
 // f(integral_constant<waves>, bool_constant<ahead>, grid)
 template <typename T, int DK, class F>
 inline void with_walk(const Args& a, F f) {
