@@ -13,13 +13,14 @@
 // Two-term operands.  The matrix cores' 16-bit products are 16 times as fast as their fp32 ones,
 // and one 16-bit rounding of a state loses what fp32 states are kept for.  So an fp32 operand is
 // scaled by a power of two and split into two fp16 terms, x = hi + lo (22 bits), and a product is
-// the sum of hi hi, hi lo and lo hi in fp32.  (With values under 2^-16 of the largest the second term runs
-// out of fp16's least steps, and one of 2^-38 is lost.  That is no loss in a sum that the largest one is in
-// too.  But T, P and what they are multiplied with hold rows that have nothing to do with each other, early
-// ones and a late one a billion times as large: there x = hi + 2^-11 lo, with the products of the second
-// terms summed by themselves, 22 bits down to 2^-27 of the largest and none at 2^-49.)  A 16-bit input needs no second term: its row is
-// scaled by a power of two that puts the row's largest value into [1, 2), and then fp16 holds
-// fp16 and bf16 values exactly down to 2^-17 of the row's largest (below that, to 2^-25 of it).
+// the sum of hi hi, hi lo and lo hi in fp32.  With values under 2^-16 of the largest the second term
+// runs out of fp16's least steps, and one of 2^-38 is lost.  That is no loss in a sum that the largest
+// one is in too.  But T, P and what they are multiplied with hold rows that have nothing to do with each
+// other, early ones and a late one a billion times as large: there x = hi + 2^-11 lo, with the products
+// of the second terms summed by themselves, 22 bits down to 2^-27 of the largest and none at 2^-49.
+// A 16-bit input needs no second term: its row is scaled by a power of two that puts the row's largest
+// value into [1, 2), and then fp16 holds fp16 and bf16 values exactly down to 2^-17 of the row's largest
+// (below that, to 2^-25 of it).
 // With k = 2^kap k' and q = 2^rho q' the rule reads the same for k', u' = 2^kap u, o' = 2^-rho o and
 // r' = s r with any s of a row's own:
 //     r' = T' (s v - t exp(gam) k' S0),   t = 2^kap s,   u' = (b / t) r',   b = 2^(2 kap) beta,

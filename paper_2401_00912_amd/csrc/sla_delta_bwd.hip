@@ -65,7 +65,7 @@ BackSpace back_space(int64_t n, int32_t W, int dtype, int32_t Hk, int32_t H, int
 
 // ------------------------------------------------------------------ the walk back
 // As k_delta_walk: a wave holds 16 columns of the state's gradient in registers.
-// Bound by the chain like it: 16,381 bf16 rows, 9 sequences, 8 heads of 128: 146 us behind 120 for the
+// Bound by the chain like it: 16,381 bf16 rows, 9 sequences, 8 heads of 128: 147 us behind 127 for the
 // parts' gradients; 1,521 fp16 windows: 85 us.
 // ENDS: only the state gradients at the parts' starts, from none at their ends (the last part: from dstate).
 template <typename T, int DK, int NW>
@@ -299,10 +299,11 @@ __global__ __launch_bounds__(64 * NW) void k_delta_back(Args a, const T* __restr
 // and four lane groups over the columns, and makes the transposed tiles: a lane ends with 8
 // neighbouring columns of its row.  The value columns go by in blocks of 32, the next block's loads in
 // flight (not at 32 state rows, where a third workgroup a CU is worth more than they are).  dq and dk are launches of their own (FOR_K; dv, dbeta and dg come with dk): together they
-// took twice the registers and waited for memory at one workgroup a CU.  Bound by the waits of two (dk)
-// to four workgroups a CU: 16,381 bf16 rows, 8 heads of 128: 74 and 170 us (together: 426); 1,521 fp16
-// windows, 4 heads of 32: 58 and 152 us (together: 228).  Eight waves, four for dq and four for dk:
-// 345 and 366.
+// took twice the registers and waited for memory at one workgroup a CU.  Bound by the waits of the workgroups
+// that a CU holds, for dk one at 128 state rows (90 KB of LDS), two at 64 and three at 32: 16,381 bf16 rows, 8
+// heads of 128: 86 and 269 us; 1,521 fp16 windows, 4 heads of 32: 60 and 154 us.  Measured before the present
+// operands, one launch for both: 426 and 228 us where two took 244 and 210; eight waves, four for dq and four
+// for dk: 345 and 366.
 //
 // Computed operands (states, mu, u, the products over columns) have two fp16 terms whatever the rows'
 // type: with one, 2^-11 of the largest value, small entries of dq and dk were off by many of their own

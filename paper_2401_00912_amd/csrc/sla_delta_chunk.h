@@ -21,8 +21,8 @@ constexpr int kLd = 68;   // floats a row of a 64 x 64 matrix in LDS: 16-byte ro
 // I + [beta_i D_ij k_i . k_j], whose rows and not columns carry beta.
 //
 // Chunks are independent here, so a batch is bound by memory: 65,536 bf16 rows, 16 heads of 128, in
-// 306 us, 1.4 GB, 4.7 TB/s (a copy reaches 5.2).  Windows of one chunk are bound by the steps between
-// the barriers, some 10 us a workgroup: 1,521 fp16 windows (59,837 rows, 4 heads of 32) in 74 us, 138
+// 326 us, 1.5 GB, 4.7 TB/s (a copy reaches 5.2).  Windows of one chunk are bound by the steps between
+// the barriers, some 10 us a workgroup: 1,521 fp16 windows (59,837 rows, 4 heads of 32) in 79 us, 148
 // with REV.  The inverse is made here and not in the walk because there it would be part of the chain
 // from chunk to chunk.
 struct PrepShared {
@@ -367,10 +367,11 @@ __global__ __launch_bounds__(256, 3) void k_delta_prep(Args a, const T* __restri
 // one's chunk is worked on, with one barrier a chunk.  fp32 rows of dk = 128 do not fit twice and are
 // staged between two barriers.
 //
-// Bound by the chain: some 4.5 us a chunk of 128 x 128 states with eight waves a workgroup, whatever else
-// the chip does.  65,536 bf16 rows, 33 uneven sequences, 16 heads: 588 us, the longest sequence's chunks
-// one after the other (1.4 GB, 2.4 TB/s); 12,289 rows cut into parts: 48 us behind 90 for the parts'
-// states; 1,521 fp16 windows of a chunk or two: 60 us, where a workgroup waits for its only chunk.
+// Bound by the chain: some 5 us a chunk of 128 x 128 states with eight waves a workgroup, whatever else
+// the chip does.  65,536 bf16 rows, 33 uneven sequences, 16 heads: 580 to 815 us with the sequences' lengths,
+// the longest one's chunks one after the other; 12,289 rows cut into parts: 57 us behind 95 for the parts'
+// states; 1,521 fp16 windows of a chunk or two: 61 us, where a workgroup waits for its only chunk.  With one
+// term for bf16 rows' outputs and one power of two for 16 columns the batch's walk took 486 to 725 us.
 struct WalkOut {
   float* state_out;    // final states or null
   float* states;       // the states before every chunk [slot][H][dv / 16], in register order, or null
@@ -490,7 +491,7 @@ __device__ __forceinline__ Part part_of(const Args& a, uint32_t slot, int lane) 
 // A walk's window (or part) and value head: grid (part slots, heads, column groups).  Where whole windows are
 // walked in more workgroups than there are CUs, the longest windows' heads come first, so that none is left
 // alone at the end: a lane a window, up to 64.  65,536 bf16 rows, 33 uneven sequences, 16 heads of 128: 588 us
-// so, 758 in the order of the windows.
+// so, 758 in the order of the windows (measured together, before the present operands).
 struct Place {
   Part part;
   int h;
@@ -965,8 +966,8 @@ __global__ __launch_bounds__(64 * NW) void k_delta_walk(Args a, const T* __restr
 // ------------------------------------------------------------------ the parts' states joined
 // A wave for 16 columns of a window's states: after the first part's end, which is there, S = M S + Z part
 // after part, each written over its Z.  BACK: from the last part's start to the second one's, with M^T.
-// A chain of products with 64 KB of M a step (at 128 x 128), moved ahead into LDS: 31 us for 7 windows
-// with 12,289 rows in all, 18 us for the 16 parts of a window at 64 x 64, 1.2 us a step.
+// A chain of products with 64 KB of M a step (at 128 x 128), moved ahead into LDS: 34 us for 7 windows
+// with 12,289 rows in all, 20 us for the 16 parts of a window at 64 x 64, 1.3 us a step.
 template <int DK, bool BACK>
 __global__ __launch_bounds__(256) void k_delta_join(Args a, float* ends, const _Float16* __restrict__ maps) {
   constexpr int ST = DK / 16, KB = DK / 32, kMap = 2 * DK * DK;   // halfs in LDS
