@@ -564,6 +564,56 @@ sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t n, int32_t 
                                      float* dbias, void* workspace, size_t workspace_bytes,
                                      sla_stream_t stream);
 
+/*
+ * The short causal convolution, channel by channel, that stands before a recurrent attention or a
+ * state space scan.  For the rows t = 0, 1, .. of window w,
+ *     y_t = act(bias + sum_{j < width} weight[c][j] x_{t - width + 1 + j}),
+ * where x_{-width + 1} .. x_{-1} are the rows of state_in[w], oldest first (zero if state_in is NULL), and
+ * state_out[w] (if not NULL) receives the window's last width - 1 inputs in that form.
+ *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.
+ *   x         [n, channels] in `dtype`, rows x_stride elements apart (>= channels; columns of a wider
+ *             array do);  y [n, channels], contiguous.  16-byte aligned rows (channels, strides and
+ *             addresses) are fastest, none of it is required.  channels up to 65,536.
+ *   weight    fp32 [channels, width], width 2 .. 8, else SLA_E_UNSUPPORTED;  bias fp32 [channels] or NULL.
+ *   states    [num_windows, width - 1, channels] in `dtype`.  state_out must not be state_in, nor y x.
+ * Sums and activations are fp32, y is rounded once.  A value that is not finite reaches only the rows whose
+ * sums it is in.  Rows in no window are left as they were.  Deterministic.
+ */
+sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order,
+                                    sla_dtype_t dtype, int32_t channels, int32_t width,
+                                    sla_activation_t activation, const void* x, int64_t x_stride,
+                                    const float* weight, const float* bias, const void* state_in, void* y,
+                                    void* state_out, sla_stream_t stream);
+
+/*
+ * Backward of sla_forward_short_conv: given dy = dL/dy (rows dy_stride elements apart) and dstate_out
+ * (NULL: zero), writes dx [n, channels] and, if not NULL, dstate_in, both in `dtype`, and dweight, dbias
+ * (fp32, sums over all rows in windows in a fixed order; dbias may be NULL).  relu's slope at 0 is 0.
+ * `workspace`: device, 256-byte aligned, sla_short_conv_backward_workspace_bytes() bytes (0 for sizes
+ * that are not supported), else SLA_E_WORKSPACE.  The outputs must not be inputs.
+ */
+size_t sla_short_conv_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                               int32_t channels, int32_t width);
+
+sla_status_t sla_backward_short_conv(const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order,
+                                     sla_dtype_t dtype, int32_t channels, int32_t width,
+                                     sla_activation_t activation, const void* x, int64_t x_stride,
+                                     const float* weight, const float* bias, const void* state_in,
+                                     const void* dy, int64_t dy_stride, const void* dstate_out, void* dx,
+                                     float* dweight, float* dbias, void* dstate_in, void* workspace,
+                                     size_t workspace_bytes, sla_stream_t stream);
+
+/*
+ * The short convolution one row at a time: `state` is a pool [num_slots, width - 1, channels] in `dtype`,
+ * row b of the batch belongs to the sequence in slot slots[b], whose state moves on by one row in place.
+ * Slots as in sla_step_delta (rows of the same slot follow each other, a slot outside the pool marks a
+ * padding row, n up to 65,536).
+ */
+sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
+                                 int32_t channels, int32_t width, sla_activation_t activation, void* state,
+                                 const void* x, int64_t x_stride, const float* weight, const float* bias, void* y,
+                                 sla_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

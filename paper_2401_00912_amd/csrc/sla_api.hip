@@ -78,6 +78,18 @@ hipError_t launch_backward_delta(const int32_t* offsets, int32_t n, int32_t W, c
 hipError_t launch_step_delta(const int32_t* slots, int32_t n, int32_t num_slots, int dtype, int32_t Hk, int32_t H,
                              int32_t dk, int32_t dv, float scale, float* state, const void* q, const void* k,
                              const void* v, const float* g, const float* beta, void* o, hipStream_t stream);
+size_t conv_backward_workspace_bytes(int64_t n, int dtype, int32_t C, int32_t K);
+hipError_t launch_forward_conv(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype, int32_t C,
+                               int32_t K, int activation, const void* x, int64_t ldx, const float* weight,
+                               const float* bias, const void* state_in, void* y, void* state_out, hipStream_t stream);
+hipError_t launch_backward_conv(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype, int32_t C,
+                                int32_t K, int activation, const void* x, int64_t ldx, const float* weight,
+                                const float* bias, const void* state_in, const void* dy, int64_t lddy,
+                                const void* dstate_out, void* dx, float* dweight, float* dbias, void* dstate_in,
+                                void* workspace, hipStream_t stream);
+hipError_t launch_step_conv(const int32_t* slots, int32_t n, int32_t num_slots, int dtype, int32_t C, int32_t K,
+                            int activation, void* state, const void* x, int64_t ldx, const float* weight,
+                            const float* bias, void* y, hipStream_t stream);
 }  // namespace sla
 
 namespace {
@@ -668,4 +680,102 @@ SLA_EXPORT sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t 
   return hip_status(sla::launch_backward_group_norm(offsets, (int32_t)n, num_windows, (int)dtype, channels, groups,
                                                     (int)activation, x, weight, bias, dy, mean, rstd, dx, dweight,
                                                     dbias, workspace, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// Sizes that the operators over rows in order share; also bounds their grids (blocks of rows, windows or
+// slots in x; HIP bounds a grid at 2^32 - 1 threads there).
+sla_status_t check_row_sizes(int64_t n, int32_t W, int dtype, int32_t channels) {
+  if (!sizes_ok(n, W) || channels < 1) return SLA_E_ARG;
+  if (dtype < 0 || dtype > 2) return SLA_E_ARG;
+  if (channels > 65536) return SLA_E_UNSUPPORTED;
+  if (n / 64 + (int64_t)W > UINT32_MAX / 512) return SLA_E_UNSUPPORTED;
+  return SLA_OK;
+}
+
+sla_status_t check_conv_sizes(int64_t n, int32_t W, int dtype, int32_t channels, int32_t width) {
+  const sla_status_t st = check_row_sizes(n, W, dtype, channels);
+  if (st != SLA_OK) return st;
+  return width < 2 || width > 8 ? SLA_E_UNSUPPORTED : SLA_OK;
+}
+
+// rows of `values` values each, `ld` apart
+bool rows_ok(const void* p, int64_t n, int64_t ld, int64_t values, uintptr_t esize) {
+  return n == 0 || (p != nullptr && aligned(p, esize) && (n == 1 || ld >= values));
+}
+
+}  // namespace
+
+SLA_EXPORT sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                               const int32_t* order, sla_dtype_t dtype, int32_t channels, int32_t width,
+                                               sla_activation_t activation, const void* x, int64_t x_stride,
+                                               const float* weight, const float* bias, const void* state_in, void* y,
+                                               void* state_out, sla_stream_t stream) {
+  const sla_status_t st = check_conv_sizes(n, num_windows, (int)dtype, channels, width);
+  if (st != SLA_OK) return st;
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2;
+  if ((int)activation < SLA_ACT_NONE || (int)activation > SLA_ACT_SILU) return SLA_E_ARG;
+  if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !weight || !aligned(weight, 4) || !aligned(bias, 4) ||
+      !aligned(state_in, es) || !aligned(state_out, es))
+    return SLA_E_ARG;
+  if (!rows_ok(x, n, x_stride, channels, es) || !rows_ok(y, n, channels, channels, es)) return SLA_E_ARG;
+  if (state_out != nullptr && state_out == state_in) return SLA_E_ARG;
+  if (n > 0 && x == y) return SLA_E_ARG;
+  if (n == 0 && !state_out) return SLA_OK;
+  return hip_status(sla::launch_forward_conv(offsets, (int32_t)n, num_windows, order, (int)dtype, channels, width,
+                                             (int)activation, x, x_stride, weight, bias, state_in, y, state_out,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT size_t sla_short_conv_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                                          int32_t channels, int32_t width) {
+  if (check_conv_sizes(n, num_windows, (int)dtype, channels, width) != SLA_OK) return 0;
+  return sla::conv_backward_workspace_bytes(n, (int)dtype, channels, width);
+}
+
+SLA_EXPORT sla_status_t sla_backward_short_conv(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                                const int32_t* order, sla_dtype_t dtype, int32_t channels,
+                                                int32_t width, sla_activation_t activation, const void* x,
+                                                int64_t x_stride, const float* weight, const float* bias,
+                                                const void* state_in, const void* dy, int64_t dy_stride,
+                                                const void* dstate_out, void* dx, float* dweight, float* dbias,
+                                                void* dstate_in, void* workspace, size_t workspace_bytes,
+                                                sla_stream_t stream) {
+  const sla_status_t st = check_conv_sizes(n, num_windows, (int)dtype, channels, width);
+  if (st != SLA_OK) return st;
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2;
+  if ((int)activation < SLA_ACT_NONE || (int)activation > SLA_ACT_SILU) return SLA_E_ARG;
+  if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !weight || !aligned(weight, 4) || !aligned(bias, 4) ||
+      !aligned(state_in, es) || !aligned(dstate_out, es) || !aligned(dstate_in, es) || !dweight ||
+      !aligned(dweight, 4) || !aligned(dbias, 4))
+    return SLA_E_ARG;
+  if (!rows_ok(x, n, x_stride, channels, es) || !rows_ok(dy, n, dy_stride, channels, es) ||
+      !rows_ok(dx, n, channels, channels, es))
+    return SLA_E_ARG;
+  if ((n > 0 && (dx == x || dx == dy)) || (dstate_in != nullptr && (dstate_in == state_in || dstate_in == dstate_out)))
+    return SLA_E_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  if (workspace_bytes < sla::conv_backward_workspace_bytes(n, (int)dtype, channels, width)) return SLA_E_WORKSPACE;
+  return hip_status(sla::launch_backward_conv(offsets, (int32_t)n, num_windows, order, (int)dtype, channels, width,
+                                              (int)activation, x, x_stride, weight, bias, state_in, dy, dy_stride,
+                                              dstate_out, dx, dweight, dbias, dstate_in, workspace,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
+                                            int32_t channels, int32_t width, sla_activation_t activation, void* state,
+                                            const void* x, int64_t x_stride, const float* weight, const float* bias,
+                                            void* y, sla_stream_t stream) {
+  const sla_status_t st = check_conv_sizes(n, num_slots, (int)dtype, channels, width);
+  if (st != SLA_OK) return st;
+  if (n > 65536) return SLA_E_UNSUPPORTED;   // each row's workgroups look through the slots of all rows
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2;
+  if ((int)activation < SLA_ACT_NONE || (int)activation > SLA_ACT_SILU) return SLA_E_ARG;
+  if (n == 0) return SLA_OK;
+  if (!slots || !aligned(slots, 4) || !state || !aligned(state, es) || !weight || !aligned(weight, 4) ||
+      !aligned(bias, 4) || !rows_ok(x, n, x_stride, channels, es) || !rows_ok(y, n, channels, channels, es) || x == y)
+    return SLA_E_ARG;
+  return hip_status(sla::launch_step_conv(slots, (int32_t)n, num_slots, (int)dtype, channels, width, (int)activation,
+                                          state, x, x_stride, weight, bias, y, static_cast<hipStream_t>(stream)));
 }

@@ -22,6 +22,7 @@
 // vectors' means and squares one by one, threads and blocks are joined around the common mean.
 #include <algorithm>
 
+#include "sla_act.h"
 #include "sla_common.h"
 
 namespace sla {
@@ -29,40 +30,6 @@ namespace {
 
 constexpr int kThreads = 256, kWavesN = 4;
 constexpr int kMaxVectors = 1024;          // channels / 4 at most
-
-enum Act { kNone = 0, kRelu = 1, kSilu = 2 };
-
-// 1 / (1 + e^-z) for -87 <= z <= 87 from the hardware's 2^x and 1 / x (each within one step): -z log2 e in two
-// terms, so that a large exponent loses nothing.  With expf and a division the activation took more time than
-// the memory (240,011 x 256 bf16 values: 56 us, 47 for the bytes).
-__device__ __forceinline__ float sigmoid(float z) {
-  constexpr float kHi = -1.44269502f, kLo = -1.92596299e-8f;   // -log2 e
-  const float t = z * kHi;
-  const float r = __builtin_fmaf(z, kHi, -t) + z * kLo;
-  const float e = __builtin_amdgcn_exp2f(t);
-  return __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, r * 0.693147181f, e));
-}
-// z between its bounds; a NaN stays one.  silu and its slope take the bounded z as their factor too: what the
-// sigmoid ends at below, 1.6e-38, is none for a z of -1e38.
-__device__ __forceinline__ float from_below(float z) { return __builtin_elementwise_maximum(z, -87.f); }
-__device__ __forceinline__ float from_above(float z) { return __builtin_elementwise_minimum(z, 87.f); }
-__device__ __forceinline__ float act(int a, float z) {
-  if (a == kRelu) return z > 0.f ? z : (z != z ? z : 0.f);
-  if (a == kSilu) {
-    z = from_below(z);
-    return z * sigmoid(from_above(z));
-  }
-  return z;
-}
-__device__ __forceinline__ float slope(int a, float z) {
-  if (a == kRelu) return z > 0.f ? 1.f : 0.f;
-  if (a == kSilu) {
-    z = from_above(from_below(z));
-    const float s = sigmoid(z);
-    return s * (1.f + z * (1.f - s));
-  }
-  return 1.f;
-}
 
 struct NormArgs {
   const int32_t* offsets;   // null: every row is a window

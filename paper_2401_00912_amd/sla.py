@@ -28,6 +28,10 @@ Functions mirror the C ABI in include/sla.h:
         -> (y, mean, rstd)
     backward_group_norm(x, groups, dy, mean, rstd, weight=None, bias=None, offsets=None, activation="none")
         -> (dx, dweight, dbias)
+    forward_short_conv(x, weight, offsets, bias=None, activation="none", order=None, state=None) -> (y, final_state)
+    backward_short_conv(x, weight, offsets, dy, bias=None, activation="none", order=None, state=None, dstate=None)
+        -> (dx, dweight, dbias, dstate_in)
+    step_short_conv(state, slots, x, weight, bias=None, activation="none") -> y
 """
 from __future__ import annotations
 
@@ -77,6 +81,10 @@ EXPORTED = (
     "sla_forward_group_norm",
     "sla_group_norm_backward_workspace_bytes",
     "sla_backward_group_norm",
+    "sla_forward_short_conv",
+    "sla_short_conv_backward_workspace_bytes",
+    "sla_backward_short_conv",
+    "sla_step_short_conv",
 )
 
 
@@ -181,6 +189,15 @@ def lib() -> ctypes.CDLL:
     L.sla_forward_group_norm.argtypes = [vp, i64, i32, en, i32, i32, f32, en] + [vp] * 7 + [sz, vp]
     L.sla_backward_group_norm.restype = ctypes.c_int
     L.sla_backward_group_norm.argtypes = [vp, i64, i32, en, i32, i32, en] + [vp] * 10 + [sz, vp]
+    L.sla_forward_short_conv.restype = ctypes.c_int
+    L.sla_forward_short_conv.argtypes = [vp, i64, i32, vp, en, i32, i32, en, vp, i64] + [vp] * 6
+    L.sla_short_conv_backward_workspace_bytes.restype = sz
+    L.sla_short_conv_backward_workspace_bytes.argtypes = [i64, i32, en, i32, i32]
+    L.sla_backward_short_conv.restype = ctypes.c_int
+    L.sla_backward_short_conv.argtypes = ([vp, i64, i32, vp, en, i32, i32, en, vp, i64] + [vp] * 4 + [i64] + [vp] * 6
+                                          + [sz, vp])
+    L.sla_step_short_conv.restype = ctypes.c_int
+    L.sla_step_short_conv.argtypes = [vp, i64, i32, en, i32, i32, en, vp, vp, i64] + [vp] * 4
     _lib = L
     return L
 
@@ -859,6 +876,114 @@ def backward_group_norm(x, groups: int, dy, mean, rstd, weight=None, bias=None, 
                                            _ptr(workspace), nbytes, _stream(x.device))
     _check(st, "sla_backward_group_norm")
     return dx, dweight, dbias
+
+
+def _row_stride(name, t, shape, dtype, device):
+    """Elements between the rows of a [n, ...] tensor whose rows are contiguous and do not overlap."""
+    if t.dim() != len(shape) or tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a {tuple(shape)} {dtype} tensor on the inputs' device")
+    n, inner = shape[0], 1
+    for size, stride in zip(t.shape[:0:-1], t.stride()[:0:-1]):
+        if size != 1 and stride != inner:
+            raise ValueError(f"the rows of {name} must be contiguous")
+        inner *= size
+    stride = t.stride(0) if n > 1 else inner
+    if stride < inner:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return stride
+
+
+def _check_activation(activation):
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, not {activation!r}")
+    return ACTIVATIONS[activation]
+
+
+def _conv_check(x, weight, bias, activation):
+    """(n, channels, width, the rows' stride, the activation's code) of a short convolution call."""
+    torch = _torch()
+    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] < 1:
+        raise ValueError("x must be a [n, channels] tensor and weight [channels, width]")
+    n, C = x.shape
+    _check_like("weight", weight, (C, weight.shape[1]), torch.float32, x.device)
+    _check_like("bias", bias, (C,), torch.float32, x.device)
+    return n, C, weight.shape[1], _row_stride("x", x, (n, C), x.dtype, x.device), _check_activation(activation)
+
+
+def forward_short_conv(x, weight, offsets, bias=None, activation="none", order=None, state=None, y=None,
+                       final_state=None):
+    """The short causal convolution over the rows of every window (sla_forward_short_conv): x
+    [n, channels] (columns of a wider tensor will do), weight float32 [channels, width], width 2 to 8,
+    offsets and order as in forward_delta, bias float32 [channels] or None, state
+    [num_windows, width - 1, channels] of x's type (the rows before each window, oldest first) or
+    None (zero).  Returns (y, final_state); rows in no window are left as they were in y."""
+    torch = _torch()
+    n, C, K, ldx, act = _conv_check(x, weight, bias, activation)
+    w = _check_windows(offsets, order, n, x.device)
+    y = torch.empty((n, C), dtype=x.dtype, device=x.device) if y is None else y
+    _check_like("y", y, (n, C), x.dtype, x.device)
+    if final_state is None:
+        final_state = torch.empty((w, max(K - 1, 0), C), dtype=x.dtype, device=x.device)
+    for name, t in (("state", state), ("final_state", final_state)):
+        _check_like(name, t, (w, max(K - 1, 0), C), x.dtype, x.device)
+    with torch.cuda.device(x.device):
+        st = lib().sla_forward_short_conv(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), C, K, act, _ptr(x),
+                                          ldx, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), _ptr(final_state),
+                                          _stream(x.device))
+    _check(st, "sla_forward_short_conv")
+    return y, final_state
+
+
+def short_conv_backward_workspace_bytes(n: int, num_windows: int, dtype, channels: int, width: int) -> int:
+    """Workspace of backward_short_conv (0: unsupported sizes); dtype a torch dtype."""
+    return int(lib().sla_short_conv_backward_workspace_bytes(int(n), int(num_windows), _dtype_code(dtype),
+                                                             int(channels), int(width)))
+
+
+def backward_short_conv(x, weight, offsets, dy, bias=None, activation="none", order=None, state=None, dstate=None,
+                        dx=None, workspace=None):
+    """Gradients of forward_short_conv (sla_backward_short_conv): dy like x, dstate (the gradient of
+    final_state) or None; returns (dx, dweight, dbias, dstate_in), dbias None without a bias and dstate_in
+    None without a state.  Rows in no window are left as they were in dx."""
+    torch = _torch()
+    n, C, K, ldx, act = _conv_check(x, weight, bias, activation)
+    w = _check_windows(offsets, order, n, x.device)
+    lddy = _row_stride("dy", dy, (n, C), x.dtype, x.device)
+    for name, t in (("state", state), ("dstate", dstate)):
+        _check_like(name, t, (w, max(K - 1, 0), C), x.dtype, x.device)
+    dx = torch.empty((n, C), dtype=x.dtype, device=x.device) if dx is None else dx
+    _check_like("dx", dx, (n, C), x.dtype, x.device)
+    dweight = torch.empty_like(weight)
+    dbias = None if bias is None else torch.empty_like(bias)
+    dstate_in = None if state is None else torch.empty_like(state)
+    workspace, nbytes = _own_workspace(short_conv_backward_workspace_bytes(n, w, x.dtype, C, K), workspace, x.device,
+                                       "sla_short_conv_backward_workspace_bytes")
+    with torch.cuda.device(x.device):
+        st = lib().sla_backward_short_conv(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), C, K, act, _ptr(x),
+                                           ldx, _ptr(weight), _ptr(bias), _ptr(state), _ptr(dy), lddy, _ptr(dstate),
+                                           _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate_in), _ptr(workspace),
+                                           nbytes, _stream(x.device))
+    _check(st, "sla_backward_short_conv")
+    return dx, dweight, dbias, dstate_in
+
+
+def step_short_conv(state, slots, x, weight, bias=None, activation="none", y=None):
+    """One row for each of many sequences (sla_step_short_conv): state [num_slots, width - 1, channels]
+    of x's type, moved on in place, slots int32 [n] as in step_delta.  Returns y, where padding rows
+    are left as they were."""
+    torch = _torch()
+    n, C, K, ldx, act = _conv_check(x, weight, bias, activation)
+    if state.dim() != 3 or state.shape[0] < 1:
+        raise ValueError("state must be a [num_slots, width - 1, channels] tensor")
+    _check_like("state", state, (state.shape[0], max(K - 1, 0), C), x.dtype, x.device)
+    _check_like("slots", slots, (n,), torch.int32, x.device)
+    y = torch.empty((n, C), dtype=x.dtype, device=x.device) if y is None else y
+    _check_like("y", y, (n, C), x.dtype, x.device)
+    with torch.cuda.device(x.device):
+        st = lib().sla_step_short_conv(_ptr(slots), n, state.shape[0], _dtype_code(x.dtype), C, K, act, _ptr(state),
+                                       _ptr(x), ldx, _ptr(weight), _ptr(bias), _ptr(y), _stream(x.device))
+    _check(st, "sla_step_short_conv")
+    return y
 
 
 def read_plan(plan: Plan):
