@@ -614,6 +614,55 @@ sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_sl
                                  const void* x, int64_t x_stride, const float* weight, const float* bias, void* y,
                                  sla_stream_t stream);
 
+/*
+ * The selective scan: a state space of `states` values for each channel whose step size, input and output
+ * maps come with every row (a linear attention in recurrent form, like the gated delta rule, whose decay
+ * is its own for every channel and state).  For window w and channel d of group g = d / (channels / groups),
+ * over the window's rows t in order, with the state h at state_in[w][d] (zero if state_in is NULL):
+ *     dt_t = softplus(delta_t + delta_bias)  (delta_softplus 0: delta_t + delta_bias),
+ *     h[s] <- exp(dt_t A[d][s]) h[s] + dt_t x_t B_t[g][s],
+ *     y_t  = (sum_s C_t[g][s] h[s] + skip[d] x_t) z_t / (1 + exp(-z_t)),
+ * and state_out[w][d] (if not NULL) receives the last h.
+ *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.
+ *   x, delta, z  [n, channels], B, C [n, groups, states], in `dtype`: the rows of each contiguous, *_stride
+ *             elements apart (not less than their length; columns of a wider array do).  z may be NULL
+ *             (no gate).  y [n, channels], contiguous, not an input.
+ *   A         fp32 [channels, states], usually < 0;  skip, delta_bias fp32 [channels] or NULL (0).
+ *   states    1 to 64, channels up to 65,536 and at most 65,535 blocks of 64 channels of a group, else
+ *             SLA_E_UNSUPPORTED; channels a multiple of groups.
+ *   states' values  fp32 [num_windows, channels, states].  state_out may be state_in.
+ *   workspace  device, 256-byte aligned, at least sla_selective_scan_workspace_bytes(...) bytes (0 for
+ *             sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
+ * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and sums of dt over
+ * up to 512 rows are fp32.  A value that is not finite reaches only its own window and channel (B's and C's,
+ * their group's).  Rows in no window are left as they were.  Deterministic.
+ */
+size_t sla_selective_scan_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t channels,
+                                          int32_t groups, int32_t states);
+
+sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                        const int32_t* order, sla_dtype_t dtype, int32_t channels,
+                                        int32_t groups, int32_t states, int32_t delta_softplus, const void* x,
+                                        int64_t x_stride, const void* delta, int64_t delta_stride, const float* A,
+                                        const void* B, int64_t B_stride, const void* C, int64_t C_stride,
+                                        const float* skip, const void* z, int64_t z_stride,
+                                        const float* delta_bias, const float* state_in, void* y,
+                                        float* state_out, void* workspace, size_t workspace_bytes,
+                                        sla_stream_t stream);
+
+/*
+ * The selective scan one row at a time: `state` is a pool [num_slots, channels, states] (fp32), row b of the
+ * batch belongs to the sequence in slot slots[b], whose state it updates in place.  Slots as in
+ * sla_step_delta (rows of the same slot follow each other, a slot outside the pool marks a padding row, n up
+ * to 65,536); other arguments as sla_forward_selective_scan.
+ */
+sla_status_t sla_step_selective_scan(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
+                                     int32_t channels, int32_t groups, int32_t states, int32_t delta_softplus,
+                                     float* state, const void* x, int64_t x_stride, const void* delta,
+                                     int64_t delta_stride, const float* A, const void* B, int64_t B_stride,
+                                     const void* C, int64_t C_stride, const float* skip, const void* z,
+                                     int64_t z_stride, const float* delta_bias, void* y, sla_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -79,3 +79,81 @@ def conv_step_ref(state, slots, x, weight, bias=None, activation="none"):
             one, st = conv_forward_ref(x[b:b + 1], weight, [0, 1], bias, activation, state=S[s:s + 1])
             y[b], S[s] = one[0], st[0]
     return y, S
+
+
+# ------------------------------------------------------------------ selective scan
+def _scan_rows(x, delta, A, B, C, skip, z, delta_bias, softplus):
+    x, delta, A = (np.asarray(t, np.float64) for t in (x, delta, A))
+    D, G = x.shape[1], B.shape[1]
+    B, C = (np.repeat(np.asarray(t, np.float64), D // G, axis=1) for t in (B, C))
+    pre = delta + (0.0 if delta_bias is None else delta_bias)
+    dt = np.logaddexp(0.0, pre) if softplus else pre
+    return x, pre, dt, A, B, C, np.zeros(D) if skip is None else np.asarray(skip, np.float64)
+
+
+def scan_forward_ref(x, delta, A, B, C, offsets, skip=None, z=None, delta_bias=None, delta_softplus=False, order=None,
+                     state=None):
+    """(y, states [windows, channels, states]); rows in no window: NaN."""
+    x, _, dt, A, B, C, skip = _scan_rows(x, delta, A, B, C, skip, z, delta_bias, delta_softplus)
+    W = len(offsets) - 1
+    h = np.zeros((W, *A.shape)) if state is None else np.array(state, np.float64)
+    y = np.full(x.shape, np.nan)
+    for w, rows in enumerate(_windows(offsets, order, x.shape[0])):
+        for r in rows:
+            h[w] = np.exp(dt[r][:, None] * A) * h[w] + (dt[r] * x[r])[:, None] * B[r]
+            y[r] = (C[r] * h[w]).sum(-1) + skip * x[r]
+    return (y if z is None else y * _act("silu", np.asarray(z, np.float64))), h
+
+
+def scan_backward_ref(x, delta, A, B, C, offsets, dy, skip=None, z=None, delta_bias=None, delta_softplus=False, order=None,
+                      state=None, dstate=None):
+    """(dx, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, dstate_in) by the chain rule of one row, from the last row
+    to the first; rows in no window: NaN."""
+    G = B.shape[1]
+    x, pre, dt, A, B, C, skip = _scan_rows(x, delta, A, B, C, skip, z, delta_bias, delta_softplus)
+    n, D = x.shape
+    N = A.shape[1]
+    dy = np.asarray(dy, np.float64)
+    W = len(offsets) - 1
+    h0 = np.zeros((W, D, N)) if state is None else np.asarray(state, np.float64)
+    back = np.zeros((W, D, N)) if dstate is None else np.array(dstate, np.float64)
+    dx, dd, dz = (np.full(x.shape, np.nan) for _ in range(3))
+    dB, dC = (np.full((n, G, N), np.nan) for _ in range(2))
+    dA, dskip, dbias = np.zeros_like(A), np.zeros(D), np.zeros(D)
+    shared = lambda t: t.reshape(G, D // G, N).sum(1)  # noqa: E731
+    for w, rows in enumerate(_windows(offsets, order, n)):
+        h, kept = h0[w], []
+        for r in rows:
+            a = np.exp(dt[r][:, None] * A) * h
+            h = a + (dt[r] * x[r])[:, None] * B[r]
+            kept.append((a, h))
+        for r, (a, h) in zip(rows[::-1], kept[::-1]):
+            g = dy[r]
+            if z is not None:
+                dz[r] = g * ((C[r] * h).sum(-1) + skip * x[r]) * _slope("silu", np.asarray(z[r], np.float64))
+                g = g * _act("silu", np.asarray(z[r], np.float64))
+            q = back[w] + g[:, None] * C[r]
+            dC[r] = shared(g[:, None] * h)
+            dB[r] = shared(q * (dt[r] * x[r])[:, None])
+            du = (q * B[r]).sum(-1)
+            dx[r] = du * dt[r] + g * skip
+            ddt = du * x[r] + (q * a * A).sum(-1)
+            dd[r] = ddt * (_sigmoid(pre[r]) if delta_softplus else 1.0)
+            dA += q * a * dt[r][:, None]
+            dskip += g * x[r]
+            dbias += dd[r]
+            back[w] = q * np.exp(dt[r][:, None] * A)
+    return dx, dd, dA, dB, dC, dskip, dz, dbias, back
+
+
+def scan_step_ref(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias=None, delta_softplus=False):
+    """(y, states): the rows of a slot in row order; padding rows' y is NaN."""
+    S = np.array(state, np.float64)
+    y = np.full(x.shape, np.nan)
+    for b, s in enumerate(slots):
+        if 0 <= s < S.shape[0]:
+            one = slice(b, b + 1)
+            out, st = scan_forward_ref(x[one], delta[one], A, B[one], C[one], [0, 1], skip, None if z is None else z[one],
+                                       delta_bias, delta_softplus, state=S[s:s + 1])
+            y[b], S[s] = out[0], st[0]
+    return y, S

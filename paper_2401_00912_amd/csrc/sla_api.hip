@@ -2,6 +2,7 @@
 // dispatch to the kernels.  No allocation, no synchronisation.
 #include "sla.h"
 #include "sla_common.h"
+#include "sla_scan.h"
 
 #define SLA_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -90,6 +91,13 @@ hipError_t launch_backward_conv(const int32_t* offsets, int32_t n, int32_t W, co
 hipError_t launch_step_conv(const int32_t* slots, int32_t n, int32_t num_slots, int dtype, int32_t C, int32_t K,
                             int activation, void* state, const void* x, int64_t ldx, const float* weight,
                             const float* bias, void* y, hipStream_t stream);
+size_t scan_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N);
+hipError_t launch_forward_scan(scan::ScanArgs a, int dtype, const void* x, const void* delta, const void* z, const void* B,
+                               const void* C, const float* state_in, void* y, float* state_out, void* workspace,
+                               hipStream_t stream);
+hipError_t launch_step_scan(scan::ScanArgs a, int dtype, const int32_t* slots, int32_t num_slots, float* state,
+                            const void* x, const void* delta, const void* z, const void* B, const void* C, void* y,
+                            hipStream_t stream);
 }  // namespace sla
 
 namespace {
@@ -778,4 +786,91 @@ SLA_EXPORT sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int
     return SLA_E_ARG;
   return hip_status(sla::launch_step_conv(slots, (int32_t)n, num_slots, (int)dtype, channels, width, (int)activation,
                                           state, x, x_stride, weight, bias, y, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+sla_status_t check_scan_sizes(int64_t n, int32_t W, int dtype, int32_t channels, int32_t groups, int32_t states) {
+  const sla_status_t st = check_row_sizes(n, W, dtype, channels);
+  if (st != SLA_OK) return st;
+  if (groups < 1 || channels % groups) return SLA_E_ARG;
+  if (states < 1 || states > 64) return SLA_E_UNSUPPORTED;
+  // a launch has a wave for 64 channels of a group in y
+  if ((int64_t)groups * ((channels / groups + 63) / 64) > 65535) return SLA_E_UNSUPPORTED;
+  return SLA_OK;
+}
+
+// The rows that every selective scan call reads, and its parameters.
+sla_status_t check_scan_rows(int64_t n, uintptr_t es, int32_t channels, int32_t groups, int32_t states, const void* x,
+                             int64_t x_stride, const void* delta, int64_t delta_stride, const float* A, const void* B,
+                             int64_t B_stride, const void* C, int64_t C_stride, const float* skip, const void* z,
+                             int64_t z_stride, const float* delta_bias) {
+  if (!A || !aligned(A, 4) || !aligned(skip, 4) || !aligned(delta_bias, 4)) return SLA_E_ARG;
+  const int64_t shared = (int64_t)groups * states;
+  if (!rows_ok(x, n, x_stride, channels, es) || !rows_ok(delta, n, delta_stride, channels, es) ||
+      !rows_ok(B, n, B_stride, shared, es) || !rows_ok(C, n, C_stride, shared, es) ||
+      (z != nullptr && !rows_ok(z, n, z_stride, channels, es)))
+    return SLA_E_ARG;
+  return SLA_OK;
+}
+
+}  // namespace
+
+SLA_EXPORT size_t sla_selective_scan_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                                     int32_t channels, int32_t groups, int32_t states) {
+  if (check_scan_sizes(n, num_windows, (int)dtype, channels, groups, states) != SLA_OK) return 0;
+  return sla::scan_workspace_bytes(n, num_windows, channels, groups, states);
+}
+
+SLA_EXPORT sla_status_t sla_forward_selective_scan(
+    const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order, sla_dtype_t dtype, int32_t channels,
+    int32_t groups, int32_t states, int32_t delta_softplus, const void* x, int64_t x_stride, const void* delta,
+    int64_t delta_stride, const float* A, const void* B, int64_t B_stride, const void* C, int64_t C_stride,
+    const float* skip, const void* z, int64_t z_stride, const float* delta_bias, const float* state_in, void* y,
+    float* state_out, void* workspace, size_t workspace_bytes, sla_stream_t stream) {
+  sla_status_t st = check_scan_sizes(n, num_windows, (int)dtype, channels, groups, states);
+  if (st != SLA_OK) return st;
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2;
+  st = check_scan_rows(n, es, channels, groups, states, x, x_stride, delta, delta_stride, A, B, B_stride, C, C_stride,
+                       skip, z, z_stride, delta_bias);
+  if (st != SLA_OK) return st;
+  if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !aligned(state_in, 4) || !aligned(state_out, 4) ||
+      !rows_ok(y, n, channels, channels, es))
+    return SLA_E_ARG;
+  if (n > 0 && (y == x || y == delta || y == z || y == B || y == C)) return SLA_E_ARG;
+  if (n == 0 && !state_out) return SLA_OK;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  if (workspace_bytes < sla::scan_workspace_bytes(n, num_windows, channels, groups, states)) return SLA_E_WORKSPACE;
+  sla::scan::ScanArgs a{};
+  a.win = {offsets, order, (int32_t)n, num_windows};
+  a.A = A, a.skip = skip, a.bias = delta_bias;
+  a.ldx = x_stride, a.ldd = delta_stride, a.ldz = z_stride, a.ldb = B_stride, a.ldc = C_stride;
+  a.D = channels, a.G = groups, a.N = states, a.softplus = delta_softplus != 0;
+  return hip_status(sla::launch_forward_scan(a, (int)dtype, x, delta, z, B, C, state_in, y, state_out, workspace,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT sla_status_t sla_step_selective_scan(
+    const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype, int32_t channels, int32_t groups,
+    int32_t states, int32_t delta_softplus, float* state, const void* x, int64_t x_stride, const void* delta,
+    int64_t delta_stride, const float* A, const void* B, int64_t B_stride, const void* C, int64_t C_stride,
+    const float* skip, const void* z, int64_t z_stride, const float* delta_bias, void* y, sla_stream_t stream) {
+  sla_status_t st = check_scan_sizes(n, num_slots, (int)dtype, channels, groups, states);
+  if (st != SLA_OK) return st;
+  if (n > 65536) return SLA_E_UNSUPPORTED;   // each row's workgroups look through the slots of all rows
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2;
+  st = check_scan_rows(n, es, channels, groups, states, x, x_stride, delta, delta_stride, A, B, B_stride, C, C_stride,
+                       skip, z, z_stride, delta_bias);
+  if (st != SLA_OK) return st;
+  if (n == 0) return SLA_OK;
+  if (!slots || !aligned(slots, 4) || !state || !aligned(state, 4) || !rows_ok(y, n, channels, channels, es))
+    return SLA_E_ARG;
+  if (y == x || y == delta || y == z || y == B || y == C) return SLA_E_ARG;
+  sla::scan::ScanArgs a{};
+  a.win = {nullptr, nullptr, (int32_t)n, 0};
+  a.A = A, a.skip = skip, a.bias = delta_bias;
+  a.ldx = x_stride, a.ldd = delta_stride, a.ldz = z_stride, a.ldb = B_stride, a.ldc = C_stride;
+  a.D = channels, a.G = groups, a.N = states, a.softplus = delta_softplus != 0;
+  return hip_status(sla::launch_step_scan(a, (int)dtype, slots, num_slots, state, x, delta, z, B, C, y,
+                                          static_cast<hipStream_t>(stream)));
 }

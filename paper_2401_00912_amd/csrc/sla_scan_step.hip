@@ -1,0 +1,89 @@
+// The selective scan one row at a time, on a pool of states (the recurrence: sla_scan.h).
+//
+// Bound by memory: a state is read and written once where it lies, four values a lane; a channel's states are
+// in neighbouring lanes, which share its row and add up its y.
+#include "sla_scan.h"
+
+namespace sla {
+namespace {
+
+using namespace scan;
+
+constexpr int kThreads = 256;
+
+// LN: lanes of a channel, 4 LN >= N
+template <typename T, int LN>
+__global__ __launch_bounds__(kThreads) void k_scan_step(ScanArgs a, const int32_t* __restrict__ slots, int32_t num_slots,
+                                                        float* __restrict__ state, const T* __restrict__ x,
+                                                        const T* __restrict__ delta, const T* __restrict__ z,
+                                                        const T* __restrict__ B, const T* __restrict__ C,
+                                                        T* __restrict__ y) {
+  __shared__ int s_table[2 * (kThreads / 64)];
+  int b = blockIdx.x;
+  const int slot = slots[b];
+  if (slot < 0 || slot >= num_slots) return;   // padding: nothing is touched
+  const SlotRows<kThreads / 64> rows{slots, a.win.n, s_table};
+  const int k = threadIdx.x % LN, at = blockIdx.y * (kThreads / LN) + threadIdx.x / LN;
+  const bool live = at < a.D;
+  const int c = live ? at : 0, g = c / a.cg, n0 = 4 * k;
+  float* st = state + ((size_t)slot * a.D + c) * a.N + n0;
+  const bool vec = by_four(state, a.N);
+  const int count = a.N - n0;
+  float A[4], h[4];
+  load_states<4>(a.A + (size_t)c * a.N + n0, count, by_four(a.A, a.N), A);
+  load_states<4>(st, count, vec, h);
+  const float bias = a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
+  for (bool first = true;; first = false) {
+    const float xv = to_float(x[b * a.ldx + c]), dt = step_size(a, to_float(delta[b * a.ldd + c]), bias), u = dt * xv;
+    const float gate = z != nullptr ? act(kSilu, to_float(z[b * a.ldz + c])) : 1.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+      if (n < count) {
+        const float Bv = to_float(B[b * a.ldb + g * a.N + n0 + n]), Cv = to_float(C[b * a.ldc + g * a.N + n0 + n]);
+        const float e = __builtin_amdgcn_exp2f(dt * (A[n] * kLog2e));
+        h[n] = __builtin_fmaf(e, h[n], u * Bv);
+        sum = __builtin_fmaf(Cv, h[n], sum);
+      }
+    const int next = rows.next(b, slot, first);
+    if (next < 0) return;
+#pragma unroll
+    for (int m = 1; m < LN; m *= 2) sum += __shfl_xor(sum, m);
+    if (live && k == 0) y[(size_t)b * a.D + c] = from_float<T>(__builtin_fmaf(skip, xv, sum) * gate);
+    if (next >= a.win.n) break;
+    b = next;
+  }
+  if (live) store_states<4>(st, count, vec, h);
+}
+
+template <typename T>
+void step_impl(const ScanArgs& a, const int32_t* slots, int32_t num_slots, float* state, const void* x,
+               const void* delta, const void* z, const void* B, const void* C, void* y, hipStream_t stream) {
+  const auto run = [&](auto lanes) {
+    constexpr int LN = decltype(lanes)::value;
+    const dim3 grid(a.win.n, (a.D + kThreads / LN - 1) / (kThreads / LN));
+    k_scan_step<T, LN><<<grid, kThreads, 0, stream>>>(a, slots, num_slots, state, static_cast<const T*>(x),
+                                                      static_cast<const T*>(delta), static_cast<const T*>(z),
+                                                      static_cast<const T*>(B), static_cast<const T*>(C),
+                                                      static_cast<T*>(y));
+  };
+  if (a.N <= 4) run(std::integral_constant<int, 1>{});
+  else if (a.N <= 8) run(std::integral_constant<int, 2>{});
+  else if (a.N <= 16) run(std::integral_constant<int, 4>{});
+  else if (a.N <= 32) run(std::integral_constant<int, 8>{});
+  else run(std::integral_constant<int, 16>{});
+}
+
+}  // namespace
+
+hipError_t launch_step_scan(scan::ScanArgs a, int dtype, const int32_t* slots, int32_t num_slots, float* state,
+                            const void* x, const void* delta, const void* z, const void* B, const void* C, void* y,
+                            hipStream_t stream) {
+  a.cg = a.D / a.G;
+  if (dtype == 0) step_impl<float>(a, slots, num_slots, state, x, delta, z, B, C, y, stream);
+  else if (dtype == 1) step_impl<_Float16>(a, slots, num_slots, state, x, delta, z, B, C, y, stream);
+  else step_impl<bf16_t>(a, slots, num_slots, state, x, delta, z, B, C, y, stream);
+  return hipGetLastError();
+}
+
+}  // namespace sla

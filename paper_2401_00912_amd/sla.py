@@ -32,6 +32,9 @@ Functions mirror the C ABI in include/sla.h:
     backward_short_conv(x, weight, offsets, dy, bias=None, activation="none", order=None, state=None, dstate=None)
         -> (dx, dweight, dbias, dstate_in)
     step_short_conv(state, slots, x, weight, bias=None, activation="none") -> y
+    forward_selective_scan(x, delta, A, B, C, offsets, skip=None, z=None, delta_bias=None, delta_softplus=False,
+                           order=None, state=None) -> (y, final_state)
+    step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias=None, delta_softplus=False) -> y
 """
 from __future__ import annotations
 
@@ -85,6 +88,9 @@ EXPORTED = (
     "sla_short_conv_backward_workspace_bytes",
     "sla_backward_short_conv",
     "sla_step_short_conv",
+    "sla_selective_scan_workspace_bytes",
+    "sla_forward_selective_scan",
+    "sla_step_selective_scan",
 )
 
 
@@ -198,6 +204,13 @@ def lib() -> ctypes.CDLL:
                                           + [sz, vp])
     L.sla_step_short_conv.restype = ctypes.c_int
     L.sla_step_short_conv.argtypes = [vp, i64, i32, en, i32, i32, en, vp, vp, i64] + [vp] * 4
+    L.sla_selective_scan_workspace_bytes.restype = sz
+    L.sla_selective_scan_workspace_bytes.argtypes = [i64, i32, en, i32, i32, i32]
+    scan_rows = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp]
+    L.sla_forward_selective_scan.restype = ctypes.c_int
+    L.sla_forward_selective_scan.argtypes = [vp, i64, i32, vp, en, i32, i32, i32, i32] + scan_rows + [vp] * 4 + [sz, vp]
+    L.sla_step_selective_scan.restype = ctypes.c_int
+    L.sla_step_selective_scan.argtypes = [vp, i64, i32, en, i32, i32, i32, i32, vp] + scan_rows + [vp, vp]
     _lib = L
     return L
 
@@ -983,6 +996,77 @@ def step_short_conv(state, slots, x, weight, bias=None, activation="none", y=Non
         st = lib().sla_step_short_conv(_ptr(slots), n, state.shape[0], _dtype_code(x.dtype), C, K, act, _ptr(state),
                                        _ptr(x), ldx, _ptr(weight), _ptr(bias), _ptr(y), _stream(x.device))
     _check(st, "sla_step_short_conv")
+    return y
+
+
+def _scan_check(x, delta, A, B, C, skip, z, delta_bias):
+    """Shapes, dtypes, devices and layouts of a selective scan's rows and parameters: (n, channels, groups,
+    states) and the rows and parameters as the library takes them."""
+    torch = _torch()
+    if x.dim() != 2 or A.dim() != 2 or B.dim() != 3 or x.shape[1] < 1:
+        raise ValueError("x must be a [n, channels] tensor, A [channels, states] and B [n, groups, states]")
+    (n, D), N, G = x.shape, A.shape[1], B.shape[1]
+    _check_like("A", A, (D, N), torch.float32, x.device)
+    for name, t in (("skip", skip), ("delta_bias", delta_bias)):
+        _check_like(name, t, (D,), torch.float32, x.device)
+    if G < 1 or D % G:
+        raise ValueError("channels must be a multiple of groups")
+    stride = lambda name, t, shape: _row_stride(name, t, shape, x.dtype, x.device)  # noqa: E731
+    rows = (_ptr(x), stride("x", x, (n, D)), _ptr(delta), stride("delta", delta, (n, D)), _ptr(A), _ptr(B),
+            stride("B", B, (n, G, N)), _ptr(C), stride("C", C, (n, G, N)), _ptr(skip), _ptr(z),
+            0 if z is None else stride("z", z, (n, D)), _ptr(delta_bias))
+    return n, D, G, N, rows
+
+
+def selective_scan_workspace_bytes(n: int, num_windows: int, dtype, channels: int, groups: int, states: int) -> int:
+    """Workspace of forward_selective_scan (0: unsupported sizes); dtype a torch dtype."""
+    return int(lib().sla_selective_scan_workspace_bytes(int(n), int(num_windows), _dtype_code(dtype), int(channels),
+                                                        int(groups), int(states)))
+
+
+def forward_selective_scan(x, delta, A, B, C, offsets, skip=None, z=None, delta_bias=None, delta_softplus=False,
+                           order=None, state=None, y=None, final_state=None, workspace=None):
+    """The selective scan over the rows of every window (sla_forward_selective_scan): x and delta
+    [n, channels], A float32 [channels, states], B and C [n, groups, states], the gate z [n, channels] or
+    None (columns of wider tensors will do for all rows), skip and delta_bias float32 [channels] or
+    None, offsets and order as in forward_delta, state float32 [num_windows, channels, states] or None
+    (zero).  Returns (y, final_state); rows in no window are left as they were in y."""
+    torch = _torch()
+    n, D, G, N, rows = _scan_check(x, delta, A, B, C, skip, z, delta_bias)
+    w = _check_windows(offsets, order, n, x.device)
+    y = torch.empty((n, D), dtype=x.dtype, device=x.device) if y is None else y
+    _check_like("y", y, (n, D), x.dtype, x.device)
+    if final_state is None:
+        final_state = torch.empty((w, D, N), dtype=torch.float32, device=x.device)
+    for name, t in (("state", state), ("final_state", final_state)):
+        _check_like(name, t, (w, D, N), torch.float32, x.device)
+    workspace, nbytes = _own_workspace(selective_scan_workspace_bytes(n, w, x.dtype, D, G, N), workspace, x.device,
+                                       "sla_selective_scan_workspace_bytes")
+    with torch.cuda.device(x.device):
+        st = lib().sla_forward_selective_scan(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), D, G, N,
+                                              int(bool(delta_softplus)), *rows, _ptr(state), _ptr(y),
+                                              _ptr(final_state), _ptr(workspace), nbytes, _stream(x.device))
+    _check(st, "sla_forward_selective_scan")
+    return y, final_state
+
+
+def step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias=None, delta_softplus=False,
+                        y=None):
+    """One row for each of many sequences (sla_step_selective_scan): state float32
+    [num_slots, channels, states], updated in place, slots int32 [n] as in step_delta, the rows as in
+    forward_selective_scan.  Returns y, where padding rows are left as they were."""
+    torch = _torch()
+    n, D, G, N, rows = _scan_check(x, delta, A, B, C, skip, z, delta_bias)
+    if state.dim() != 3 or state.shape[0] < 1:
+        raise ValueError("state must be a [num_slots, channels, states] tensor")
+    _check_like("state", state, (state.shape[0], D, N), torch.float32, x.device)
+    _check_like("slots", slots, (n,), torch.int32, x.device)
+    y = torch.empty((n, D), dtype=x.dtype, device=x.device) if y is None else y
+    _check_like("y", y, (n, D), x.dtype, x.device)
+    with torch.cuda.device(x.device):
+        st = lib().sla_step_selective_scan(_ptr(slots), n, state.shape[0], _dtype_code(x.dtype), D, G, N,
+                                           int(bool(delta_softplus)), _ptr(state), *rows, _ptr(y), _stream(x.device))
+    _check(st, "sla_step_selective_scan")
     return y
 
 
