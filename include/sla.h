@@ -651,6 +651,31 @@ sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32
                                         sla_stream_t stream);
 
 /*
+ * Backward of sla_forward_selective_scan (the chain rule of the recurrence): given dy = dL/dy (rows dy_stride
+ * elements apart) and dstate_out = dL/d(state_out) (NULL: zero), writes dx, ddelta and, with z, dz
+ * [n, channels], dB and dC [n, groups, states] (sums over the group's channels) in `dtype`, dA (fp32
+ * [channels, states]), dskip and ddelta_bias (fp32 [channels], each may be NULL), the three summed over all
+ * rows in windows, and, if not NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  States are made
+ * again from the inputs.  Every sum over rows or channels is fp32 in a fixed order.  Rows in no window are
+ * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; the outputs must not be
+ * inputs.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes.  Deterministic.
+ */
+size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                                   int32_t channels, int32_t groups, int32_t states);
+
+sla_status_t sla_backward_selective_scan(const int32_t* offsets, int64_t n, int32_t num_windows,
+                                         const int32_t* order, sla_dtype_t dtype, int32_t channels,
+                                         int32_t groups, int32_t states, int32_t delta_softplus, const void* x,
+                                         int64_t x_stride, const void* delta, int64_t delta_stride, const float* A,
+                                         const void* B, int64_t B_stride, const void* C, int64_t C_stride,
+                                         const float* skip, const void* z, int64_t z_stride,
+                                         const float* delta_bias, const float* state_in, const void* dy,
+                                         int64_t dy_stride, const float* dstate_out, void* dx, void* ddelta,
+                                         float* dA, void* dB, void* dC, float* dskip, void* dz,
+                                         float* ddelta_bias, float* dstate_in, void* workspace,
+                                         size_t workspace_bytes, sla_stream_t stream);
+
+/*
  * The selective scan one row at a time: `state` is a pool [num_slots, channels, states] (fp32), row b of the
  * batch belongs to the sequence in slot slots[b], whose state it updates in place.  Slots as in
  * sla_step_delta (rows of the same slot follow each other, a slot outside the pool marks a padding row, n up

@@ -95,6 +95,12 @@ size_t scan_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t 
 hipError_t launch_forward_scan(scan::ScanArgs a, int dtype, const void* x, const void* delta, const void* z, const void* B,
                                const void* C, const float* state_in, void* y, float* state_out, void* workspace,
                                hipStream_t stream);
+size_t scan_backward_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N);
+hipError_t launch_backward_scan(scan::ScanArgs a, int dtype, const void* x, const void* delta, const void* z,
+                                const void* B, const void* C, const float* state_in, const void* dy,
+                                const float* dstate_out, void* dx, void* ddelta, float* dA, void* dB, void* dC,
+                                float* dskip, void* dz, float* dbias, float* dstate_in, void* workspace,
+                                hipStream_t stream);
 hipError_t launch_step_scan(scan::ScanArgs a, int dtype, const int32_t* slots, int32_t num_slots, float* state,
                             const void* x, const void* delta, const void* z, const void* B, const void* C, void* y,
                             hipStream_t stream);
@@ -848,6 +854,54 @@ SLA_EXPORT sla_status_t sla_forward_selective_scan(
   a.D = channels, a.G = groups, a.N = states, a.softplus = delta_softplus != 0;
   return hip_status(sla::launch_forward_scan(a, (int)dtype, x, delta, z, B, C, state_in, y, state_out, workspace,
                                              static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
+                                                              int32_t channels, int32_t groups, int32_t states) {
+  if (check_scan_sizes(n, num_windows, (int)dtype, channels, groups, states) != SLA_OK) return 0;
+  return sla::scan_backward_workspace_bytes(n, num_windows, channels, groups, states);
+}
+
+SLA_EXPORT sla_status_t sla_backward_selective_scan(
+    const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order, sla_dtype_t dtype, int32_t channels,
+    int32_t groups, int32_t states, int32_t delta_softplus, const void* x, int64_t x_stride, const void* delta,
+    int64_t delta_stride, const float* A, const void* B, int64_t B_stride, const void* C, int64_t C_stride,
+    const float* skip, const void* z, int64_t z_stride, const float* delta_bias, const float* state_in, const void* dy,
+    int64_t dy_stride, const float* dstate_out, void* dx, void* ddelta, float* dA, void* dB, void* dC, float* dskip,
+    void* dz, float* ddelta_bias, float* dstate_in, void* workspace, size_t workspace_bytes, sla_stream_t stream) {
+  sla_status_t st = check_scan_sizes(n, num_windows, (int)dtype, channels, groups, states);
+  if (st != SLA_OK) return st;
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2;
+  st = check_scan_rows(n, es, channels, groups, states, x, x_stride, delta, delta_stride, A, B, B_stride, C, C_stride,
+                       skip, z, z_stride, delta_bias);
+  if (st != SLA_OK) return st;
+  const int64_t shared = (int64_t)groups * states;
+  if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !aligned(state_in, 4) || !aligned(dstate_out, 4) ||
+      !rows_ok(dy, n, dy_stride, channels, es))
+    return SLA_E_ARG;
+  if (!rows_ok(dx, n, channels, channels, es) || !rows_ok(ddelta, n, channels, channels, es) || !dA || !aligned(dA, 4) ||
+      !rows_ok(dB, n, shared, shared, es) || !rows_ok(dC, n, shared, shared, es) || !aligned(dskip, 4) ||
+      !aligned(ddelta_bias, 4) || !aligned(dstate_in, 4) || (z != nullptr && !rows_ok(dz, n, channels, channels, es)))
+    return SLA_E_ARG;
+  if (n > 0) {
+    const void* in[] = {x, delta, z, B, C, dy};
+    const void* out[] = {dx, ddelta, z != nullptr ? dz : nullptr, dB, dC};
+    for (const void* o : out)
+      for (const void* i : in)
+        if (o != nullptr && o == i) return SLA_E_ARG;
+  }
+  if (dstate_in != nullptr && dstate_in == state_in) return SLA_E_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  if (workspace_bytes < sla::scan_backward_workspace_bytes(n, num_windows, channels, groups, states))
+    return SLA_E_WORKSPACE;
+  sla::scan::ScanArgs a{};
+  a.win = {offsets, order, (int32_t)n, num_windows};
+  a.A = A, a.skip = skip, a.bias = delta_bias;
+  a.ldx = x_stride, a.ldd = delta_stride, a.ldz = z_stride, a.ldb = B_stride, a.ldc = C_stride, a.ldy = dy_stride;
+  a.D = channels, a.G = groups, a.N = states, a.softplus = delta_softplus != 0;
+  return hip_status(sla::launch_backward_scan(a, (int)dtype, x, delta, z, B, C, state_in, dy, dstate_out, dx, ddelta, dA,
+                                              dB, dC, dskip, dz, ddelta_bias, dstate_in, workspace,
+                                              static_cast<hipStream_t>(stream)));
 }
 
 SLA_EXPORT sla_status_t sla_step_selective_scan(

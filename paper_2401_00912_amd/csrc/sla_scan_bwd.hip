@@ -1,0 +1,596 @@
+// Gradients of the selective scan (the recurrence and how windows are cut: sla_scan.h).
+//
+// With g_t = dy_t silu(z_t), a_t = exp(dt_t A) h_{t-1}, so h_t = a_t + u_t B_t, and q_t the gradient of h_t, from
+// a window's last row to its first:
+//     q_t = C_t g_t + exp(dt_{t+1} A) q_{t+1},
+//     dC_t = sum_d h_t g_t,  dB_t = sum_d q_t u_t,  du_t = sum_n q_t B_t,  dx_t = dt_t du_t + skip g_t,
+//     ddt_t = x_t du_t + sum_n A q_t a_t,  dA = sum_t dt_t q_t a_t,
+// ddelta = ddt softplus'(delta + bias), dz = dy (y before the gate) silu'(z), and the parameters' sums over rows.
+//
+// Four launches.  The first makes the maps of a window's parts, forward (S, sum dt) and back: what a part adds
+// to the gradient of the state before it, R = sum_t exp(A sum_{s <= t} dt_s) C_t g_t.  The second joins them along
+// the window both ways.  The third walks every part: forward once for the states at its 16-row tiles, then
+// tile by tile from the last, forward through the tile with every row's a and decay kept in registers, and
+// back.  A lane holds four states of a channel, so the sums over states go over the lane's few neighbours and
+// those over channels over the wave, then over the workgroup's waves in LDS, and what is left of them (over a
+// group's workgroups, and the parameters' over the parts) is added by the last launch in a fixed order.
+//
+// Bound by the vector unit: about 25 instructions for each state and row.
+#include <algorithm>
+
+#include "sla_scan.h"
+
+namespace sla {
+namespace {
+
+using namespace scan;
+
+constexpr int kTile = 16, kMaxTiles = 8, kThreads = 256, kWaves = 4;
+constexpr float kLn2 = 0.693147181f;
+
+struct BackArgs {
+  ScanArgs a;
+  int32_t cw;            // channels of a workgroup
+  int32_t wpg;           // workgroups across a group's channels
+  Parts fwd;             // S, sum dt
+  float* R;              // [slots][N][D]
+  float* bc;             // [G wpg][n][2 N]: sums over a workgroup's channels, by position
+  float *pA, *pskip, *pbias;   // [slots][D N], [slots][D], [slots][D]
+};
+
+// ------------------------------------------------------------------ the parts' maps
+// A wave takes 64 channels and NS of their states, as the forward does.
+template <typename T, int NS>
+__global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restrict__ x, const T* __restrict__ delta,
+                                                  const T* __restrict__ z, const T* __restrict__ B,
+                                                  const T* __restrict__ C, const T* __restrict__ dy) {
+  constexpr int U = 4, V = 2 * NS, J = (U * V + 63) / 64;
+  __shared__ __attribute__((aligned(16))) float s_bc[J * 64];
+  const ScanArgs& a = k.a;
+  Part part;
+  if (!part_of(a.win, a.per, blockIdx.x, part)) return;
+  if (part.first && part.last) return;   // the whole window
+  const int lane = threadIdx.x, n0 = blockIdx.z * NS, N = min(a.N - n0, NS);
+  const Tile tile(a, blockIdx.y, lane);
+  const int c = tile.c;
+  float A[NS], h[NS], P[NS], R[NS];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    A[n] = n < N ? a.A[(size_t)c * a.N + n0 + n] * kLog2e : 0.f;
+    h[n] = R[n] = 0.f;
+    P[n] = 1.f;
+  }
+  const float bias = a.bias ? a.bias[c] : 0.f;
+  float dts = 0.f;
+  T xr[U], dr[U], zr[U], gr[U], bc[J];
+  const auto ask = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int r = p0 + i < part.end ? a.win.row(p0 + i) : -1;
+      xr[i] = dr[i] = zr[i] = gr[i] = from_float<T>(0.f);
+      if (r >= 0) {
+        xr[i] = x[r * a.ldx + c];
+        dr[i] = delta[r * a.ldd + c];
+        gr[i] = dy[r * a.ldy + c];
+        if (z != nullptr) zr[i] = z[r * a.ldz + c];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int at = lane + 64 * j, p = p0 + at / V, v = at % V, n = v % NS;
+      bc[j] = from_float<T>(0.f);
+      const int r = p < part.end && at < U * V && n < N ? a.win.row(p) : -1;
+      if (r >= 0) bc[j] = v < NS ? B[r * a.ldb + tile.g * a.N + n0 + n] : C[r * a.ldc + tile.g * a.N + n0 + n];
+    }
+  };
+  ask(part.begin);
+  for (int p0 = part.begin; p0 < part.end; p0 += U) {
+    T xc[U], dc[U], zc[U], gc[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) xc[i] = xr[i], dc[i] = dr[i], zc[i] = zr[i], gc[i] = gr[i];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = to_float(bc[j]);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    ask(p0 + U);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (p0 + i >= part.end) break;
+      const float dt = step_size(a, to_float(dc[i]), bias), u = dt * to_float(xc[i]);
+      float g = to_float(gc[i]);
+      if (z != nullptr) g *= act(kSilu, to_float(zc[i]));
+      dts += dt;
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const float e = __builtin_amdgcn_exp2f(dt * A[n]);
+        h[n] = __builtin_fmaf(e, h[n], u * s_bc[i * V + n]);
+        P[n] *= e;
+        R[n] = __builtin_fmaf(P[n], g * s_bc[i * V + NS + n], R[n]);
+      }
+    }
+  }
+  if (!tile.live) return;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+    if (n < N) {
+      const size_t at = ((size_t)blockIdx.x * a.N + n0 + n) * a.D + c;
+      k.fwd.S[at] = h[n];
+      k.R[at] = R[n];
+    }
+  if (n0 == 0) k.fwd.dts[(size_t)blockIdx.x * a.D + c] = dts;
+}
+
+// Along the parts of every window: S becomes the state behind its part and R the gradient of the state
+// before it; the two ends' places, which are free, take copies of the window's state and of its gradient (the
+// outputs may lie where these are read).  Windows without rows hand their gradient on.
+__global__ __launch_bounds__(256) void k_scan_carry_back(BackArgs k, const float* __restrict__ state,
+                                                         const float* __restrict__ dstate,
+                                                         float* __restrict__ dstate_in) {
+  constexpr int kAhead = 8;
+  const ScanArgs& a = k.a;
+  const int w = blockIdx.x;
+  const int b = a.win.edge(w), e = a.win.edge(w + 1);
+  const int64_t at = (int64_t)blockIdx.y * 256 + threadIdx.x, size = (int64_t)a.N * a.D;
+  if (at >= size) return;
+  const int n = (int)(at / a.D), c = (int)(at % a.D);
+  const size_t mine = ((size_t)w * a.D + c) * a.N + n;
+  if (e <= b) {
+    if (dstate_in != nullptr) dstate_in[mine] = dstate != nullptr ? dstate[mine] : 0.f;
+    return;
+  }
+  const int count = (e - b - 1) / a.per;   // parts but one
+  if (count == 0) return;
+  const int64_t first = (int64_t)(b / a.per) + w;
+  const float A = a.A[(size_t)c * a.N + n] * kLog2e;
+  float h = state != nullptr ? state[mine] : 0.f, q = dstate != nullptr ? dstate[mine] : 0.f;
+  k.fwd.S[(first + count) * size + at] = h;
+  k.R[first * size + at] = q;
+  for (int i0 = 0; i0 < count; i0 += kAhead) {
+    float S[kAhead], d[kAhead], R[kAhead], f[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t s = first + min(i0 + i, count - 1), r = first + max(count - i0 - i, 1);
+      S[i] = k.fwd.S[s * size + at];
+      d[i] = k.fwd.dts[s * a.D + c];
+      R[i] = k.R[r * size + at];
+      f[i] = k.fwd.dts[r * a.D + c];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i0 + i < count) {
+        h = decayed(A * d[i], h) + S[i];
+        k.fwd.S[(first + i0 + i) * size + at] = h;
+        q = decayed(A * f[i], q) + R[i];
+        k.R[(first + count - i0 - i) * size + at] = q;
+      }
+  }
+}
+
+// ------------------------------------------------------------------ sums over lanes
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+// x of the lane whose number differs in bit S; below 8 in lower bits too unless EXACT (then the sum over those
+// is still to come, and the pairing does not matter)
+template <int S, bool EXACT>
+__device__ __forceinline__ float other(float x) {
+  if constexpr (S == 1) return dpp<0xb1>(x);
+  else if constexpr (S == 2) return dpp<0x4e>(x);
+  else if constexpr (S == 4 && !EXACT) return dpp<0x141>(x);
+  else if constexpr (S == 8) return dpp<0x128>(x);
+  else return __shfl_xor(x, S);
+}
+// Sums of pairs of lanes, a where bit S of the lane is clear, b where it is set.
+template <int S, bool EXACT>
+__device__ __forceinline__ float halve(float a, float b, int lane) {
+  if constexpr (S == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else if constexpr (S == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    const bool up = lane & S;
+    const float keep = up ? b : a, send = up ? a : b;
+    return keep + other<S, EXACT>(send);
+  }
+}
+// x[0 .. M - 1] summed over the lanes that differ in bits S, S / 2, .. LOW: lane bit S chooses between x[k] and
+// x[k + M / 2], the next bit halves what is left, and so on; where one value is left, every lane has its sum.
+template <int M, int S, int LOW, bool EXACT>
+__device__ __forceinline__ void sum_lanes(float* x, int lane) {
+  if constexpr (S >= LOW) {
+    if constexpr (M > 1) {
+#pragma unroll
+      for (int k = 0; k < M / 2; ++k) x[k] = halve<S, EXACT>(x[k], x[k + M / 2], lane);
+      sum_lanes<M / 2, S / 2, LOW, EXACT>(x, lane);
+    } else {
+      x[0] += other<S, EXACT>(x[0]);
+      sum_lanes<1, S / 2, LOW, EXACT>(x, lane);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ the walk
+// NG lanes a channel, four states each; lane = ng CW + channel.  Of a 16-row tile a lane takes the rows
+// j NG + ng of its channel wherever rows are taken one by one (step sizes, gates, results).
+template <typename T, int NG>
+__global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* __restrict__ x,
+                                                           const T* __restrict__ delta, const T* __restrict__ z,
+                                                           const T* __restrict__ B, const T* __restrict__ C,
+                                                           const float* __restrict__ state, const T* __restrict__ dy,
+                                                           const float* __restrict__ dstate, T* __restrict__ dx,
+                                                           T* __restrict__ ddelta, T* __restrict__ dz,
+                                                           float* __restrict__ dstate_in) {
+  constexpr int CW = 64 / NG, E = kTile / NG, NP = 4 * NG;
+  constexpr int kStage = (kTile * 2 * NP + kThreads - 1) / kThreads;
+  __shared__ floatx4 s_in[kWaves][kTile][CW];            // dt, u, g of the wave's channels
+  __shared__ floatx4 s_start[kWaves][kMaxTiles][64];     // states before each tile
+  __shared__ __attribute__((aligned(16))) float s_bc[kTile][2][NP];
+  __shared__ float s_red[kWaves][kTile][2][NP];
+  const ScanArgs& a = k.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ng = lane / CW, ch = lane % CW;
+  const int g = blockIdx.y / k.wpg, at = (blockIdx.y % k.wpg) * k.cw + wave * CW + ch;
+  const bool live = at < a.cg;
+  const int c = g * a.cg + (live ? at : 0), n0 = 4 * ng;
+  const size_t slot = blockIdx.x;
+  Part part;
+  if (!part_of(a.win, a.per, blockIdx.x, part)) {
+    // a slot without a part: nothing to the parameters' sums
+    if (live) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (n0 + r < a.N) k.pA[slot * a.D * a.N + (size_t)c * a.N + n0 + r] = 0.f;
+      if (ng == 0) k.pskip[slot * a.D + c] = k.pbias[slot * a.D + c] = 0.f;
+    }
+    return;
+  }
+  const int count = (a.win.edge(part.w + 1) - a.win.edge(part.w) - 1) / a.per;   // the window's parts but one
+  float A[4], h[4], q[4], dA[4] = {};
+  const auto from_parts = [&](const float* p, size_t s, float (&v)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = n0 + r < a.N ? p[(s * a.N + n0 + r) * a.D + c] : 0.f;
+  };
+  const auto from_window = [&](const float* p, float (&v)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = p != nullptr && n0 + r < a.N ? p[((size_t)part.w * a.D + c) * a.N + n0 + r] : 0.f;
+  };
+#pragma unroll
+  for (int r = 0; r < 4; ++r) A[r] = n0 + r < a.N ? a.A[(size_t)c * a.N + n0 + r] * kLog2e : 0.f;
+  if (!part.first) from_parts(k.fwd.S, slot - 1, h);
+  else if (!part.last && state != nullptr) from_parts(k.fwd.S, slot + count, h);
+  else from_window(state, h);
+  if (!part.last) from_parts(k.R, slot + 1, q);
+  else if (!part.first && dstate != nullptr) from_parts(k.R, slot - count, q);
+  else from_window(dstate, q);
+  const float bias = a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
+  float sum_skip = 0.f, sum_bias = 0.f;
+
+  T xr[E], dr[E], zr[E], gr[E], bc[kStage];
+  int row[E];
+  // a tile's rows: x and delta, and with them all else that the way back needs
+  const auto ask = [&](int p0, bool back) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const int p = p0 + j * NG + ng;
+      row[j] = p < part.end && live ? a.win.row(p) : -1;
+      xr[j] = dr[j] = zr[j] = gr[j] = from_float<T>(0.f);
+      if (row[j] >= 0) {
+        xr[j] = x[row[j] * a.ldx + c];
+        dr[j] = delta[row[j] * a.ldd + c];
+        if (back) {
+          gr[j] = dy[row[j] * a.ldy + c];
+          if (z != nullptr) zr[j] = z[row[j] * a.ldz + c];
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kStage; ++j) {
+      const int i = tid + kThreads * j, t = i / (2 * NP), v = i % (2 * NP), n = v % NP;
+      bc[j] = from_float<T>(0.f);
+      const int r = t < kTile && p0 + t < part.end && n < a.N ? a.win.row(p0 + t) : -1;
+      if (r >= 0) bc[j] = v < NP ? B[r * a.ldb + g * a.N + n] : C[r * a.ldc + g * a.N + n];
+    }
+  };
+  float pre[E], dt[E], gate[E];
+  const auto stage = [&](bool back) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      pre[j] = to_float(dr[j]) + bias;
+      dt[j] = row[j] >= 0 ? step_size(a, to_float(dr[j]), bias) : 0.f;
+      gate[j] = back && z != nullptr ? act(kSilu, to_float(zr[j])) : 1.f;
+      s_in[wave][j * NG + ng][ch] = floatx4{dt[j], dt[j] * to_float(xr[j]), to_float(gr[j]) * gate[j], 0.f};
+    }
+    float* flat = &s_bc[0][0][0];
+#pragma unroll
+    for (int j = 0; j < kStage; ++j)
+      if (tid + kThreads * j < kTile * 2 * NP) flat[tid + kThreads * j] = to_float(bc[j]);
+  };
+
+  const int tiles = (part.end - part.begin + kTile - 1) / kTile;
+  // the states before every tile
+  s_start[wave][0][lane] = floatx4{h[0], h[1], h[2], h[3]};
+  if (tiles > 1) ask(part.begin, false);
+  for (int i = 0; i + 1 < tiles; ++i) {
+    __syncthreads();
+    stage(false);
+    __syncthreads();
+    if (i + 2 < tiles) ask(part.begin + (i + 1) * kTile, false);
+#pragma unroll
+    for (int t = 0; t < kTile; ++t) {
+      const floatx4 in = s_in[wave][t][ch], Bv = *reinterpret_cast<const floatx4*>(&s_bc[t][0][n0]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        h[r] = __builtin_fmaf(__builtin_amdgcn_exp2f(in[0] * A[r]), h[r], in[1] * Bv[r]);
+    }
+    s_start[wave][i + 1][lane] = floatx4{h[0], h[1], h[2], h[3]};
+  }
+
+  for (int i = tiles - 1; i >= 0; --i) {
+    const int p0 = part.begin + i * kTile;
+    ask(p0, true);
+    __syncthreads();
+    stage(true);
+    __syncthreads();
+    float kept[kTile][4], e[kTile][4];
+    {
+      const floatx4 s = s_start[wave][i][lane];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) h[r] = s[r];
+    }
+#pragma unroll
+    for (int t = 0; t < kTile; ++t) {
+      const floatx4 in = s_in[wave][t][ch], Bv = *reinterpret_cast<const floatx4*>(&s_bc[t][0][n0]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        e[t][r] = __builtin_amdgcn_exp2f(in[0] * A[r]);
+        kept[t][r] = e[t][r] * h[r];
+        h[r] = __builtin_fmaf(in[1], Bv[r], kept[t][r]);
+      }
+    }
+    float du[NG], dda[NG], yl[NG];
+#pragma unroll
+    for (int t = kTile - 1; t >= 0; --t) {
+      const floatx4 in = s_in[wave][t][ch], Bv = *reinterpret_cast<const floatx4*>(&s_bc[t][0][n0]),
+                    Cv = *reinterpret_cast<const floatx4*>(&s_bc[t][1][n0]);
+      float shared[8];
+      float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float ht = __builtin_fmaf(in[1], Bv[r], kept[t][r]);
+        q[r] = __builtin_fmaf(Cv[r], in[2], q[r]);
+        shared[r] = q[r] * in[1];
+        shared[4 + r] = ht * in[2];
+        s0 = __builtin_fmaf(q[r], Bv[r], s0);
+        s2 = __builtin_fmaf(Cv[r], ht, s2);
+        const float da = q[r] * kept[t][r];
+        s1 = __builtin_fmaf(da, A[r], s1);
+        dA[r] = __builtin_fmaf(da, in[0], dA[r]);
+        q[r] *= e[t][r];
+      }
+      du[t % NG] = s0;
+      dda[t % NG] = s1;
+      yl[t % NG] = s2;
+      sum_lanes<8, CW / 2, 1, false>(shared, lane);
+      // the halvings chose: the first lane bit B or C, the next two the state
+      if constexpr (CW >= 8) {
+        constexpr int b0 = CW / 2, b1 = CW / 4, b2 = CW / 8;
+        const int v = n0 + ((lane & b1) ? 2 : 0) + ((lane & b2) ? 1 : 0);
+        if ((lane & (b2 - 1)) == 0) s_red[wave][t][(lane & b0) ? 1 : 0][v] = shared[0];
+      } else {
+        const int v = n0 + ((lane & 1) ? 2 : 0);
+        s_red[wave][t][(lane & 2) ? 1 : 0][v] = shared[0];
+        s_red[wave][t][(lane & 2) ? 1 : 0][v + 1] = shared[1];
+      }
+      if (t % NG == 0) {
+        sum_lanes<NG, 32, CW, true>(du, lane);
+        sum_lanes<NG, 32, CW, true>(dda, lane);
+        sum_lanes<NG, 32, CW, true>(yl, lane);
+        const int j = t / NG;
+        if (row[j] >= 0) {
+          const float xv = to_float(xr[j]), gv = to_float(gr[j]) * gate[j];
+          float dd = __builtin_fmaf(du[0], xv, dda[0] * kLn2);
+          if (a.softplus) dd *= sigmoid(from_above(from_below(pre[j])));
+          const size_t o = (size_t)row[j] * a.D + c;
+          dx[o] = from_float<T>(__builtin_fmaf(du[0], dt[j], gv * skip));
+          ddelta[o] = from_float<T>(dd);
+          if (z != nullptr)
+            dz[o] = from_float<T>(to_float(gr[j]) * __builtin_fmaf(skip, xv, yl[0]) * slope(kSilu, to_float(zr[j])));
+          sum_skip = __builtin_fmaf(gv, xv, sum_skip);
+          sum_bias += dd;
+        }
+      }
+    }
+    __syncthreads();
+    // the waves' sums over their channels
+    const float* red = &s_red[0][0][0][0];
+    for (int v = tid; v < kTile * 2 * NP; v += kThreads) {
+      const int t = v / (2 * NP), which = v / NP % 2, n = v % NP;
+      if (p0 + t < part.end && n < a.N) {
+        float sum = red[v];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) sum += red[w * kTile * 2 * NP + v];
+        k.bc[((size_t)blockIdx.y * a.win.n + p0 + t) * 2 * a.N + which * a.N + n] = sum;
+      }
+    }
+  }
+  float sums[1] = {sum_skip};
+  sum_lanes<1, 32, CW, true>(sums, lane);
+  sum_skip = sums[0];
+  sums[0] = sum_bias;
+  sum_lanes<1, 32, CW, true>(sums, lane);
+  sum_bias = sums[0];
+  if (!live) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (n0 + r < a.N) {
+      k.pA[slot * a.D * a.N + (size_t)c * a.N + n0 + r] = dA[r];
+      if (part.first && dstate_in != nullptr) dstate_in[((size_t)part.w * a.D + c) * a.N + n0 + r] = q[r];
+    }
+  if (ng == 0) {
+    k.pskip[slot * a.D + c] = sum_skip;
+    k.pbias[slot * a.D + c] = sum_bias;
+  }
+}
+
+// ------------------------------------------------------------------ the last sums
+// dB and dC: over the workgroups of a group, in their order; one value a thread.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_scan_shared(BackArgs k, T* __restrict__ dB, T* __restrict__ dC) {
+  const ScanArgs& a = k.a;
+  const int64_t per_row = 2 * (int64_t)a.G * a.N;
+  const int first = a.win.edge(0), last = a.win.edge(a.win.W);
+  for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < per_row * a.win.n;
+       at += (int64_t)gridDim.x * kThreads) {
+    const int p = (int)(at / per_row);
+    const int r = p >= first && p < last ? a.win.row(p) : -1;
+    if (r < 0) continue;
+    const int v = (int)(at % per_row), g = v / (2 * a.N), i = v % (2 * a.N);
+    const float* src = k.bc + ((size_t)g * k.wpg * a.win.n + p) * 2 * a.N + i;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int w = 0; w < k.wpg; ++w) sum += src[(size_t)w * a.win.n * 2 * a.N];
+    T* out = i < a.N ? dB : dC;
+    out[((size_t)r * a.G + g) * a.N + i % a.N] = from_float<T>(sum);
+  }
+}
+
+// The parameters: over all parts, 64 values a workgroup, sixteen runs of parts side by side.
+__global__ __launch_bounds__(1024) void k_scan_params(BackArgs k, int32_t slots, float* __restrict__ dA,
+                                                      float* __restrict__ dskip, float* __restrict__ dbias) {
+  __shared__ float s_sum[16][64];
+  const ScanArgs& a = k.a;
+  const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+  const int64_t size = (int64_t)a.D * a.N, at = (int64_t)blockIdx.x * 64 + lane;
+  const float* src = nullptr;
+  float* out = nullptr;
+  int64_t step = a.D;
+  if (at < size) src = k.pA + at, out = dA + at, step = size;
+  else if (at < size + a.D) src = k.pskip + (at - size), out = dskip ? dskip + (at - size) : nullptr;
+  else if (at < size + 2 * a.D) src = k.pbias + (at - size - a.D), out = dbias ? dbias + (at - size - a.D) : nullptr;
+  float sum = 0.f;
+  if (src != nullptr) {
+    const int lo = (int)((int64_t)slots * run / 16), hi = (int)((int64_t)slots * (run + 1) / 16);
+#pragma unroll 8
+    for (int s = lo; s < hi; ++s) sum += src[(size_t)s * step];
+  }
+  s_sum[run][lane] = sum;
+  __syncthreads();
+  if (run || out == nullptr) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) sum += s_sum[i][lane];
+  *out = sum;
+}
+
+int rows_per_part_back(int64_t n, int64_t blocks) {
+  // whole tiles; enough workgroups for two a CU
+  int64_t per = n * blocks / 1024 / kTile * kTile;
+  per = per < 32 ? 32 : per > kTile * kMaxTiles ? kTile * kMaxTiles : per;
+  return (int)per;
+}
+
+int lane_groups(int32_t N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
+
+struct BackLayout {
+  int32_t ng, cw, wpg, per;
+  int64_t slots;
+  size_t S, dts, R, bc, pA, pskip, pbias, total;
+};
+BackLayout back_layout(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
+  BackLayout L;
+  L.ng = lane_groups(N);
+  L.cw = 64 / L.ng * kWaves;
+  L.wpg = (D / G + L.cw - 1) / L.cw;
+  L.per = rows_per_part_back(n, (int64_t)G * L.wpg);
+  L.slots = n / L.per + W;
+  size_t off = 0;
+  const auto take = [&](size_t floats) {
+    const size_t at = off;
+    off = align_up(off + floats * 4, 256);
+    return at;
+  };
+  const size_t slots = (size_t)L.slots;
+  L.S = take(slots * D * N);
+  L.R = take(slots * D * N);
+  L.pA = take(slots * D * N);
+  L.dts = take(slots * D);
+  L.pskip = take(slots * D);
+  L.pbias = take(slots * D);
+  L.bc = take((size_t)G * L.wpg * n * 2 * N);
+  L.total = off;
+  return L;
+}
+
+}  // namespace
+
+size_t scan_backward_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
+  return back_layout(n, W, D, G, N).total;
+}
+
+hipError_t launch_backward_scan(scan::ScanArgs a, int dtype, const void* x, const void* delta, const void* z,
+                                const void* B, const void* C, const float* state_in, const void* dy,
+                                const float* dstate_out, void* dx, void* ddelta, float* dA, void* dB, void* dC,
+                                float* dskip, void* dz, float* dbias, float* dstate_in, void* workspace,
+                                hipStream_t stream) {
+  const BackLayout L = back_layout(a.win.n, a.win.W, a.D, a.G, a.N);
+  a.cg = a.D / a.G;
+  a.tpg = (a.cg + 63) / 64;
+  a.per = L.per;
+  char* ws = static_cast<char*>(workspace);
+  const auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  BackArgs k;
+  k.a = a;
+  k.cw = L.cw;
+  k.wpg = L.wpg;
+  k.fwd.S = at(L.S);
+  k.fwd.dts = at(L.dts);
+  k.R = at(L.R);
+  k.bc = at(L.bc);
+  k.pA = at(L.pA);
+  k.pskip = at(L.pskip);
+  k.pbias = at(L.pbias);
+  const int64_t values = (int64_t)a.D * a.N;
+  const bool cut = a.win.n > a.per;
+  const auto run = [&](auto type) {
+    using T = decltype(type);
+    const auto *xp = static_cast<const T*>(x), *dp = static_cast<const T*>(delta), *zp = static_cast<const T*>(z),
+               *bp = static_cast<const T*>(B), *cp = static_cast<const T*>(C), *yp = static_cast<const T*>(dy);
+    if (cut) {
+      const dim3 grid((uint32_t)L.slots, (uint32_t)(a.G * a.tpg), (a.N + 15) / 16);
+      const auto maps = [&](auto kernel) { kernel<<<grid, 64, 0, stream>>>(k, xp, dp, zp, bp, cp, yp); };
+      if (a.N <= 4) maps(k_scan_maps<T, 4>);
+      else if (a.N <= 8) maps(k_scan_maps<T, 8>);
+      else maps(k_scan_maps<T, 16>);
+    }
+    if (cut || dstate_in != nullptr)
+      k_scan_carry_back<<<dim3(a.win.W, (uint32_t)((values + 255) / 256)), 256, 0, stream>>>(k, state_in, dstate_out,
+                                                                                            dstate_in);
+    if (a.win.n > 0) {
+      const dim3 grid((uint32_t)L.slots, (uint32_t)(a.G * L.wpg));
+      const auto walk = [&](auto kernel) {
+        kernel<<<grid, kThreads, 0, stream>>>(k, xp, dp, zp, bp, cp, state_in, yp, dstate_out, static_cast<T*>(dx),
+                                              static_cast<T*>(ddelta), static_cast<T*>(dz), dstate_in);
+      };
+      switch (L.ng) {
+        case 1: walk(k_scan_back<T, 1>); break;
+        case 2: walk(k_scan_back<T, 2>); break;
+        case 4: walk(k_scan_back<T, 4>); break;
+        case 8: walk(k_scan_back<T, 8>); break;
+        default: walk(k_scan_back<T, 16>); break;
+      }
+      const int64_t shared = 2 * (int64_t)a.win.n * a.G * a.N;
+      k_scan_shared<T><<<(uint32_t)std::min<int64_t>((shared + kThreads - 1) / kThreads, 1 << 20), kThreads, 0, stream>>>(
+          k, static_cast<T*>(dB), static_cast<T*>(dC));
+    }
+    k_scan_params<<<(uint32_t)((values + 2 * a.D + 63) / 64), 1024, 0, stream>>>(
+        k, a.win.n > 0 ? (int32_t)L.slots : 0, dA, dskip, dbias);
+  };
+  if (dtype == 0) run(float{});
+  else if (dtype == 1) run(_Float16{});
+  else run(bf16_t{});
+  return hipGetLastError();
+}
+
+}  // namespace sla

@@ -34,6 +34,9 @@ Functions mirror the C ABI in include/sla.h:
     step_short_conv(state, slots, x, weight, bias=None, activation="none") -> y
     forward_selective_scan(x, delta, A, B, C, offsets, skip=None, z=None, delta_bias=None, delta_softplus=False,
                            order=None, state=None) -> (y, final_state)
+    backward_selective_scan(x, delta, A, B, C, offsets, dy, dstate=None, skip=None, z=None, delta_bias=None,
+                            delta_softplus=False, order=None, state=None)
+        -> (dx, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, dstate_in)
     step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias=None, delta_softplus=False) -> y
 """
 from __future__ import annotations
@@ -90,6 +93,8 @@ EXPORTED = (
     "sla_step_short_conv",
     "sla_selective_scan_workspace_bytes",
     "sla_forward_selective_scan",
+    "sla_selective_scan_backward_workspace_bytes",
+    "sla_backward_selective_scan",
     "sla_step_selective_scan",
 )
 
@@ -209,6 +214,11 @@ def lib() -> ctypes.CDLL:
     scan_rows = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp]
     L.sla_forward_selective_scan.restype = ctypes.c_int
     L.sla_forward_selective_scan.argtypes = [vp, i64, i32, vp, en, i32, i32, i32, i32] + scan_rows + [vp] * 4 + [sz, vp]
+    L.sla_selective_scan_backward_workspace_bytes.restype = sz
+    L.sla_selective_scan_backward_workspace_bytes.argtypes = [i64, i32, en, i32, i32, i32]
+    L.sla_backward_selective_scan.restype = ctypes.c_int
+    L.sla_backward_selective_scan.argtypes = ([vp, i64, i32, vp, en, i32, i32, i32, i32] + scan_rows
+                                              + [vp, vp, i64] + [vp] * 11 + [sz, vp])
     L.sla_step_selective_scan.restype = ctypes.c_int
     L.sla_step_selective_scan.argtypes = [vp, i64, i32, en, i32, i32, i32, i32, vp] + scan_rows + [vp, vp]
     _lib = L
@@ -1048,6 +1058,50 @@ def forward_selective_scan(x, delta, A, B, C, offsets, skip=None, z=None, delta_
                                               _ptr(final_state), _ptr(workspace), nbytes, _stream(x.device))
     _check(st, "sla_forward_selective_scan")
     return y, final_state
+
+
+def selective_scan_backward_workspace_bytes(n: int, num_windows: int, dtype, channels: int, groups: int,
+                                            states: int) -> int:
+    """Workspace of backward_selective_scan (0: unsupported sizes); dtype a torch dtype."""
+    return int(lib().sla_selective_scan_backward_workspace_bytes(int(n), int(num_windows), _dtype_code(dtype),
+                                                                 int(channels), int(groups), int(states)))
+
+
+def backward_selective_scan(x, delta, A, B, C, offsets, dy, dstate=None, skip=None, z=None, delta_bias=None,
+                            delta_softplus=False, order=None, state=None, out=None, workspace=None):
+    """Gradients of forward_selective_scan (sla_backward_selective_scan): dy like x, dstate (the gradient of
+    final_state) or None; returns (dx, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, dstate_in), where what belongs
+    to an argument that is None is None.  out: contiguous tensors to write dx, ddelta, dB, dC, dz into (rows in
+    no window are left as they were)."""
+    torch = _torch()
+    n, D, G, N, rows = _scan_check(x, delta, A, B, C, skip, z, delta_bias)
+    w = _check_windows(offsets, order, n, x.device)
+    lddy = _row_stride("dy", dy, (n, D), x.dtype, x.device)
+    for name, t in (("state", state), ("dstate", dstate)):
+        _check_like(name, t, (w, D, N), torch.float32, x.device)
+    shapes = [(n, D), (n, D), (n, G, N), (n, G, N), None if z is None else (n, D)]
+    if out is None:
+        out = [None if s is None else torch.empty(s, dtype=x.dtype, device=x.device) for s in shapes]
+    out = list(out)
+    if len(out) != 5 or any((t is None) != (s is None) for t, s in zip(out, shapes)):
+        raise ValueError("out must be the tensors dx, ddelta, dB, dC and dz (None without z)")
+    for name, t, s in zip(("dx", "ddelta", "dB", "dC", "dz"), out, shapes):
+        _check_like(name, t, s, x.dtype, x.device)
+    dx, ddelta, dB, dC, dz = out
+    dA = torch.empty_like(A)
+    dskip = None if skip is None else torch.empty_like(skip)
+    dbias = None if delta_bias is None else torch.empty_like(delta_bias)
+    dstate_in = None if state is None else torch.empty_like(state)
+    workspace, nbytes = _own_workspace(selective_scan_backward_workspace_bytes(n, w, x.dtype, D, G, N), workspace,
+                                       x.device, "sla_selective_scan_backward_workspace_bytes")
+    with torch.cuda.device(x.device):
+        st = lib().sla_backward_selective_scan(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), D, G, N,
+                                               int(bool(delta_softplus)), *rows, _ptr(state), _ptr(dy), lddy,
+                                               _ptr(dstate), _ptr(dx), _ptr(ddelta), _ptr(dA), _ptr(dB), _ptr(dC),
+                                               _ptr(dskip), _ptr(dz), _ptr(dbias), _ptr(dstate_in),
+                                               _ptr(workspace), nbytes, _stream(x.device))
+    _check(st, "sla_backward_selective_scan")
+    return dx, ddelta, dA, dB, dC, dskip, dz, dbias, dstate_in
 
 
 def step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias=None, delta_softplus=False,

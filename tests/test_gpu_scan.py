@@ -275,3 +275,125 @@ def test_wrong_offsets_stay_in_range(sla, offsets, fill):
         torch.cuda.synchronize()
         for t in (y, fin):
             assert (t[0] == 7.0).all() and (t[2] == 7.0).all()
+
+
+# ------------------------------------------------------------------ gradients
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("D,N,G", SHAPES)
+def test_backward_shapes(sla, dtype, D, N, G):
+    Case([5, 0, 1, 70, 33, 2, 0, 140], D, N, dtype, G, seed=D + N, state=N % 2 == 0, front=2, behind=3).backward(sla)
+
+
+@pytest.mark.parametrize("lengths", LENGTHS)
+def test_backward_lengths(sla, lengths):
+    for state in (False, True):
+        Case(lengths, 40, 16, "f32", seed=3, state=state).backward(sla)
+        Case(lengths, 9, 6, "bf16", 3, seed=4, state=state, behind=1).backward(sla)
+
+
+@pytest.mark.parametrize("kw", [dict(skip=False), dict(gate=False), dict(bias=False), dict(softplus=False),
+                                dict(skip=False, gate=False, bias=False, softplus=False)])
+def test_backward_options(sla, kw):
+    Case([40, 90, 3], 80, 16, "f32", seed=5, state=True, **kw).backward(sla)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_strided_rows_and_order(sla, dtype):
+    for kw in (dict(strided=True), dict(order=True), dict(order=True, strided=True)):
+        Case([30, 4, 150], 96, 16, dtype, 2, seed=6, state=True, behind=2, front=1, **kw).backward(sla)
+
+
+def test_backward_of_long_windows(sla):
+    """Many parts; where nothing is forgotten, all of 2,300 rows' roundings stay."""
+    Case([1800, 500], 24, 16, "f32", seed=7, state=True).backward(sla)
+    Case([1800, 500], 24, 16, "f32", seed=7, state=True, slow=True).backward(sla, bar=2300 * 2.0 ** -23)
+    Case([3000], 300, 4, "bf16", seed=8).backward(sla)
+
+
+def test_gradients_by_differences(sla):
+    import torch
+
+    c = Case([30, 3, 41], 12, 5, "f32", 2, seed=18, state=True)
+    got = dict(zip(GRADS, c.gradients(sla)))
+    rows = {k: c.r[k] for k in (*ROWS, *OPTIONS)}
+    rows["state"] = c.state
+
+    def loss(r):
+        host = {k: num(v) for k, v in r.items()}
+        y, st = space_ref.scan_forward_ref(*(host[k] for k in ROWS), c.offsets, *(host[k] for k in OPTIONS),
+                                           delta_softplus=True, state=host["state"])
+        return (y * num(c.r["dy"])).sum() + (st * num(c.dstate)).sum()
+
+    gen = torch.Generator().manual_seed(1)
+    for name, grad in (("x", "dx"), ("delta", "ddelta"), ("A", "dA"), ("B", "dB"), ("C", "dC"), ("skip", "dskip"),
+                       ("z", "dz"), ("delta_bias", "ddelta_bias"), ("state", "dstate_in")):
+        d = torch.randn(rows[name].shape, generator=gen, dtype=torch.float64)
+        up, down = (loss({**rows, name: rows[name].double().cpu() + s * 1e-4 * d}) for s in (1, -1))
+        mine = float((got[grad].double().cpu() * d).sum())
+        # the difference's own error is 1e-8 of a third derivative; the gradient's 1e-5 of its size
+        assert abs((up - down) / 2e-4 - mine) <= 1e-5 * float(got[grad].double().norm() * d.norm()) + 1e-6, name
+
+
+def test_gradient_of_the_state_in_place(sla):
+    """dstate_in where dstate_out lies: the first part's workgroup writes what the last one's reads."""
+    import torch
+
+    for lengths in ([40, 0, 3], [700, 64, 33, 0, 400]):
+        c = Case(lengths, 72, 16, "f32", seed=19, state=True)
+        want = c.gradients(sla)
+        n, w = c.n, c.w
+        for _ in range(3):
+            ds = c.dstate.clone()
+            outs = [torch.zeros_like(c.r[k]) for k in ("x", "delta")]
+            par = [torch.zeros_like(c.r["A"]), torch.zeros_like(c.r["B"]), torch.zeros_like(c.r["C"]),
+                   torch.zeros_like(c.r["skip"]), torch.zeros_like(c.r["z"]), torch.zeros_like(c.r["skip"])]
+            need = sla.selective_scan_backward_workspace_bytes(n, w, torch.float32, 72, 1, 16)
+            ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+            p = lambda t: t.data_ptr()  # noqa: E731
+            r = c.r
+            rc = sla.lib().sla_backward_selective_scan(
+                p(c.off), n, w, None, 0, 72, 1, 16, 1, p(r["x"]), 72, p(r["delta"]), 72, p(r["A"]), p(r["B"]), 16, p(r["C"]),
+                16, p(r["skip"]), p(r["z"]), 72, p(r["delta_bias"]), p(c.state), p(r["dy"]), 72, p(ds), *map(p, outs),
+                *map(p, par), p(ds), p(ws), need, torch.cuda.current_stream().cuda_stream)
+            assert rc == 0
+            for a, b in zip((*outs, *par, ds), want):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fill", [0, 0x7f, 0xff])
+@pytest.mark.parametrize("offsets", WRONG)
+def test_backward_wrong_offsets_stay_in_range(sla, offsets, fill):
+    import torch
+
+    n, D, N = 700, 40, 8
+    c = Case([n], D, N, "bf16", seed=17)
+    off = torch.tensor(offsets, dtype=torch.int32).cuda()
+    w = len(offsets) - 1
+    state = torch.randn(w, D, N).cuda()
+    bad = torch.arange(n, dtype=torch.int32).cuda() * 3 - n
+    for order in (None, bad):
+        ws = torch.full((sla.selective_scan_backward_workspace_bytes(n, w, torch.bfloat16, D, 1, N),), fill,
+                        dtype=torch.uint8).cuda()
+        outs = [torch.full((3, *c.r[k].shape), 7.0, dtype=torch.bfloat16).cuda() for k in ("x", "delta", "B", "C", "z")]
+        sla.backward_selective_scan(*c.args(), off, c.r["dy"], dstate=state, out=[t[1] for t in outs], workspace=ws,
+                                    **{**c.kw, "order": order, "state": state})
+        torch.cuda.synchronize()
+        for t in outs:
+            assert (t[0] == 7.0).all() and (t[2] == 7.0).all()
+
+
+def test_workspace_contents_do_not_matter(sla):
+    import torch
+
+    for lengths, N in (([130, 1, 0, 64, 7], 16), ([700, 300], 5)):
+        c = Case(lengths, 72, N, "f32", seed=20, behind=5, order=True, state=True)
+        got = []
+        for fill in (0, 0xff, 0x7b):
+            size = (c.n, c.w, torch.float32, 72, 1, N)
+            ws = torch.full((max(sla.selective_scan_backward_workspace_bytes(*size),
+                                 sla.selective_scan_workspace_bytes(*size)),), fill, dtype=torch.uint8).cuda()
+            y, st = sla.forward_selective_scan(*c.args(), c.off, y=c.new(c.r["x"]), workspace=ws, **c.kw)
+            ws.fill_(fill)
+            got.append([y, st, *c.gradients(sla, workspace=ws)])
+        for g in got[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(got[0], g))
