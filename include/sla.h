@@ -688,6 +688,47 @@ sla_status_t sla_step_selective_scan(const int32_t* slots, int64_t n, int32_t nu
                                      const void* C, int64_t C_stride, const float* skip, const void* z,
                                      int64_t z_stride, const float* delta_bias, void* y, sla_stream_t stream);
 
+/*
+ * The normalisation between two blocks, row by row: the norm of a block's output x, its gate and scale, the
+ * residual sum, and the norm that the next block reads.  With rms(v) = v / sqrt(mean(v^2) + eps),
+ *     u = rms(x) post_weight  (post_weight NULL: x),
+ *     residual_out = residual + scale act(gate) u,      y = rms(residual_out) weight.
+ *   x, gate, y  [n, channels] in `dtype`, contiguous; gate may be NULL (1).
+ *   residual, residual_out  [n, channels] in `residual_dtype` (`dtype` or SLA_F32, else SLA_E_ARG), contiguous;
+ *             residual may be NULL (0), residual_out may be residual.
+ *   weight, post_weight  fp32 [channels]; weight may be NULL (1).  channels up to 8,192, else
+ *             SLA_E_UNSUPPORTED.  16-byte aligned rows are fastest, none of it is required.
+ *   rstd, post_rstd  fp32 [n], outputs: 1 / sqrt(mean + eps) of both norms (the backward reads them; post_rstd
+ *             may be NULL without post_weight).
+ *   eps       finite and >= 0;  scale finite.
+ * All arithmetic is fp32 and y comes from the sum as it is before residual_out is rounded; squares beyond
+ * fp32's range are taken at the row's power of two.  A value that is not finite reaches only its row.
+ * Deterministic.  y must not be an input.
+ */
+sla_status_t sla_forward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t residual_dtype, int32_t channels,
+                                       float eps, float scale, sla_activation_t activation, const void* x,
+                                       const void* residual, const void* gate, const float* post_weight,
+                                       const float* weight, void* y, void* residual_out, float* rstd,
+                                       float* post_rstd, sla_stream_t stream);
+
+/*
+ * Backward of sla_forward_residual_norm (the chain rule), from its x, gate, residual_out and statistics, dy =
+ * dL/dy and dresidual_out = dL/d(residual_out) by its other uses (NULL: zero): dx, dgate (with a gate) in
+ * `dtype`, dresidual in `residual_dtype` (may be NULL, or dresidual_out), dweight and dpost_weight (fp32
+ * [channels], each may be NULL), summed over all rows in a fixed order.  relu's slope at 0 is 0.
+ * `workspace`: device, 256-byte aligned, sla_residual_norm_backward_workspace_bytes() bytes (0 for sizes that
+ * are not supported), else SLA_E_WORKSPACE.  The other outputs must not be inputs.
+ */
+size_t sla_residual_norm_backward_workspace_bytes(int64_t n, sla_dtype_t dtype, int32_t channels);
+
+sla_status_t sla_backward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t residual_dtype, int32_t channels,
+                                        float scale, sla_activation_t activation, const void* x,
+                                        const void* residual_out, const void* gate, const float* post_weight,
+                                        const float* weight, const float* rstd, const float* post_rstd,
+                                        const void* dy, const void* dresidual_out, void* dx, void* dresidual,
+                                        void* dgate, float* dweight, float* dpost_weight, void* workspace,
+                                        size_t workspace_bytes, sla_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

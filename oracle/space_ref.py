@@ -157,3 +157,45 @@ def scan_step_ref(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias
                                        delta_bias, delta_softplus, state=S[s:s + 1])
             y[b], S[s] = out[0], st[0]
     return y, S
+
+
+# ------------------------------------------------------------------ residual normalisation
+def rnorm_forward_ref(x, residual, weight=None, post_weight=None, gate=None, activation="none", scale=1.0, eps=1e-5):
+    """(y, residual_out, rstd, post_rstd)"""
+    u = np.asarray(x, np.float64)
+    post = None
+    if post_weight is not None:
+        post = 1 / np.sqrt((u * u).mean(-1) + eps)
+        u = u * post[:, None] * post_weight
+    if gate is not None:
+        u = u * _act(activation, np.asarray(gate, np.float64))
+    r = scale * u + (0.0 if residual is None else np.asarray(residual, np.float64))
+    rstd = 1 / np.sqrt((r * r).mean(-1) + eps)
+    return r * rstd[:, None] * (1.0 if weight is None else weight), r, rstd, post
+
+
+def rnorm_backward_ref(x, residual_out, dy, rstd, weight=None, post_weight=None, post_rstd=None, gate=None,
+                       activation="none", scale=1.0, dresidual_out=None):
+    """(dx, dresidual, dweight, dpost_weight, dgate)"""
+    x, r, dy = (np.asarray(t, np.float64) for t in (x, residual_out, dy))
+
+    def norm(v, s, d):
+        hat = v * s[:, None]
+        return s[:, None] * (d - hat * (d * hat).mean(-1, keepdims=True)), hat
+
+    dr, hat = norm(r, rstd, dy if weight is None else dy * weight)
+    dweight = (dy * hat).sum(0)
+    if dresidual_out is not None:
+        dr = dr + dresidual_out
+    d = scale * dr
+    u = x if post_weight is None else x * post_rstd[:, None] * post_weight
+    dgate = None
+    if gate is not None:
+        gate = np.asarray(gate, np.float64)
+        dgate = d * u * _slope(activation, gate)
+        d = d * _act(activation, gate)
+    dpost = None
+    if post_weight is not None:
+        dpost = (d * x * post_rstd[:, None]).sum(0)
+        d, _ = norm(x, post_rstd, d * post_weight)
+    return d, dr, dweight, dpost, dgate

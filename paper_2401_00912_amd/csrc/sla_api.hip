@@ -91,6 +91,16 @@ hipError_t launch_backward_conv(const int32_t* offsets, int32_t n, int32_t W, co
 hipError_t launch_step_conv(const int32_t* slots, int32_t n, int32_t num_slots, int dtype, int32_t C, int32_t K,
                             int activation, void* state, const void* x, int64_t ldx, const float* weight,
                             const float* bias, void* y, hipStream_t stream);
+size_t rnorm_backward_workspace_bytes(int64_t n, int32_t C);
+hipError_t launch_forward_rnorm(int64_t n, int dtype, int rtype, int32_t C, float eps, float scale, int activation,
+                                const void* x, const void* residual, const void* gate, const float* post_weight,
+                                const float* weight, void* y, void* residual_out, float* rstd, float* post_rstd,
+                                hipStream_t stream);
+hipError_t launch_backward_rnorm(int64_t n, int dtype, int rtype, int32_t C, float scale, int activation, const void* x,
+                                 const void* residual_out, const void* gate, const float* post_weight,
+                                 const float* weight, const float* rstd, const float* post_rstd, const void* dy,
+                                 const void* dresidual_out, void* dx, void* dresidual, void* dgate, float* dweight,
+                                 float* dpost_weight, void* workspace, hipStream_t stream);
 size_t scan_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N);
 hipError_t launch_forward_scan(scan::ScanArgs a, int dtype, const void* x, const void* delta, const void* z, const void* B,
                                const void* C, const float* state_in, void* y, float* state_out, void* workspace,
@@ -927,4 +937,82 @@ SLA_EXPORT sla_status_t sla_step_selective_scan(
   a.D = channels, a.G = groups, a.N = states, a.softplus = delta_softplus != 0;
   return hip_status(sla::launch_step_scan(a, (int)dtype, slots, num_slots, state, x, delta, z, B, C, y,
                                           static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// What both residual normalisation calls are given.
+sla_status_t check_rnorm(int64_t n, int dtype, int rtype, int32_t channels, int activation, const float* weight,
+                         const float* post_weight, float scale) {
+  if (n < 0 || n >= INT32_MAX || channels < 1) return SLA_E_ARG;
+  if (dtype < 0 || dtype > 2 || (rtype != dtype && rtype != SLA_F32)) return SLA_E_ARG;
+  if (channels > 8192) return SLA_E_UNSUPPORTED;
+  if (activation < SLA_ACT_NONE || activation > SLA_ACT_SILU) return SLA_E_ARG;
+  if (!aligned(weight, 4) || !aligned(post_weight, 4) || !finite(scale)) return SLA_E_ARG;
+  return SLA_OK;
+}
+
+}  // namespace
+
+SLA_EXPORT sla_status_t sla_forward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t residual_dtype,
+                                                  int32_t channels, float eps, float scale,
+                                                  sla_activation_t activation, const void* x, const void* residual,
+                                                  const void* gate, const float* post_weight, const float* weight,
+                                                  void* y, void* residual_out, float* rstd, float* post_rstd,
+                                                  sla_stream_t stream) {
+  const sla_status_t st =
+      check_rnorm(n, (int)dtype, (int)residual_dtype, channels, (int)activation, weight, post_weight, scale);
+  if (st != SLA_OK) return st;
+  if (!(eps >= 0.f && finite(eps))) return SLA_E_ARG;
+  if (n == 0) return SLA_OK;
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2, rs = residual_dtype == SLA_F32 ? 4 : 2;
+  if (!x || !y || !residual_out || !rstd || !aligned(x, es) || !aligned(y, es) || !aligned(gate, es) ||
+      !aligned(residual, rs) || !aligned(residual_out, rs) || !aligned(rstd, 4) || !aligned(post_rstd, 4) ||
+      (post_weight != nullptr && post_rstd == nullptr))
+    return SLA_E_ARG;
+  if (y == x || y == gate || y == residual || y == residual_out || residual_out == x || residual_out == gate)
+    return SLA_E_ARG;
+  return hip_status(sla::launch_forward_rnorm(n, (int)dtype, (int)residual_dtype, channels, eps, scale, (int)activation,
+                                              x, residual, gate, post_weight, weight, y, residual_out, rstd, post_rstd,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+SLA_EXPORT size_t sla_residual_norm_backward_workspace_bytes(int64_t n, sla_dtype_t dtype, int32_t channels) {
+  if (check_rnorm(n, (int)dtype, (int)dtype, channels, SLA_ACT_NONE, nullptr, nullptr, 1.f) != SLA_OK) return 0;
+  return sla::rnorm_backward_workspace_bytes(n, channels);
+}
+
+SLA_EXPORT sla_status_t sla_backward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t residual_dtype,
+                                                   int32_t channels, float scale, sla_activation_t activation,
+                                                   const void* x, const void* residual_out, const void* gate,
+                                                   const float* post_weight, const float* weight, const float* rstd,
+                                                   const float* post_rstd, const void* dy, const void* dresidual_out,
+                                                   void* dx, void* dresidual, void* dgate, float* dweight,
+                                                   float* dpost_weight, void* workspace, size_t workspace_bytes,
+                                                   sla_stream_t stream) {
+  const sla_status_t st =
+      check_rnorm(n, (int)dtype, (int)residual_dtype, channels, (int)activation, weight, post_weight, scale);
+  if (st != SLA_OK) return st;
+  const uintptr_t es = dtype == SLA_F32 ? 4 : 2, rs = residual_dtype == SLA_F32 ? 4 : 2;
+  if (!aligned(x, es) || !aligned(residual_out, rs) || !aligned(gate, es) || !aligned(rstd, 4) ||
+      !aligned(post_rstd, 4) || !aligned(dy, es) || !aligned(dresidual_out, rs) || !aligned(dx, es) ||
+      !aligned(dresidual, rs) || !aligned(dgate, es) || !aligned(dweight, 4) || !aligned(dpost_weight, 4))
+    return SLA_E_ARG;
+  if (n > 0) {
+    if (!x || !residual_out || !rstd || !dy || !dx || (gate != nullptr && !dgate) ||
+        (post_weight != nullptr && !post_rstd))
+      return SLA_E_ARG;
+    const void* in[] = {x, residual_out, gate, dy};
+    const void* out[] = {dx, dresidual, gate != nullptr ? dgate : nullptr};
+    for (const void* o : out)
+      for (const void* i : in)
+        if (o != nullptr && o == i) return SLA_E_ARG;
+    if (dx == dresidual_out || (gate != nullptr && dgate == dresidual_out)) return SLA_E_ARG;
+  }
+  if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
+  if (workspace_bytes < sla::rnorm_backward_workspace_bytes(n, channels)) return SLA_E_WORKSPACE;
+  return hip_status(sla::launch_backward_rnorm(n, (int)dtype, (int)residual_dtype, channels, scale, (int)activation, x,
+                                               residual_out, gate, post_weight, weight, rstd, post_rstd, dy,
+                                               dresidual_out, dx, dresidual, dgate, dweight, dpost_weight, workspace,
+                                               static_cast<hipStream_t>(stream)));
 }

@@ -38,6 +38,11 @@ Functions mirror the C ABI in include/sla.h:
                             delta_softplus=False, order=None, state=None)
         -> (dx, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, dstate_in)
     step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delta_bias=None, delta_softplus=False) -> y
+    forward_residual_norm(x, residual, weight=None, post_weight=None, gate=None, activation="none", scale=1.0,
+                          eps=1e-5) -> (y, residual_out, rstd, post_rstd)
+    backward_residual_norm(x, residual_out, dy, rstd, weight=None, post_weight=None, post_rstd=None, gate=None,
+                           activation="none", scale=1.0, dresidual_out=None)
+        -> (dx, dresidual, dweight, dpost_weight, dgate)
 """
 from __future__ import annotations
 
@@ -96,6 +101,9 @@ EXPORTED = (
     "sla_selective_scan_backward_workspace_bytes",
     "sla_backward_selective_scan",
     "sla_step_selective_scan",
+    "sla_forward_residual_norm",
+    "sla_residual_norm_backward_workspace_bytes",
+    "sla_backward_residual_norm",
 )
 
 
@@ -221,6 +229,12 @@ def lib() -> ctypes.CDLL:
                                               + [vp, vp, i64] + [vp] * 11 + [sz, vp])
     L.sla_step_selective_scan.restype = ctypes.c_int
     L.sla_step_selective_scan.argtypes = [vp, i64, i32, en, i32, i32, i32, i32, vp] + scan_rows + [vp, vp]
+    L.sla_forward_residual_norm.restype = ctypes.c_int
+    L.sla_forward_residual_norm.argtypes = [i64, en, en, i32, f32, f32, en] + [vp] * 10
+    L.sla_residual_norm_backward_workspace_bytes.restype = sz
+    L.sla_residual_norm_backward_workspace_bytes.argtypes = [i64, en, i32]
+    L.sla_backward_residual_norm.restype = ctypes.c_int
+    L.sla_backward_residual_norm.argtypes = [i64, en, en, i32, f32, en] + [vp] * 15 + [sz, vp]
     _lib = L
     return L
 
@@ -1122,6 +1136,83 @@ def step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delt
                                            int(bool(delta_softplus)), _ptr(state), *rows, _ptr(y), _stream(x.device))
     _check(st, "sla_step_selective_scan")
     return y
+
+
+def _residual_norm_check(x, residual, weight, post_weight, gate, activation):
+    """Shapes, dtypes, devices and layouts of a residual normalisation call: (n, channels, the activation's
+    code)."""
+    torch = _torch()
+    if x.dim() != 2 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous [n, channels] tensor")
+    for name, t in (("weight", weight), ("post_weight", post_weight)):
+        _check_like(name, t, (x.shape[1],), torch.float32, x.device)
+    _check_like("gate", gate, x.shape, x.dtype, x.device)
+    if residual is not None:
+        _check_like("residual", residual, x.shape, torch.float32 if residual.dtype == torch.float32 else x.dtype, x.device)
+    return x.shape[0], x.shape[1], _check_activation(activation)
+
+
+def forward_residual_norm(x, residual, weight=None, post_weight=None, gate=None, activation="none", scale=1.0, eps=1e-5,
+                          y=None, residual_out=None):
+    """The normalisation between two blocks (sla_forward_residual_norm): x [n, channels] a block's output,
+    residual [n, channels] of x's type or float32, or None (zero, of x's type), weight and post_weight float32
+    [channels] (post_weight None: x is not normalised), gate like x or None, activation that of the
+    gate.  Returns (y, residual_out, rstd, post_rstd): the next block's input, the new residual rows and
+    the statistics float32 [n], post_rstd None without post_weight."""
+    torch = _torch()
+    n, C, act = _residual_norm_check(x, residual, weight, post_weight, gate, activation)
+    rtype = x.dtype if residual is None else residual.dtype
+    y = torch.empty_like(x) if y is None else y
+    _check_like("y", y, x.shape, x.dtype, x.device)
+    residual_out = torch.empty(x.shape, dtype=rtype, device=x.device) if residual_out is None else residual_out
+    _check_like("residual_out", residual_out, x.shape, rtype, x.device)
+    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    post_rstd = None if post_weight is None else torch.empty(n, dtype=torch.float32, device=x.device)
+    with torch.cuda.device(x.device):
+        st = lib().sla_forward_residual_norm(n, _dtype_code(x.dtype), _dtype_code(rtype), C, float(eps), float(scale),
+                                             act, _ptr(x), _ptr(residual), _ptr(gate), _ptr(post_weight),
+                                             _ptr(weight), _ptr(y), _ptr(residual_out), _ptr(rstd), _ptr(post_rstd),
+                                             _stream(x.device))
+    _check(st, "sla_forward_residual_norm")
+    return y, residual_out, rstd, post_rstd
+
+
+def residual_norm_backward_workspace_bytes(n: int, dtype, channels: int) -> int:
+    """Workspace of backward_residual_norm (0: unsupported sizes); dtype a torch dtype."""
+    return int(lib().sla_residual_norm_backward_workspace_bytes(int(n), _dtype_code(dtype), int(channels)))
+
+
+def backward_residual_norm(x, residual_out, dy, rstd, weight=None, post_weight=None, post_rstd=None, gate=None,
+                           activation="none", scale=1.0, dresidual_out=None, dx=None, dresidual=None, workspace=None):
+    """Gradients of forward_residual_norm (sla_backward_residual_norm), from its input, new residual rows and
+    statistics: dy like x, dresidual_out (the gradient of residual_out by its other uses) like it or
+    None.  Returns (dx, dresidual, dweight, dpost_weight, dgate), where what belongs to an argument that is
+    None is None."""
+    torch = _torch()
+    n, C, act = _residual_norm_check(x, residual_out, weight, post_weight, gate, activation)
+    _check_like("dy", dy, x.shape, x.dtype, x.device)
+    _check_like("rstd", rstd, (n,), torch.float32, x.device)
+    if (post_rstd is None) != (post_weight is None):
+        raise ValueError("post_rstd is the forward's with post_weight, and None without")
+    _check_like("post_rstd", post_rstd, (n,), torch.float32, x.device)
+    _check_like("dresidual_out", dresidual_out, x.shape, residual_out.dtype, x.device)
+    dx = torch.empty_like(x) if dx is None else dx
+    _check_like("dx", dx, x.shape, x.dtype, x.device)
+    dresidual = torch.empty_like(residual_out) if dresidual is None else dresidual
+    _check_like("dresidual", dresidual, x.shape, residual_out.dtype, x.device)
+    dgate = None if gate is None else torch.empty_like(gate)
+    dweight = None if weight is None else torch.empty_like(weight)
+    dpost = None if post_weight is None else torch.empty_like(post_weight)
+    workspace, nbytes = _own_workspace(residual_norm_backward_workspace_bytes(n, x.dtype, C), workspace, x.device,
+                                       "sla_residual_norm_backward_workspace_bytes")
+    with torch.cuda.device(x.device):
+        st = lib().sla_backward_residual_norm(n, _dtype_code(x.dtype), _dtype_code(residual_out.dtype), C, float(scale),
+                                              act, _ptr(x), _ptr(residual_out), _ptr(gate), _ptr(post_weight),
+                                              _ptr(weight), _ptr(rstd), _ptr(post_rstd), _ptr(dy),
+                                              _ptr(dresidual_out), _ptr(dx), _ptr(dresidual), _ptr(dgate),
+                                              _ptr(dweight), _ptr(dpost), _ptr(workspace), nbytes, _stream(x.device))
+    _check(st, "sla_backward_residual_norm")
+    return dx, dresidual, dweight, dpost, dgate
 
 
 def read_plan(plan: Plan):

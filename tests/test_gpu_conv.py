@@ -32,9 +32,9 @@ def sla():
     return S
 
 
-def close(got, ref, dtype, name, bar=1e-5):
-    """Every value within half a step of its type and `bar` of the largest; NaN where the reference has it
-    stands for a row that is left as it was (7)."""
+def close(got, ref, dtype, name, bar=1e-5, size=None):
+    """Every value within half a step of its type and `bar` of the largest (or of `size`, the largest term of
+    results that cancel); NaN where the reference has it stands for a row that is left as it was (7)."""
     got = got.detach().double().cpu().numpy()
     assert got.shape == ref.shape, name
     real = ~np.isnan(ref)
@@ -43,7 +43,7 @@ def close(got, ref, dtype, name, bar=1e-5):
     if not ref.size:
         return
     assert np.isfinite(got).all(), name
-    limit = HALF_STEP[dtype] * np.abs(ref) + bar * max(np.abs(ref).max(), 1e-30) + (2.0 ** -25 if dtype == "f16" else 0)
+    limit = HALF_STEP[dtype] * np.abs(ref) + bar * max(np.abs(ref).max(), size or 1e-30) + (2.0 ** -25 if dtype == "f16" else 0)
     worst = np.max(np.abs(got - ref) / limit)
     assert worst <= 1.0, f"{name}: {worst:.3g} times its limit"
 
