@@ -38,24 +38,22 @@ __device__ __forceinline__ float slope(int a, float z) {
   return 1.f;
 }
 
-// log(1 + e^x) to 2^-21 of its value: the larger of x and 0, and log(1 + e) of e = e^-|x| in [0, 1] as
-// 2 atanh(s), s = e / (2 + e) <= 1 / 3, by its power series (what is left out is 2^-26 of the sum at most).
-// A logarithm of 1 + e would lose the bits of a small e: step sizes of 0.001 are usual.  The exponent in two
-// terms, as above.
+// z / (1 + e^-z) and log(1 + e^x) where they are a small part of the work of every row, with the exponent in one
+// term: e^-|x| is off by |x| 2^-23 of itself, which is what the values below 0 are off by.
+__device__ __forceinline__ float quick_silu(float z) {
+  z = from_below(z);
+  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+}
+// The larger of x and 0, and log(1 + e) of e = e^-|x| in [0, 1] as 2 atanh(s), s = e / (2 + e) <= 1 / 3, with atanh(s)
+// / s a polynomial in s^2 through the Chebyshev points of [0, 1 / 9] (off by 2^-26).  A logarithm of 1 + e would lose
+// the bits of a small e: step sizes of 0.001 are usual.
 __device__ __forceinline__ float softplus(float x) {
-  constexpr float kHi = -1.44269502f, kLo = -1.92596299e-8f;
-  const float y = __builtin_elementwise_minimum(__builtin_fabsf(x), 128.f);
-  const float t = y * kHi;
-  const float r = __builtin_fmaf(y, kHi, -t) + y * kLo;
-  float e = __builtin_amdgcn_exp2f(t);
-  e = __builtin_fmaf(e, r * 0.693147181f, e);
+  const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(x));
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
-  float p = 1.f / 13.f;
-  p = __builtin_fmaf(p, q, 1.f / 11.f);
-  p = __builtin_fmaf(p, q, 1.f / 9.f);
-  p = __builtin_fmaf(p, q, 1.f / 7.f);
-  p = __builtin_fmaf(p, q, 1.f / 5.f);
-  p = __builtin_fmaf(p, q, 1.f / 3.f);
+  float p = 0.1407889f;
+  p = __builtin_fmaf(p, q, 0.13982579f);
+  p = __builtin_fmaf(p, q, 0.20012298f);
+  p = __builtin_fmaf(p, q, 0.3333316f);
   p = __builtin_fmaf(p, q, 1.f);
   return __builtin_fmaf(2.f * s, p, __builtin_elementwise_maximum(x, 0.f));
 }

@@ -3,7 +3,9 @@
 //     h_t[n] = exp(dt_t A[d][n]) h_{t-1}[n] + u_t B_t[n],
 //     y_t = (sum_n C_t[n] h_t[n] + skip x_t) silu(z_t).
 // A wave takes 64 channels of one group (the channels that share B and C), a lane a channel: h is in
-// registers, and the only thing lanes share, the rows' B and C, comes from LDS as a broadcast.
+// registers, and what all lanes share, the rows' B and C, comes from LDS as a broadcast into vector registers
+// too: an instruction whose operands are all there takes 2.4 cycles with two waves or more on a SIMD, one
+// with a scalar operand 4.2 (measured; an exponential 8.2).
 //
 // Windows are cut into parts of at most `per` rows that waves walk at the same time.  What a part hands on is
 // a linear map of what it is given, h -> exp(A sum dt) h + S: a first launch makes S and sum dt of each part
@@ -39,9 +41,16 @@ struct Tile {
   }
 };
 
+__device__ __forceinline__ int tile_group(const ScanArgs& a, int tile) { return tile / a.tpg; }
+
 __device__ __forceinline__ float step_size(const ScanArgs& a, float delta, float bias) {
   const float x = delta + bias;
   return a.softplus ? softplus(x) : x;
+}
+
+// A as the exponent of two; finite, so that a step of 0 keeps the state whatever A is.
+__device__ __forceinline__ float exponent(float A) {
+  return __builtin_elementwise_minimum(__builtin_elementwise_maximum(A * kLog2e, -3e38f), 3e38f);
 }
 
 // NS >= N values of a channel from [N] consecutive floats; fill beyond
@@ -92,14 +101,26 @@ struct Parts {
   float *S, *dts;
 };
 
+// the states that a lane is built for
+inline int padded_states(int N) { return N <= 1 ? 1 : N <= 4 ? 4 : N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
 template <class F>
 void by_states(int N, F f) {
-  if (N <= 1) f(std::integral_constant<int, 1>{});
-  else if (N <= 4) f(std::integral_constant<int, 4>{});
-  else if (N <= 8) f(std::integral_constant<int, 8>{});
-  else if (N <= 16) f(std::integral_constant<int, 16>{});
-  else if (N <= 32) f(std::integral_constant<int, 32>{});
-  else f(std::integral_constant<int, 64>{});
+  switch (padded_states(N)) {
+    case 1: f(std::integral_constant<int, 1>{}); break;
+    case 4: f(std::integral_constant<int, 4>{}); break;
+    case 8: f(std::integral_constant<int, 8>{}); break;
+    case 16: f(std::integral_constant<int, 16>{}); break;
+    case 32: f(std::integral_constant<int, 32>{}); break;
+    default: f(std::integral_constant<int, 64>{}); break;
+  }
+}
+
+// Workgroups across the states of a window where its parts are joined: one value a thread for few windows,
+// where that is latency; several for many, most of which have one part and nothing to do.
+inline uint32_t carry_blocks(const ScanArgs& a) {
+  const int64_t all = ((int64_t)a.N * a.D + 255) / 256;
+  const int64_t some = 4096 / a.win.W;
+  return (uint32_t)(all < some ? all : some < 1 ? 1 : some);
 }
 
 inline int64_t slots_of(const ScanArgs& a) { return (int64_t)a.win.n / a.per + a.win.W; }

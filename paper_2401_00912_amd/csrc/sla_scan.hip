@@ -9,17 +9,17 @@ namespace {
 
 using namespace scan;
 
-// Rows a wave loads at once: the next ones are on their way while these are computed.
-template <int NS>
-constexpr int kRows = NS <= 16 ? 8 : 4;
+// Rows a wave takes at once: the next ones are on their way while these are computed.
+constexpr int kRows = 4;
 
-// OUT: the walk that makes y; else the one that makes a part's map.
-template <typename T, int NS, bool OUT>
+// OUT: the walk that makes y; else the one that makes a part's map.  ORDER: positions are not rows.
+template <typename T, int NS, bool OUT, bool ORDER>
 __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x, const T* __restrict__ delta,
                                              const T* __restrict__ z, const T* __restrict__ B, const T* __restrict__ C,
                                              const float* __restrict__ state, T* __restrict__ y,
                                              float* __restrict__ state_out, Parts parts) {
-  constexpr int U = kRows<NS>, V = OUT ? 2 * NS : NS, J = (U * V + 63) / 64;
+  // a row's B and, behind it, C; J of a batch's values a lane
+  constexpr int U = kRows, V = OUT ? 2 * NS : NS, J = (U * V + 63) / 64;
   __shared__ __attribute__((aligned(16))) float s_bc[J * 64];
   Part part;
   if (!part_of(a.win, a.per, blockIdx.x, part)) return;
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x
   float A[NS], h[NS];
   load_states<NS>(a.A + (size_t)c * a.N, a.N, by_four(a.A, a.N), A);
 #pragma unroll
-  for (int n = 0; n < NS; ++n) A[n] *= kLog2e;
+  for (int n = 0; n < NS; ++n) A[n] = exponent(A[n]);
   if (OUT && !part.first) {
     const float* p = parts.S + (size_t)(blockIdx.x - 1) * a.N * a.D + c;
 #pragma unroll
@@ -51,62 +51,80 @@ __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x
   const float bias = a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
   float dts = 0.f;
 
-  T xr[U], dr[U], zr[U], bc[J];
+  // x, delta and z of the next rows
+  T xr[U], dr[U], zr[U] = {}, bc[J];
   const auto ask = [&](int p0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int r = p0 + i < part.end ? a.win.row(p0 + i) : -1;
-      xr[i] = dr[i] = zr[i] = from_float<T>(0.f);
-      if (r >= 0) {
-        xr[i] = x[r * a.ldx + c];
-        dr[i] = delta[r * a.ldd + c];
-        if (OUT && z != nullptr) zr[i] = z[r * a.ldz + c];
-      }
-    }
-#pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int at = lane + 64 * j, p = p0 + at / V, v = at % V, n = v % NS;
+      const int i = (lane + 64 * j) / V, v = (lane + 64 * j) % V, n = v % NS, p = p0 + i;
+      int r = i < U && n < a.N && p < part.end ? p : -1;
+      if (ORDER && r >= 0) r = a.win.row(r);
       bc[j] = from_float<T>(0.f);
-      const int r = p < part.end && at < U * V && n < a.N ? a.win.row(p) : -1;
       if (r >= 0) bc[j] = v < NS ? B[r * a.ldb + tile.g * a.N + n] : C[r * a.ldc + tile.g * a.N + n];
+    }
+    // rows past the end are the last one, and are not used
+    uint32_t off = c;
+    asm volatile("" : "+v"(off));   // the lane's part of an address stays 32 bits beside a scalar base
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = min(p0 + i, part.end - 1), r = ORDER ? max(a.win.row(at), 0) : at;
+      xr[i] = lane_at(x + r * a.ldx, off);
+      dr[i] = lane_at(delta + r * a.ldd, off);
+      if (OUT && z != nullptr) zr[i] = lane_at(z + r * a.ldz, off);
     }
   };
   ask(part.begin);
   for (int p0 = part.begin; p0 < part.end; p0 += U) {
-    T xc[U], dc[U], zc[U];
+    float xv[U], dt[U], zv[U], sum[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) xc[i] = xr[i], dc[i] = dr[i], zc[i] = zr[i];
+    for (int i = 0; i < U; ++i) {
+      xv[i] = to_float(xr[i]);
+      dt[i] = to_float(dr[i]) + bias;
+      zv[i] = to_float(zr[i]);
+    }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = to_float(bc[j]);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     ask(p0 + U);
+    if (a.softplus)
+#pragma unroll
+      for (int i = 0; i < U; ++i) dt[i] = softplus(dt[i]);
+    // past the part's end a row's step and input are 0, as its B and C: h stays as it is, bit for bit
+    if (p0 + U > part.end || ORDER)
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (p0 + i >= part.end || (ORDER && a.win.row(p0 + i) < 0)) dt[i] = xv[i] = 0.f;
     const auto row = [&](int i) __attribute__((always_inline)) {
-      const float xv = to_float(xc[i]), dt = step_size(a, to_float(dc[i]), bias), u = dt * xv;
-      float sum[4] = {};
+      const float u = dt[i] * xv[i];
+      float s[4] = {};
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
-        const float e = __builtin_amdgcn_exp2f(dt * A[n]);
+        const float e = __builtin_amdgcn_exp2f(dt[i] * A[n]);
         h[n] = __builtin_fmaf(e, h[n], u * s_bc[i * V + n]);
-        if (OUT) sum[n % 4] = __builtin_fmaf(s_bc[i * V + NS + n], h[n], sum[n % 4]);
+        if (OUT) s[n % 4] = __builtin_fmaf(s_bc[i * V + NS + n], h[n], s[n % 4]);
       }
-      if (!OUT) {
-        dts += dt;
-        return;
-      }
-      float out = __builtin_fmaf(skip, xv, (sum[0] + sum[1]) + (sum[2] + sum[3]));
-      if (z != nullptr) out *= act(kSilu, to_float(zc[i]));
-      const int r = a.win.row(p0 + i);
-      if (tile.live && r >= 0) y[(size_t)r * a.D + c] = from_float<T>(out);
+      sum[i] = (s[0] + s[1]) + (s[2] + s[3]);
+      if (!OUT) dts += dt[i];
     };
-    if (p0 + U <= part.end) {
 #pragma unroll
-      for (int i = 0; i < U; ++i) row(i);
-    } else {
+    for (int i = 0; i < U; ++i) row(i);
+    if (!OUT) continue;
 #pragma unroll
-      for (int i = 0; i < U - 1; ++i)
-        if (p0 + i < part.end) row(i);
+    for (int i = 0; i < U; ++i) sum[i] = __builtin_fmaf(skip, xv[i], sum[i]);
+    if (z != nullptr)
+#pragma unroll
+      for (int i = 0; i < U; ++i) sum[i] *= quick_silu(zv[i]);
+    if (tile.live) {
+      uint32_t off = c;
+      asm volatile("" : "+v"(off));
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (p0 + i >= part.end) break;
+        const int r = ORDER ? a.win.row(p0 + i) : p0 + i;
+        if (!ORDER || r >= 0) lane_at(y + (int64_t)r * a.D, off) = from_float<T>(sum[i]);
+      }
     }
   }
   if (!tile.live) return;
@@ -126,46 +144,52 @@ __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x
 // state on.
 __global__ __launch_bounds__(256) void k_scan_carry(ScanArgs a, const float* __restrict__ state,
                                                     float* __restrict__ state_out, Parts parts) {
-  constexpr int kAhead = 8;
   const int w = blockIdx.x;
   const int b = a.win.edge(w), e = a.win.edge(w + 1);
-  const int64_t at = (int64_t)blockIdx.y * 256 + threadIdx.x, size = (int64_t)a.N * a.D;
-  if (at >= size) return;
-  const int n = (int)(at / a.D), c = (int)(at % a.D);
-  if (e <= b) {
-    if (state_out != nullptr) {
-      const size_t i = ((size_t)w * a.D + c) * a.N + n;
-      state_out[i] = state != nullptr ? state[i] : 0.f;
+  const int count = e > b ? (e - b - 1) / a.per : 0;   // parts but the last
+  if (e > b && count == 0) return;
+  const int64_t size = (int64_t)a.N * a.D, first = (int64_t)(b / a.per) + w;
+  for (int64_t at = (int64_t)blockIdx.y * 256 + threadIdx.x; at < size; at += (int64_t)gridDim.y * 256) {
+    const int n = (int)(at / a.D), c = (int)(at % a.D);
+    const size_t mine = ((size_t)w * a.D + c) * a.N + n;
+    float h = state != nullptr ? state[mine] : 0.f;
+    if (e <= b) {
+      if (state_out != nullptr) state_out[mine] = h;
+      continue;
     }
-    return;
-  }
-  const int count = (e - b - 1) / a.per;   // parts but the last
-  if (count == 0) return;
-  const int64_t first = (int64_t)(b / a.per) + w;
-  const float A = a.A[(size_t)c * a.N + n] * kLog2e;
-  float h = state != nullptr ? state[((size_t)w * a.D + c) * a.N + n] : 0.f;
-  parts.S[(first + count) * size + at] = h;   // the last part's place is free: a copy for the first part
-  for (int i0 = 0; i0 < count; i0 += kAhead) {
-    float S[kAhead], d[kAhead];
+    const float A = a.A[(size_t)c * a.N + n] * kLog2e;
+    parts.S[(first + count) * size + at] = h;   // the last part's place is free: a copy for the first part
+    const auto join = [&](int i0, auto ahead) __attribute__((always_inline)) {
+      constexpr int K = decltype(ahead)::value;
+      float S[K], d[K];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t s = first + min(i0 + i, count - 1);
-      S[i] = parts.S[s * size + at];
-      d[i] = parts.dts[s * a.D + c];
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (i0 + i < count) {
-        h = decayed(A * d[i], h) + S[i];
-        parts.S[(first + i0 + i) * size + at] = h;
+      for (int i = 0; i < K; ++i) {
+        const int64_t s = first + min(i0 + i, count - 1);
+        S[i] = parts.S[s * size + at];
+        d[i] = parts.dts[s * a.D + c];
       }
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (i0 + i < count) {
+          h = decayed(A * d[i], h) + S[i];
+          parts.S[(first + i0 + i) * size + at] = h;
+        }
+      return i0 + K;
+    };
+    for (int i = 0; i < count;)
+      i = count - i > 8 ? join(i, std::integral_constant<int, 32>{}) : join(i, std::integral_constant<int, 8>{});
   }
 }
 
-// Rows of a part: waves for all SIMDs, but parts long enough that joining them costs little.
+// Rows of a part: waves for all SIMDs, but parts long enough that joining them costs little; where there are
+// waves enough without cutting, only windows of four times the mean are.
 int rows_per_part(int64_t n, int32_t W, int64_t tiles) {
-  int64_t per = n * tiles / 4096 / 8 * 8;
-  per = per < 64 ? 64 : per > 512 ? 512 : per;
+  int64_t per = n * tiles / 8192 / 8 * 8;
+  per = per < 64 ? 64 : per > 128 ? 128 : per;
+  if (W * tiles >= 4096) {
+    const int64_t whole = 4 * n / W / 8 * 8;
+    per = whole < per ? per : whole > 512 ? 512 : whole;
+  }
   return (int)per;
 }
 
@@ -200,11 +224,11 @@ hipError_t launch_forward_scan(scan::ScanArgs a, int dtype, const void* x, const
                                         state_in, static_cast<T*>(y), state_out, parts);
       };
       const bool cut = a.win.n > a.per;
-      if (cut) args(k_scan<T, NS, false>);
+      if (cut) a.win.order ? args(k_scan<T, NS, false, true>) : args(k_scan<T, NS, false, false>);
       if (cut || state_out != nullptr)
-        k_scan_carry<<<dim3(a.win.W, (uint32_t)(((int64_t)a.N * a.D + 255) / 256)), 256, 0, stream>>>(a, state_in,
+        k_scan_carry<<<dim3(a.win.W, carry_blocks(a)), 256, 0, stream>>>(a, state_in,
                                                                                                      state_out, parts);
-      if (a.win.n > 0) args(k_scan<T, NS, true>);
+      if (a.win.n > 0) a.win.order ? args(k_scan<T, NS, true, true>) : args(k_scan<T, NS, true, false>);
     });
   };
   if (dtype == 0) run(float{});
