@@ -40,9 +40,17 @@ __device__ __forceinline__ float slope(int a, float z) {
 
 // z / (1 + e^-z) and log(1 + e^x) where they are a small part of the work of every row, with the exponent in one
 // term: e^-|x| is off by |x| 2^-23 of itself, which is what the values below 0 are off by.
+__device__ __forceinline__ float quick_sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+}
 __device__ __forceinline__ float quick_silu(float z) {
   z = from_below(z);
-  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+  return z * quick_sigmoid(z);
+}
+__device__ __forceinline__ float quick_silu_slope(float z) {
+  z = from_above(from_below(z));
+  const float s = quick_sigmoid(z);
+  return s * __builtin_fmaf(z, 1.f - s, 1.f);
 }
 // The larger of x and 0, and log(1 + e) of e = e^-|x| in [0, 1] as 2 atanh(s), s = e / (2 + e) <= 1 / 3, with atanh(s)
 // / s a polynomial in s^2 through the Chebyshev points of [0, 1 / 9] (off by 2^-26).  A logarithm of 1 + e would lose

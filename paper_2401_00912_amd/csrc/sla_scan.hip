@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void k_scan_carry(ScanArgs a, const float* __r
       if (state_out != nullptr) state_out[mine] = h;
       continue;
     }
-    const float A = a.A[(size_t)c * a.N + n] * kLog2e;
+    const float A = exponent(a.A[(size_t)c * a.N + n]);
     parts.S[(first + count) * size + at] = h;   // the last part's place is free: a copy for the first part
     const auto join = [&](int i0, auto ahead) __attribute__((always_inline)) {
       constexpr int K = decltype(ahead)::value;

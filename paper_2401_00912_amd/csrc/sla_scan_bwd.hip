@@ -25,7 +25,10 @@ namespace {
 
 using namespace scan;
 
-constexpr int kTile = 16, kMaxTiles = 8, kThreads = 256, kWaves = 4;
+constexpr int kMaxTiles = 8, kThreads = 256, kWaves = 4;
+// Rows of a tile: their states' a and decays are in registers, 8 for each row.
+template <int NG>
+constexpr int kTileOf = NG <= 8 ? 8 : 16;
 constexpr float kLn2 = 0.693147181f;
 
 struct BackArgs {
@@ -56,24 +59,22 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
   float A[NS], h[NS], P[NS], R[NS];
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
-    A[n] = n < N ? a.A[(size_t)c * a.N + n0 + n] * kLog2e : 0.f;
+    A[n] = n < N ? exponent(a.A[(size_t)c * a.N + n0 + n]) : 0.f;
     h[n] = R[n] = 0.f;
     P[n] = 1.f;
   }
   const float bias = a.bias ? a.bias[c] : 0.f;
   float dts = 0.f;
-  T xr[U], dr[U], zr[U], gr[U], bc[J];
+  T xr[U], dr[U], zr[U] = {}, gr[U], bc[J];
   const auto ask = [&](int p0) __attribute__((always_inline)) {
+    // rows past the end are the last one, and are not used
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int r = p0 + i < part.end ? a.win.row(p0 + i) : -1;
-      xr[i] = dr[i] = zr[i] = gr[i] = from_float<T>(0.f);
-      if (r >= 0) {
-        xr[i] = x[r * a.ldx + c];
-        dr[i] = delta[r * a.ldd + c];
-        gr[i] = dy[r * a.ldy + c];
-        if (z != nullptr) zr[i] = z[r * a.ldz + c];
-      }
+      const int r = max(a.win.row(min(p0 + i, part.end - 1)), 0);
+      xr[i] = lane_at(x + r * a.ldx, c);
+      dr[i] = lane_at(delta + r * a.ldd, c);
+      gr[i] = lane_at(dy + r * a.ldy, c);
+      if (z != nullptr) zr[i] = lane_at(z + r * a.ldz, c);
     }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -85,28 +86,41 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
   };
   ask(part.begin);
   for (int p0 = part.begin; p0 < part.end; p0 += U) {
-    T xc[U], dc[U], zc[U], gc[U];
+    float xv[U], dt[U], zv[U], gv[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) xc[i] = xr[i], dc[i] = dr[i], zc[i] = zr[i], gc[i] = gr[i];
+    for (int i = 0; i < U; ++i) {
+      xv[i] = to_float(xr[i]);
+      dt[i] = to_float(dr[i]) + bias;
+      zv[i] = to_float(zr[i]);
+      gv[i] = to_float(gr[i]);
+    }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = to_float(bc[j]);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     ask(p0 + U);
+    if (a.softplus)
+#pragma unroll
+      for (int i = 0; i < U; ++i) dt[i] = softplus(dt[i]);
+    if (z != nullptr)
+#pragma unroll
+      for (int i = 0; i < U; ++i) gv[i] *= quick_silu(zv[i]);
+    // past the part's end a row's step, input and gradient are 0, as its B and C: nothing changes
+    if (p0 + U > part.end || a.win.order != nullptr)
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (p0 + i >= part.end || a.win.row(p0 + i) < 0) dt[i] = xv[i] = gv[i] = 0.f;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (p0 + i >= part.end) break;
-      const float dt = step_size(a, to_float(dc[i]), bias), u = dt * to_float(xc[i]);
-      float g = to_float(gc[i]);
-      if (z != nullptr) g *= act(kSilu, to_float(zc[i]));
-      dts += dt;
+      const float u = dt[i] * xv[i];
+      dts += dt[i];
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
-        const float e = __builtin_amdgcn_exp2f(dt * A[n]);
+        const float e = __builtin_amdgcn_exp2f(dt[i] * A[n]);
         h[n] = __builtin_fmaf(e, h[n], u * s_bc[i * V + n]);
         P[n] *= e;
-        R[n] = __builtin_fmaf(P[n], g * s_bc[i * V + NS + n], R[n]);
+        R[n] = __builtin_fmaf(P[n], gv[i] * s_bc[i * V + NS + n], R[n]);
       }
     }
   }
@@ -127,43 +141,46 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
 __global__ __launch_bounds__(256) void k_scan_carry_back(BackArgs k, const float* __restrict__ state,
                                                          const float* __restrict__ dstate,
                                                          float* __restrict__ dstate_in) {
-  constexpr int kAhead = 8;
   const ScanArgs& a = k.a;
   const int w = blockIdx.x;
   const int b = a.win.edge(w), e = a.win.edge(w + 1);
-  const int64_t at = (int64_t)blockIdx.y * 256 + threadIdx.x, size = (int64_t)a.N * a.D;
-  if (at >= size) return;
-  const int n = (int)(at / a.D), c = (int)(at % a.D);
-  const size_t mine = ((size_t)w * a.D + c) * a.N + n;
-  if (e <= b) {
-    if (dstate_in != nullptr) dstate_in[mine] = dstate != nullptr ? dstate[mine] : 0.f;
-    return;
-  }
-  const int count = (e - b - 1) / a.per;   // parts but one
-  if (count == 0) return;
-  const int64_t first = (int64_t)(b / a.per) + w;
-  const float A = a.A[(size_t)c * a.N + n] * kLog2e;
-  float h = state != nullptr ? state[mine] : 0.f, q = dstate != nullptr ? dstate[mine] : 0.f;
-  k.fwd.S[(first + count) * size + at] = h;
-  k.R[first * size + at] = q;
-  for (int i0 = 0; i0 < count; i0 += kAhead) {
-    float S[kAhead], d[kAhead], R[kAhead], f[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t s = first + min(i0 + i, count - 1), r = first + max(count - i0 - i, 1);
-      S[i] = k.fwd.S[s * size + at];
-      d[i] = k.fwd.dts[s * a.D + c];
-      R[i] = k.R[r * size + at];
-      f[i] = k.fwd.dts[r * a.D + c];
+  const int count = e > b ? (e - b - 1) / a.per : 0;   // parts but one
+  if (e > b && count == 0) return;
+  const int64_t size = (int64_t)a.N * a.D, first = (int64_t)(b / a.per) + w;
+  for (int64_t at = (int64_t)blockIdx.y * 256 + threadIdx.x; at < size; at += (int64_t)gridDim.y * 256) {
+    const int n = (int)(at / a.D), c = (int)(at % a.D);
+    const size_t mine = ((size_t)w * a.D + c) * a.N + n;
+    float h = state != nullptr ? state[mine] : 0.f, q = dstate != nullptr ? dstate[mine] : 0.f;
+    if (e <= b) {
+      if (dstate_in != nullptr) dstate_in[mine] = q;
+      continue;
     }
+    const float A = exponent(a.A[(size_t)c * a.N + n]);
+    k.fwd.S[(first + count) * size + at] = h;
+    k.R[first * size + at] = q;
+    const auto join = [&](int i0, auto ahead) __attribute__((always_inline)) {
+      constexpr int K = decltype(ahead)::value;
+      float S[K], d[K], R[K], f[K];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (i0 + i < count) {
-        h = decayed(A * d[i], h) + S[i];
-        k.fwd.S[(first + i0 + i) * size + at] = h;
-        q = decayed(A * f[i], q) + R[i];
-        k.R[(first + count - i0 - i) * size + at] = q;
+      for (int i = 0; i < K; ++i) {
+        const int64_t s = first + min(i0 + i, count - 1), r = first + max(count - i0 - i, 1);
+        S[i] = k.fwd.S[s * size + at];
+        d[i] = k.fwd.dts[s * a.D + c];
+        R[i] = k.R[r * size + at];
+        f[i] = k.fwd.dts[r * a.D + c];
       }
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (i0 + i < count) {
+          h = decayed(A * d[i], h) + S[i];
+          k.fwd.S[(first + i0 + i) * size + at] = h;
+          q = decayed(A * f[i], q) + R[i];
+          k.R[(first + count - i0 - i) * size + at] = q;
+        }
+      return i0 + K;
+    };
+    for (int i = 0; i < count;)
+      i = count - i > 8 ? join(i, std::integral_constant<int, 24>{}) : join(i, std::integral_constant<int, 8>{});
   }
 }
 
@@ -197,14 +214,45 @@ __device__ __forceinline__ float halve(float a, float b, int lane) {
     return keep + other<S, EXACT>(send);
   }
 }
+// The same for M / 2 pairs x[k], x[k + M / 2] at once where S is 8 or 4: two additions a pair, each written to the
+// banks of four lanes that it is for.  A lane's neighbour may have been written just before: two wait states.
+#define SLA_PAIR(DST, SRC, SHIFT, LOW, HIGH)                                              \
+  "v_add_f32_dpp " DST ", " DST ", " DST " " SHIFT " row_mask:0xf bank_mask:" LOW "\n"     \
+  "v_add_f32_dpp " DST ", " SRC ", " SRC " " SHIFT " row_mask:0xf bank_mask:" HIGH "\n"
+template <int M, int S>
+__device__ __forceinline__ void halve_banks(float* x) {
+  static_assert((M == 2 || M == 4 || M == 8) && (S == 4 || S == 8));
+  if constexpr (M == 8 && S == 8)
+    asm("s_nop 1\n" SLA_PAIR("%0", "%4", "row_ror:8", "0x3", "0xc") SLA_PAIR("%1", "%5", "row_ror:8", "0x3", "0xc")
+        SLA_PAIR("%2", "%6", "row_ror:8", "0x3", "0xc") SLA_PAIR("%3", "%7", "row_ror:8", "0x3", "0xc")
+        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]) : "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]));
+  else if constexpr (M == 8)
+    asm("s_nop 1\n" SLA_PAIR("%0", "%4", "row_half_mirror", "0x5", "0xa") SLA_PAIR("%1", "%5", "row_half_mirror", "0x5", "0xa")
+        SLA_PAIR("%2", "%6", "row_half_mirror", "0x5", "0xa") SLA_PAIR("%3", "%7", "row_half_mirror", "0x5", "0xa")
+        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]) : "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]));
+  else if constexpr (M == 4 && S == 8)
+    asm("s_nop 1\n" SLA_PAIR("%0", "%2", "row_ror:8", "0x3", "0xc") SLA_PAIR("%1", "%3", "row_ror:8", "0x3", "0xc")
+        : "+v"(x[0]), "+v"(x[1]) : "v"(x[2]), "v"(x[3]));
+  else if constexpr (M == 4)
+    asm("s_nop 1\n" SLA_PAIR("%0", "%2", "row_half_mirror", "0x5", "0xa") SLA_PAIR("%1", "%3", "row_half_mirror", "0x5", "0xa")
+        : "+v"(x[0]), "+v"(x[1]) : "v"(x[2]), "v"(x[3]));
+  else if constexpr (S == 8)
+    asm("s_nop 1\n" SLA_PAIR("%0", "%1", "row_ror:8", "0x3", "0xc") : "+v"(x[0]) : "v"(x[1]));
+  else
+    asm("s_nop 1\n" SLA_PAIR("%0", "%1", "row_half_mirror", "0x5", "0xa") : "+v"(x[0]) : "v"(x[1]));
+}
+#undef SLA_PAIR
 // x[0 .. M - 1] summed over the lanes that differ in bits S, S / 2, .. LOW: lane bit S chooses between x[k] and
 // x[k + M / 2], the next bit halves what is left, and so on; where one value is left, every lane has its sum.
 template <int M, int S, int LOW, bool EXACT>
 __device__ __forceinline__ void sum_lanes(float* x, int lane) {
   if constexpr (S >= LOW) {
-    if constexpr (M > 1) {
+    if constexpr (M > 8 || (M > 1 && S != 8 && (S != 4 || EXACT))) {
 #pragma unroll
       for (int k = 0; k < M / 2; ++k) x[k] = halve<S, EXACT>(x[k], x[k + M / 2], lane);
+      sum_lanes<M / 2, S / 2, LOW, EXACT>(x, lane);
+    } else if constexpr (M > 1) {
+      halve_banks<M, S>(x);
       sum_lanes<M / 2, S / 2, LOW, EXACT>(x, lane);
     } else {
       x[0] += other<S, EXACT>(x[0]);
@@ -214,7 +262,7 @@ __device__ __forceinline__ void sum_lanes(float* x, int lane) {
 }
 
 // ------------------------------------------------------------------ the walk
-// NG lanes a channel, four states each; lane = ng CW + channel.  Of a 16-row tile a lane takes the rows
+// NG lanes a channel, four states each; lane = ng CW + channel.  Of a tile a lane takes the rows
 // j NG + ng of its channel wherever rows are taken one by one (step sizes, gates, results).
 template <typename T, int NG>
 __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* __restrict__ x,
@@ -224,7 +272,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
                                                            const float* __restrict__ dstate, T* __restrict__ dx,
                                                            T* __restrict__ ddelta, T* __restrict__ dz,
                                                            float* __restrict__ dstate_in) {
-  constexpr int CW = 64 / NG, E = kTile / NG, NP = 4 * NG;
+  constexpr int kTile = kTileOf<NG>, CW = 64 / NG, E = kTile / NG, NP = 4 * NG;
   constexpr int kStage = (kTile * 2 * NP + kThreads - 1) / kThreads;
   __shared__ floatx4 s_in[kWaves][kTile][CW];            // dt, u, g of the wave's channels
   __shared__ floatx4 s_start[kWaves][kMaxTiles][64];     // states before each tile
@@ -258,7 +306,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
     for (int r = 0; r < 4; ++r) v[r] = p != nullptr && n0 + r < a.N ? p[((size_t)part.w * a.D + c) * a.N + n0 + r] : 0.f;
   };
 #pragma unroll
-  for (int r = 0; r < 4; ++r) A[r] = n0 + r < a.N ? a.A[(size_t)c * a.N + n0 + r] * kLog2e : 0.f;
+  for (int r = 0; r < 4; ++r) A[r] = n0 + r < a.N ? exponent(a.A[(size_t)c * a.N + n0 + r]) : 0.f;
   if (!part.first) from_parts(k.fwd.S, slot - 1, h);
   else if (!part.last && state != nullptr) from_parts(k.fwd.S, slot + count, h);
   else from_window(state, h);
@@ -300,7 +348,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
     for (int j = 0; j < E; ++j) {
       pre[j] = to_float(dr[j]) + bias;
       dt[j] = row[j] >= 0 ? step_size(a, to_float(dr[j]), bias) : 0.f;
-      gate[j] = back && z != nullptr ? act(kSilu, to_float(zr[j])) : 1.f;
+      gate[j] = back && z != nullptr ? quick_silu(to_float(zr[j])) : 1.f;
       s_in[wave][j * NG + ng][ch] = floatx4{dt[j], dt[j] * to_float(xr[j]), to_float(gr[j]) * gate[j], 0.f};
     }
     float* flat = &s_bc[0][0][0];
@@ -328,12 +376,31 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
     s_start[wave][i + 1][lane] = floatx4{h[0], h[1], h[2], h[3]};
   }
 
+  // the waves' sums over their channels of the tile at p0
+  const auto hand_on = [&](int p0) __attribute__((always_inline)) {
+    const float* red = &s_red[0][0][0][0];
+    for (int v = tid; v < kTile * 2 * NP; v += kThreads) {
+      const int t = v / (2 * NP), which = v / NP % 2, n = v % NP;
+      if (p0 + t < part.end && n < a.N) {
+        float sum = red[v];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) sum += red[w * kTile * 2 * NP + v];
+        k.bc[((size_t)blockIdx.y * a.win.n + p0 + t) * 2 * a.N + which * a.N + n] = sum;
+      }
+    }
+  };
+  ask(part.begin + (tiles - 1) * kTile, true);
   for (int i = tiles - 1; i >= 0; --i) {
     const int p0 = part.begin + i * kTile;
-    ask(p0, true);
     __syncthreads();
+    if (i + 1 < tiles) hand_on(p0 + kTile);
     stage(true);
+    float xv[E], zv[E], gv[E];
+    int at_row[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) xv[j] = to_float(xr[j]), zv[j] = to_float(zr[j]), gv[j] = to_float(gr[j]), at_row[j] = row[j];
     __syncthreads();
+    if (i > 0) ask(p0 - kTile, true);
     float kept[kTile][4], e[kTile][4];
     {
       const floatx4 s = s_start[wave][i][lane];
@@ -389,33 +456,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
         sum_lanes<NG, 32, CW, true>(dda, lane);
         sum_lanes<NG, 32, CW, true>(yl, lane);
         const int j = t / NG;
-        if (row[j] >= 0) {
-          const float xv = to_float(xr[j]), gv = to_float(gr[j]) * gate[j];
-          float dd = __builtin_fmaf(du[0], xv, dda[0] * kLn2);
-          if (a.softplus) dd *= sigmoid(from_above(from_below(pre[j])));
-          const size_t o = (size_t)row[j] * a.D + c;
-          dx[o] = from_float<T>(__builtin_fmaf(du[0], dt[j], gv * skip));
+        if (at_row[j] >= 0) {
+          const float g1 = gv[j] * gate[j];
+          float dd = __builtin_fmaf(du[0], xv[j], dda[0] * kLn2);
+          if (a.softplus) dd *= quick_sigmoid(pre[j]);
+          const size_t o = (size_t)at_row[j] * a.D + c;
+          dx[o] = from_float<T>(__builtin_fmaf(du[0], dt[j], g1 * skip));
           ddelta[o] = from_float<T>(dd);
           if (z != nullptr)
-            dz[o] = from_float<T>(to_float(gr[j]) * __builtin_fmaf(skip, xv, yl[0]) * slope(kSilu, to_float(zr[j])));
-          sum_skip = __builtin_fmaf(gv, xv, sum_skip);
+            dz[o] = from_float<T>(gv[j] * __builtin_fmaf(skip, xv[j], yl[0]) * quick_silu_slope(zv[j]));
+          sum_skip = __builtin_fmaf(g1, xv[j], sum_skip);
           sum_bias += dd;
         }
       }
     }
-    __syncthreads();
-    // the waves' sums over their channels
-    const float* red = &s_red[0][0][0][0];
-    for (int v = tid; v < kTile * 2 * NP; v += kThreads) {
-      const int t = v / (2 * NP), which = v / NP % 2, n = v % NP;
-      if (p0 + t < part.end && n < a.N) {
-        float sum = red[v];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) sum += red[w * kTile * 2 * NP + v];
-        k.bc[((size_t)blockIdx.y * a.win.n + p0 + t) * 2 * a.N + which * a.N + n] = sum;
-      }
-    }
   }
+  __syncthreads();
+  hand_on(part.begin);
   float sums[1] = {sum_skip};
   sum_lanes<1, 32, CW, true>(sums, lane);
   sum_skip = sums[0];
@@ -484,10 +541,11 @@ __global__ __launch_bounds__(1024) void k_scan_params(BackArgs k, int32_t slots,
   *out = sum;
 }
 
-int rows_per_part_back(int64_t n, int64_t blocks) {
-  // whole tiles; enough workgroups for two a CU
-  int64_t per = n * blocks / 1024 / kTile * kTile;
-  per = per < 32 ? 32 : per > kTile * kMaxTiles ? kTile * kMaxTiles : per;
+// Whole tiles; enough workgroups for three a CU, but parts of eight tiles at most, whose states LDS holds.  Where
+// there are windows enough, parts as long as they can be.
+int rows_per_part_back(int64_t n, int32_t W, int64_t blocks, int tile) {
+  int64_t per = W * blocks >= 1024 ? n : n * blocks / 1024 / tile * tile;
+  per = per < 4 * tile ? 4 * tile : per > tile * kMaxTiles ? tile * kMaxTiles : per;
   return (int)per;
 }
 
@@ -503,7 +561,7 @@ BackLayout back_layout(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
   L.ng = lane_groups(N);
   L.cw = 64 / L.ng * kWaves;
   L.wpg = (D / G + L.cw - 1) / L.cw;
-  L.per = rows_per_part_back(n, (int64_t)G * L.wpg);
+  L.per = rows_per_part_back(n, W, (int64_t)G * L.wpg, L.ng <= 8 ? 8 : 16);
   L.slots = n / L.per + W;
   size_t off = 0;
   const auto take = [&](size_t floats) {
@@ -565,7 +623,7 @@ hipError_t launch_backward_scan(scan::ScanArgs a, int dtype, const void* x, cons
       else maps(k_scan_maps<T, 16>);
     }
     if (cut || dstate_in != nullptr)
-      k_scan_carry_back<<<dim3(a.win.W, (uint32_t)((values + 255) / 256)), 256, 0, stream>>>(k, state_in, dstate_out,
+      k_scan_carry_back<<<dim3(a.win.W, carry_blocks(a)), 256, 0, stream>>>(k, state_in, dstate_out,
                                                                                             dstate_in);
     if (a.win.n > 0) {
       const dim3 grid((uint32_t)L.slots, (uint32_t)(a.G * L.wpg));
