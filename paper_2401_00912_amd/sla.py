@@ -259,27 +259,58 @@ def plan_layout(n: int, num_windows: int) -> PlanLayout:
 
 
 # ----------------------------------------------------------------- torch glue
-def _torch():
-    import torch
+_torch_module = None
+_dtype_codes = {}
 
-    return torch
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+
+        _torch_module = torch
+        _dtype_codes.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    return _torch_module
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(device):
     torch = _torch()
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the handle alone: no Stream object is made
+    if raw is not None and device.index is not None:
+        return raw(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+class _OnDevice:
+    """A call's device as the current one: nothing to do where it already is (a single row's whole call is
+    a few microseconds, and so is changing the device)."""
+
+    def __init__(self, device):
+        torch = _torch()
+        if device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, not on {device}")
+        self.other = None
+        if device.index is not None and torch.cuda.current_device() != device.index:
+            self.other = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
 
 
 def _dtype_code(dt) -> int:
-    torch = _torch()
-    codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-    if dt not in codes:
+    _torch()
+    if dt not in _dtype_codes:
         raise TypeError(f"SLA supports float32, float16 and bfloat16, not {dt}")
-    return codes[dt]
+    return _dtype_codes[dt]
 
 
 @dataclass
@@ -713,8 +744,7 @@ def forward_scatter(plan: Plan, q, k, v, out=None, workspace=None):
 
 
 def _check_like(name, t, shape, dtype, device):
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device
-                          or not t.is_contiguous()):
+    if t is not None and (t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous {tuple(shape)} {dtype} tensor on the inputs' device")
 
 
@@ -777,7 +807,7 @@ def forward_delta(q, k, v, g, beta, offsets, scale=None, order=None, state=None,
         _check_like(name, t, (w, h, dk, dv), torch.float32, q.device)
     workspace, nbytes = _own_workspace(delta_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace, q.device,
                                          "sla_delta_workspace_bytes")
-    with torch.cuda.device(q.device):
+    with _OnDevice(q.device):
         st = lib().sla_forward_delta(_ptr(offsets), n, w, _ptr(order), _dtype_code(q.dtype), hk, h, dk, dv,
                                      float(dk ** -0.5 if scale is None else scale), _ptr(q), _ptr(k), _ptr(v),
                                      _ptr(g), _ptr(beta), _ptr(state), _ptr(out), _ptr(final_state),
@@ -814,7 +844,7 @@ def backward_delta(q, k, v, g, beta, offsets, dout, dstate=None, scale=None, ord
     dstate_in = None if state is None else torch.empty_like(state)
     workspace, nbytes = _own_workspace(delta_backward_workspace_bytes(n, w, q.dtype, hk, h, dk, dv), workspace,
                                          q.device, "sla_delta_backward_workspace_bytes")
-    with torch.cuda.device(q.device):
+    with _OnDevice(q.device):
         st = lib().sla_backward_delta(_ptr(offsets), n, w, _ptr(order), _dtype_code(q.dtype), hk, h, dk, dv,
                                       float(dk ** -0.5 if scale is None else scale), _ptr(q), _ptr(k), _ptr(v),
                                       _ptr(g), _ptr(beta), _ptr(state), _ptr(dout), _ptr(dstate),
@@ -837,7 +867,7 @@ def step_delta(state, slots, q, k, v, g, beta, scale=None, out=None):
     _check_like("slots", slots, (n,), torch.int32, q.device)
     out = torch.empty_like(v) if out is None else out
     _check_like("out", out, v.shape, q.dtype, q.device)
-    with torch.cuda.device(q.device):
+    with _OnDevice(q.device):
         st = lib().sla_step_delta(_ptr(slots), n, state.shape[0], _dtype_code(q.dtype), hk, h, dk, dv,
                                   float(dk ** -0.5 if scale is None else scale), _ptr(state), _ptr(q), _ptr(k),
                                   _ptr(v), _ptr(g), _ptr(beta), _ptr(out), _stream(q.device))
@@ -884,7 +914,7 @@ def forward_group_norm(x, groups: int, weight=None, bias=None, offsets=None, eps
         _check_like(name, t, (w, groups), torch.float32, x.device)
     need = group_norm_workspace_bytes(n, 0 if offsets is None else w, x.dtype, C, groups)
     workspace, nbytes = _own_workspace(need, workspace, x.device, "sla_group_norm_workspace_bytes")
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_forward_group_norm(_ptr(offsets), n, w, _dtype_code(x.dtype), C, groups, float(eps),
                                           ACTIVATIONS[activation], _ptr(x), _ptr(weight), _ptr(bias), _ptr(y),
                                           _ptr(mean), _ptr(rstd), _ptr(workspace), nbytes, _stream(x.device))
@@ -906,7 +936,7 @@ def backward_group_norm(x, groups: int, dy, mean, rstd, weight=None, bias=None, 
     dweight, dbias = (torch.empty(C, dtype=torch.float32, device=x.device) for _ in range(2))
     need = group_norm_workspace_bytes(n, 0 if offsets is None else w, x.dtype, C, groups, backward=True)
     workspace, nbytes = _own_workspace(need, workspace, x.device, "sla_group_norm_backward_workspace_bytes")
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_backward_group_norm(_ptr(offsets), n, w, _dtype_code(x.dtype), C, groups,
                                            ACTIVATIONS[activation], _ptr(x), _ptr(weight), _ptr(bias), _ptr(dy),
                                            _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dweight), _ptr(dbias),
@@ -917,17 +947,18 @@ def backward_group_norm(x, groups: int, dy, mean, rstd, weight=None, bias=None, 
 
 def _row_stride(name, t, shape, dtype, device):
     """Elements between the rows of a [n, ...] tensor whose rows are contiguous and do not overlap."""
-    if t.dim() != len(shape) or tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+    if t.shape != shape or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a {tuple(shape)} {dtype} tensor on the inputs' device")
-    n, inner = shape[0], 1
-    for size, stride in zip(t.shape[:0:-1], t.stride()[:0:-1]):
-        if size != 1 and stride != inner:
+    strides, inner = t.stride(), 1
+    for i in range(len(shape) - 1, 0, -1):
+        if strides[i] != inner and shape[i] != 1:
             raise ValueError(f"the rows of {name} must be contiguous")
-        inner *= size
-    stride = t.stride(0) if n > 1 else inner
-    if stride < inner:
+        inner *= shape[i]
+    if shape[0] <= 1:
+        return inner
+    if strides[0] < inner:
         raise ValueError(f"the rows of {name} must not overlap")
-    return stride
+    return strides[0]
 
 
 def _check_activation(activation):
@@ -963,7 +994,7 @@ def forward_short_conv(x, weight, offsets, bias=None, activation="none", order=N
         final_state = torch.empty((w, max(K - 1, 0), C), dtype=x.dtype, device=x.device)
     for name, t in (("state", state), ("final_state", final_state)):
         _check_like(name, t, (w, max(K - 1, 0), C), x.dtype, x.device)
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_forward_short_conv(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), C, K, act, _ptr(x),
                                           ldx, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), _ptr(final_state),
                                           _stream(x.device))
@@ -995,7 +1026,7 @@ def backward_short_conv(x, weight, offsets, dy, bias=None, activation="none", or
     dstate_in = None if state is None else torch.empty_like(state)
     workspace, nbytes = _own_workspace(short_conv_backward_workspace_bytes(n, w, x.dtype, C, K), workspace, x.device,
                                        "sla_short_conv_backward_workspace_bytes")
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_backward_short_conv(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), C, K, act, _ptr(x),
                                            ldx, _ptr(weight), _ptr(bias), _ptr(state), _ptr(dy), lddy, _ptr(dstate),
                                            _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate_in), _ptr(workspace),
@@ -1016,7 +1047,7 @@ def step_short_conv(state, slots, x, weight, bias=None, activation="none", y=Non
     _check_like("slots", slots, (n,), torch.int32, x.device)
     y = torch.empty((n, C), dtype=x.dtype, device=x.device) if y is None else y
     _check_like("y", y, (n, C), x.dtype, x.device)
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_step_short_conv(_ptr(slots), n, state.shape[0], _dtype_code(x.dtype), C, K, act, _ptr(state),
                                        _ptr(x), ldx, _ptr(weight), _ptr(bias), _ptr(y), _stream(x.device))
     _check(st, "sla_step_short_conv")
@@ -1066,7 +1097,7 @@ def forward_selective_scan(x, delta, A, B, C, offsets, skip=None, z=None, delta_
         _check_like(name, t, (w, D, N), torch.float32, x.device)
     workspace, nbytes = _own_workspace(selective_scan_workspace_bytes(n, w, x.dtype, D, G, N), workspace, x.device,
                                        "sla_selective_scan_workspace_bytes")
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_forward_selective_scan(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), D, G, N,
                                               int(bool(delta_softplus)), *rows, _ptr(state), _ptr(y),
                                               _ptr(final_state), _ptr(workspace), nbytes, _stream(x.device))
@@ -1108,7 +1139,7 @@ def backward_selective_scan(x, delta, A, B, C, offsets, dy, dstate=None, skip=No
     dstate_in = None if state is None else torch.empty_like(state)
     workspace, nbytes = _own_workspace(selective_scan_backward_workspace_bytes(n, w, x.dtype, D, G, N), workspace,
                                        x.device, "sla_selective_scan_backward_workspace_bytes")
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_backward_selective_scan(_ptr(offsets), n, w, _ptr(order), _dtype_code(x.dtype), D, G, N,
                                                int(bool(delta_softplus)), *rows, _ptr(state), _ptr(dy), lddy,
                                                _ptr(dstate), _ptr(dx), _ptr(ddelta), _ptr(dA), _ptr(dB), _ptr(dC),
@@ -1131,7 +1162,7 @@ def step_selective_scan(state, slots, x, delta, A, B, C, skip=None, z=None, delt
     _check_like("slots", slots, (n,), torch.int32, x.device)
     y = torch.empty((n, D), dtype=x.dtype, device=x.device) if y is None else y
     _check_like("y", y, (n, D), x.dtype, x.device)
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_step_selective_scan(_ptr(slots), n, state.shape[0], _dtype_code(x.dtype), D, G, N,
                                            int(bool(delta_softplus)), _ptr(state), *rows, _ptr(y), _stream(x.device))
     _check(st, "sla_step_selective_scan")
@@ -1168,7 +1199,7 @@ def forward_residual_norm(x, residual, weight=None, post_weight=None, gate=None,
     _check_like("residual_out", residual_out, x.shape, rtype, x.device)
     rstd = torch.empty(n, dtype=torch.float32, device=x.device)
     post_rstd = None if post_weight is None else torch.empty(n, dtype=torch.float32, device=x.device)
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_forward_residual_norm(n, _dtype_code(x.dtype), _dtype_code(rtype), C, float(eps), float(scale),
                                              act, _ptr(x), _ptr(residual), _ptr(gate), _ptr(post_weight),
                                              _ptr(weight), _ptr(y), _ptr(residual_out), _ptr(rstd), _ptr(post_rstd),
@@ -1205,7 +1236,7 @@ def backward_residual_norm(x, residual_out, dy, rstd, weight=None, post_weight=N
     dpost = None if post_weight is None else torch.empty_like(post_weight)
     workspace, nbytes = _own_workspace(residual_norm_backward_workspace_bytes(n, x.dtype, C), workspace, x.device,
                                        "sla_residual_norm_backward_workspace_bytes")
-    with torch.cuda.device(x.device):
+    with _OnDevice(x.device):
         st = lib().sla_backward_residual_norm(n, _dtype_code(x.dtype), _dtype_code(residual_out.dtype), C, float(scale),
                                               act, _ptr(x), _ptr(residual_out), _ptr(gate), _ptr(post_weight),
                                               _ptr(weight), _ptr(rstd), _ptr(post_rstd), _ptr(dy),
