@@ -52,6 +52,28 @@ __device__ __forceinline__ float quick_silu_slope(float z) {
   const float s = quick_sigmoid(z);
   return s * __builtin_fmaf(z, 1.f - s, 1.f);
 }
+// Of a vector, one branch for all values.
+template <int N>
+__device__ __forceinline__ void act_all(int a, float (&z)[N]) {
+  if (a == kSilu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = quick_silu(z[e]);
+  } else if (a == kRelu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = act(kRelu, z[e]);
+  }
+}
+// d times the slope at z
+template <int N>
+__device__ __forceinline__ void slope_all(int a, const float (&z)[N], float (&d)[N]) {
+  if (a == kSilu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) d[e] *= quick_silu_slope(z[e]);
+  } else if (a == kRelu) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) d[e] = z[e] > 0.f ? d[e] : 0.f;
+  }
+}
 // The larger of x and 0, and log(1 + e) of e = e^-|x| in [0, 1] as 2 atanh(s), s = e / (2 + e) <= 1 / 3, with atanh(s)
 // / s a polynomial in s^2 through the Chebyshev points of [0, 1 / 9] (off by 2^-26).  A logarithm of 1 + e would lose
 // the bits of a small e: step sizes of 0.001 are usual.

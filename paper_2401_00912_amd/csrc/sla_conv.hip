@@ -17,7 +17,8 @@
 namespace sla {
 namespace {
 
-constexpr int kThreads = 256, kBatch = 8;
+// Rows that a thread loads together: the next ones are on their way while these are computed.
+constexpr int kThreads = 256, kBatch = 4;
 
 struct ConvArgs {
   Windows win;
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_fwd(ConvArgs a, const T* __re
     }
     return;
   }
-  const int strip = (int)xcd_place(blockIdx.x, a.strip_blocks) * strips + ty;
+  const int strip = (int)blockIdx.x * strips + ty;
   if (strip >= a.strips) return;
   const int ps = strip * a.per, pe = min(ps + a.per, a.win.n);
   Taps<T, VEC, K> taps;
@@ -144,14 +145,20 @@ __global__ __launch_bounds__(kThreads) void k_conv_fwd(ConvArgs a, const T* __re
   at.at(a.win, ps);
   float h[K][VEC];
   before<T, VEC, K>(a, at, ps, x, state, c, h);
-  for (int p0 = ps; p0 < pe; p0 += kBatch) {
-    typename V::R raw[kBatch];
-    int row[kBatch];
+  typename V::R ahead[kBatch];
+  const auto ask = [&](int p0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      row[i] = p0 + i < pe ? a.win.row(p0 + i) : -1;
-      raw[i] = row[i] >= 0 ? V::load(x + row[i] * a.ldx + c) : V::zero();
+      const int r = p0 + i < pe ? a.win.row(p0 + i) : -1;
+      ahead[i] = r >= 0 ? V::load(x + r * a.ldx + c) : V::zero();
     }
+  };
+  ask(ps);
+  for (int p0 = ps; p0 < pe; p0 += kBatch) {
+    typename V::R raw[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) raw[i] = ahead[i];
+    ask(p0 + kBatch);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int p = p0 + i;
@@ -164,9 +171,10 @@ __global__ __launch_bounds__(kThreads) void k_conv_fwd(ConvArgs a, const T* __re
           z[e] = taps.b[e];
 #pragma unroll
           for (int j = 0; j < K; ++j) z[e] = __builtin_fmaf(taps.w[j][e], h[j][e], z[e]);
-          z[e] = act(a.act, z[e]);
         }
-        if (at.in(p) && row[i] >= 0) V::store(y + (size_t)row[i] * a.C + c, z);
+        act_all(a.act, z);
+        const int r = at.in(p) ? a.win.row(p) : -1;
+        if (r >= 0) V::store(y + (size_t)r * a.C + c, z);
 #pragma unroll
         for (int j = 0; j < K - 1; ++j)
 #pragma unroll
@@ -203,15 +211,18 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
     for (int t = 0; t < K - 1; ++t) {
       if (t >= rows) break;
       const int row = a.win.row(b + t);
-      float dz[VEC], d[VEC];
+      float dz[VEC], z[VEC];
       V::wide(row >= 0 ? V::load(x + row * a.ldx + c) : V::zero(), h[K - 1]);
-      V::wide(row >= 0 ? V::load(dy + row * a.lddy + c) : V::zero(), d);
+      V::wide(row >= 0 ? V::load(dy + row * a.lddy + c) : V::zero(), dz);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        float z = taps.b[e];
+        z[e] = taps.b[e];
 #pragma unroll
-        for (int j = 0; j < K; ++j) z = __builtin_fmaf(taps.w[j][e], h[j][e], z);
-        dz[e] = d[e] * slope(a.act, z);
+        for (int j = 0; j < K; ++j) z[e] = __builtin_fmaf(taps.w[j][e], h[j][e], z[e]);
+      }
+      slope_all(a.act, z, dz);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
 #pragma unroll
         for (int j = 0; j < K - 1 - t; ++j) g[t + j][e] = __builtin_fmaf(taps.w[j][e], dz[e], g[t + j][e]);
 #pragma unroll
@@ -230,7 +241,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
     }
     return;
   }
-  const int strip = (int)xcd_place(blockIdx.x, a.strip_blocks) * strips + ty;
+  const int strip = (int)blockIdx.x * strips + ty;
   if (strip >= a.strips) return;
   const int ps = strip * a.per, pe = min(ps + a.per, a.win.n), last = pe + K - 1;
   taps.load(a, c);
@@ -239,15 +250,23 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
   float h[K][VEC], acc[K][VEC] = {}, dw[K][VEC] = {}, db[VEC] = {};
   uint32_t live = 0;   // bit j: position p - K + 1 + j is a row of a window
   before<T, VEC, K>(a, at, ps, x, state, c, h);
+  typename V::R nx[kBatch], nd[kBatch];
+  int nr[kBatch];
+  const auto ask = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      nr[i] = p0 + i < min(last, a.win.n) ? a.win.row(p0 + i) : -1;
+      nx[i] = nr[i] >= 0 ? V::load(x + nr[i] * a.ldx + c) : V::zero();
+      nd[i] = nr[i] >= 0 ? V::load(dy + nr[i] * a.lddy + c) : V::zero();
+    }
+  };
+  ask(ps);
   for (int p0 = ps; p0 < last; p0 += kBatch) {
     typename V::R rx[kBatch], rd[kBatch];
     int row[kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      row[i] = p0 + i < min(last, a.win.n) ? a.win.row(p0 + i) : -1;
-      rx[i] = row[i] >= 0 ? V::load(x + row[i] * a.ldx + c) : V::zero();
-      rd[i] = row[i] >= 0 ? V::load(dy + row[i] * a.lddy + c) : V::zero();
-    }
+    for (int i = 0; i < kBatch; ++i) rx[i] = nx[i], rd[i] = nd[i], row[i] = nr[i];
+    ask(p0 + kBatch);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int p = p0 + i;
@@ -259,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
         live = live >> 1 | (in ? 1u << (K - 1) : 0u);
         if (in) {
           V::wide(rx[i], h[K - 1]);
-          float d[VEC];
+          float d[VEC], z[VEC];
           V::wide(rd[i], d);
           if (dstate != nullptr && p >= at.end - (K - 1))
             V::wide(V::load(dstate + ((size_t)at.w * (K - 1) + p - (at.end - (K - 1))) * a.C + c), acc[K - 1]);
@@ -267,11 +286,11 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
           const int t = p - at.begin;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            float z = taps.b[e];
+            z[e] = taps.b[e];
 #pragma unroll
-            for (int j = 0; j < K; ++j) z = __builtin_fmaf(taps.w[j][e], h[j][e], z);
-            d[e] *= slope(a.act, z);
+            for (int j = 0; j < K; ++j) z[e] = __builtin_fmaf(taps.w[j][e], h[j][e], z[e]);
           }
+          slope_all(a.act, z, d);
           if (own) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -364,8 +383,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_step(ConvArgs a, const int32_
 #pragma unroll
         for (int e = 0; e < VEC; ++e) z[e] = __builtin_fmaf(taps.w[j][e], h[e], z[e]);
       }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) z[e] = act(a.act, z[e]);
+      act_all(a.act, z);
       V::store(y + (size_t)b * a.C + c, z);
 #pragma unroll
       for (int j = 0; j < K - 1; ++j) r[j] = r[j + 1];
@@ -381,8 +399,8 @@ __global__ __launch_bounds__(kThreads) void k_conv_step(ConvArgs a, const int32_
 
 int rows_per_strip(int64_t n, int32_t C, int dtype) {
   const int64_t threads = n * ((C + (dtype == 0 ? 3 : 7)) / (dtype == 0 ? 4 : 8));
-  int64_t per = (threads >> 17) / kBatch * kBatch;
-  per = per < 2 * kBatch ? 2 * kBatch : per > 256 ? 256 : per;
+  int64_t per = (threads >> 17) / 8 * 8;
+  per = per < 16 ? 16 : per > 256 ? 256 : per;
   return (int)per;
 }
 

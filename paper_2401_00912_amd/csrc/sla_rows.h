@@ -144,12 +144,4 @@ __device__ __forceinline__ T& lane_at(T* p, uint32_t i) {
   return *reinterpret_cast<T*>(reinterpret_cast<B*>(p) + (uint32_t)(i * (uint32_t)sizeof(T)));
 }
 
-// Workgroups of one launch go round the eight XCDs; neighbours that share rows are given to one XCD: the
-// place of workgroup b of count.
-__device__ __forceinline__ uint32_t xcd_place(uint32_t b, uint32_t count) {
-  constexpr uint32_t kXcds = 8;
-  const uint32_t x = b % kXcds, i = b / kXcds, full = count / kXcds, more = count % kXcds;
-  return x * full + (x < more ? x : more) + i;
-}
-
 }  // namespace sla

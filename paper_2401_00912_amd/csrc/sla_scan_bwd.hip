@@ -299,11 +299,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
   float A[4], h[4], q[4], dA[4] = {};
   const auto from_parts = [&](const float* p, size_t s, float (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = n0 + r < a.N ? p[(s * a.N + n0 + r) * a.D + c] : 0.f;
+    for (int r = 0; r < 4; ++r) v[r] = live && n0 + r < a.N ? p[(s * a.N + n0 + r) * a.D + c] : 0.f;
   };
   const auto from_window = [&](const float* p, float (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = p != nullptr && n0 + r < a.N ? p[((size_t)part.w * a.D + c) * a.N + n0 + r] : 0.f;
+    for (int r = 0; r < 4; ++r)
+      v[r] = p != nullptr && live && n0 + r < a.N ? p[((size_t)part.w * a.D + c) * a.N + n0 + r] : 0.f;
   };
 #pragma unroll
   for (int r = 0; r < 4; ++r) A[r] = n0 + r < a.N ? exponent(a.A[(size_t)c * a.N + n0 + r]) : 0.f;
