@@ -41,8 +41,6 @@ struct Tile {
   }
 };
 
-__device__ __forceinline__ int tile_group(const ScanArgs& a, int tile) { return tile / a.tpg; }
-
 __device__ __forceinline__ float step_size(const ScanArgs& a, float delta, float bias) {
   const float x = delta + bias;
   return a.softplus ? softplus(x) : x;

@@ -12,9 +12,10 @@ using namespace scan;
 // Rows a wave takes at once: the next ones are on their way while these are computed.
 constexpr int kRows = 4;
 
-// OUT: the walk that makes y; else the one that makes a part's map.  ORDER: positions are not rows.
-template <typename T, int NS, bool OUT, bool ORDER>
-__global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x, const T* __restrict__ delta,
+// OUT: the walk that makes y; else the one that makes a part's map.  ORDER: positions are not rows.  GATE: z is
+// given.
+template <typename T, int NS, bool OUT, bool ORDER, bool GATE>
+__global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const T* __restrict__ x, const T* __restrict__ delta,
                                              const T* __restrict__ z, const T* __restrict__ B, const T* __restrict__ C,
                                              const float* __restrict__ state, T* __restrict__ y,
                                              float* __restrict__ state_out, Parts parts) {
@@ -70,7 +71,21 @@ __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x
       const int at = min(p0 + i, part.end - 1), r = ORDER ? max(a.win.row(at), 0) : at;
       xr[i] = lane_at(x + r * a.ldx, off);
       dr[i] = lane_at(delta + r * a.ldd, off);
-      if (OUT && z != nullptr) zr[i] = lane_at(z + r * a.ldz, off);
+      if (GATE) zr[i] = lane_at(z + r * a.ldz, off);
+    }
+  };
+  // A batch's results are stored when the next one's rows are there and before those after it are asked for: loads
+  // and stores end in order, and stores at the batch's end would be waited for at once.
+  T late[U];
+  const auto put = [&](int p0) __attribute__((always_inline)) {
+    if (!tile.live) return;
+    uint32_t off = c;
+    asm volatile("" : "+v"(off));
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (p0 + i >= part.end) break;
+      const int r = ORDER ? a.win.row(p0 + i) : p0 + i;
+      if (!ORDER || r >= 0) lane_at(y + (int64_t)r * a.D, off) = late[i];
     }
   };
   ask(part.begin);
@@ -81,12 +96,16 @@ __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x
       xv[i] = to_float(xr[i]);
       dt[i] = to_float(dr[i]) + bias;
       zv[i] = to_float(zr[i]);
+      // widened here, so that the registers are free for the next rows: a value that is still to be widened when
+      // those arrive is copied at the loop's end, and that waits for them and for the stores before them
+      asm volatile("" : "+v"(xv[i]), "+v"(dt[i]), "+v"(zv[i]));
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = to_float(bc[j]);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    if (OUT && p0 > part.begin) put(p0 - U);
     ask(p0 + U);
     if (a.softplus)
 #pragma unroll
@@ -113,20 +132,13 @@ __global__ __launch_bounds__(64) void k_scan(ScanArgs a, const T* __restrict__ x
     if (!OUT) continue;
 #pragma unroll
     for (int i = 0; i < U; ++i) sum[i] = __builtin_fmaf(skip, xv[i], sum[i]);
-    if (z != nullptr)
+    if (GATE)
 #pragma unroll
       for (int i = 0; i < U; ++i) sum[i] *= quick_silu(zv[i]);
-    if (tile.live) {
-      uint32_t off = c;
-      asm volatile("" : "+v"(off));
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (p0 + i >= part.end) break;
-        const int r = ORDER ? a.win.row(p0 + i) : p0 + i;
-        if (!ORDER || r >= 0) lane_at(y + (int64_t)r * a.D, off) = from_float<T>(sum[i]);
-      }
-    }
+    for (int i = 0; i < U; ++i) late[i] = from_float<T>(sum[i]);
   }
+  if (OUT) put(part.begin + (part.end - 1 - part.begin) / U * U);
   if (!tile.live) return;
   if (OUT) {
     if (part.last && state_out != nullptr)
@@ -224,11 +236,13 @@ hipError_t launch_forward_scan(scan::ScanArgs a, int dtype, const void* x, const
                                         state_in, static_cast<T*>(y), state_out, parts);
       };
       const bool cut = a.win.n > a.per;
-      if (cut) a.win.order ? args(k_scan<T, NS, false, true>) : args(k_scan<T, NS, false, false>);
+      if (cut) a.win.order ? args(k_scan<T, NS, false, true, false>) : args(k_scan<T, NS, false, false, false>);
       if (cut || state_out != nullptr)
         k_scan_carry<<<dim3(a.win.W, carry_blocks(a)), 256, 0, stream>>>(a, state_in,
                                                                                                      state_out, parts);
-      if (a.win.n > 0) a.win.order ? args(k_scan<T, NS, true, true>) : args(k_scan<T, NS, true, false>);
+      if (a.win.n == 0) return;
+      if (z != nullptr) a.win.order ? args(k_scan<T, NS, true, true, true>) : args(k_scan<T, NS, true, false, true>);
+      else a.win.order ? args(k_scan<T, NS, true, true, false>) : args(k_scan<T, NS, true, false, false>);
     });
   };
   if (dtype == 0) run(float{});
