@@ -11,6 +11,23 @@ using namespace scan;
 
 constexpr int kThreads = 256;
 
+// Four states' B or C of a row, in one load where they lie so; 0 past the last.
+template <typename T>
+__device__ __forceinline__ void load_shared(const T* p, int count, bool vec, float (&v)[4]) {
+  if (vec) {
+    if (count > 0) {
+      Vec<T, 4>::wide(Vec<T, 4>::load(p), v);
+      return;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n) v[n] = n < count ? to_float(p[n]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ bool shared_by_four(const T* p, int64_t ld, int N) {
+  return N % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0;
+}
+
 // LN: lanes of a channel, 4 LN >= N
 template <typename T, int LN>
 __global__ __launch_bounds__(kThreads) void k_scan_step(ScanArgs a, const int32_t* __restrict__ slots, int32_t num_slots,
@@ -27,24 +44,25 @@ __global__ __launch_bounds__(kThreads) void k_scan_step(ScanArgs a, const int32_
   const bool live = at < a.D;
   const int c = live ? at : 0, g = c / a.cg, n0 = 4 * k;
   float* st = state + ((size_t)slot * a.D + c) * a.N + n0;
-  const bool vec = by_four(state, a.N);
+  const bool vec = by_four(state, a.N), vecB = shared_by_four(B, a.ldb, a.N), vecC = shared_by_four(C, a.ldc, a.N);
   const int count = a.N - n0;
   float A[4], h[4];
   load_states<4>(a.A + (size_t)c * a.N + n0, count, by_four(a.A, a.N), A);
   load_states<4>(st, count, vec, h);
+#pragma unroll
+  for (int n = 0; n < 4; ++n) A[n] = exponent(A[n]);
   const float bias = a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
   for (bool first = true;; first = false) {
     const float xv = to_float(x[b * a.ldx + c]), dt = step_size(a, to_float(delta[b * a.ldd + c]), bias), u = dt * xv;
-    const float gate = z != nullptr ? act(kSilu, to_float(z[b * a.ldz + c])) : 1.f;
-    float sum = 0.f;
+    const float gate = z != nullptr ? quick_silu(to_float(z[b * a.ldz + c])) : 1.f;
+    float Bv[4], Cv[4], sum = 0.f;
+    load_shared(B + b * a.ldb + g * a.N + n0, count, vecB, Bv);
+    load_shared(C + b * a.ldc + g * a.N + n0, count, vecC, Cv);
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
-      if (n < count) {
-        const float Bv = to_float(B[b * a.ldb + g * a.N + n0 + n]), Cv = to_float(C[b * a.ldc + g * a.N + n0 + n]);
-        const float e = __builtin_amdgcn_exp2f(dt * (A[n] * kLog2e));
-        h[n] = __builtin_fmaf(e, h[n], u * Bv);
-        sum = __builtin_fmaf(Cv, h[n], sum);
-      }
+    for (int n = 0; n < 4; ++n) {
+      h[n] = __builtin_fmaf(__builtin_amdgcn_exp2f(dt * A[n]), h[n], u * Bv[n]);
+      sum = __builtin_fmaf(Cv[n], h[n], sum);
+    }
     const int next = rows.next(b, slot, first);
     if (next < 0) return;
 #pragma unroll
