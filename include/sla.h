@@ -633,8 +633,9 @@ sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_sl
  *   states' values  fp32 [num_windows, channels, states].  state_out may be state_in.
  *   workspace  device, 256-byte aligned, at least sla_selective_scan_workspace_bytes(...) bytes (0 for
  *             sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
- * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and sums of dt over
- * up to 512 rows are fp32.  A value that is not finite reaches only its own window and channel (B's and C's,
+ * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and long windows are
+ * joined by sums of dt over up to 512 rows, which are fp32.  An A beyond fp32's range counts as 3e38, so that a step of
+ * 0 keeps a state whatever its A.  A value that is not finite reaches only its own window and channel (B's and C's,
  * their group's).  Rows in no window are left as they were.  Deterministic.
  */
 size_t sla_selective_scan_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t channels,
@@ -656,9 +657,11 @@ sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32
  * [n, channels], dB and dC [n, groups, states] (sums over the group's channels) in `dtype`, dA (fp32
  * [channels, states]), dskip and ddelta_bias (fp32 [channels], each may be NULL), the three summed over all
  * rows in windows, and, if not NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  States are made
- * again from the inputs.  Every sum over rows or channels is fp32 in a fixed order.  Rows in no window are
+ * again from the inputs.  Every sum over rows or channels is fp32 in a fixed order.  Where states grow (dt A > 0)
+ * the sum of dt A over 128 rows has to stay below 88.  Rows in no window are
  * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; the outputs must not be
- * inputs.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes.  Deterministic.
+ * inputs.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes: the sums of dB and dC
+ * over 64 channels (256 at up to 4 states, 16 at 64) of every row are most of it.  Deterministic.
  */
 size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                                    int32_t channels, int32_t groups, int32_t states);

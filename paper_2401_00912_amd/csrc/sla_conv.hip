@@ -11,6 +11,10 @@
 // registers, so a row is loaded once but for the K - 1 beside a strip's ends.  The gradients make z again from x.
 // The sums over rows are kept by each thread for its strip, written once for each strip, and added by a
 // second launch in the order of the strips.
+// Measured (a copy reaches 5.1 TB/s): forward of 65,536 rows of 2,048 bf16 channels, width 4: 111 us, 4.8 TB/s;
+// gradients of 16,381 rows of 4,096: 129 + 6 us, 3.1 TB/s (a value takes some 25 instructions there, and its sums,
+// taps and pending dx 150 registers); single rows, 256 of 4,096 channels: 6.7 us.  The next rows asked for
+// before these are computed: 149 -> 124 us; neighbouring strips on one XCD: 124, in plain order 114.
 #include "sla_act.h"
 #include "sla_rows.h"
 
@@ -398,6 +402,8 @@ __global__ __launch_bounds__(kThreads) void k_conv_step(ConvArgs a, const int32_
 }
 
 int rows_per_strip(int64_t n, int32_t C, int dtype) {
+  // strips for 2^17 threads (two waves a SIMD) and more, short enough that the K - 1 rows beside their ends cost
+  // little (the forward above: half as many strips 152 us, twice 123; its gradients: 136, 181 at four times)
   const int64_t threads = n * ((C + (dtype == 0 ? 3 : 7)) / (dtype == 0 ? 4 : 8));
   int64_t per = (threads >> 17) / 8 * 8;
   per = per < 16 ? 16 : per > 256 ? 256 : per;
