@@ -74,15 +74,18 @@ __device__ __forceinline__ float inverse_rms(const RnormArgs& a, RowSum<TPR>& su
     for (int e = 0; e < VEC; ++e) s = __builtin_fmaf(v[j][e], v[j][e], s);
   s = sum(s);
   const float inv = 1.f / (float)a.C;
-  if (s < 1e37f && s > 1e-24f) return 1.f / sqrtf(__builtin_fmaf(s, inv, a.eps));
+  const float plain = 1.f / sqrtf(__builtin_fmaf(s, inv, a.eps));
+  // small squares are lost only beside an eps that is as small
+  if (s < 1e37f && (s > 1e-24f || a.eps > 1e-20f)) return plain;
   float m = 0.f;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) m = fmaxf(m, fabsf(v[j][e]));
   m = sum.largest(m);
-  if (s != s || !(m > 0.f && m <= 3.40282347e38f)) return 1.f / sqrtf(__builtin_fmaf(s, inv, a.eps));
-  const int k = ilogbf(m);
+  if (s != s || !(m > 0.f && m <= 3.40282347e38f)) return plain;
+  // eps goes with the squares: no further up than where it would leave the range instead (there it is all that counts)
+  const int k = a.eps > 0.f ? max(ilogbf(m), -62) : ilogbf(m);
   float q = 0.f;
 #pragma unroll
   for (int j = 0; j < NV; ++j)

@@ -152,6 +152,47 @@ def test_values_whose_squares_leave_the_range(sla):
         assert not torch.isfinite(y[4]).all() and torch.isfinite(y[[0, 1, 2, 3, 5]]).all()
 
 
+@pytest.mark.parametrize("eps", [1e-5, 1e-12, 1e-21, 1e-30, 1000.0])
+def test_small_rows_beside_any_eps(sla, eps):
+    """Rows whose squares are far below eps are scaled by 1 / sqrt(eps); those far above are normalised."""
+    import torch
+
+    for C in (64, 2048, 100):
+        gen = torch.Generator().manual_seed(C)
+        size = torch.tensor([1.0, 1e-8, 1e-13, 1e-16, 1e-25, 1e-30, 1e-38, 0.0]).cuda()[:, None]
+        r = torch.randn(8, C, generator=gen).cuda() * size
+        zero = torch.zeros_like(r)
+        y, _, rstd, _ = sla.forward_residual_norm(zero, r, eps=eps)
+        ry, _, rs, _ = space_ref.rnorm_forward_ref(num(zero), num(r), eps=np.float64(np.float32(eps)))
+        # a statistic is off by its sum's roundings; a denormal input by 2^-149
+        assert (np.abs(num(rstd) / rs - 1) < 1e-5).all()
+        for k in range(8):
+            close(y[k:k + 1], ry[k:k + 1], "f32", f"row {k}", size=1e-38 * rs[k])
+
+
+def test_parameters_at_any_address(sla):
+    import torch
+
+    gen = torch.Generator().manual_seed(5)
+    x, r, g, dy = (torch.randn(9, 512, generator=gen).cuda() for _ in range(4))
+    w, pw = (torch.randn(512, generator=gen).cuda() for _ in range(2))
+    odd = lambda t: torch.cat([t.new_zeros(1), t.flatten()])[1:].view(t.shape)  # noqa: E731
+    kw = dict(weight=w, post_weight=pw, gate=g, activation="silu")
+    a = sla.forward_residual_norm(x, r, **kw)
+    want = sla.backward_residual_norm(x, a[1], dy, a[2], post_rstd=a[3], **kw)
+    kw.update(weight=odd(w), post_weight=odd(pw))
+    b = sla.forward_residual_norm(x, r, **kw)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    got = sla.backward_residual_norm(x, a[1], dy, a[2], post_rstd=a[3], **kw)
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    # rows there too: one value a load, another order of sums
+    kw.update(gate=odd(g))
+    c = sla.forward_residual_norm(odd(x), odd(r), **kw)
+    got = sla.backward_residual_norm(odd(x), odd(a[1]), odd(dy), a[2], post_rstd=a[3], **kw)
+    for p, q in zip((*a, *want), (*c, *got)):
+        assert (p - q).abs().max() <= 2e-5 * p.abs().max()
+
+
 def test_gradients_by_differences(sla):
     import torch
 

@@ -397,3 +397,44 @@ def test_workspace_contents_do_not_matter(sla):
             got.append([y, st, *c.gradients(sla, workspace=ws)])
         for g in got[1:]:
             assert all(torch.equal(a, b) for a, b in zip(got[0], g))
+
+
+def test_parameters_and_states_at_any_address(sla):
+    import torch
+
+    c = Case([70, 30], 72, 16, "f32", seed=21, state=True)
+    odd = lambda t: torch.cat([t.new_zeros(1), t.flatten()])[1:].view(t.shape)  # noqa: E731
+    a = [*c.forward(sla), *c.gradients(sla)]
+    slots = torch.tensor([1, 0], dtype=torch.int32).cuda()
+    row = {k: c.r[k][:2] for k in ("x", "delta", "B", "C", "z")}
+    step = lambda pool, A, skip: sla.step_selective_scan(  # noqa: E731
+        pool, slots, row["x"], row["delta"], A, row["B"], row["C"], skip=skip, z=row["z"], delta_softplus=True)
+    pool, other = c.state.clone(), odd(c.state)
+    y = step(pool, c.r["A"], c.r["skip"])
+    for k in ("A", "skip", "delta_bias"):
+        c.r[k] = odd(c.r[k])
+    c.kw.update(skip=c.r["skip"], delta_bias=c.r["delta_bias"], state=odd(c.state))
+    c.dstate = odd(c.dstate)
+    b = [*c.forward(sla), *c.gradients(sla)]
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert torch.equal(y, step(other, c.r["A"], c.r["skip"])) and torch.equal(pool, other)
+
+
+def test_an_infinite_gradient_stays_in_its_row_and_window(sla):
+    """dy of one row: its own gradients, and those of the rows before it in its window and channel (its group's
+    for B and C), are not finite; no others are."""
+    import torch
+
+    c = Case([40, 50], 32, 8, "f32", 2, seed=22, state=True)
+    c.r["dy"][60, 20] = float("inf")
+    got = dict(zip(GRADS, c.gradients(sla)))
+    for name in ("dx", "ddelta", "dz"):
+        bad = ~torch.isfinite(got[name])
+        assert bad[60, 20] and not bad[:40].any() and not bad[61:].any(), name
+        bad[:, 20] = False
+        assert not bad.any(), name
+    for name in ("dB", "dC"):
+        bad = ~torch.isfinite(got[name])
+        assert not bad[:, 0].any() and not bad[:40].any() and not bad[61:].any(), name
+    assert torch.isfinite(got["dstate_in"][0]).all()
+    assert torch.isfinite(got["dA"][:16]).all() and torch.isfinite(got["dskip"][:16]).all()
