@@ -62,14 +62,18 @@ __global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const
 
   // x, delta and z of the next rows
   T xr[U], dr[U], zr[U] = {}, bc[J];
+  int shared_row[J];
   const auto ask = [&](int p0) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int i = (lane + 64 * j) / V, v = (lane + 64 * j) % V, n = v % NS, p = p0 + i;
-      int r = i < U && n < a.N && p < part.end ? p : -1;
-      if (ORDER && r >= 0) r = a.win.row(r);
-      bc[j] = from_float<T>(0.f);
-      if (r >= 0) bc[j] = v < NS ? B[r * a.ldb + tile.g * a.N + n] : C[r * a.ldc + tile.g * a.N + n];
+      int r = min(p, part.end - 1);
+      if (ORDER) r = a.win.row(r);
+      shared_row[j] = i < U && n < a.N && p < part.end ? r : -1;
+      const int64_t row = max(r, 0);
+      const int m = tile.g * a.N + min(n, a.N - 1);
+      const T* src = v < NS ? B + (row * a.ldb + m) : C + (row * a.ldc + m);
+      bc[j] = *src;
     }
     // rows past the end are the last one, and are not used
     uint32_t off = c;
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = to_float(bc[j]);
+    for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = shared_row[j] >= 0 ? to_float(bc[j]) : 0.f;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     if (OUT && p0 > part.begin) put(p0 - U);

@@ -71,7 +71,10 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
   }
   const float bias = a.bias ? a.bias[c] : 0.f;
   float dts = 0.f;
-  T xr[U], dr[U], zr[U] = {}, gr[U], bc[J];
+  T xr[U], dr[U], zr[U], gr[U], bc[J];
+  int shared_row[J];
+  const T* zp = z != nullptr ? z : dy;   // without a gate something that is there, and is not used
+  const int64_t ldz = z != nullptr ? a.ldz : a.ldy;
   const auto ask = [&](int p0) __attribute__((always_inline)) {
     // rows past the end are the last one, and are not used
 #pragma unroll
@@ -80,14 +83,17 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
       xr[i] = lane_at(x + r * a.ldx, c);
       dr[i] = lane_at(delta + r * a.ldd, c);
       gr[i] = lane_at(dy + r * a.ldy, c);
-      if (z != nullptr) zr[i] = lane_at(z + r * a.ldz, c);
+      zr[i] = lane_at(zp + r * ldz, c);
     }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int at = lane + 64 * j, p = p0 + at / V, v = at % V, n = v % NS;
-      bc[j] = from_float<T>(0.f);
-      const int r = p < part.end && at < U * V && n < N ? a.win.row(p) : -1;
-      if (r >= 0) bc[j] = v < NS ? B[r * a.ldb + tile.g * a.N + n0 + n] : C[r * a.ldc + tile.g * a.N + n0 + n];
+      const int r = a.win.row(min(p, part.end - 1));
+      shared_row[j] = p < part.end && at < U * V && n < N ? r : -1;
+      const int64_t row = max(r, 0);
+      const int m = tile.g * a.N + n0 + min(n, N - 1);
+      const T* src = v < NS ? B + (row * a.ldb + m) : C + (row * a.ldc + m);
+      bc[j] = *src;
     }
   };
   ask(part.begin);
@@ -99,10 +105,11 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
       dt[i] = to_float(dr[i]) + bias;
       zv[i] = to_float(zr[i]);
       gv[i] = to_float(gr[i]);
+      asm volatile("" : "+v"(xv[i]), "+v"(dt[i]), "+v"(zv[i]), "+v"(gv[i]));   // the registers are the next rows'
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = to_float(bc[j]);
+    for (int j = 0; j < J; ++j) s_bc[lane + 64 * j] = shared_row[j] >= 0 ? to_float(bc[j]) : 0.f;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     ask(p0 + U);
@@ -323,45 +330,53 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
   const float bias = a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
   float sum_skip = 0.f, sum_bias = 0.f;
 
-  T xr[E], dr[E], zr[E], gr[E], bc[kStage];
-  int row[E];
-  // a tile's rows: x and delta, and with them all else that the way back needs
+  T xr[E], dr[E], zr[E] = {}, gr[E] = {}, bc[kStage];
+  int row[E], shared_row[kStage];
+  const T* zp = z != nullptr ? z : dy;   // without a gate something that is there, and is not used
+  const int64_t ldz = z != nullptr ? a.ldz : a.ldy;
+  // A tile's rows: x and delta, and with them all else that the way back needs.  Loads without conditions (row 0 for a
+  // row that is none): where a register has one value or another, the compiler copies it, and waits for it, at once.
   const auto ask = [&](int p0, bool back) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      const int p = p0 + j * NG + ng;
-      row[j] = p < part.end && live ? a.win.row(p) : -1;
-      xr[j] = dr[j] = zr[j] = gr[j] = from_float<T>(0.f);
-      if (row[j] >= 0) {
-        xr[j] = x[row[j] * a.ldx + c];
-        dr[j] = delta[row[j] * a.ldd + c];
-        if (back) {
-          gr[j] = dy[row[j] * a.ldy + c];
-          if (z != nullptr) zr[j] = z[row[j] * a.ldz + c];
-        }
+      const int p = p0 + j * NG + ng, r = a.win.row(min(p, part.end - 1));
+      row[j] = p < part.end && live ? r : -1;
+      const int at = max(r, 0);
+      xr[j] = x[at * a.ldx + c];
+      dr[j] = delta[at * a.ldd + c];
+      if (back) {
+        gr[j] = dy[at * a.ldy + c];
+        zr[j] = zp[at * ldz + c];
       }
     }
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
       const int i = tid + kThreads * j, t = i / (2 * NP), v = i % (2 * NP), n = v % NP;
-      bc[j] = from_float<T>(0.f);
-      const int r = t < kTile && p0 + t < part.end && n < a.N ? a.win.row(p0 + t) : -1;
-      if (r >= 0) bc[j] = v < NP ? B[r * a.ldb + g * a.N + n] : C[r * a.ldc + g * a.N + n];
+      const int r = a.win.row(min(p0 + t, part.end - 1));
+      shared_row[j] = t < kTile && p0 + t < part.end && n < a.N ? r : -1;
+      const int at = max(r, 0), m = g * a.N + min(n, a.N - 1);
+      const T* src = v < NP ? B + (at * a.ldb + m) : C + (at * a.ldc + m);
+      bc[j] = *src;
     }
   };
-  float pre[E], dt[E], gate[E];
+  float pre[E], dt[E], gate[E], xv[E], zv[E], gv[E];
   const auto stage = [&](bool back) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < E; ++j) {
+      xv[j] = to_float(xr[j]);
       pre[j] = to_float(dr[j]) + bias;
-      dt[j] = row[j] >= 0 ? step_size(a, to_float(dr[j]), bias) : 0.f;
-      gate[j] = back && z != nullptr ? quick_silu(to_float(zr[j])) : 1.f;
-      s_in[wave][j * NG + ng][ch] = floatx4{dt[j], dt[j] * to_float(xr[j]), to_float(gr[j]) * gate[j], 0.f};
+      zv[j] = to_float(zr[j]);
+      gv[j] = to_float(gr[j]);
+      asm volatile("" : "+v"(xv[j]), "+v"(pre[j]), "+v"(zv[j]), "+v"(gv[j]));   // the registers are the next rows'
+      const bool real = row[j] >= 0;
+      dt[j] = real ? (a.softplus ? softplus(pre[j]) : pre[j]) : 0.f;
+      gate[j] = back && z != nullptr ? quick_silu(zv[j]) : 1.f;
+      s_in[wave][j * NG + ng][ch] = floatx4{dt[j], real ? dt[j] * xv[j] : 0.f, real ? gv[j] * gate[j] : 0.f, 0.f};
     }
     float* flat = &s_bc[0][0][0];
 #pragma unroll
     for (int j = 0; j < kStage; ++j)
-      if (tid + kThreads * j < kTile * 2 * NP) flat[tid + kThreads * j] = to_float(bc[j]);
+      if (tid + kThreads * j < kTile * 2 * NP) flat[tid + kThreads * j] = shared_row[j] >= 0 ? to_float(bc[j]) : 0.f;
   };
 
   const int tiles = (part.end - part.begin + kTile - 1) / kTile;
@@ -402,10 +417,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
     __syncthreads();
     if (i + 1 < tiles) hand_on(p0 + kTile);
     stage(true);
-    float xv[E], zv[E], gv[E];
     int at_row[E];
 #pragma unroll
-    for (int j = 0; j < E; ++j) xv[j] = to_float(xr[j]), zv[j] = to_float(zr[j]), gv[j] = to_float(gr[j]), at_row[j] = row[j];
+    for (int j = 0; j < E; ++j) at_row[j] = row[j];
     __syncthreads();
     if (i > 0) ask(p0 - kTile, true);
     float kept[kTile][4], e[kTile][4];
