@@ -2,10 +2,10 @@
 //
 // Bound by the vector unit: a state and row take a product, an exponential, a product and two multiply-adds (one
 // in the walk that makes a part's map); the memory's part (x, delta, z in, y out) is a third of that at 16 states.
-// Measured: 32,768 bf16 rows of 2,048 channels and 16 states in 17 sequences: 202 to 229 + 22 + 294 to 329 us
+// Measured: 32,768 bf16 rows of 2,048 channels and 16 states in 17 sequences: 200 to 222 + 22 + 291 to 321 us
 // (maps, joining, results), some 690 cycles a row and wave where its 104 vector instructions and 19 exponentials
-// and reciprocals take 570 issued one by one; 59,837 fp16 rows of 256 channels in 1,521 windows: 4.8 + 5.5 +
-// 119 us, of which the longest window's 144 rows are the most; 8,191 fp32 rows of 1,024 channels in one: 35 + 17 +
+// and reciprocals take 570 issued one by one; 59,837 fp16 rows of 256 channels in 1,521 windows: 4.7 + 5.6 +
+// 122 us, of which the longest window's 144 rows are the most; 8,191 fp32 rows of 1,024 channels in one: 33 + 18 +
 // 45 us, 64 rows one after the other twice and 127 parts joined.
 // What was not faster: B and C in scalar registers (454 -> 538 us for the results alone), matrix products for u B
 // or the sum over states (fp32 ones take the vector unit's time: measured 31 ns for one with 16 products beside it,

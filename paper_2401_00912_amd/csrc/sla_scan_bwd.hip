@@ -9,7 +9,7 @@
 //
 // Four launches.  The first makes the maps of a window's parts, forward (S, sum dt) and back: what a part adds
 // to the gradient of the state before it, R = sum_t exp(A sum_{s <= t} dt_s) C_t g_t.  The second joins them along
-// the window both ways.  The third walks every part: forward once for the states at its 16-row tiles, then
+// the window both ways.  The third walks every part: forward once for the states at its tiles, then
 // tile by tile from the last, forward through the tile with every row's a and decay kept in registers, and
 // back.  A lane holds four states of a channel, so the sums over states go over the lane's few neighbours and
 // those over channels over the wave, then over the workgroup's waves in LDS, and what is left of them (over a
@@ -17,9 +17,9 @@
 //
 // Bound by the vector unit: about 45 instructions for each state and row, 7 of them in the maps, 5 in the walk for the
 // tiles' states, 15 to step a state and its gradient, the rest sums over lanes and what each row needs once.
-// Measured: 16,381 bf16 rows of 2,048 channels and 16 states in 9 sequences: 197 + 36 + 764 + 14 + 10 us (maps,
-// joining, walk, dB and dC, parameters), the vector unit busy for 71% of the walk; 59,837 fp16 rows of 256 channels
-// and 8 states in 1,521 windows: 49 + 16 + 266 + 7 + 11 us.  Tiles of 16 rows, without the next tile's rows on their
+// Measured: 16,381 bf16 rows of 2,048 channels and 16 states in 9 sequences: 188 + 36 + 692 + 14 + 10 us (maps,
+// joining, walk, dB and dC, parameters), the vector unit busy for 73% of the walk; 59,837 fp16 rows of 256 channels
+// and 8 states in 1,521 windows: 49 + 16 + 247 + 7 + 11 us.  Tiles of 16 rows, without the next tile's rows on their
 // way and with selects in the sums over channels: 875 us for the first walk; three workgroups a CU (168 registers,
 // 64 of them spilled): 1,450; decays made again on the way back instead of kept: 971 us in all against 941.
 #include <algorithm>
@@ -289,8 +289,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
   constexpr int kStage = (kTile * 2 * NP + kThreads - 1) / kThreads;
   __shared__ floatx4 s_in[kWaves][kTile][CW];            // dt, u, g of the wave's channels
   __shared__ floatx4 s_start[kWaves][kMaxTiles][64];     // states before each tile
-  __shared__ __attribute__((aligned(16))) float s_bc[kTile][2][NP];
-  __shared__ float s_red[kWaves][kTile][2][NP];
+  // two of what the waves share, for tiles in turn, so that a tile has one barrier; at 64 states they would need 120 KB
+  constexpr int kTurns = NG <= 8 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float s_shared[kTurns][kTile][2][NP];
+  __shared__ float s_sums[kTurns][kWaves][kTile][2][NP];
   const ScanArgs& a = k.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ng = lane / CW, ch = lane % CW;
   const int g = blockIdx.y / k.wpg, at = (blockIdx.y % k.wpg) * k.cw + wave * CW + ch;
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
     }
   };
   float pre[E], dt[E], gate[E], xv[E], zv[E], gv[E];
-  const auto stage = [&](bool back) __attribute__((always_inline)) {
+  const auto stage = [&](int turn, bool back) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < E; ++j) {
       xv[j] = to_float(xr[j]);
@@ -373,7 +375,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
       gate[j] = back && z != nullptr ? quick_silu(zv[j]) : 1.f;
       s_in[wave][j * NG + ng][ch] = floatx4{dt[j], real ? dt[j] * xv[j] : 0.f, real ? gv[j] * gate[j] : 0.f, 0.f};
     }
-    float* flat = &s_bc[0][0][0];
+    float* flat = &s_shared[turn][0][0][0];
 #pragma unroll
     for (int j = 0; j < kStage; ++j)
       if (tid + kThreads * j < kTile * 2 * NP) flat[tid + kThreads * j] = shared_row[j] >= 0 ? to_float(bc[j]) : 0.f;
@@ -384,9 +386,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
   s_start[wave][0][lane] = floatx4{h[0], h[1], h[2], h[3]};
   if (tiles > 1) ask(part.begin, false);
   for (int i = 0; i + 1 < tiles; ++i) {
+    const int turn = i % kTurns;
+    if (kTurns == 1) __syncthreads();
+    stage(turn, false);
     __syncthreads();
-    stage(false);
-    __syncthreads();
+    const auto& s_bc = s_shared[turn];
     if (i + 2 < tiles) ask(part.begin + (i + 1) * kTile, false);
 #pragma unroll
     for (int t = 0; t < kTile; ++t) {
@@ -399,8 +403,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
   }
 
   // the waves' sums over their channels of the tile at p0
-  const auto hand_on = [&](int p0) __attribute__((always_inline)) {
-    const float* red = &s_red[0][0][0][0];
+  const auto hand_on = [&](int p0, int turn) __attribute__((always_inline)) {
+    const float* red = &s_sums[turn][0][0][0][0];
     for (int v = tid; v < kTile * 2 * NP; v += kThreads) {
       const int t = v / (2 * NP), which = v / NP % 2, n = v % NP;
       if (p0 + t < part.end && n < a.N) {
@@ -414,13 +418,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
   ask(part.begin + (tiles - 1) * kTile, true);
   for (int i = tiles - 1; i >= 0; --i) {
     const int p0 = part.begin + i * kTile;
-    __syncthreads();
-    if (i + 1 < tiles) hand_on(p0 + kTile);
-    stage(true);
+    const int turn = i % kTurns;
+    if (kTurns == 1) {
+      __syncthreads();
+      if (i + 1 < tiles) hand_on(p0 + kTile, 0);
+    }
+    stage(turn, true);
     int at_row[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) at_row[j] = row[j];
     __syncthreads();
+    if (kTurns > 1 && i + 1 < tiles) hand_on(p0 + kTile, turn ^ 1);
+    const auto& s_bc = s_shared[turn];
+    auto& s_red = s_sums[turn];
     if (i > 0) ask(p0 - kTile, true);
     float kept[kTile][4], e[kTile][4];
     {
@@ -493,7 +503,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_back(BackArgs k, const T* 
     }
   }
   __syncthreads();
-  hand_on(part.begin);
+  hand_on(part.begin, 0);
   float sums[1] = {sum_skip};
   sum_lanes<1, 32, CW, true>(sums, lane);
   sum_skip = sums[0];
