@@ -659,8 +659,8 @@ sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32
  * rows in windows, and, if not NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  States are made
  * again from the inputs.  Every sum over rows or channels is fp32 in a fixed order.  Where states grow (dt A > 0)
  * the sum of dt A over 128 rows has to stay below 88.  Rows in no window are
- * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; the outputs must not be
- * inputs.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes: the sums of dB and dC
+ * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; no output may be an
+ * input or another output.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes: the sums of dB and dC
  * over 64 channels (256 at up to 4 states, 16 at 64) of every row are most of it.  Deterministic.
  */
 size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
@@ -720,7 +720,7 @@ sla_status_t sla_forward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t
  * `dtype`, dresidual in `residual_dtype` (may be NULL, or dresidual_out), dweight and dpost_weight (fp32
  * [channels], each may be NULL), summed over all rows in a fixed order.  relu's slope at 0 is 0.
  * `workspace`: device, 256-byte aligned, sla_residual_norm_backward_workspace_bytes() bytes (0 for sizes that
- * are not supported), else SLA_E_WORKSPACE.  The other outputs must not be inputs.
+ * are not supported), else SLA_E_WORKSPACE.  No other output may be an input, and none another output.
  */
 size_t sla_residual_norm_backward_workspace_bytes(int64_t n, sla_dtype_t dtype, int32_t channels);
 

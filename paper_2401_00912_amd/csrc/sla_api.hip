@@ -729,6 +729,19 @@ bool rows_ok(const void* p, int64_t n, int64_t ld, int64_t values, uintptr_t esi
   return n == 0 || (p != nullptr && aligned(p, esize) && (n == 1 || ld >= values));
 }
 
+// no output that is an input or another output (null: one that is not asked for)
+template <size_t I, size_t O>
+bool outputs_apart(const void* const (&in)[I], const void* const (&out)[O]) {
+  for (size_t o = 0; o < O; ++o) {
+    if (out[o] == nullptr) continue;
+    for (const void* i : in)
+      if (i == out[o]) return false;
+    for (size_t p = 0; p < o; ++p)
+      if (out[p] == out[o]) return false;
+  }
+  return true;
+}
+
 }  // namespace
 
 SLA_EXPORT sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t num_windows,
@@ -896,9 +909,7 @@ SLA_EXPORT sla_status_t sla_backward_selective_scan(
   if (n > 0) {
     const void* in[] = {x, delta, z, B, C, dy};
     const void* out[] = {dx, ddelta, z != nullptr ? dz : nullptr, dB, dC};
-    for (const void* o : out)
-      for (const void* i : in)
-        if (o != nullptr && o == i) return SLA_E_ARG;
+    if (!outputs_apart(in, out)) return SLA_E_ARG;
   }
   if (dstate_in != nullptr && dstate_in == state_in) return SLA_E_ARG;
   if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
@@ -1004,9 +1015,7 @@ SLA_EXPORT sla_status_t sla_backward_residual_norm(int64_t n, sla_dtype_t dtype,
       return SLA_E_ARG;
     const void* in[] = {x, residual_out, gate, dy};
     const void* out[] = {dx, dresidual, gate != nullptr ? dgate : nullptr};
-    for (const void* o : out)
-      for (const void* i : in)
-        if (o != nullptr && o == i) return SLA_E_ARG;
+    if (!outputs_apart(in, out)) return SLA_E_ARG;
     if (dx == dresidual_out || (gate != nullptr && dgate == dresidual_out)) return SLA_E_ARG;
   }
   if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;

@@ -171,6 +171,13 @@ def test_norm_refusals_of_one(L):
     assert L.sla_residual_norm_backward_workspace_bytes(100, 2, 8193) == 0
 
 
+def test_one_output_for_two_gradients_is_refused(L):
+    for kw in (dict(dd=SCAN["dx"]), dict(dz=SCAN["dd"]), dict(dC=SCAN["dB"]), dict(dB=SCAN["dz"])):
+        assert call(L.sla_backward_selective_scan, SCAN_BWD, SCAN, kw) == sla.SLA_E_ARG, kw
+    for kw in (dict(dr=NORM["dx"]), dict(dg=NORM["dx"]), dict(dg=NORM["dr"])):
+        assert call(L.sla_backward_residual_norm, NORM_BWD, NORM, kw) == sla.SLA_E_ARG, kw
+
+
 # ------------------------------------------------------------------ the binding
 def test_conv_binding():
     import torch
