@@ -570,7 +570,8 @@ sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t n, int32_t 
  *     y_t = act(bias + sum_{j < width} weight[c][j] x_{t - width + 1 + j}),
  * where x_{-width + 1} .. x_{-1} are the rows of state_in[w], oldest first (zero if state_in is NULL), and
  * state_out[w] (if not NULL) receives the window's last width - 1 inputs in that form.
- *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.
+ *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.  A position whose order
+ *             is no row (below 0, or n and more) is a row of zeros that has no result.
  *   x         [n, channels] in `dtype`, rows x_stride elements apart (>= channels; columns of a wider
  *             array do);  y [n, channels], contiguous.  16-byte aligned rows (channels, strides and
  *             addresses) are fastest, none of it is required.  channels up to 65,536.

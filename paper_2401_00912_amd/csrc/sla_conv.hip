@@ -227,8 +227,9 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
       slope_all(a.act, z, dz);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
+        if (row >= 0)
 #pragma unroll
-        for (int j = 0; j < K - 1 - t; ++j) g[t + j][e] = __builtin_fmaf(taps.w[j][e], dz[e], g[t + j][e]);
+          for (int j = 0; j < K - 1 - t; ++j) g[t + j][e] = __builtin_fmaf(taps.w[j][e], dz[e], g[t + j][e]);
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) h[j][e] = h[j + 1][e];
       }
@@ -276,12 +277,13 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
       const int p = p0 + i;
       if (p < last) {
         if (p < a.win.n && at.to(a.win, p)) from_state<T, VEC, K>(a, at.w, state, c, h);
+        // a position whose order names no row is a row of zeros that has no result, as in the forward
         const bool in = at.in(p) && row[i] >= 0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc[K - 1][e] = 0.f;
         live = live >> 1 | (in ? 1u << (K - 1) : 0u);
+        V::wide(rx[i], h[K - 1]);
         if (in) {
-          V::wide(rx[i], h[K - 1]);
           float d[VEC], z[VEC];
           V::wide(rd[i], d);
           if (dstate != nullptr && p >= at.end - (K - 1))
@@ -308,11 +310,11 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(ConvArgs a, const T* __re
             if (t >= K - 1 - j)
 #pragma unroll
               for (int e = 0; e < VEC; ++e) acc[j][e] = __builtin_fmaf(taps.w[j][e], d[e], acc[j][e]);
-#pragma unroll
-          for (int j = 0; j < K - 1; ++j)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) h[j][e] = h[j + 1][e];
         }
+#pragma unroll
+        for (int j = 0; j < K - 1; ++j)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) h[j][e] = h[j + 1][e];
         const int q = p - (K - 1);
         if (q >= ps && (live & 1u)) V::store(dx + (size_t)a.win.row(q) * a.C + c, acc[0]);
 #pragma unroll
