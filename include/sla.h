@@ -576,7 +576,7 @@ sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t n, int32_t 
  *             array do);  y [n, channels], contiguous.  16-byte aligned rows (channels, strides and
  *             addresses) are fastest, none of it is required.  channels up to 65,536.
  *   weight    fp32 [channels, width], width 2 .. 8, else SLA_E_UNSUPPORTED;  bias fp32 [channels] or NULL.
- *   states    [num_windows, width - 1, channels] in `dtype`.  state_out must not be state_in, nor y x.
+ *   states    [num_windows, width - 1, channels] in `dtype`.  No output may be an input or another output.
  * Sums and activations are fp32, y is rounded once.  A value that is not finite reaches only the rows whose
  * sums it is in.  Rows in no window are left as they were.  Deterministic.
  */
@@ -591,7 +591,7 @@ sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t n
  * (NULL: zero), writes dx [n, channels] and, if not NULL, dstate_in, both in `dtype`, and dweight, dbias
  * (fp32, sums over all rows in windows in a fixed order; dbias may be NULL).  relu's slope at 0 is 0.
  * `workspace`: device, 256-byte aligned, sla_short_conv_backward_workspace_bytes() bytes (0 for sizes
- * that are not supported), else SLA_E_WORKSPACE.  The outputs must not be inputs.
+ * that are not supported), else SLA_E_WORKSPACE.  No output may be an input or another output.
  */
 size_t sla_short_conv_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                                int32_t channels, int32_t width);
@@ -608,7 +608,7 @@ sla_status_t sla_backward_short_conv(const int32_t* offsets, int64_t n, int32_t 
  * The short convolution one row at a time: `state` is a pool [num_slots, width - 1, channels] in `dtype`,
  * row b of the batch belongs to the sequence in slot slots[b], whose state moves on by one row in place.
  * Slots as in sla_step_delta (rows of the same slot follow each other, a slot outside the pool marks a
- * padding row, n up to 65,536).
+ * padding row, n up to 65,536).  y is neither an input nor the pool, and the pool no other input.
  */
 sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
                                  int32_t channels, int32_t width, sla_activation_t activation, void* state,
@@ -627,11 +627,12 @@ sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_sl
  *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.
  *   x, delta, z  [n, channels], B, C [n, groups, states], in `dtype`: the rows of each contiguous, *_stride
  *             elements apart (not less than their length; columns of a wider array do).  z may be NULL
- *             (no gate).  y [n, channels], contiguous, not an input.
+ *             (no gate).  y [n, channels], contiguous.
  *   A         fp32 [channels, states], usually < 0;  skip, delta_bias fp32 [channels] or NULL (0).
  *   states    1 to 64, channels up to 65,536 and at most 65,535 blocks of 64 channels of a group, else
  *             SLA_E_UNSUPPORTED; channels a multiple of groups.
- *   states' values  fp32 [num_windows, channels, states].  state_out may be state_in.
+ *   states' values  fp32 [num_windows, channels, states].  state_out may be state_in.  No other output may be an
+ *             input, and none another output.
  *   workspace  device, 256-byte aligned, at least sla_selective_scan_workspace_bytes(...) bytes (0 for
  *             sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
  * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and long windows are
@@ -660,8 +661,8 @@ sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32
  * rows in windows, and, if not NULL, dstate_in = dL/d(state_in) (fp32; may be dstate_out).  States are made
  * again from the inputs.  Every sum over rows or channels is fp32 in a fixed order.  Where states grow (dt A > 0)
  * the sum of dt A over 128 rows has to stay below 88.  Rows in no window are
- * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; no output may be an
- * input or another output.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes: the sums of dB and dC
+ * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; no other output may be
+ * an input, and none another output.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes: the sums of dB and dC
  * over 64 channels (256 at up to 4 states, 16 at 64) of every row are most of it.  Deterministic.
  */
 size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
@@ -683,7 +684,8 @@ sla_status_t sla_backward_selective_scan(const int32_t* offsets, int64_t n, int3
  * The selective scan one row at a time: `state` is a pool [num_slots, channels, states] (fp32), row b of the
  * batch belongs to the sequence in slot slots[b], whose state it updates in place.  Slots as in
  * sla_step_delta (rows of the same slot follow each other, a slot outside the pool marks a padding row, n up
- * to 65,536); other arguments as sla_forward_selective_scan.
+ * to 65,536); other arguments as sla_forward_selective_scan.  y is neither an input nor the pool, and the pool
+ * no other input.
  */
 sla_status_t sla_step_selective_scan(const int32_t* slots, int64_t n, int32_t num_slots, sla_dtype_t dtype,
                                      int32_t channels, int32_t groups, int32_t states, int32_t delta_softplus,
@@ -707,7 +709,7 @@ sla_status_t sla_step_selective_scan(const int32_t* slots, int64_t n, int32_t nu
  *   eps       finite and >= 0;  scale finite.
  * All arithmetic is fp32 and y comes from the sum as it is before residual_out is rounded; squares beyond
  * fp32's range are taken at the row's power of two.  A value that is not finite reaches only its row.
- * Deterministic.  y must not be an input.
+ * Deterministic.  No other output may be an input, and none another output.
  */
 sla_status_t sla_forward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t residual_dtype, int32_t channels,
                                        float eps, float scale, sla_activation_t activation, const void* x,

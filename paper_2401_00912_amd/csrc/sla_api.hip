@@ -729,6 +729,9 @@ bool rows_ok(const void* p, int64_t n, int64_t ld, int64_t values, uintptr_t esi
   return n == 0 || (p != nullptr && aligned(p, esize) && (n == 1 || ld >= values));
 }
 
+// a tensor's address where there are rows: without any it is none, whatever it is
+const void* of_rows(int64_t n, const void* p) { return n > 0 ? p : nullptr; }
+
 // no output that is an input or another output (null: one that is not asked for)
 template <size_t I, size_t O>
 bool outputs_apart(const void* const (&in)[I], const void* const (&out)[O]) {
@@ -757,8 +760,9 @@ SLA_EXPORT sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n
       !aligned(state_in, es) || !aligned(state_out, es))
     return SLA_E_ARG;
   if (!rows_ok(x, n, x_stride, channels, es) || !rows_ok(y, n, channels, channels, es)) return SLA_E_ARG;
-  if (state_out != nullptr && state_out == state_in) return SLA_E_ARG;
-  if (n > 0 && x == y) return SLA_E_ARG;
+  const void* in[] = {of_rows(n, x), weight, bias, state_in, offsets, order};
+  const void* out[] = {of_rows(n, y), state_out};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
   if (n == 0 && !state_out) return SLA_OK;
   return hip_status(sla::launch_forward_conv(offsets, (int32_t)n, num_windows, order, (int)dtype, channels, width,
                                              (int)activation, x, x_stride, weight, bias, state_in, y, state_out,
@@ -790,8 +794,9 @@ SLA_EXPORT sla_status_t sla_backward_short_conv(const int32_t* offsets, int64_t 
   if (!rows_ok(x, n, x_stride, channels, es) || !rows_ok(dy, n, dy_stride, channels, es) ||
       !rows_ok(dx, n, channels, channels, es))
     return SLA_E_ARG;
-  if ((n > 0 && (dx == x || dx == dy)) || (dstate_in != nullptr && (dstate_in == state_in || dstate_in == dstate_out)))
-    return SLA_E_ARG;
+  const void* in[] = {of_rows(n, x), of_rows(n, dy), weight, bias, state_in, dstate_out, offsets, order};
+  const void* out[] = {of_rows(n, dx), dweight, dbias, dstate_in};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
   if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
   if (workspace_bytes < sla::conv_backward_workspace_bytes(n, (int)dtype, channels, width)) return SLA_E_WORKSPACE;
   return hip_status(sla::launch_backward_conv(offsets, (int32_t)n, num_windows, order, (int)dtype, channels, width,
@@ -811,8 +816,11 @@ SLA_EXPORT sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int
   if ((int)activation < SLA_ACT_NONE || (int)activation > SLA_ACT_SILU) return SLA_E_ARG;
   if (n == 0) return SLA_OK;
   if (!slots || !aligned(slots, 4) || !state || !aligned(state, es) || !weight || !aligned(weight, 4) ||
-      !aligned(bias, 4) || !rows_ok(x, n, x_stride, channels, es) || !rows_ok(y, n, channels, channels, es) || x == y)
+      !aligned(bias, 4) || !rows_ok(x, n, x_stride, channels, es) || !rows_ok(y, n, channels, channels, es))
     return SLA_E_ARG;
+  const void* in[] = {x, weight, bias, slots};
+  const void* out[] = {y, state};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
   return hip_status(sla::launch_step_conv(slots, (int32_t)n, num_slots, (int)dtype, channels, width, (int)activation,
                                           state, x, x_stride, weight, bias, y, static_cast<hipStream_t>(stream)));
 }
@@ -866,7 +874,10 @@ SLA_EXPORT sla_status_t sla_forward_selective_scan(
   if (!offsets || !aligned(offsets, 4) || !aligned(order, 4) || !aligned(state_in, 4) || !aligned(state_out, 4) ||
       !rows_ok(y, n, channels, channels, es))
     return SLA_E_ARG;
-  if (n > 0 && (y == x || y == delta || y == z || y == B || y == C)) return SLA_E_ARG;
+  const void* in[] = {of_rows(n, x), of_rows(n, delta), of_rows(n, z), of_rows(n, B), of_rows(n, C), A, skip, delta_bias,
+                      offsets, order};
+  const void* out[] = {of_rows(n, y), state_out};
+  if (!outputs_apart(in, out) || (n > 0 && y == state_in)) return SLA_E_ARG;   // state_out may be state_in
   if (n == 0 && !state_out) return SLA_OK;
   if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
   if (workspace_bytes < sla::scan_workspace_bytes(n, num_windows, channels, groups, states)) return SLA_E_WORKSPACE;
@@ -906,12 +917,13 @@ SLA_EXPORT sla_status_t sla_backward_selective_scan(
       !rows_ok(dB, n, shared, shared, es) || !rows_ok(dC, n, shared, shared, es) || !aligned(dskip, 4) ||
       !aligned(ddelta_bias, 4) || !aligned(dstate_in, 4) || (z != nullptr && !rows_ok(dz, n, channels, channels, es)))
     return SLA_E_ARG;
-  if (n > 0) {
-    const void* in[] = {x, delta, z, B, C, dy};
-    const void* out[] = {dx, ddelta, z != nullptr ? dz : nullptr, dB, dC};
-    if (!outputs_apart(in, out)) return SLA_E_ARG;
-  }
-  if (dstate_in != nullptr && dstate_in == state_in) return SLA_E_ARG;
+  const void* in[] = {of_rows(n, x), of_rows(n, delta), of_rows(n, z), of_rows(n, B), of_rows(n, C), of_rows(n, dy), A, skip,
+                      delta_bias, state_in, offsets, order};
+  const void* out[] = {of_rows(n, dx), of_rows(n, ddelta), z != nullptr ? of_rows(n, dz) : nullptr, of_rows(n, dB),
+                       of_rows(n, dC), dA, dskip, ddelta_bias, dstate_in};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
+  for (const void* o : out)   // dstate_in, the last, may be dstate_out
+    if (dstate_out != nullptr && o == dstate_out && o != dstate_in) return SLA_E_ARG;
   if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
   if (workspace_bytes < sla::scan_backward_workspace_bytes(n, num_windows, channels, groups, states))
     return SLA_E_WORKSPACE;
@@ -940,7 +952,9 @@ SLA_EXPORT sla_status_t sla_step_selective_scan(
   if (n == 0) return SLA_OK;
   if (!slots || !aligned(slots, 4) || !state || !aligned(state, 4) || !rows_ok(y, n, channels, channels, es))
     return SLA_E_ARG;
-  if (y == x || y == delta || y == z || y == B || y == C) return SLA_E_ARG;
+  const void* in[] = {x, delta, z, B, C, A, skip, delta_bias, slots};
+  const void* out[] = {y, state};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
   sla::scan::ScanArgs a{};
   a.win = {nullptr, nullptr, (int32_t)n, 0};
   a.A = A, a.skip = skip, a.bias = delta_bias;
@@ -981,8 +995,11 @@ SLA_EXPORT sla_status_t sla_forward_residual_norm(int64_t n, sla_dtype_t dtype, 
       !aligned(residual, rs) || !aligned(residual_out, rs) || !aligned(rstd, 4) || !aligned(post_rstd, 4) ||
       (post_weight != nullptr && post_rstd == nullptr))
     return SLA_E_ARG;
-  if (y == x || y == gate || y == residual || y == residual_out || residual_out == x || residual_out == gate)
-    return SLA_E_ARG;
+  const void* in[] = {x, gate, weight, post_weight};
+  const void* out[] = {y, rstd, post_weight != nullptr ? post_rstd : nullptr, residual_out};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
+  for (const void* o : out)   // residual_out, the last, may be residual
+    if (residual != nullptr && o == residual && o != residual_out) return SLA_E_ARG;
   return hip_status(sla::launch_forward_rnorm(n, (int)dtype, (int)residual_dtype, channels, eps, scale, (int)activation,
                                               x, residual, gate, post_weight, weight, y, residual_out, rstd, post_rstd,
                                               static_cast<hipStream_t>(stream)));
@@ -1013,11 +1030,14 @@ SLA_EXPORT sla_status_t sla_backward_residual_norm(int64_t n, sla_dtype_t dtype,
     if (!x || !residual_out || !rstd || !dy || !dx || (gate != nullptr && !dgate) ||
         (post_weight != nullptr && !post_rstd))
       return SLA_E_ARG;
-    const void* in[] = {x, residual_out, gate, dy};
-    const void* out[] = {dx, dresidual, gate != nullptr ? dgate : nullptr};
-    if (!outputs_apart(in, out)) return SLA_E_ARG;
-    if (dx == dresidual_out || (gate != nullptr && dgate == dresidual_out)) return SLA_E_ARG;
   }
+  const void* in[] = {of_rows(n, x), of_rows(n, residual_out), of_rows(n, gate), of_rows(n, dy), of_rows(n, rstd),
+                      post_weight != nullptr ? of_rows(n, post_rstd) : nullptr, weight, post_weight};
+  const void* out[] = {of_rows(n, dx), gate != nullptr ? of_rows(n, dgate) : nullptr, dweight, dpost_weight,
+                       of_rows(n, dresidual)};
+  if (!outputs_apart(in, out)) return SLA_E_ARG;
+  for (const void* o : out)   // dresidual, the last, may be dresidual_out
+    if (n > 0 && dresidual_out != nullptr && o == dresidual_out && o != dresidual) return SLA_E_ARG;
   if (workspace == nullptr || !aligned(workspace, 256)) return SLA_E_ARG;
   if (workspace_bytes < sla::rnorm_backward_workspace_bytes(n, channels)) return SLA_E_WORKSPACE;
   return hip_status(sla::launch_backward_rnorm(n, (int)dtype, (int)residual_dtype, channels, scale, (int)activation, x,
