@@ -268,8 +268,8 @@ def _torch():
     if _torch_module is None:
         import torch
 
-        _torch_module = torch
         _dtype_codes.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+        _torch_module = torch   # last: another thread's first call that finds it finds the table filled
     return _torch_module
 
 

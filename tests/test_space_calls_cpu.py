@@ -69,3 +69,32 @@ def test_without_rows_only_the_parameters_count(L):
         empty = dict({k: one for k in keys}, n=0, nbytes=0)
         assert call(f, order, defaults, empty) == sla.SLA_E_WORKSPACE
         assert call(f, order, defaults, dict(empty, **same)) == sla.SLA_E_ARG
+
+
+# ------------------------------------------------------------------ first calls by several threads
+def test_a_first_call_beside_another_threads_first_call(monkeypatch):
+    """A second thread whose first call falls into the first one's own finds every type."""
+    import threading
+
+    import torch
+
+    found = []
+
+    def second():
+        try:
+            found.extend(sla._dtype_code(t) for t in (torch.float32, torch.float16, torch.bfloat16))
+        except TypeError as e:
+            found.append(str(e))
+
+    class Codes(dict):
+        def update(self, *args):
+            if threading.current_thread() is threading.main_thread():
+                other = threading.Thread(target=second)
+                other.start()
+                other.join(30)
+            super().update(*args)
+
+    monkeypatch.setattr(sla, "_dtype_codes", Codes())
+    monkeypatch.setattr(sla, "_torch_module", None)
+    assert sla._dtype_code(torch.bfloat16) == 2
+    assert found == [0, 1, 2]
