@@ -591,7 +591,7 @@ sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t n
  * (NULL: zero), writes dx [n, channels] and, if not NULL, dstate_in, both in `dtype`, and dweight, dbias
  * (fp32, sums over all rows in windows in a fixed order; dbias may be NULL).  relu's slope at 0 is 0.
  * `workspace`: device, 256-byte aligned, sla_short_conv_backward_workspace_bytes() bytes (0 for sizes
- * that are not supported), else SLA_E_WORKSPACE.  No output may be an input or another output.
+ * that are not supported; enough for fewer rows and windows too), else SLA_E_WORKSPACE.  No output may be an input or another output.
  */
 size_t sla_short_conv_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                                int32_t channels, int32_t width);
@@ -634,7 +634,7 @@ sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_sl
  *   states' values  fp32 [num_windows, channels, states].  state_out may be state_in.  No other output may be an
  *             input, and none another output.
  *   workspace  device, 256-byte aligned, at least sla_selective_scan_workspace_bytes(...) bytes (0 for
- *             sizes that are not supported), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
+ *             sizes that are not supported; enough for fewer rows and windows too), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
  * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and long windows are
  * joined by sums of dt over up to 512 rows, which are fp32.  An A beyond fp32's range counts as 3e38, so that a step of
  * 0 keeps a state whatever its A.  A value that is not finite reaches only its own window and channel (B's and C's,
@@ -662,7 +662,8 @@ sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32
  * again from the inputs.  Every sum over rows or channels is fp32 in a fixed order.  Where states grow (dt A > 0)
  * the sum of dt A over 128 rows has to stay below 88.  Rows in no window are
  * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; no other output may be
- * an input, and none another output.  `workspace` has at least sla_selective_scan_backward_workspace_bytes(...) bytes: the sums of dB and dC
+ * an input, and none another output.  `workspace` has at least
+ * sla_selective_scan_backward_workspace_bytes(...) bytes (enough for fewer rows and windows too): the sums of dB and dC
  * over 64 channels (256 at up to 4 states, 16 at 64) of every row are most of it.  Deterministic.
  */
 size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
@@ -723,7 +724,7 @@ sla_status_t sla_forward_residual_norm(int64_t n, sla_dtype_t dtype, sla_dtype_t
  * `dtype`, dresidual in `residual_dtype` (may be NULL, or dresidual_out), dweight and dpost_weight (fp32
  * [channels], each may be NULL), summed over all rows in a fixed order.  relu's slope at 0 is 0.
  * `workspace`: device, 256-byte aligned, sla_residual_norm_backward_workspace_bytes() bytes (0 for sizes that
- * are not supported), else SLA_E_WORKSPACE.  No other output may be an input, and none another output.
+ * are not supported; enough for fewer rows too), else SLA_E_WORKSPACE.  No other output may be an input, and none another output.
  */
 size_t sla_residual_norm_backward_workspace_bytes(int64_t n, sla_dtype_t dtype, int32_t channels);
 

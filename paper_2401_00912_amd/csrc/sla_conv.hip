@@ -15,6 +15,8 @@
 // gradients of 16,381 rows of 4,096: 129 + 6 us, 3.1 TB/s (a value takes some 25 instructions there, and its sums,
 // taps and pending dx 150 registers); single rows, 256 of 4,096 channels: 6.7 us.  The next rows asked for
 // before these are computed: 149 -> 124 us; neighbouring strips on one XCD: 124, in plain order 114.
+#include <algorithm>
+
 #include "sla_act.h"
 #include "sla_rows.h"
 
@@ -403,13 +405,22 @@ __global__ __launch_bounds__(kThreads) void k_conv_step(ConvArgs a, const int32_
     for (int j = 0; j < K - 1; ++j) *reinterpret_cast<typename V::R*>(st + (size_t)j * a.C) = r[j];
 }
 
+int64_t lanes_of(int32_t C, int dtype) { return dtype == 0 ? ((int64_t)C + 3) / 4 : ((int64_t)C + 7) / 8; }
+
 int rows_per_strip(int64_t n, int32_t C, int dtype) {
   // strips for 2^17 threads (two waves a SIMD) and more, short enough that the K - 1 rows beside their ends cost
   // little (the forward above: half as many strips 152 us, twice 123; its gradients: 136, 181 at four times)
-  const int64_t threads = n * ((C + (dtype == 0 ? 3 : 7)) / (dtype == 0 ? 4 : 8));
+  const int64_t threads = n * lanes_of(C, dtype);
   int64_t per = (threads >> 17) / 8 * 8;
   per = per < 16 ? 16 : per > 256 ? 256 : per;
   return (int)per;
+}
+
+// The strips of any number of rows up to n, of which there are fewer where strips get longer.  A strip of `per` = 16
+// to 248 rows means fewer than (per + 8) 2^17 / lanes rows, so at most 1.5 2^17 / lanes strips.
+int64_t most_strips(int64_t n, int32_t C, int dtype) {
+  const int64_t lanes = lanes_of(C, dtype), some = ((3 << 16) + lanes - 1) / lanes;
+  return std::max(std::min((n + 15) / 16, some), (n + 255) / 256);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -502,8 +513,7 @@ void step_impl(const ConvArgs& a, int K, const int32_t* slots, int32_t num_slots
 }  // namespace
 
 size_t conv_backward_workspace_bytes(int64_t n, int dtype, int32_t C, int32_t K) {
-  const int64_t per = rows_per_strip(n, C, dtype);
-  return align_up((size_t)((n + per - 1) / per) * (K + 1) * C * 4 + 256, 256);
+  return align_up((size_t)most_strips(n, C, dtype) * (K + 1) * C * 4 + 256, 256);
 }
 
 hipError_t launch_forward_conv(const int32_t* offsets, int32_t n, int32_t W, const int32_t* order, int dtype, int32_t C,

@@ -10,6 +10,8 @@
 // What was not faster: B and C in scalar registers (454 -> 538 us for the results alone), matrix products for u B
 // or the sum over states (fp32 ones take the vector unit's time: measured 31 ns for one with 16 products beside it,
 // 14 and 16 alone), eight rows at once, workgroups of four waves (482).
+#include <algorithm>
+
 #include "sla_scan.h"
 
 namespace sla {
@@ -219,12 +221,19 @@ int rows_per_part(int64_t n, int32_t W, int64_t tiles) {
   return (int)per;
 }
 
+// The parts of any numbers of rows and windows up to n and W, of which there are fewer where parts get longer.  Parts
+// of `per` = 64 to 120 rows mean fewer than (per + 8) 8192 / tiles rows, so at most 9216 / tiles parts beside the
+// windows' own; those of windows that are not cut are longer.
+int64_t most_parts(int64_t n, int32_t W, int64_t tiles) {
+  return std::max(std::min(n / 64, (9216 + tiles - 1) / tiles), n / 128) + W;
+}
+
 int64_t tiles_of(int32_t D, int32_t G) { return (int64_t)G * ((D / G + 63) / 64); }
 
 }  // namespace
 
 size_t scan_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
-  const int64_t slots = n / rows_per_part(n, W, tiles_of(D, G)) + W;
+  const int64_t slots = most_parts(n, W, tiles_of(D, G));
   return align_up((size_t)slots * D * N * 4, 256) + align_up((size_t)slots * D * 4, 256);
 }
 

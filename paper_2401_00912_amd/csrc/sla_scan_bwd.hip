@@ -580,6 +580,12 @@ int rows_per_part_back(int64_t n, int32_t W, int64_t blocks, int tile) {
   return (int)per;
 }
 
+// The parts of any numbers of rows and windows up to n and W, as the forward's: parts of 4 to 7 tiles mean fewer than
+// (per + tile) 1024 / blocks rows, so at most 1280 / blocks beside the windows' own.
+int64_t most_parts_back(int64_t n, int32_t W, int64_t blocks, int tile) {
+  return std::max(std::min(n / (4 * tile), (1280 + blocks - 1) / blocks), n / (tile * kMaxTiles)) + W;
+}
+
 int lane_groups(int32_t N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 
 struct BackLayout {
@@ -587,13 +593,16 @@ struct BackLayout {
   int64_t slots;
   size_t S, dts, R, bc, pA, pskip, pbias, total;
 };
-BackLayout back_layout(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
+// most: with the places that fewer rows or windows may need
+BackLayout back_layout(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N, bool most) {
   BackLayout L;
   L.ng = lane_groups(N);
   L.cw = 64 / L.ng * kWaves;
   L.wpg = (D / G + L.cw - 1) / L.cw;
-  L.per = rows_per_part_back(n, W, (int64_t)G * L.wpg, L.ng <= 8 ? 8 : 16);
-  L.slots = n / L.per + W;
+  const int64_t blocks = (int64_t)G * L.wpg;
+  const int tile = L.ng <= 8 ? 8 : 16;
+  L.per = rows_per_part_back(n, W, blocks, tile);
+  L.slots = most ? most_parts_back(n, W, blocks, tile) : n / L.per + W;
   size_t off = 0;
   const auto take = [&](size_t floats) {
     const size_t at = off;
@@ -615,7 +624,7 @@ BackLayout back_layout(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
 }  // namespace
 
 size_t scan_backward_workspace_bytes(int64_t n, int32_t W, int32_t D, int32_t G, int32_t N) {
-  return back_layout(n, W, D, G, N).total;
+  return back_layout(n, W, D, G, N, true).total;
 }
 
 hipError_t launch_backward_scan(scan::ScanArgs a, int dtype, const void* x, const void* delta, const void* z,
@@ -623,7 +632,7 @@ hipError_t launch_backward_scan(scan::ScanArgs a, int dtype, const void* x, cons
                                 const float* dstate_out, void* dx, void* ddelta, float* dA, void* dB, void* dC,
                                 float* dskip, void* dz, float* dbias, float* dstate_in, void* workspace,
                                 hipStream_t stream) {
-  const BackLayout L = back_layout(a.win.n, a.win.W, a.D, a.G, a.N);
+  const BackLayout L = back_layout(a.win.n, a.win.W, a.D, a.G, a.N, false);
   a.cg = a.D / a.G;
   a.tpg = (a.cg + 63) / 64;
   a.per = L.per;

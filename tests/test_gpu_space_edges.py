@@ -56,3 +56,37 @@ def test_an_order_that_names_no_row_is_a_row_of_zeros(sla, dtype, C, K):
                                                activation="none", state=np.abs(h["s"]), order=order)
     within(dw, gw, 1.1 * 2.0e-5 * sw, "dweight")
     within(db, gb, 1.1 * 2.0e-5 * sb, "dbias")
+
+
+# ------------------------------------------------------------------ workspaces
+@pytest.mark.parametrize("n,W", [(159, 1), (160, 3), (160, 4), (255, 2), (256, 8), (383, 1), (384, 1), (575, 1), (576, 3),
+                                 (640, 5), (1024, 2), (1100, 4)])
+def test_calls_stay_in_their_workspace(sla, n, W):
+    """Workspaces of just the bytes asked for, at the widths whose cuts change with these rows and windows, and one of
+    more rows and windows for the same calls: the bytes beside them stay, the results are the same."""
+    import torch
+
+    D = 65536
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    rows = lambda *s: torch.randn(*s, device="cuda", generator=gen).half()  # noqa: E731
+    x, delta, dy, B, C = rows(n, D), rows(n, D), rows(n, D), rows(n, 1, 1), rows(n, 1, 1)
+    A, weight = -torch.ones(D, 1, device="cuda"), torch.randn(D, 2, device="cuda", generator=gen)
+    cuts = sorted(torch.randint(0, n + 1, (W - 1,), generator=torch.Generator().manual_seed(n)).tolist())
+    off = torch.tensor([0, *cuts, n], dtype=torch.int32, device="cuda")
+
+    def run(need, f):
+        buf = torch.full((need + 8192,), 0x5A, dtype=torch.uint8, device="cuda")
+        got = f(buf[4096:-4096])
+        torch.cuda.synchronize()
+        assert (buf[:4096] == 0x5A).all() and (buf[-4096:] == 0x5A).all()
+        return [t for t in got if t is not None]
+
+    for need, f in (
+            (lambda n, W: sla.short_conv_backward_workspace_bytes(n, W, x.dtype, D, 2),
+             lambda ws: sla.backward_short_conv(x, weight, off, dy, workspace=ws)),
+            (lambda n, W: sla.selective_scan_workspace_bytes(n, W, x.dtype, D, 1, 1),
+             lambda ws: sla.forward_selective_scan(x, delta, A, B, C, off, delta_softplus=True, workspace=ws)),
+            (lambda n, W: sla.selective_scan_backward_workspace_bytes(n, W, x.dtype, D, 1, 1),
+             lambda ws: sla.backward_selective_scan(x, delta, A, B, C, off, dy, delta_softplus=True, workspace=ws))):
+        a, b = run(need(n, W), f), run(need(n + 37, W + 5), f)
+        assert all(torch.equal(p, q) for p, q in zip(a, b))

@@ -98,3 +98,25 @@ def test_a_first_call_beside_another_threads_first_call(monkeypatch):
     monkeypatch.setattr(sla, "_torch_module", None)
     assert sla._dtype_code(torch.bfloat16) == 2
     assert found == [0, 1, 2]
+
+
+# ------------------------------------------------------------------ workspaces
+def test_a_workspace_is_enough_for_fewer_rows_and_windows(L):
+    """Where strips and parts get longer, and at sizes all over the range."""
+    import random
+
+    conv = lambda n, W, dtype, D, N: L.sla_short_conv_backward_workspace_bytes(n, W, dtype, D, 4)  # noqa: E731
+    forward = lambda n, W, dtype, D, N: L.sla_selective_scan_workspace_bytes(n, W, dtype, D, 1, N)  # noqa: E731
+    back = lambda n, W, dtype, D, N: L.sla_selective_scan_backward_workspace_bytes(n, W, dtype, D, 1, N)  # noqa: E731
+    norm = lambda n, W, dtype, D, N: L.sla_residual_norm_backward_workspace_bytes(n, dtype, D)  # noqa: E731
+    assert conv(12223, 9, 2, 2048, 0) <= conv(16394, 9, 2, 2048, 0)
+    assert forward(59837, 1023, 1, 256, 16) <= forward(59837, 1024, 1, 256, 16)
+    assert back(10234, 2, 2, 1024, 1) <= back(10287, 2, 2, 1024, 1)
+    rng = random.Random(11)
+    size = lambda hi: int(hi ** rng.random())  # noqa: E731
+    for _ in range(4000):
+        dtype, D, N = rng.randrange(3), rng.choice([1, 70, 256, 1024, 2048, 8192]), rng.choice([1, 4, 8, 16, 32, 64])
+        n, W = size(300000), size(5000)
+        more_n, more_W = n + rng.choice([0, 1, 8, size(60000)]), W + rng.choice([0, 1, size(3000)])
+        for f in (conv, forward, back, norm):
+            assert 0 < f(n, W, dtype, D, N) <= f(more_n, more_W, dtype, D, N), (n, W, more_n, more_W, dtype, D, N)
