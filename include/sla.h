@@ -624,7 +624,8 @@ sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_sl
  *     h[s] <- exp(dt_t A[d][s]) h[s] + dt_t x_t B_t[g][s],
  *     y_t  = (sum_s C_t[g][s] h[s] + skip[d] x_t) z_t / (1 + exp(-z_t)),
  * and state_out[w][d] (if not NULL) receives the last h.
- *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.
+ *   offsets, order  as in sla_forward_delta; a window without rows hands its state on.  A position whose order
+ *             is no row (below 0, or n and more) is left out.
  *   x, delta, z  [n, channels], B, C [n, groups, states], in `dtype`: the rows of each contiguous, *_stride
  *             elements apart (not less than their length; columns of a wider array do).  z may be NULL
  *             (no gate).  y [n, channels], contiguous.

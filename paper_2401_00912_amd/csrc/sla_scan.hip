@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const
 
   // x, delta and z of the next rows
   T xr[U], dr[U], zr[U] = {}, bc[J];
-  int shared_row[J];
+  int next_row[U], shared_row[J];
   const auto ask = [&](int p0) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -82,7 +82,8 @@ __global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const
     asm volatile("" : "+v"(off));   // the lane's part of an address stays 32 bits beside a scalar base
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int at = min(p0 + i, part.end - 1), r = ORDER ? max(a.win.row(at), 0) : at;
+      const int at = min(p0 + i, part.end - 1), named = ORDER ? a.win.row(at) : at, r = max(named, 0);
+      next_row[i] = p0 + i < part.end ? named : -1;
       xr[i] = lane_at(x + r * a.ldx, off);
       dr[i] = lane_at(delta + r * a.ldd, off);
       if (GATE) zr[i] = lane_at(z + r * a.ldz, off);
@@ -105,8 +106,10 @@ __global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const
   ask(part.begin);
   for (int p0 = part.begin; p0 < part.end; p0 += U) {
     float xv[U], dt[U], zv[U], sum[U];
+    int row_of[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      row_of[i] = next_row[i];
       xv[i] = to_float(xr[i]);
       dt[i] = to_float(dr[i]) + bias;
       zv[i] = to_float(zr[i]);
@@ -124,11 +127,14 @@ __global__ __launch_bounds__(64, NS <= 16 ? 3 : 1) void k_scan(ScanArgs a, const
     if (a.softplus)
 #pragma unroll
       for (int i = 0; i < U; ++i) dt[i] = softplus(dt[i]);
-    // past the part's end a row's step and input are 0, as its B and C: h stays as it is, bit for bit
+    // past the part's end, and where the order names no row, a row's step and input are 0, as its B and C: h stays as
+    // it is, bit for bit (by selects: k_scan_maps says why)
     if (p0 + U > part.end || ORDER)
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (p0 + i >= part.end || (ORDER && a.win.row(p0 + i) < 0)) dt[i] = xv[i] = 0.f;
+      for (int i = 0; i < U; ++i) {
+        dt[i] = row_of[i] >= 0 ? dt[i] : 0.f;
+        xv[i] = row_of[i] >= 0 ? xv[i] : 0.f;
+      }
     const auto row = [&](int i) __attribute__((always_inline)) {
       const float u = dt[i] * xv[i];
       float s[4] = {};

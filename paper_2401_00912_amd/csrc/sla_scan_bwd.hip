@@ -72,14 +72,15 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
   const float bias = a.bias ? a.bias[c] : 0.f;
   float dts = 0.f;
   T xr[U], dr[U], zr[U], gr[U], bc[J];
-  int shared_row[J];
+  int next_row[U], shared_row[J];
   const T* zp = z != nullptr ? z : dy;   // without a gate something that is there, and is not used
   const int64_t ldz = z != nullptr ? a.ldz : a.ldy;
   const auto ask = [&](int p0) __attribute__((always_inline)) {
     // rows past the end are the last one, and are not used
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int r = max(a.win.row(min(p0 + i, part.end - 1)), 0);
+      const int at = a.win.row(min(p0 + i, part.end - 1)), r = max(at, 0);
+      next_row[i] = p0 + i < part.end ? at : -1;
       xr[i] = lane_at(x + r * a.ldx, c);
       dr[i] = lane_at(delta + r * a.ldd, c);
       gr[i] = lane_at(dy + r * a.ldy, c);
@@ -99,8 +100,10 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
   ask(part.begin);
   for (int p0 = part.begin; p0 < part.end; p0 += U) {
     float xv[U], dt[U], zv[U], gv[U];
+    int row[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      row[i] = next_row[i];
       xv[i] = to_float(xr[i]);
       dt[i] = to_float(dr[i]) + bias;
       zv[i] = to_float(zr[i]);
@@ -119,11 +122,15 @@ __global__ __launch_bounds__(64) void k_scan_maps(BackArgs k, const T* __restric
     if (z != nullptr)
 #pragma unroll
       for (int i = 0; i < U; ++i) gv[i] *= quick_silu(zv[i]);
-    // past the part's end a row's step, input and gradient are 0, as its B and C: nothing changes
+    // past the part's end, and where the order names no row, a row's step, input and gradient are 0, as its B and C:
+    // nothing changes.  By selects: of branches on rows that the order holds the compiler dropped all but the first.
     if (p0 + U > part.end || a.win.order != nullptr)
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (p0 + i >= part.end || a.win.row(p0 + i) < 0) dt[i] = xv[i] = gv[i] = 0.f;
+      for (int i = 0; i < U; ++i) {
+        dt[i] = row[i] >= 0 ? dt[i] : 0.f;
+        xv[i] = row[i] >= 0 ? xv[i] : 0.f;
+        gv[i] = row[i] >= 0 ? gv[i] : 0.f;
+      }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const float u = dt[i] * xv[i];

@@ -1,6 +1,5 @@
-"""The short convolution's and the selective scan's edges: orders that name no row, and the sizes at which a call
-goes another way (two channels a lane in single rows, long parts, many windows), against the float64 reference.
-Tolerances are those of the operators' own tests."""
+"""The short convolution's and the selective scan's edges: orders that name no row and workspaces of just the bytes
+that are needed, against the float64 reference.  Tolerances are those of the operators' own tests."""
 from __future__ import annotations
 
 import numpy as np
@@ -10,6 +9,7 @@ from oracle import space_ref
 from tests.gpu_util import torch_dtype
 from tests.test_gpu_conv import Case as ConvCase
 from tests.test_gpu_conv import close, within
+from tests.test_gpu_scan import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -30,7 +30,9 @@ num = lambda t: None if t is None else t.double().cpu().numpy()  # noqa: E731
 
 
 # ------------------------------------------------------------------ short convolution
-@pytest.mark.parametrize("dtype,C,K", [("f32", 24, 4), ("bf16", 9, 8), ("f16", 64, 2)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K", [2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("C", [9, 24, 64])
 def test_an_order_that_names_no_row_is_a_row_of_zeros(sla, dtype, C, K):
     """Forward and gradients of the same function: a position whose order is out of range is a row of zeros whose
     result is not written and has no gradient."""
@@ -90,3 +92,22 @@ def test_calls_stay_in_their_workspace(sla, n, W):
              lambda ws: sla.backward_selective_scan(x, delta, A, B, C, off, dy, delta_softplus=True, workspace=ws))):
         a, b = run(need(n, W), f), run(need(n + 37, W + 5), f)
         assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+# ------------------------------------------------------------------ selective scan
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [1, 3, 8, 16, 32, 64])
+def test_an_order_that_names_no_row_is_left_out(sla, dtype, N, gate):
+    """As if the windows were without these positions: states go past them, and no other row knows."""
+    import torch
+
+    c = Case([70, 3, 0, 150], 72, N, dtype, 2, seed=32, state=True, order=True, gate=gate)
+    bad = [0, 5, 6, 7, 8, 69, 71, 73, 222, 100, 101, 102]   # in all four places of a batch, at parts' ends too
+    order = c.ref_kw["order"]
+    c.order[bad] = torch.tensor([-1, c.n, 2 ** 31 - 1, -2 ** 31] * 3, dtype=torch.int32, device="cuda")
+    kept = [[p for p in range(lo, hi) if p not in bad] for lo, hi in zip(c.offsets[:-1], c.offsets[1:])]
+    c.ref_kw["order"] = order[sum(kept, [])]
+    c.offsets = np.cumsum([0] + [len(k) for k in kept])
+    c.forward(sla)
+    c.backward(sla)
