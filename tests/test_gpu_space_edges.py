@@ -1,5 +1,9 @@
-"""The short convolution's and the selective scan's edges: orders that name no row and workspaces of just the bytes
-that are needed, against the float64 reference.  Tolerances are those of the operators' own tests."""
+"""The short convolution's and the selective scan's edges: orders that name no row, and the sizes at which a call
+goes another way (two channels a lane in single rows, long parts, many windows), against the float64 reference.
+Tolerances are those of the operators' own tests.  A parameter's gradient is summed by a lane over a part's rows, over
+a sixteenth of the parts and over sixteen of those sums, so by at most rows + parts / 16 + 16 roundings of 2^-24 of the
+terms' sizes: with parts of 64 rows and up to 520 parts 6.7e-6, which leaves the terms' own 2e-6 below 1e-5; with
+parts of 128 rows and up to 170 of them 9.3e-6, so that 1.5e-5 is the limit there."""
 from __future__ import annotations
 
 import numpy as np
@@ -9,7 +13,7 @@ from oracle import space_ref
 from tests.gpu_util import torch_dtype
 from tests.test_gpu_conv import Case as ConvCase
 from tests.test_gpu_conv import close, within
-from tests.test_gpu_scan import Case
+from tests.test_gpu_scan import OPTIONS, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -111,3 +115,60 @@ def test_an_order_that_names_no_row_is_left_out(sla, dtype, N, gate):
     c.offsets = np.cumsum([0] + [len(k) for k in kept])
     c.forward(sla)
     c.backward(sla)
+
+
+# 256 rows and more: two channels a lane from n channels LN = 2^20 on, LN the lanes of a channel
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,D,N", [(256, 1030, 16), (255, 1028, 16), (256, 4096, 5), (100, 1031, 64), (257, 4100, 4),
+                                   (70, 3001, 24)])
+def test_many_single_rows(sla, dtype, n, D, N):
+    import torch
+
+    gen = torch.Generator().manual_seed(n + D)
+    slots = torch.randint(0, n, (n,), generator=gen).to(torch.int32)   # some twice and more
+    slots[::17], slots[5::31] = -1, n + 3                              # and some that are none
+    for strided in (False, True):
+        c = Case([n], D, N, dtype, seed=D, strided=strided)
+        pool = torch.randn(n, D, N, generator=gen).cuda()
+        opts = {k: c.r[k] for k in OPTIONS}
+        ry, rs = space_ref.scan_step_ref(num(pool), slots.numpy(), *map(num, c.args()), **{k: num(v) for k, v in opts.items()},
+                                         delta_softplus=True)
+        y = sla.step_selective_scan(pool, slots.cuda(), *c.args(), **opts, delta_softplus=True, y=c.new(c.r["x"]))
+        close(y, ry, dtype, "y")
+        close(pool, rs, "f32", "state")
+
+
+def uneven(W, mean, longest, seed):
+    """Rows of W windows: most below twice the mean, some empty, a few long."""
+    rng = np.random.default_rng(seed)
+    lengths = rng.integers(0, 2 * mean, W)
+    lengths[rng.integers(0, W, W // 12)] = 0
+    lengths[rng.choice(W, len(longest), replace=False)] = longest
+    return lengths.tolist()
+
+
+# Waves across the channels and, in the gradients, workgroups there: with 32 or 64 groups as many of both, at
+# 1,024 channels of one group 16 and 4 (at 4 states), at 256 channels of 16 groups 16 and 16.
+@pytest.mark.parametrize("lengths,D,N,G,dtype,kw", [
+    # 4,096 waves and more: parts of four times the mean, 72 to 136 rows here, of which some windows have several
+    (uneven(130, 26, [600, 135, 136, 137, 272, 273], 1), 64, 16, 32, "f32", dict(state=True)),
+    (uneven(130, 26, [600, 121, 300], 2), 64, 8, 32, "bf16", dict(state=True, order=True)),
+    # parts of 512, the longest there are
+    (uneven(130, 120, [1300, 512, 513, 511, 1024, 1025], 3), 64, 4, 32, "f32", dict(state=True, gate=False)),
+    (uneven(260, 24, [400, 100, 101], 4), 1024, 4, 1, "f16", dict(strided=True)),
+    (uneven(260, 20, [300, 64, 65, 129], 5), 256, 16, 16, "bf16", dict(state=True, front=3, behind=5)),
+    # 64 states: the gradients' parts have 128 rows
+    (uneven(130, 20, [500, 128, 129, 256, 257], 6), 64, 64, 32, "f32", dict(state=True)),
+    # few windows, parts of 72, 112 and 128 rows
+    ([6000, 0, 3999, 1], 64, 4, 64, "f32", dict(state=True)),
+    ([14999], 64, 1, 64, "bf16", dict()),
+    ([10000, 6601], 64, 4, 64, "f16", dict(state=True, order=True)),
+    # few windows, the gradients' parts of 40, 56 and 64 rows
+    ([1400, 101], 64, 16, 32, "f32", dict(state=True)),
+    ([1999], 64, 12, 32, "bf16", dict(strided=True)),
+    ([1290, 1000], 64, 32, 32, "f32", dict(state=True)),
+])
+def test_long_parts_and_many_windows(sla, lengths, D, N, G, dtype, kw):
+    c = Case(lengths, D, N, dtype, G, seed=D + N, **kw)
+    c.forward(sla)
+    c.backward(sla, bar=1.5e-5 if N == 64 else 1e-5)
