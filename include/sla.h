@@ -577,8 +577,9 @@ sla_status_t sla_backward_group_norm(const int32_t* offsets, int64_t n, int32_t 
  *             addresses) are fastest, none of it is required.  channels up to 65,536.
  *   weight    fp32 [channels, width], width 2 .. 8, else SLA_E_UNSUPPORTED;  bias fp32 [channels] or NULL.
  *   states    [num_windows, width - 1, channels] in `dtype`.  No output may be an input or another output.
- * Sums and activations are fp32, y is rounded once.  A value that is not finite reaches only the rows whose
- * sums it is in.  Rows in no window are left as they were.  Deterministic.
+ * Sums and activations are fp32, y is rounded once.  silu, and the terms of its slope, are off by |z| 2^-23 of
+ * themselves where z is below 0 (from -87 down they are what they are at -87).  A value that is not finite
+ * reaches only the rows whose sums it is in.  Rows in no window are left as they were.  Deterministic.
  */
 sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t num_windows, const int32_t* order,
                                     sla_dtype_t dtype, int32_t channels, int32_t width,
@@ -591,7 +592,8 @@ sla_status_t sla_forward_short_conv(const int32_t* offsets, int64_t n, int32_t n
  * (NULL: zero), writes dx [n, channels] and, if not NULL, dstate_in, both in `dtype`, and dweight, dbias
  * (fp32, sums over all rows in windows in a fixed order; dbias may be NULL).  relu's slope at 0 is 0.
  * `workspace`: device, 256-byte aligned, sla_short_conv_backward_workspace_bytes() bytes (0 for sizes
- * that are not supported; enough for fewer rows and windows too), else SLA_E_WORKSPACE.  No output may be an input or another output.
+ * that are not supported; enough for fewer rows and windows too), else SLA_E_WORKSPACE.  No output may be an
+ * input or another output.
  */
 size_t sla_short_conv_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                                int32_t channels, int32_t width);
@@ -635,11 +637,15 @@ sla_status_t sla_step_short_conv(const int32_t* slots, int64_t n, int32_t num_sl
  *   states' values  fp32 [num_windows, channels, states].  state_out may be state_in.  No other output may be an
  *             input, and none another output.
  *   workspace  device, 256-byte aligned, at least sla_selective_scan_workspace_bytes(...) bytes (0 for
- *             sizes that are not supported; enough for fewer rows and windows too), else SLA_E_WORKSPACE.  Calls that may overlap need one each.
- * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and long windows are
+ *             sizes that are not supported; enough for fewer rows and windows too), else SLA_E_WORKSPACE.
+ *             Calls that may overlap need one each.
+ * All arithmetic is fp32; y is rounded once.  A decay exp(x) is off by |x| 2^-23 of itself, and so is softplus below
+ * 0 (the gate is the silu of sla_forward_short_conv); long windows are
  * joined by sums of dt over up to 512 rows, which are fp32.  An A beyond fp32's range counts as 3e38, so that a step of
  * 0 keeps a state whatever its A.  A value that is not finite reaches only its own window and channel (B's and C's,
- * their group's).  Rows in no window are left as they were.  Deterministic.
+ * their group's).  Rows in no window are left as they were.  Equal calls give equal bits; how long windows are
+ * cut, and so the order of their sums, goes by n and num_windows, so that the same window beside others differs
+ * by roundings.
  */
 size_t sla_selective_scan_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype, int32_t channels,
                                           int32_t groups, int32_t states);
@@ -665,7 +671,8 @@ sla_status_t sla_forward_selective_scan(const int32_t* offsets, int64_t n, int32
  * left as they were.  Other arguments, limits and errors as sla_forward_selective_scan; no other output may be
  * an input, and none another output.  `workspace` has at least
  * sla_selective_scan_backward_workspace_bytes(...) bytes (enough for fewer rows and windows too): the sums of dB and dC
- * over 64 channels (256 at up to 4 states, 16 at 64) of every row are most of it.  Deterministic.
+ * over 64 channels (256 at up to 4 states, 16 at 64) of every row are most of it.  Equal calls give equal bits, as in
+ * the forward.
  */
 size_t sla_selective_scan_backward_workspace_bytes(int64_t n, int32_t num_windows, sla_dtype_t dtype,
                                                    int32_t channels, int32_t groups, int32_t states);

@@ -11,10 +11,12 @@
 // registers, so a row is loaded once but for the K - 1 beside a strip's ends.  The gradients make z again from x.
 // The sums over rows are kept by each thread for its strip, written once for each strip, and added by a
 // second launch in the order of the strips.
-// Measured (a copy reaches 5.1 TB/s): forward of 65,536 rows of 2,048 bf16 channels, width 4: 111 us, 4.8 TB/s;
-// gradients of 16,381 rows of 4,096: 129 + 6 us, 3.1 TB/s (a value takes some 25 instructions there, and its sums,
-// taps and pending dx 150 registers); single rows, 256 of 4,096 channels: 6.7 us.  The next rows asked for
-// before these are computed: 149 -> 124 us; neighbouring strips on one XCD: 124, in plain order 114.
+// Measured (a copy reaches 5.1 TB/s): forward of 65,536 rows of 2,048 bf16 channels, width 4: 112 us, 4.8 TB/s;
+// gradients of 16,381 rows of 4,096: 129 + 6 us, 3.1 TB/s: taps, sums, rows before, pending dx and two batches of rows
+// take 152 registers, which leaves three waves a SIMD (the some 25 instructions a value alone would take 26 to 43 us);
+// single rows, 256 of 4,096 channels: 6.6 us.  The next rows asked for before these are computed: 149 -> 124 us;
+// neighbouring strips on one XCD: 124, in plain order 114.  Over an order that scatters the rows each row's index is a
+// load that its own loads wait for: forward 232 us, gradients 216.
 #include <algorithm>
 
 #include "sla_act.h"

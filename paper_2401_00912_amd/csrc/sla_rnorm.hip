@@ -8,10 +8,15 @@
 //     dgate = scale dr u act'(gate),  du = scale dr act(gate),  dpost_weight = sum du xhat,
 //     dx = post_rstd (du post_weight - xhat mean(du post_weight xhat))  (du without a norm).
 //
-// Bound by memory: every row is loaded once and stays in registers through both norms; the next row of a
-// workgroup is asked for before this one's sums.  Measured (a copy reaches 5.1 TB/s): 32,768 rows of 2,048 bf16
-// channels with fp32 residual rows: 194 us, 4.8 TB/s; gradients of 16,381 rows of 4,096: 201 + 5 us, 5.2 TB/s.  The gradients' sums over rows are kept by each thread for
-// its columns, written once for each workgroup, and added by a second launch in a fixed order.
+// Bound by memory up to 4,096 channels: every row is loaded once and stays in registers through both norms; the next
+// row of a workgroup is asked for before this one's sums.  Measured (a copy reaches 5.1 TB/s): 32,768 rows of 2,048
+// bf16 channels with fp32 residual rows: 197 us, 4.8 TB/s; gradients of 16,381 rows of 4,096: 210 + 5 us, 5.1 TB/s.
+// Wider rows, 5,120 and 8,192 channels: forward 4.1 and 4.4 TB/s, bf16 gradients 2.8 and 3.8 (454 to 506 registers,
+// one wave a SIMD), fp32 gradients 1.6 and 1.8 (194 registers spilled).  Rows that are not 16-byte aligned take 4
+// values a thread up to 1,024 channels, and 32 above, with 98 to 382 registers spilled: 0.2 to 1.0 TB/s at 1,025
+// and 5,001 channels.
+// The gradients' sums over rows are kept by each thread for its columns, written once for each workgroup, and added
+// by a second launch in a fixed order.
 #include <algorithm>
 
 #include "sla_act.h"

@@ -2,11 +2,12 @@
 //
 // Bound by the vector unit: a state and row take a product, an exponential, a product and two multiply-adds (one
 // in the walk that makes a part's map); the memory's part (x, delta, z in, y out) is a third of that at 16 states.
-// Measured: 32,768 bf16 rows of 2,048 channels and 16 states in 17 sequences: 200 to 222 + 22 + 291 to 321 us
-// (maps, joining, results), some 690 cycles a row and wave where its 104 vector instructions and 19 exponentials
-// and reciprocals take 570 issued one by one; 59,837 fp16 rows of 256 channels in 1,521 windows: 4.7 + 5.6 +
-// 122 us, of which the longest window's 144 rows are the most; 8,191 fp32 rows of 1,024 channels in one: 33 + 18 +
-// 45 us, 64 rows one after the other twice and 127 parts joined.
+// Measured: 32,768 bf16 rows of 2,048 channels and 16 states in 17 sequences: 203 + 23 + 294 us (maps, joining,
+// results), some 690 cycles a row and wave where its 104 vector instructions and 19 exponentials
+// and reciprocals take 570 issued one by one; 59,837 fp16 rows of 256 channels in 1,521 windows: 4.7 + 5.5 +
+// 118 us, of which the longest window's 144 rows are the most; 8,191 fp32 rows of 1,024 channels in one: 32 + 17 +
+// 44 us, 64 rows one after the other twice and 127 parts joined.  Over an order that scatters the rows, whose indices
+// are loads that the rows' loads wait for, a call takes 778 us instead of 458 and 196 instead of 125 (the first two).
 // What was not faster: B and C in scalar registers (454 -> 538 us for the results alone), matrix products for u B
 // or the sum over states (fp32 ones take the vector unit's time: measured 31 ns for one with 16 products beside it,
 // 14 and 16 alone), eight rows at once, workgroups of four waves (482).
@@ -213,7 +214,8 @@ __global__ __launch_bounds__(256) void k_scan_carry(ScanArgs a, const float* __r
   }
 }
 
-// Rows of a part: waves for all SIMDs, but parts long enough that joining them costs little (the first case above
+// Rows of a part, and so the order of a window's sums, by all rows and windows of the call: waves for all SIMDs,
+// but parts long enough that joining them costs little (the first case above
 // with at most 64 rows: 475 us, 128: 469, 256: 550, 512: 672).  Where there are waves enough without cutting, only
 // windows of four times the mean are cut (the second case: 124 us; cut at twice the mean 169, at 64 rows 160: a
 // map takes as long as its part's rows one after the other, however few are cut).

@@ -17,9 +17,10 @@
 //
 // Bound by the vector unit: about 45 instructions for each state and row, 7 of them in the maps, 5 in the walk for the
 // tiles' states, 15 to step a state and its gradient, the rest sums over lanes and what each row needs once.
-// Measured: 16,381 bf16 rows of 2,048 channels and 16 states in 9 sequences: 188 + 36 + 692 + 14 + 10 us (maps,
+// Measured: 16,381 bf16 rows of 2,048 channels and 16 states in 9 sequences: 180 + 36 + 650 + 14 + 10 us (maps,
 // joining, walk, dB and dC, parameters), the vector unit busy for 73% of the walk; 59,837 fp16 rows of 256 channels
-// and 8 states in 1,521 windows: 49 + 16 + 247 + 7 + 11 us.  Tiles of 16 rows, without the next tile's rows on their
+// and 8 states in 1,521 windows: 49 + 16 + 245 + 7 + 11 us (these calls 843 and 311 us; over an order that scatters
+// the rows 1,209 and 411).  Tiles of 16 rows, without the next tile's rows on their
 // way and with selects in the sums over channels: 875 us for the first walk; three workgroups a CU (168 registers,
 // 64 of them spilled): 1,450; decays made again on the way back instead of kept: 971 us in all against 941.
 #include <algorithm>
@@ -579,8 +580,8 @@ __global__ __launch_bounds__(1024) void k_scan_params(BackArgs k, int32_t slots,
   *out = sum;
 }
 
-// Whole tiles; enough workgroups for three a CU, but parts of eight tiles at most, whose states LDS holds.  Where
-// there are windows enough, parts as long as they can be.
+// Whole tiles; 1,024 workgroups, four for every CU, of which two are there at a time, but parts of eight tiles at most,
+// whose states LDS holds.  Where there are windows enough, parts as long as they can be.
 int rows_per_part_back(int64_t n, int32_t W, int64_t blocks, int tile) {
   int64_t per = W * blocks >= 1024 ? n : n * blocks / 1024 / tile * tile;
   per = per < 4 * tile ? 4 * tile : per > tile * kMaxTiles ? tile * kMaxTiles : per;

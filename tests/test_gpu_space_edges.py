@@ -1,5 +1,6 @@
-"""The short convolution's and the selective scan's edges: orders that name no row, and the sizes at which a call
-goes another way (two channels a lane in single rows, long parts, many windows), against the float64 reference.
+"""The short convolution's and the selective scan's edges: orders that name no row, workspaces of just the bytes that
+are needed, and the sizes at which a call goes another way (two channels a lane in single rows, long parts, many
+windows), against the float64 reference.
 Tolerances are those of the operators' own tests.  A parameter's gradient is summed by a lane over a part's rows, over
 a sixteenth of the parts and over sixteen of those sums, so by at most rows + parts / 16 + 16 roundings of 2^-24 of the
 terms' sizes: with parts of 64 rows and up to 520 parts 6.7e-6, which leaves the terms' own 2e-6 below 1e-5; with
@@ -172,3 +173,12 @@ def test_long_parts_and_many_windows(sla, lengths, D, N, G, dtype, kw):
     c = Case(lengths, D, N, dtype, G, seed=D + N, **kw)
     c.forward(sla)
     c.backward(sla, bar=1.5e-5 if N == 64 else 1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [1, 4, 8, 16, 32, 64])
+def test_rows_alone(sla, dtype, N):
+    """Neither gate nor skip, bias or softplus, in every type and at every number of states a lane is built for."""
+    c = Case([90, 0, 3, 180], 70, N, dtype, seed=33, state=True, gate=False, skip=False, bias=False, softplus=False)
+    c.forward(sla)
+    c.backward(sla)
